@@ -1,4 +1,4 @@
-"""``torch.autograd`` front-ends of the library: the selective scan and the layer around it.
+"""``torch.autograd`` front-ends of the library: the selective scan, the layer around it, layer norm and the gated recurrence.
 
 Still marshalling only: ``forward`` enqueues ``ss_scan_fwd`` / ``ss_layer_fwd`` and keeps the
 workspace the library filled, ``backward`` enqueues ``ss_scan_bwd`` / ``ss_layer_bwd``; all
@@ -84,3 +84,52 @@ def selective_ssm_layer(x, z, conv_w, conv_b, W_x, W_dt, dt_bias, A, Dskip):
     """Differentiable layer around the scan: conv + SiLU, Delta/B/C projections, scan, gate (Section 3.4,
     Algorithm 2); only x, z, the small projection output and the scan's checkpoints are kept for backward."""
     return _SelectiveSSMLayer.apply(x, z, conv_w, conv_b, W_x, W_dt, dt_bias, A, Dskip)
+
+
+class _LayerNorm(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, weight, bias, residual, eps):
+        out, summed, stats = B.ss_norm_fwd(x, weight, bias, residual=residual, eps=eps, save_stats=True)
+        ctx.save_for_backward(x if summed is None else summed, weight, stats)
+        ctx.opts = (bias is not None, None if residual is None else residual.dtype, eps, x.dtype)
+        ctx.set_materialize_grads(False)
+        return out if summed is None else (out, summed)
+
+    @staticmethod
+    def backward(ctx, dout, dsummed=None):
+        s, weight, stats = ctx.saved_tensors
+        has_bias, held, eps, io = ctx.opts
+        if dout is None:   # only the sum was used
+            return (None if dsummed is None else dsummed.to(io)), None, None, dsummed, None
+        g = B.ss_norm_bwd(dout.contiguous(), s, stats, weight, has_bias=has_bias, residual_dtype=held, eps=eps,
+                          dsummed=None if dsummed is None else dsummed.contiguous())
+        return g["dx"], g["dweight"], g["dbias"], g["dresidual"], None
+
+
+def layer_norm(x, weight=None, bias=None, residual=None, eps=1e-5):
+    """Differentiable layer norm over the last axis.  With ``residual`` (float32 or x's dtype) the sum of the two is normalised
+    and returned as well, in residual's dtype: (out, summed), the residual stream that the next block continues."""
+    return _LayerNorm.apply(x, weight, bias, residual, eps)
+
+
+class _GatedRecurrence(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, f, rate, i, z, f_bias, i_bias, reset, h0, return_last_state):
+        ws = torch.empty(max(256, B.ss_gate_workspace_bytes(*x.shape)), dtype=torch.uint8, device=x.device)
+        out, h_last = B.ss_gate_fwd(x, f, rate, i=i, z=z, f_bias=f_bias, i_bias=i_bias, reset=reset, h0=h0,
+                                    return_last_state=return_last_state, workspace=ws, save_for_bwd=True)
+        ctx.save_for_backward(x, f, rate, i, z, f_bias, i_bias, reset, h0, ws)
+        return (out, h_last) if return_last_state else out
+
+    @staticmethod
+    def backward(ctx, dout, dh_last=None):
+        x, f, rate, i, z, f_bias, i_bias, reset, h0, ws = ctx.saved_tensors
+        g = B.ss_gate_bwd(dout.contiguous(), x, f, rate, ws, i=i, z=z, f_bias=f_bias, i_bias=i_bias, reset=reset, h0=h0,
+                          dh_last=None if dh_last is None else dh_last.contiguous(), want_dh0=h0 is not None)
+        return g["dx"], g["df"], g["drate"], g["di"], g["dz"], g["df_bias"], g["di_bias"], None, g["dh0"], None
+
+
+def gated_recurrence(x, f, rate, i=None, z=None, f_bias=None, i_bias=None, reset=None, h0=None, return_last_state=False):
+    """Differentiable gated linear recurrence (include/ss_gate.h): h <- a h + sqrt(1 - a^2) sigmoid(i) x with
+    a = exp(-rate sigmoid(f)), gated by SiLU(z).  Returns out, or (out, h_last) with ``return_last_state``."""
+    return _GatedRecurrence.apply(x, f, rate, i, z, f_bias, i_bias, reset, h0, return_last_state)

@@ -1,4 +1,5 @@
-"""Thin binding (ctypes, and a compiled module for the hot calls) of the C-ABI library declared in ``include/ss_scan.h``, ``include/ss_conv.h`` and ``include/ss_layer.h``.
+"""Thin binding (ctypes, and a compiled module for the hot calls) of the C-ABI library declared in the headers of ``include/`` (``ss_scan.h``, ``ss_conv.h``, ``ss_layer.h``,
+``ss_norm.h``, ``ss_gate.h``, ``ss_quant.h``).
 
 Argument marshalling only: every step of the path runs in the library's HIP kernels.
 PyTorch appears here solely as the owner of device memory and streams.  The library must
@@ -112,10 +113,58 @@ class GemmParams(ctypes.Structure):
                 ("workspace", _vp), ("workspace_bytes", ctypes.c_size_t)]
 
 
+class NormParams(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int32), ("width", ctypes.c_int32), ("io_dtype", ctypes.c_int32), ("flags", ctypes.c_uint32),
+                ("eps", ctypes.c_float), ("x", _vp), ("residual", _vp), ("weight", _vp), ("bias", _vp), ("out", _vp),
+                ("summed", _vp), ("stats", _vp)]
+
+
+class NormBwdParams(ctypes.Structure):
+    _fields_ = [("fwd", NormParams), ("dout", _vp), ("dsummed", _vp), ("dx", _vp), ("dresidual", _vp),
+                ("dweight", _vp), ("dbias", _vp), ("workspace", _vp), ("workspace_bytes", ctypes.c_size_t)]
+
+
+class GateParams(ctypes.Structure):
+    _fields_ = [("batch", ctypes.c_int32), ("dim", ctypes.c_int32), ("seqlen", ctypes.c_int32), ("io_dtype", ctypes.c_int32),
+                ("flags", ctypes.c_uint32), ("x", _vp), ("f", _vp), ("i", _vp), ("z", _vp),
+                ("x_batch", ctypes.c_int64), ("f_batch", ctypes.c_int64), ("i_batch", ctypes.c_int64), ("z_batch", ctypes.c_int64),
+                ("rate", _vp), ("f_bias", _vp), ("i_bias", _vp), ("reset", _vp), ("h0", _vp), ("out", _vp), ("h_last", _vp),
+                ("workspace", _vp), ("workspace_bytes", ctypes.c_size_t)]
+
+
+class GateBwdParams(ctypes.Structure):
+    _fields_ = [("fwd", GateParams), ("dout", _vp), ("dh_last", _vp), ("dx", _vp), ("df", _vp), ("di", _vp), ("dz", _vp),
+                ("dx_batch", ctypes.c_int64), ("df_batch", ctypes.c_int64), ("di_batch", ctypes.c_int64), ("dz_batch", ctypes.c_int64),
+                ("drate", _vp), ("df_bias", _vp), ("di_bias", _vp), ("dh0", _vp)]
+
+
+class GateStepParams(ctypes.Structure):
+    _fields_ = [("batch", ctypes.c_int32), ("dim", ctypes.c_int32), ("io_dtype", ctypes.c_int32), ("flags", ctypes.c_uint32),
+                ("h", _vp), ("x_t", _vp), ("f_t", _vp), ("i_t", _vp), ("z_t", _vp),
+                ("x_batch", ctypes.c_int64), ("f_batch", ctypes.c_int64), ("i_batch", ctypes.c_int64), ("z_batch", ctypes.c_int64),
+                ("rate", _vp), ("f_bias", _vp), ("i_bias", _vp), ("reset_t", _vp), ("out_t", _vp)]
+
+
+class QuantParams(ctypes.Structure):
+    _fields_ = [("batch", ctypes.c_int32), ("seqlen", ctypes.c_int32), ("dim", ctypes.c_int32), ("io_dtype", ctypes.c_int32),
+                ("flags", ctypes.c_uint32), ("x", _vp), ("q", _vp), ("scale", _vp), ("scratch", _vp), ("scratch_bytes", ctypes.c_size_t)]
+
+
+class QLinearParams(ctypes.Structure):
+    _fields_ = [("batch", ctypes.c_int32), ("seqlen", ctypes.c_int32), ("dim", ctypes.c_int32), ("features", ctypes.c_int32),
+                ("io_dtype", ctypes.c_int32), ("flags", ctypes.c_uint32), ("x", _vp), ("x_scale", _vp), ("weight", _vp),
+                ("scale", _vp), ("bias", _vp), ("out", _vp), ("scratch", _vp), ("scratch_bytes", ctypes.c_size_t)]
+
+
 SS_GEMM_C_FLOAT, SS_GEMM_ACCUMULATE, SS_GEMM_GENERAL = 1, 2, 4
 SS_ERR_BACKEND = -7
 SS_CONV_SILU, SS_CONV_HAS_BIAS, SS_CONV_HAS_STATE, SS_CONV_WRITE_STATE = 1, 2, 4, 8
 SS_CONV_MAX_WIDTH = 4
+SS_NORM_HAS_WEIGHT, SS_NORM_HAS_BIAS, SS_NORM_HAS_RESIDUAL, SS_NORM_RESIDUAL_F32, SS_NORM_SAVE_STATS = 1, 2, 4, 8, 16
+SS_GATE_HAS_I, SS_GATE_HAS_Z, SS_GATE_HAS_F_BIAS, SS_GATE_HAS_I_BIAS = 1, 2, 4, 8
+SS_GATE_HAS_RESET, SS_GATE_HAS_H0, SS_GATE_WRITE_H_LAST, SS_GATE_SAVE_FOR_BWD = 16, 32, 64, 128
+SS_Q_X_SEQ_LAST, SS_Q_OUT_SEQ_LAST, SS_Q_HAS_BIAS, SS_Q_X_QUANTISED = 1, 2, 4, 8
+SS_QUANT_MAX_DIM = 131072
 
 _lib = None
 
@@ -162,6 +211,17 @@ def lib():
         l.ss_proj_gemm_workspace_bytes.argtypes = [ctypes.POINTER(GemmParams)]
         l.ss_proj_gemm_workspace_bytes.restype = ctypes.c_size_t
         l.ss_strerror.argtypes = [ctypes.c_int]
+        for name, params in (("ss_norm_fwd", NormParams), ("ss_norm_bwd", NormBwdParams), ("ss_gate_fwd", GateParams),
+                             ("ss_gate_bwd", GateBwdParams), ("ss_gate_step", GateStepParams), ("ss_quant_rows", QuantParams),
+                             ("ss_qlinear", QLinearParams)):
+            getattr(l, name).restype = ctypes.c_int
+            getattr(l, name).argtypes = [ctypes.POINTER(params), _vp]
+        for name, args in (("ss_norm_workspace_bytes", [ctypes.POINTER(NormParams)]),
+                           ("ss_gate_workspace_bytes", [ctypes.POINTER(GateParams), ctypes.c_int]),
+                           ("ss_quant_rows_scratch_bytes", [ctypes.POINTER(QuantParams)]),
+                           ("ss_qlinear_scratch_bytes", [ctypes.POINTER(QLinearParams)]), ("ss_quant_pitch", [ctypes.c_int32])):
+            getattr(l, name).restype = ctypes.c_size_t
+            getattr(l, name).argtypes = args
         l.ss_version.restype = ctypes.c_int
         l.ss_version.argtypes = []
         _lib = l
@@ -771,3 +831,347 @@ def ss_proj_gemm_workspace_bytes(C):
     p.M, p.N = C.shape[-2], C.shape[-1]
     p.batch = C.shape[0] if C.dim() == 3 else 1
     return int(lib().ss_proj_gemm_workspace_bytes(ctypes.byref(p)))
+
+
+# ---------------------------------------------------------------- layer norm
+def _check(rc):
+    if rc != SS_OK:
+        raise SsError(rc)
+
+
+def _bytes(n, device):
+    return torch.empty(max(256, n), dtype=torch.uint8, device=device)
+
+
+def _lend(given, need, device, name):
+    """The caller's scratch tensor, or one of our own."""
+    if given is None:
+        given = _bytes(need, device)
+    return _ptr(given, torch.uint8, None, name), given.numel()
+
+
+def _norm_params(x, weight, bias, residual, eps):
+    f32 = torch.float32
+    p = NormParams()
+    width = x.shape[-1]
+    p.rows, p.width = (x.numel() // width if width else 0), width
+    p.eps = eps
+    if weight is not None:
+        p.weight = _ptr(weight, f32, (width,), "weight")
+        p.flags |= SS_NORM_HAS_WEIGHT
+    if bias is not None:
+        p.bias = _ptr(bias, f32, (width,), "bias")
+        p.flags |= SS_NORM_HAS_BIAS
+    if residual is not None:
+        if residual.dtype != torch.float32 and residual.dtype != x.dtype:
+            raise TypeError("residual must be float32 or of x's dtype, got %s" % residual.dtype)
+        p.flags |= SS_NORM_HAS_RESIDUAL | (SS_NORM_RESIDUAL_F32 if residual.dtype == torch.float32 else 0)
+    return p
+
+
+def ss_norm_fwd(x, weight=None, bias=None, residual=None, eps=1e-5, out=None, summed=None, save_stats=False, stream=None):
+    """Enqueue layer norm over the last axis, of ``x`` or of ``x + residual`` (float32 or of x's dtype; the sum is held in its
+    dtype and normalised as held).  Returns (out, summed or None, stats or None); ``summed`` may be given as ``residual`` itself,
+    ``stats`` (2, rows) is what ``ss_norm_bwd`` needs."""
+    p = _norm_params(x, weight, bias, residual, eps)
+    p.io_dtype = _io_code(x)
+    p.x = _ptr(x, None, None, "x")
+    if out is None:
+        out = torch.empty_like(x)
+    p.out = _ptr(out, x.dtype, x.shape, "out")
+    if residual is not None:
+        p.residual = _ptr(residual, None, x.shape, "residual")
+        if summed is None:
+            summed = torch.empty_like(residual)
+        p.summed = _ptr(summed, residual.dtype, x.shape, "summed")
+    elif summed is not None:
+        raise ValueError("summed is given, residual is not")
+    stats = None
+    if save_stats:
+        stats = torch.empty((2, p.rows), dtype=torch.float32, device=x.device)
+        p.stats = stats.data_ptr()
+        p.flags |= SS_NORM_SAVE_STATS
+    _check(lib().ss_norm_fwd(ctypes.byref(p), _stream(stream)))
+    return out, summed, stats
+
+
+def ss_norm_workspace_bytes(rows, width):
+    p = NormParams()
+    p.rows, p.width = rows, width
+    return int(lib().ss_norm_workspace_bytes(ctypes.byref(p)))
+
+
+def ss_norm_bwd(dout, s, stats, weight=None, has_bias=False, residual_dtype=None, dsummed=None, eps=1e-5, workspace=None, stream=None):
+    """Enqueue the backward pass.  ``s`` is what was normalised (``summed``, or ``x`` of a call without a residual, with
+    ``residual_dtype`` None) and ``dsummed`` the gradient that reaches the sum from behind, or None.  Returns a dict with dx,
+    dresidual (dx itself where the dtypes agree), dweight and dbias."""
+    p = NormBwdParams()
+    p.fwd = _norm_params(dout, weight, None, None, eps)
+    p.fwd.io_dtype = _io_code(dout)
+    held = dout.dtype if residual_dtype is None else residual_dtype
+    if has_bias:
+        p.fwd.flags |= SS_NORM_HAS_BIAS
+    if residual_dtype is not None:
+        if held != torch.float32 and held != dout.dtype:
+            raise TypeError("residual_dtype must be float32 or dout's dtype, got %s" % held)
+        p.fwd.flags |= SS_NORM_HAS_RESIDUAL | (SS_NORM_RESIDUAL_F32 if held == torch.float32 else 0)
+        p.fwd.summed = _ptr(s, held, dout.shape, "s")
+        p.dsummed = _ptr(dsummed, held, dout.shape, "dsummed")
+    else:
+        if dsummed is not None:
+            raise ValueError("dsummed without a residual")
+        p.fwd.x = _ptr(s, held, dout.shape, "s")
+    p.fwd.stats = _ptr(stats, torch.float32, (2, p.fwd.rows), "stats")
+    p.dout = _ptr(dout, None, None, "dout")
+    dev, width = dout.device, p.fwd.width
+    g = {"dx": torch.empty_like(dout), "dresidual": None,
+         "dweight": torch.empty(width, dtype=torch.float32, device=dev) if weight is not None else None,
+         "dbias": torch.empty(width, dtype=torch.float32, device=dev) if has_bias else None}
+    if residual_dtype is not None:
+        g["dresidual"] = g["dx"] if held == dout.dtype else torch.empty(dout.shape, dtype=held, device=dev)
+        if held != dout.dtype:
+            p.dresidual = g["dresidual"].data_ptr()
+    p.dx = g["dx"].data_ptr()
+    p.dweight, p.dbias = (None if g[k] is None else g[k].data_ptr() for k in ("dweight", "dbias"))
+    need = int(lib().ss_norm_workspace_bytes(ctypes.byref(p.fwd)))
+    p.workspace, p.workspace_bytes = _lend(workspace, need, dev, "workspace")
+    _check(lib().ss_norm_bwd(ctypes.byref(p), _stream(stream)))
+    return g
+
+
+# ---------------------------------------------------------------- gated linear recurrence
+def _rows_of(t, io, shape, name):
+    """(pointer, elements between batch entries) of a tensor whose batch entries are dense: a slice of a wider one along dim 1 is."""
+    if t is None:
+        return None, 0
+    if not t.is_cuda:
+        raise ValueError("%s must live on the GPU" % name)
+    if t.dtype != io:
+        raise TypeError("%s must be %s, got %s" % (name, io, t.dtype))
+    if tuple(t.shape) != tuple(shape):
+        raise ValueError("%s must have shape %s, got %s" % (name, tuple(shape), tuple(t.shape)))
+    dense = 1
+    for n in shape[1:]:
+        dense *= n
+    if t.is_contiguous():
+        return t.data_ptr(), dense
+    if not t[0].is_contiguous() or t.stride(0) < dense:
+        raise ValueError("the batch entries of %s must be contiguous and not overlap" % name)
+    return t.data_ptr(), t.stride(0)
+
+
+def _gate_inputs(p, x, f, i, z, rate, f_bias, i_bias, names=("x", "f", "i", "z")):
+    f32, shape, io = torch.float32, x.shape, x.dtype
+    p.batch, p.dim = shape[0], shape[1]
+    p.io_dtype = _io_code(x)
+    for name, t in zip(names, (x, f, i, z)):
+        ptr, batch = _rows_of(t, io, shape, name)
+        setattr(p, name, ptr)
+        setattr(p, name[0] + "_batch", batch)
+    flags = (SS_GATE_HAS_I if i is not None else 0) | (SS_GATE_HAS_Z if z is not None else 0)
+    p.rate = _ptr(rate, f32, (shape[1],), "rate")
+    if f_bias is not None:
+        p.f_bias = _ptr(f_bias, f32, (shape[1],), "f_bias")
+        flags |= SS_GATE_HAS_F_BIAS
+    if i_bias is not None:
+        if i is None:
+            raise ValueError("i_bias is given, i is not")
+        p.i_bias = _ptr(i_bias, f32, (shape[1],), "i_bias")
+        flags |= SS_GATE_HAS_I_BIAS
+    p.flags = flags
+    return p
+
+
+def _marks(reset, shape, name):
+    if reset.dtype is not torch.bool and reset.dtype is not torch.uint8:
+        raise TypeError("%s must be bool or uint8, got %s" % (name, reset.dtype))
+    return _ptr(reset, None, shape, name)
+
+
+def _gate_params(x, f, rate, i, z, f_bias, i_bias, reset, h0):
+    p = _gate_inputs(GateParams(), x, f, i, z, rate, f_bias, i_bias)
+    nb, nd, nl = x.shape
+    p.seqlen = nl
+    if reset is not None:
+        p.reset = _marks(reset, (nb, nl), "reset")
+        p.flags |= SS_GATE_HAS_RESET
+    if h0 is not None:
+        p.h0 = _ptr(h0, torch.float32, (nb, nd), "h0")
+        p.flags |= SS_GATE_HAS_H0
+    return p
+
+
+def ss_gate_workspace_bytes(batch, dim, seqlen, for_backward=True):
+    p = GateParams()
+    p.batch, p.dim, p.seqlen = batch, dim, seqlen
+    return int(lib().ss_gate_workspace_bytes(ctypes.byref(p), int(bool(for_backward))))
+
+
+def ss_gate_fwd(x, f, rate, i=None, z=None, f_bias=None, i_bias=None, reset=None, h0=None, out=None, h_last=None,
+                return_last_state=False, workspace=None, save_for_bwd=False, stream=None):
+    """Enqueue the gated linear recurrence.  Returns (out, h_last or None).
+
+    x, f, i, z are (B,D,L), each dense or a slice along dim 1 of a wider tensor; rate, f_bias, i_bias (D) float32; ``reset`` (B,L)
+    bool or uint8, not 0 where a sequence begins; h0 (B,D) float32.  ``workspace``: a uint8 tensor of
+    ``ss_gate_workspace_bytes`` bytes; with ``save_for_bwd`` it is filled for ``ss_gate_bwd``, without it serves as
+    scratch (one of the call's own if not given)."""
+    p = _gate_params(x, f, rate, i, z, f_bias, i_bias, reset, h0)
+    if out is None:
+        out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+    p.out = _ptr(out, x.dtype, x.shape, "out")
+    if return_last_state or h_last is not None:
+        if h_last is None:
+            h_last = torch.empty((p.batch, p.dim), dtype=torch.float32, device=x.device)
+        p.h_last = _ptr(h_last, torch.float32, (p.batch, p.dim), "h_last")
+        p.flags |= SS_GATE_WRITE_H_LAST
+    if save_for_bwd:
+        if workspace is None:
+            raise ValueError("save_for_bwd needs a workspace")
+        p.flags |= SS_GATE_SAVE_FOR_BWD
+    need = int(lib().ss_gate_workspace_bytes(ctypes.byref(p), 0))
+    if workspace is not None or need:
+        p.workspace, p.workspace_bytes = _lend(workspace, need, x.device, "workspace")
+    _check(lib().ss_gate_fwd(ctypes.byref(p), _stream(stream)))
+    return out, h_last
+
+
+def ss_gate_bwd(dout, x, f, rate, workspace, i=None, z=None, f_bias=None, i_bias=None, reset=None, h0=None, dh_last=None,
+                want_dh0=False, grads=None, stream=None):
+    """Enqueue the backward pass after a forward call that filled ``workspace``.  Returns a dict with dx, df, di, dz, drate,
+    df_bias, di_bias, dh0 (None where the input was not given).  ``grads``: tensors under these names to write into
+    instead of new ones; dx, df, di and dz may be slices along dim 1 of a wider tensor."""
+    f32 = torch.float32
+    q = GateBwdParams()
+    q.fwd = _gate_params(x, f, rate, i, z, f_bias, i_bias, reset, h0)
+    q.fwd.workspace = _ptr(workspace, torch.uint8, None, "workspace")
+    q.fwd.workspace_bytes = workspace.numel()
+    q.dout = _ptr(dout, x.dtype, x.shape, "dout")
+    state = (q.fwd.batch, q.fwd.dim)
+    q.dh_last = _ptr(dh_last, f32, state, "dh_last")
+    need = {"dx": True, "df": True, "di": i is not None, "dz": z is not None, "drate": True, "df_bias": f_bias is not None,
+            "di_bias": i_bias is not None, "dh0": want_dh0}
+    shapes = {"dx": x.shape, "df": x.shape, "di": x.shape, "dz": x.shape, "drate": state[1:], "df_bias": state[1:],
+              "di_bias": state[1:], "dh0": state}
+    g = {}
+    for name, wanted in need.items():
+        t = None if grads is None else grads.get(name)
+        if t is not None and not wanted:
+            raise ValueError("grads[%r] given but that gradient is not produced" % name)
+        io = x.dtype if name in ("dx", "df", "di", "dz") else f32
+        if wanted and t is None:
+            t = torch.empty(shapes[name], dtype=io, device=x.device)
+        g[name] = t
+        if name in ("dx", "df", "di", "dz"):
+            ptr, batch = _rows_of(t, io, shapes[name], name)
+            setattr(q, name, ptr)
+            setattr(q, name + "_batch", batch)
+        else:
+            setattr(q, name, _ptr(t, io, shapes[name], name))
+    _check(lib().ss_gate_bwd(ctypes.byref(q), _stream(stream)))
+    return g
+
+
+def ss_gate_step(h, x_t, f_t, rate, i_t=None, z_t=None, f_bias=None, i_bias=None, reset_t=None, out_t=None, stream=None):
+    """Enqueue one token of the recurrence; ``h`` (B,D) float32 is updated in place.  x_t, f_t, i_t, z_t are (B,D), each dense or
+    a slice along dim 1; ``reset_t`` (B) marks entries whose sequence begins with this token.  Returns out_t."""
+    p = _gate_inputs(GateStepParams(), x_t, f_t, i_t, z_t, rate, f_bias, i_bias, ("x_t", "f_t", "i_t", "z_t"))
+    p.h = _ptr(h, torch.float32, x_t.shape, "h")
+    if reset_t is not None:
+        p.reset_t = _marks(reset_t, (p.batch,), "reset_t")
+        p.flags |= SS_GATE_HAS_RESET
+    if out_t is None:
+        out_t = torch.empty(x_t.shape, dtype=x_t.dtype, device=x_t.device)
+    p.out_t = _ptr(out_t, x_t.dtype, x_t.shape, "out_t")
+    _check(lib().ss_gate_step(ctypes.byref(p), _stream(stream)))
+    return out_t
+
+
+# ---------------------------------------------------------------- products in 8-bit integers
+def ss_quant_pitch(dim):
+    """Bytes from one quantised row of ``dim`` values to the next."""
+    return int(lib().ss_quant_pitch(dim))
+
+
+def ss_quant_rows(x, seq_last=False, scratch=None, stream=None):
+    """Enqueue the quantiser: (q, scale) of the rows of ``x`` (..., K), or with ``seq_last`` of the tokens of ``x`` (B,K,L).
+    q is (rows, ss_quant_pitch(K)) int8, scale (rows) float32; a weight (features, K) is brought to 8 bits the same way."""
+    p = QuantParams()
+    if seq_last:
+        p.batch, p.dim, p.seqlen = x.shape
+        p.flags = SS_Q_X_SEQ_LAST
+    else:
+        p.dim = x.shape[-1]
+        p.batch, p.seqlen = 1, x.numel() // max(1, p.dim)
+    p.io_dtype = _io_code(x)
+    p.x = _ptr(x, None, None, "x")
+    rows = p.batch * p.seqlen
+    q = torch.empty((rows, ss_quant_pitch(p.dim)), dtype=torch.int8, device=x.device)
+    scale = torch.empty(rows, dtype=torch.float32, device=x.device)
+    p.q, p.scale = q.data_ptr(), scale.data_ptr()
+    need = int(lib().ss_quant_rows_scratch_bytes(ctypes.byref(p)))
+    if need:
+        p.scratch, p.scratch_bytes = _lend(scratch, need, x.device, "scratch")
+    _check(lib().ss_quant_rows(ctypes.byref(p), _stream(stream)))
+    return q, scale
+
+
+def _qlinear_sizes(batch, seqlen, dim, features, x_seq_last, out_seq_last, quantised):
+    p = QLinearParams()
+    p.batch, p.seqlen, p.dim, p.features = batch, seqlen, dim, features
+    p.flags = ((SS_Q_X_SEQ_LAST if x_seq_last else 0) | (SS_Q_OUT_SEQ_LAST if out_seq_last else 0)
+               | (SS_Q_X_QUANTISED if quantised else 0))
+    return p
+
+
+def ss_qlinear_scratch_bytes(batch, seqlen, dim, features, x_seq_last=False, out_seq_last=False, quantised=False):
+    p = _qlinear_sizes(batch, seqlen, dim, features, x_seq_last, out_seq_last, quantised)
+    return int(lib().ss_qlinear_scratch_bytes(ctypes.byref(p)))
+
+
+def ss_qlinear(x, weight, scale, bias=None, x_seq_last=False, out_seq_last=False, x_scale=None, dim=None, out_dtype=None, out=None,
+               scratch=None, stream=None):
+    """Enqueue tokens times a weight held in 8 bits (``ss_quant_rows`` of it).  ``x`` is (..., K), with ``x_seq_last`` (B,K,L);
+    the result (..., features), with ``out_seq_last`` (B,features,L), which takes x of three axes.  With ``x_scale`` x is itself
+    quantised, (rows, pitch) int8 or (B, L, pitch), of ``dim`` values each, and the result has ``out_dtype`` (bfloat16 unless
+    given).  ``scratch``: uint8 tensor of ``ss_qlinear_scratch_bytes`` bytes, or None: the call takes its own."""
+    if weight.dim() != 2:
+        raise ValueError("weight must have two axes")
+    quantised = x_scale is not None
+    lead = tuple(x.shape[:-1])
+    if x_seq_last or out_seq_last:
+        if x.dim() != 3:
+            raise ValueError("a sequence axis that comes last takes x of three axes")
+        batch, seqlen = (x.shape[0], x.shape[2]) if x_seq_last else x.shape[:2]
+    else:
+        batch, seqlen = 1, x.numel() // max(1, x.shape[-1])
+    if not quantised:
+        dim = x.shape[1] if x_seq_last else x.shape[-1]
+    elif dim is None:
+        raise ValueError("quantised tokens need dim")
+    features = weight.shape[0]
+    p = _qlinear_sizes(batch, seqlen, dim, features, x_seq_last, out_seq_last, quantised)
+    pitch = ss_quant_pitch(dim)
+    if quantised:
+        io = torch.bfloat16 if out_dtype is None else out_dtype
+        p.x = _ptr(x, torch.int8, lead + (pitch,), "x")
+        p.x_scale = _ptr(x_scale, torch.float32, (batch * seqlen,), "x_scale")
+    else:
+        io = x.dtype
+        if out_dtype is not None and out_dtype != io:
+            raise TypeError("the result has x's dtype")
+        p.x = _ptr(x, None, None, "x")
+    p.weight = _ptr(weight, torch.int8, (features, pitch), "weight")
+    p.scale = _ptr(scale, torch.float32, (features,), "scale")
+    if bias is not None:
+        p.bias = _ptr(bias, torch.float32, (features,), "bias")
+        p.flags |= SS_Q_HAS_BIAS
+    shape = (batch, features, seqlen) if out_seq_last else ((batch, seqlen) if x_seq_last else lead) + (features,)
+    if out is None:
+        out = torch.empty(shape, dtype=io, device=x.device)
+    p.io_dtype = _io_code(out)
+    p.out = _ptr(out, io, shape, "out")
+    need = int(lib().ss_qlinear_scratch_bytes(ctypes.byref(p)))
+    if need:
+        p.scratch, p.scratch_bytes = _lend(scratch, need, x.device, "scratch")
+    _check(lib().ss_qlinear(ctypes.byref(p), _stream(stream)))
+    return out
