@@ -237,6 +237,7 @@ class _NoMarshal:
         return None
 
     step = layer_step = scan_fwd = scan_bwd = layer_fwd = layer_bwd = staticmethod(_none)
+    norm_fwd = norm_bwd = gate_fwd = gate_bwd = gate_step = qlinear = staticmethod(_none)
 
 
 def _marshal():
@@ -873,6 +874,10 @@ def ss_norm_fwd(x, weight=None, bias=None, residual=None, eps=1e-5, out=None, su
     """Enqueue layer norm over the last axis, of ``x`` or of ``x + residual`` (float32 or of x's dtype; the sum is held in its
     dtype and normalised as held).  Returns (out, summed or None, stats or None); ``summed`` may be given as ``residual`` itself,
     ``stats`` (2, rows) is what ``ss_norm_bwd`` needs."""
+    if out is None and summed is None and x.is_cuda:
+        r = (_native or _marshal()).norm_fwd(x, weight, bias, residual, eps, bool(save_stats), _stream(stream))
+        if r is not None:
+            return _result(r)
     p = _norm_params(x, weight, bias, residual, eps)
     p.io_dtype = _io_code(x)
     p.x = _ptr(x, None, None, "x")
@@ -905,6 +910,10 @@ def ss_norm_bwd(dout, s, stats, weight=None, has_bias=False, residual_dtype=None
     """Enqueue the backward pass.  ``s`` is what was normalised (``summed``, or ``x`` of a call without a residual, with
     ``residual_dtype`` None) and ``dsummed`` the gradient that reaches the sum from behind, or None.  Returns a dict with dx,
     dresidual (dx itself where the dtypes agree), dweight and dbias."""
+    if workspace is None and dout.is_cuda and (residual_dtype is None or s.dtype == residual_dtype):
+        r = (_native or _marshal()).norm_bwd(dout, s, stats, weight, bool(has_bias), residual_dtype is not None, dsummed, eps, _stream(stream))
+        if r is not None:
+            return _result(r)
     p = NormBwdParams()
     p.fwd = _norm_params(dout, weight, None, None, eps)
     p.fwd.io_dtype = _io_code(dout)
@@ -1015,6 +1024,11 @@ def ss_gate_fwd(x, f, rate, i=None, z=None, f_bias=None, i_bias=None, reset=None
     bool or uint8, not 0 where a sequence begins; h0 (B,D) float32.  ``workspace``: a uint8 tensor of
     ``ss_gate_workspace_bytes`` bytes; with ``save_for_bwd`` it is filled for ``ss_gate_bwd``, without it serves as
     scratch (one of the call's own if not given)."""
+    if out is None and h_last is None and x.is_cuda:
+        r = (_native or _marshal()).gate_fwd(x, f, i, z, rate, f_bias, i_bias, reset, h0, workspace, bool(save_for_bwd), bool(return_last_state),
+                                             _stream(stream))
+        if r is not None:
+            return _result(r)
     p = _gate_params(x, f, rate, i, z, f_bias, i_bias, reset, h0)
     if out is None:
         out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
@@ -1040,6 +1054,10 @@ def ss_gate_bwd(dout, x, f, rate, workspace, i=None, z=None, f_bias=None, i_bias
     """Enqueue the backward pass after a forward call that filled ``workspace``.  Returns a dict with dx, df, di, dz, drate,
     df_bias, di_bias, dh0 (None where the input was not given).  ``grads``: tensors under these names to write into
     instead of new ones; dx, df, di and dz may be slices along dim 1 of a wider tensor."""
+    if grads is None and x.is_cuda:
+        r = (_native or _marshal()).gate_bwd(x, f, i, z, rate, f_bias, i_bias, reset, h0, workspace, dout, dh_last, bool(want_dh0), _stream(stream))
+        if r is not None:
+            return _result(r)
     f32 = torch.float32
     q = GateBwdParams()
     q.fwd = _gate_params(x, f, rate, i, z, f_bias, i_bias, reset, h0)
@@ -1074,6 +1092,10 @@ def ss_gate_bwd(dout, x, f, rate, workspace, i=None, z=None, f_bias=None, i_bias
 def ss_gate_step(h, x_t, f_t, rate, i_t=None, z_t=None, f_bias=None, i_bias=None, reset_t=None, out_t=None, stream=None):
     """Enqueue one token of the recurrence; ``h`` (B,D) float32 is updated in place.  x_t, f_t, i_t, z_t are (B,D), each dense or
     a slice along dim 1; ``reset_t`` (B) marks entries whose sequence begins with this token.  Returns out_t."""
+    if x_t.is_cuda:
+        r = (_native or _marshal()).gate_step(x_t, f_t, i_t, z_t, rate, f_bias, i_bias, reset_t, h, out_t, _stream(stream))
+        if r is not None:
+            return _result(r)
     p = _gate_inputs(GateStepParams(), x_t, f_t, i_t, z_t, rate, f_bias, i_bias, ("x_t", "f_t", "i_t", "z_t"))
     p.h = _ptr(h, torch.float32, x_t.shape, "h")
     if reset_t is not None:
@@ -1134,6 +1156,11 @@ def ss_qlinear(x, weight, scale, bias=None, x_seq_last=False, out_seq_last=False
     the result (..., features), with ``out_seq_last`` (B,features,L), which takes x of three axes.  With ``x_scale`` x is itself
     quantised, (rows, pitch) int8 or (B, L, pitch), of ``dim`` values each, and the result has ``out_dtype`` (bfloat16 unless
     given).  ``scratch``: uint8 tensor of ``ss_qlinear_scratch_bytes`` bytes, or None: the call takes its own."""
+    if x_scale is None and out is None and scratch is None and out_dtype is None and x.is_cuda:
+        r = (_native or _marshal()).qlinear(x, weight, scale, bias, (SS_Q_X_SEQ_LAST if x_seq_last else 0) | (SS_Q_OUT_SEQ_LAST if out_seq_last else 0),
+                                            _stream(stream))
+        if r is not None:
+            return _result(r)
     if weight.dim() != 2:
         raise ValueError("weight must have two axes")
     quantised = x_scale is not None

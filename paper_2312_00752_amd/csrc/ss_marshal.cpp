@@ -14,7 +14,10 @@
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
 
+#include "ss_gate.h"
 #include "ss_layer.h"
+#include "ss_norm.h"
+#include "ss_quant.h"
 #include "ss_scan.h"
 
 namespace {
@@ -388,9 +391,379 @@ PyObject* py_layer_bwd(PyObject*, PyObject* const* argv, Py_ssize_t n)
     END_HANDLE_TH_ERRORS
 }
 
+// ---- layer norm, gated recurrence, 8-bit products --------------------------------------------------
+PyObject* wrapped_or_none(const at::Tensor& t)
+{
+    if (t.defined()) return wrapped(t);
+    Py_RETURN_NONE;
+}
+PyObject* tuple_of(std::initializer_list<at::Tensor> ts)
+{
+    PyObject* res = PyTuple_New((Py_ssize_t)ts.size());
+    if (!res) return nullptr;
+    Py_ssize_t i = 0;
+    for (const at::Tensor& t : ts) {
+        PyObject* o = wrapped_or_none(t);
+        if (!o) {
+            Py_DECREF(res);
+            return nullptr;
+        }
+        PyTuple_SET_ITEM(res, i++, o);
+    }
+    return res;
+}
+struct Named {
+    const char* name;
+    const at::Tensor& t;
+};
+PyObject* dict_of(std::initializer_list<Named> ts)
+{
+    PyObject* res = PyDict_New();
+    if (!res) return nullptr;
+    for (const Named& n : ts) {
+        PyObject* o = wrapped_or_none(n.t);
+        const bool good = o && PyDict_SetItemString(res, n.name, o) == 0;
+        Py_XDECREF(o);
+        if (!good) {
+            Py_DECREF(res);
+            return nullptr;
+        }
+    }
+    return res;
+}
+template <typename T = void>
+T* data(const at::Tensor& t) { return t.defined() ? static_cast<T*>(t.data_ptr()) : nullptr; }
+at::Tensor empty_bytes(size_t n, const at::Tensor& like)
+{
+    return at::empty({(int64_t)(n < 256 ? 256 : n)}, like.options().dtype(at::kByte).requires_grad(false));
+}
+at::Tensor empty_io(const at::Tensor& like) { return at::empty(like.sizes(), like.options().requires_grad(false)); }
+
+// rows and width of a tensor whose last axis is normalised
+bool norm_sizes(const at::Tensor& x, ss_norm_params& p)
+{
+    if (x.dim() < 1 || !io_type(x, p.io_dtype)) return false;
+    const int64_t width = x.size(-1), rows = width ? x.numel() / width : 0;
+    if (!fits(width) || !fits(rows)) return false;
+    p.rows = (int32_t)rows;
+    p.width = (int32_t)width;
+    return true;
+}
+// a tensor of x's shape held in float32 or in x's type
+const at::Tensor* held(Args& a, int i, const at::Tensor& x)
+{
+    const at::Tensor* t = a.tensor(i);
+    if (!t) return nullptr;
+    if (!t->sizes().equals(x.sizes()) || (t->scalar_type() != at::kFloat && t->scalar_type() != x.scalar_type())) {
+        a.ok = false;
+        return nullptr;
+    }
+    return t;
+}
+
+// norm_fwd(x, weight, bias, residual, eps, save, stream) -> (out, summed or None, stats or None)
+PyObject* py_norm_fwd(PyObject*, PyObject* const* argv, Py_ssize_t n)
+{
+    HANDLE_TH_ERRORS
+    if (n != 7) Py_RETURN_NONE;
+    Args a{argv};
+    ss_norm_params p{};
+    const at::Tensor* x = a.tensor(0);
+    if (!x || !norm_sizes(*x, p) || !PyFloat_CheckExact(argv[4])) Py_RETURN_NONE;
+    p.eps = (float)PyFloat_AS_DOUBLE(argv[4]);
+    p.x = x->data_ptr();
+    p.weight = static_cast<const float*>(a.ptr(1, at::kFloat, {p.width}, true));
+    p.bias = static_cast<const float*>(a.ptr(2, at::kFloat, {p.width}, true));
+    const at::Tensor* r = a.ok && !a.none(3) ? held(a, 3, *x) : nullptr;
+    void* stream = a.stream(6);
+    if (!a.ok) Py_RETURN_NONE;
+    if (p.weight) p.flags |= SS_NORM_HAS_WEIGHT;
+    if (p.bias) p.flags |= SS_NORM_HAS_BIAS;
+    at::Tensor out = empty_io(*x), summed, stats;
+    p.out = out.data_ptr();
+    if (r) {
+        p.flags |= SS_NORM_HAS_RESIDUAL | (r->scalar_type() == at::kFloat ? SS_NORM_RESIDUAL_F32 : 0u);
+        p.residual = r->data_ptr();
+        summed = empty_io(*r);
+        p.summed = summed.data_ptr();
+    }
+    if (argv[5] == Py_True) {
+        p.flags |= SS_NORM_SAVE_STATS;
+        stats = empty_f32({2, p.rows}, *x);
+        p.stats = data<float>(stats);
+    }
+    const int rc = call(ss_norm_fwd, p, stream);
+    if (rc != SS_OK) return PyLong_FromLong(rc);
+    return tuple_of({out, summed, stats});
+    END_HANDLE_TH_ERRORS
+}
+
+// norm_bwd(dout, s, stats, weight, has_bias, has_residual, dsummed, eps, stream) -> dict of gradients
+PyObject* py_norm_bwd(PyObject*, PyObject* const* argv, Py_ssize_t n)
+{
+    HANDLE_TH_ERRORS
+    if (n != 9) Py_RETURN_NONE;
+    Args a{argv};
+    ss_norm_bwd_params q{};
+    ss_norm_params& p = q.fwd;
+    const at::Tensor* dout = a.tensor(0);
+    if (!dout || !norm_sizes(*dout, p) || !PyFloat_CheckExact(argv[7])) Py_RETURN_NONE;
+    const bool res = argv[5] == Py_True;
+    const at::Tensor* s = held(a, 1, *dout);
+    if (!s || (!res && (s->scalar_type() != dout->scalar_type() || !a.none(6)))) Py_RETURN_NONE;
+    p.eps = (float)PyFloat_AS_DOUBLE(argv[7]);
+    p.stats = static_cast<float*>(a.ptr(2, at::kFloat, {2, p.rows}));
+    p.weight = static_cast<const float*>(a.ptr(3, at::kFloat, {p.width}, true));
+    const at::Tensor* more = a.ok && !a.none(6) ? held(a, 6, *dout) : nullptr;
+    void* stream = a.stream(8);
+    if (!a.ok || (more && more->scalar_type() != s->scalar_type())) Py_RETURN_NONE;
+    at::Tensor dx = empty_io(*dout), dresidual, dweight, dbias;
+    const bool two = res && s->scalar_type() != dout->scalar_type();
+    if (res) {
+        p.flags |= SS_NORM_HAS_RESIDUAL | (s->scalar_type() == at::kFloat ? SS_NORM_RESIDUAL_F32 : 0u);
+        p.summed = s->data_ptr();
+        dresidual = two ? empty_io(*s) : dx;
+    } else {
+        p.x = s->data_ptr();
+    }
+    if (p.weight) {
+        p.flags |= SS_NORM_HAS_WEIGHT;
+        dweight = empty_f32({p.width}, *dout);
+    }
+    if (argv[4] == Py_True) {
+        p.flags |= SS_NORM_HAS_BIAS;
+        dbias = empty_f32({p.width}, *dout);
+    }
+    q.dout = dout->data_ptr();
+    q.dsummed = more ? more->data_ptr() : nullptr;
+    q.dx = dx.data_ptr();
+    q.dresidual = two ? dresidual.data_ptr() : nullptr;
+    q.dweight = data<float>(dweight);
+    q.dbias = data<float>(dbias);
+    const at::Tensor ws = empty_bytes(ss_norm_workspace_bytes(&p), *dout);
+    q.workspace = ws.data_ptr();
+    q.workspace_bytes = (size_t)ws.numel();
+    const int rc = call(ss_norm_bwd, q, stream);
+    if (rc != SS_OK) return PyLong_FromLong(rc);
+    return dict_of({{"dx", dx}, {"dresidual", dresidual}, {"dweight", dweight}, {"dbias", dbias}});
+    END_HANDLE_TH_ERRORS
+}
+
+// A (B,D,L) or (B,D) tensor whose batch entries are dense.
+void* rows_of(Args& a, int i, at::ScalarType io, at::IntArrayRef shape, int64_t& batch)
+{
+    if (a.none(i) || !a.ok) return nullptr;
+    if (!THPVariable_CheckExact(a.a[i])) { a.ok = false; return nullptr; }
+    const at::Tensor& t = THPVariable_Unpack(a.a[i]);
+    if (!t.is_cuda() || !t.has_storage() || t.scalar_type() != io || !t.sizes().equals(shape)) { a.ok = false; return nullptr; }
+    int64_t dense = 1;
+    for (size_t k = shape.size(); k-- > 1;) {
+        if (shape[k] != 1 && t.stride((int64_t)k) != dense) { a.ok = false; return nullptr; }
+        dense *= shape[k];
+    }
+    batch = shape[0] == 1 ? dense : t.stride(0);
+    if (batch < dense) { a.ok = false; return nullptr; }
+    return t.data_ptr();
+}
+// x, f, i, z, rate, f_bias, i_bias from argument `at` on
+template <typename P>
+bool gate_inputs(Args& a, int at, const at::Tensor& x, P& p, const void*& px, const void*& pf, const void*& pi, const void*& pz)
+{
+    if (!io_type(x, p.io_dtype) || !fits(x.size(0)) || !fits(x.size(1))) return false;
+    const at::ScalarType io = x.scalar_type();
+    const int64_t nd = x.size(1);
+    p.batch = (int32_t)x.size(0);
+    p.dim = (int32_t)nd;
+    px = rows_of(a, at, io, x.sizes(), p.x_batch);
+    pf = rows_of(a, at + 1, io, x.sizes(), p.f_batch);
+    pi = rows_of(a, at + 2, io, x.sizes(), p.i_batch);
+    pz = rows_of(a, at + 3, io, x.sizes(), p.z_batch);
+    p.rate = static_cast<const float*>(a.ptr(at + 4, at::kFloat, {nd}));
+    p.f_bias = static_cast<const float*>(a.ptr(at + 5, at::kFloat, {nd}, true));
+    p.i_bias = static_cast<const float*>(a.ptr(at + 6, at::kFloat, {nd}, true));
+    if (!a.ok || a.none(at + 1) || (a.none(at + 2) && !a.none(at + 6))) return false;
+    p.flags |= (a.none(at + 2) ? 0u : SS_GATE_HAS_I) | (a.none(at + 3) ? 0u : SS_GATE_HAS_Z) | (a.none(at + 5) ? 0u : SS_GATE_HAS_F_BIAS) |
+               (a.none(at + 6) ? 0u : SS_GATE_HAS_I_BIAS);
+    return true;
+}
+const uint8_t* marks_of(Args& a, int i, Shape shape)
+{
+    if (a.none(i) || !a.ok) return nullptr;
+    const at::Tensor* t = a.tensor(i);
+    if (!t) return nullptr;
+    if ((t->scalar_type() != at::kBool && t->scalar_type() != at::kByte) || !t->sizes().equals(at::IntArrayRef(shape))) {
+        a.ok = false;
+        return nullptr;
+    }
+    return static_cast<const uint8_t*>(t->data_ptr());
+}
+const at::Tensor* gate_x(Args& a, int i, int64_t dim)
+{
+    if (!THPVariable_CheckExact(a.a[i])) return nullptr;
+    const at::Tensor& x = THPVariable_Unpack(a.a[i]);
+    return x.is_cuda() && x.dim() == dim ? &x : nullptr;
+}
+// x, f, i, z, rate, f_bias, i_bias, reset, h0
+bool gate_all(Args& a, int at, const at::Tensor& x, ss_gate_params& p)
+{
+    if (!fits(x.size(2)) || !gate_inputs(a, at, x, p, p.x, p.f, p.i, p.z)) return false;
+    p.seqlen = (int32_t)x.size(2);
+    p.reset = marks_of(a, at + 7, {x.size(0), x.size(2)});
+    p.h0 = static_cast<const float*>(a.ptr(at + 8, at::kFloat, {x.size(0), x.size(1)}, true));
+    p.flags |= (a.none(at + 7) ? 0u : SS_GATE_HAS_RESET) | (a.none(at + 8) ? 0u : SS_GATE_HAS_H0);
+    return a.ok;
+}
+
+// gate_fwd(x, f, i, z, rate, f_bias, i_bias, reset, h0, workspace, save, want_last, stream) -> (out, h_last or None)
+PyObject* py_gate_fwd(PyObject*, PyObject* const* argv, Py_ssize_t n)
+{
+    HANDLE_TH_ERRORS
+    if (n != 13) Py_RETURN_NONE;
+    Args a{argv};
+    ss_gate_params p{};
+    const at::Tensor* x = gate_x(a, 0, 3);
+    void* stream = a.stream(12);
+    if (!x || !a.ok || !gate_all(a, 0, *x, p)) Py_RETURN_NONE;
+    at::Tensor ws;
+    const bool save = argv[10] == Py_True;
+    if (!a.none(9)) {
+        const at::Tensor* t = a.tensor(9);
+        if (!t || t->scalar_type() != at::kByte) Py_RETURN_NONE;
+        ws = *t;
+    } else if (save) {
+        Py_RETURN_NONE;
+    } else {
+        const size_t need = ss_gate_workspace_bytes(&p, 0);
+        if (need) ws = empty_bytes(need, *x);
+    }
+    if (ws.defined()) {
+        p.workspace = ws.data_ptr();
+        p.workspace_bytes = (size_t)ws.numel();
+    }
+    if (save) p.flags |= SS_GATE_SAVE_FOR_BWD;
+    at::Tensor out = empty_io(*x), h_last;
+    p.out = out.data_ptr();
+    if (argv[11] == Py_True) {
+        h_last = empty_f32({p.batch, p.dim}, *x);
+        p.h_last = data<float>(h_last);
+        p.flags |= SS_GATE_WRITE_H_LAST;
+    }
+    const int rc = call(ss_gate_fwd, p, stream);
+    if (rc != SS_OK) return PyLong_FromLong(rc);
+    return tuple_of({out, h_last});
+    END_HANDLE_TH_ERRORS
+}
+
+// gate_bwd(x, f, i, z, rate, f_bias, i_bias, reset, h0, workspace, dout, dh_last, want_dh0, stream) -> dict of gradients
+PyObject* py_gate_bwd(PyObject*, PyObject* const* argv, Py_ssize_t n)
+{
+    HANDLE_TH_ERRORS
+    if (n != 14) Py_RETURN_NONE;
+    Args a{argv};
+    ss_gate_bwd_params q{};
+    const at::Tensor* x = gate_x(a, 0, 3);
+    void* stream = a.stream(13);
+    if (!x || !a.ok || !gate_all(a, 0, *x, q.fwd)) Py_RETURN_NONE;
+    const at::Tensor* ws = a.tensor(9);
+    if (!ws || ws->scalar_type() != at::kByte) Py_RETURN_NONE;
+    q.fwd.workspace = ws->data_ptr();
+    q.fwd.workspace_bytes = (size_t)ws->numel();
+    q.dout = a.ptr(10, x->scalar_type(), {q.fwd.batch, q.fwd.dim, q.fwd.seqlen});
+    q.dh_last = static_cast<const float*>(a.ptr(11, at::kFloat, {q.fwd.batch, q.fwd.dim}, true));
+    if (!a.ok) Py_RETURN_NONE;
+    const int64_t nd = q.fwd.dim;
+    const uint32_t flags = q.fwd.flags;
+    at::Tensor dx = empty_io(*x), df = empty_io(*x), di, dz, drate = empty_f32({nd}, *x), dfb, dib, dh0;
+    if (flags & SS_GATE_HAS_I) di = empty_io(*x);
+    if (flags & SS_GATE_HAS_Z) dz = empty_io(*x);
+    if (flags & SS_GATE_HAS_F_BIAS) dfb = empty_f32({nd}, *x);
+    if (flags & SS_GATE_HAS_I_BIAS) dib = empty_f32({nd}, *x);
+    if (argv[12] == Py_True) dh0 = empty_f32({q.fwd.batch, nd}, *x);
+    q.dx = dx.data_ptr(); q.df = df.data_ptr(); q.di = data(di); q.dz = data(dz);
+    q.dx_batch = q.df_batch = q.di_batch = q.dz_batch = nd * q.fwd.seqlen;
+    q.drate = data<float>(drate); q.df_bias = data<float>(dfb); q.di_bias = data<float>(dib); q.dh0 = data<float>(dh0);
+    const int rc = call(ss_gate_bwd, q, stream);
+    if (rc != SS_OK) return PyLong_FromLong(rc);
+    return dict_of({{"dx", dx}, {"df", df}, {"di", di}, {"dz", dz}, {"drate", drate}, {"df_bias", dfb}, {"di_bias", dib}, {"dh0", dh0}});
+    END_HANDLE_TH_ERRORS
+}
+
+// gate_step(x_t, f_t, i_t, z_t, rate, f_bias, i_bias, reset_t, h, out_t, stream) -> out_t
+PyObject* py_gate_step(PyObject*, PyObject* const* argv, Py_ssize_t n)
+{
+    HANDLE_TH_ERRORS
+    if (n != 11) Py_RETURN_NONE;
+    Args a{argv};
+    ss_gate_step_params p{};
+    const at::Tensor* x = gate_x(a, 0, 2);
+    void* stream = a.stream(10);
+    if (!x || !a.ok || !gate_inputs(a, 0, *x, p, p.x_t, p.f_t, p.i_t, p.z_t)) Py_RETURN_NONE;
+    p.reset_t = marks_of(a, 7, {p.batch});
+    if (!a.none(7)) p.flags |= SS_GATE_HAS_RESET;
+    p.h = static_cast<float*>(a.ptr(8, at::kFloat, {p.batch, p.dim}));
+    void* out = a.ptr(9, x->scalar_type(), {p.batch, p.dim}, true);
+    if (!a.ok) Py_RETURN_NONE;
+    at::Tensor fresh;
+    if (a.none(9)) {
+        fresh = empty_io(*x);
+        out = fresh.data_ptr();
+    }
+    p.out_t = out;
+    const int rc = call(ss_gate_step, p, stream);
+    if (rc != SS_OK) return PyLong_FromLong(rc);
+    if (a.none(9)) return wrapped(fresh);
+    Py_INCREF(argv[9]);
+    return argv[9];
+    END_HANDLE_TH_ERRORS
+}
+
+// qlinear(x, weight, scale, bias, flags, stream) -> out: tokens that are not quantised yet, scratch of the call's own
+PyObject* py_qlinear(PyObject*, PyObject* const* argv, Py_ssize_t n)
+{
+    HANDLE_TH_ERRORS
+    if (n != 6) Py_RETURN_NONE;
+    Args a{argv};
+    ss_qlinear_params p{};
+    const at::Tensor *x = a.tensor(0), *w = a.ok ? a.tensor(1) : nullptr;
+    p.flags = (uint32_t)a.number(4);
+    void* stream = a.stream(5);
+    if (!a.ok || w->dim() != 2 || x->dim() < 1 || !io_type(*x, p.io_dtype)) Py_RETURN_NONE;
+    const bool x_last = p.flags & SS_Q_X_SEQ_LAST, out_last = p.flags & SS_Q_OUT_SEQ_LAST;
+    if ((x_last || out_last) && x->dim() != 3) Py_RETURN_NONE;
+    const int64_t dim = x_last ? x->size(1) : x->size(-1), features = w->size(0);
+    if (dim < 1 || !fits(dim) || !fits(features)) Py_RETURN_NONE;
+    const int64_t batch = x_last || out_last ? x->size(0) : 1, seqlen = x_last ? x->size(2) : (out_last ? x->size(1) : x->numel() / dim);
+    if (!fits(batch) || !fits(seqlen)) Py_RETURN_NONE;
+    p.batch = (int32_t)batch; p.seqlen = (int32_t)seqlen; p.dim = (int32_t)dim; p.features = (int32_t)features;
+    p.x = x->data_ptr();
+    p.weight = a.ptr(1, at::kChar, {features, (int64_t)ss_quant_pitch((int32_t)dim)});
+    p.scale = static_cast<const float*>(a.ptr(2, at::kFloat, {features}));
+    p.bias = static_cast<const float*>(a.ptr(3, at::kFloat, {features}, true));
+    if (!a.ok) Py_RETURN_NONE;
+    if (p.bias) p.flags |= SS_Q_HAS_BIAS;
+    at::Tensor out;
+    const at::TensorOptions options = x->options().requires_grad(false);
+    if (out_last) out = at::empty({batch, features, seqlen}, options);
+    else if (x_last) out = at::empty({batch, seqlen, features}, options);
+    else {
+        c10::SmallVector<int64_t, 6> shape(x->sizes().begin(), x->sizes().end());
+        shape.back() = features;
+        out = at::empty(shape, options);
+    }
+    p.out = out.data_ptr();
+    const at::Tensor ws = empty_bytes(ss_qlinear_scratch_bytes(&p), *x);
+    p.scratch = ws.data_ptr();
+    p.scratch_bytes = (size_t)ws.numel();
+    const int rc = call(ss_qlinear, p, stream);
+    if (rc != SS_OK) return PyLong_FromLong(rc);
+    return wrapped(out);
+    END_HANDLE_TH_ERRORS
+}
+
 #define SS_METHOD(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)(void)>(py_##name)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {SS_METHOD(step), SS_METHOD(layer_step), SS_METHOD(scan_fwd), SS_METHOD(scan_bwd),
-                         SS_METHOD(layer_fwd), SS_METHOD(layer_bwd), {nullptr, nullptr, 0, nullptr}};
+                         SS_METHOD(layer_fwd), SS_METHOD(layer_bwd), SS_METHOD(norm_fwd), SS_METHOD(norm_bwd), SS_METHOD(gate_fwd),
+                         SS_METHOD(gate_bwd), SS_METHOD(gate_step), SS_METHOD(qlinear), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_marshal", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace
