@@ -194,7 +194,7 @@ __global__ __launch_bounds__(256) void quant_turn_kernel(const T* x, const uint3
 
 // ---- the product -----------------------------------------------------------------------------------
 struct QGemmArgs {
-    int M, N, K;                       // K: bytes of a row, a multiple of Q_STEP
+    int M, N, K, batch;                // K: bytes of a row, a multiple of Q_STEP
     const int8_t *A, *B;
     int64_t a_batch, b_batch;          // bytes
     const float *a_scale, *b_scale;
@@ -205,75 +205,361 @@ struct QGemmArgs {
     int64_t c_batch;                   // elements; rows N apart
 };
 
-// One workgroup: a tile of 128 x 128, 4 waves of 64 x 64 on v_mfma_i32_32x32x32_i8 (lane l supplies row l % 32 at the 16
-// contraction indices from 16 (l / 32); accumulator element i of lane l is row 8 (i / 4) + 4 (l / 32) + i % 4, column l % 32).
-// A step's 128 bytes of the tile's rows go straight from memory to LDS, in pieces of 16 bytes whose place in the row is the
-// piece's number XOR the row's last three bits, so that the lanes of a read, which take one piece of 32 rows, spread over the banks.
-template <typename T>
-__global__ __launch_bounds__(256) void qgemm_kernel(QGemmArgs a)
+// Tiles of BM x BN by WM x WN waves, each TM x TN products of v_mfma_i32_32x32x32_i8 (lane l supplies row l % 32 of an operand at
+// the 16 contraction indices from 16 (l / 32); accumulator element e of lane l is row 8 (e / 4) + 4 (l / 32) + e % 4, column l % 32).
+// B's rows are the instruction's rows, so that a lane holds four neighbours of a row of C.
+//
+// A step's 128 bytes of the tile's rows go straight from memory to LDS, one step ahead, in pieces of 16 bytes whose place in the
+// row is the piece's number XOR the row's last three bits, so that the lanes of a read, which take one piece of 32 rows, spread
+// over the banks.  Results are turned through a strip of LDS that each wave has to itself and leave in whole lines.
+//
+// What bounds it: with all units at work the clock, which the matrix cores' power sets: 8192 x 16384 x 2048 takes 295 us (1860
+// TOP/s), 16384 x 2048 x 4096 133 us (2060; the library's 8-bit product reaches 1981 at 8192^3, the matrix cores by
+// themselves, on constants, 4300).  A workgroup alone takes 1.13 us a step: 256 x 256 x 128 products are 0.87 us at the peak, its 8
+// waves of 64 x 128 read 192 KB of LDS, which is as long again, beside them.  What each part brought at 8192 x 16384 x 2048: 128 x 128
+// tiles 425 us, 256 x 256 342, turned results 322, staying for the next tile, whose first step is requested before this one's
+// results are stored (PERSISTENT), 310, requests through buffer resources 304 (behind global ones the compiler waits for all
+// LDS reads at once, as it counts such requests among them), requests between the products 295.
+// bytes of a wave's strip: 32 rows of 32 results; 16-bit rows are set 16 bytes apart, 32-bit ones swizzled like the tiles
+template <typename T> constexpr int strip_pitch() { return sizeof(T) == 2 ? 80 : 128; }
+
+template <typename T, int WM, int WN, int TM, int TN, bool PERSISTENT>
+__global__ __launch_bounds__(WM* WN* WAVE) void qgemm_kernel(QGemmArgs a)
 {
-    constexpr int TILE = 128;
-    __shared__ __align__(16) int8_t lds[2][2][TILE * Q_STEP];
-    const int lane = threadIdx.x % WAVE, wave = threadIdx.x / WAVE, b = blockIdx.z;
-    const int m0 = blockIdx.y * TILE, n0 = blockIdx.x * TILE;
-    const int8_t *A = a.A + b * a.a_batch, *B = a.B + b * a.b_batch;
-    auto load = [&](int k0, int buf) {
-        // 8 lanes a row, 8 rows a wave and request, 4 requests a wave and operand
+    constexpr int BM = WM * TM * 32, BN = WN * TN * 32, WAVES = WM * WN, RA = BM / 8 / WAVES, RB = BN / 8 / WAVES;
+    constexpr int PITCH = strip_pitch<T>(), STRIP = 32 * PITCH, STAGE = (BM + BN) * Q_STEP;
+    __shared__ __align__(16) int8_t lds[2 * STAGE + WAVES * STRIP];
+    const int lane = threadIdx.x % WAVE, wave = threadIdx.x / WAVE;
+    const int nm = (a.M + BM - 1) / BM, nn = (a.N + BN - 1) / BN, tiles = nm * nn;
+    const int64_t total = (int64_t)tiles * a.batch;
+    const int wm = (wave / WN) * TM * 32, wn = (wave % WN) * TN * 32;
+    int8_t* const strip = lds + 2 * STAGE + wave * STRIP;
+    rsrc_t ra, rb;   // the tile's rows of both operands, and where in them a lane reads
+    uint32_t oa[RA], ob[RB];
+    int m0, n0, b;
+    // Where tile `id` lies: the XCDs get contiguous shares, and within one eight tiles of M are taken for each of N, so that what
+    // is worked on at a time shares rows of both operands.
+    auto place = [&](int64_t id) {
+        if (total % 8 == 0) id = (id % 8) * (total / 8) + id / 8;
+        b = (int)(id / tiles);
+        const int t = (int)(id - (int64_t)b * tiles), group = t / (8 * nn), first = group * 8, size = min(nm - first, 8), in = t - group * 8 * nn;
+        m0 = (first + in % size) * BM;
+        n0 = in / size * BN;
+        ra = make_rsrc(a.A + b * a.a_batch + (int64_t)m0 * a.K, (uint32_t)BM * (uint32_t)a.K);
+        rb = make_rsrc(a.B + b * a.b_batch + (int64_t)n0 * a.K, (uint32_t)BN * (uint32_t)a.K);
+        // 8 lanes a row, 8 rows a wave and request; rows past the end read the last one
 #pragma unroll
-        for (int r = 0; r < 4; ++r) {
-            const int row = (r * 4 + wave) * 8 + lane / 8, piece = (lane & 7) ^ (row & 7);
-            const int8_t* pa = A + (int64_t)min(m0 + row, a.M - 1) * a.K + k0 + 16 * piece;
-            const int8_t* pb = B + (int64_t)min(n0 + row, a.N - 1) * a.K + k0 + 16 * piece;
-            int8_t* la = &lds[buf][0][(r * 4 + wave) * 8 * Q_STEP];
-            int8_t* lb = &lds[buf][1][(r * 4 + wave) * 8 * Q_STEP];
-            __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)pa, (__attribute__((address_space(3))) void*)la, 16, 0, 0);
-            __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)pb, (__attribute__((address_space(3))) void*)lb, 16, 0, 0);
+        for (int r = 0; r < RA; ++r) {
+            const int row = (r * WAVES + wave) * 8 + lane / 8;
+            oa[r] = (uint32_t)min(row, a.M - 1 - m0) * (uint32_t)a.K + 16 * ((lane & 7) ^ (row & 7));
+        }
+#pragma unroll
+        for (int r = 0; r < RB; ++r) {
+            const int row = (r * WAVES + wave) * 8 + lane / 8;
+            ob[r] = (uint32_t)min(row, a.N - 1 - n0) * (uint32_t)a.K + 16 * ((lane & 7) ^ (row & 7));
         }
     };
-    const int wm = (wave / 2) * 64, wn = (wave % 2) * 64;
-    i32x16 acc[2][2] = {};
-    load(0, 0);
-    for (int k0 = 0, buf = 0; k0 < a.K; k0 += Q_STEP, buf ^= 1) {
-        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // this wave's requests of the step have arrived in LDS
-        __syncthreads();   // everybody's have, and the other buffer's have been read
-        if (k0 + Q_STEP < a.K) load(k0 + Q_STEP, buf ^ 1);
+    // requests [from, to) of the RA + RB of a step
+    auto load = [&](int k0, int buf, int from, int to) {
+        int8_t* const l = lds + buf * STAGE + wave * 8 * Q_STEP;
 #pragma unroll
-        for (int kk = 0; kk < 4; ++kk) {
-            i32x4 fa[2], fb[2];
-#pragma unroll
-            for (int t = 0; t < 2; ++t) {
-                const int ra = wm + 32 * t + lane % 32, rb = wn + 32 * t + lane % 32, piece = 2 * kk + lane / 32;
-                fa[t] = *reinterpret_cast<const i32x4*>(&lds[buf][0][ra * Q_STEP + 16 * (piece ^ (ra & 7))]);
-                fb[t] = *reinterpret_cast<const i32x4*>(&lds[buf][1][rb * Q_STEP + 16 * (piece ^ (rb & 7))]);
+        for (int r = 0; r < RA + RB; ++r)
+            if (r >= from && r < to)
+                __builtin_amdgcn_raw_ptr_buffer_load_lds(r < RA ? ra : rb, (__attribute__((address_space(3))) void*)(l + (r < RA ? 0 : BM - RA * WAVES * 8) * Q_STEP + r * WAVES * 8 * Q_STEP),
+                                                         16, (int)(r < RA ? oa[r < RA ? r : 0] : ob[r < RA ? 0 : r - RA]), k0, 0, 0);
+    };
+    int64_t id = blockIdx.x;
+    int buf = 0;   // of the step at hand; the other one gets the next step
+    place(id);
+    load(0, 0, 0, RA + RB);
+    for (;;) {
+        const int64_t next = id + gridDim.x;
+        const bool more = PERSISTENT && next < total;
+        const int cm = m0 + wm, cn = n0 + wn, cb = b;
+        i32x16 acc[TM][TN] = {};
+        for (int k0 = 0; k0 < a.K; k0 += Q_STEP, buf ^= 1) {
+            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // this wave's requests of the step have arrived in LDS
+            __syncthreads();   // everybody's have, and the other buffer has been read
+            int k_ahead = k0 + Q_STEP;
+            bool request = k_ahead < a.K;
+            if (!request && more) {
+                place(next);
+                k_ahead = 0;
+                request = true;
             }
+            const int8_t* const from = lds + buf * STAGE;
+// The operands of AT of the step's four products a tile are read together: one by one their latency (about 130 clocks, four times a
+            // step) is all that a wave of few tiles sees.
+            constexpr int AT = TM * TN <= 4 ? 4 : 1;
 #pragma unroll
-            for (int i = 0; i < 2; ++i)
+            for (int k4 = 0; k4 < Q_STEP / 32; k4 += AT) {
+                i32x4 fa[AT][TM], fb[AT][TN];
 #pragma unroll
-                for (int j = 0; j < 2; ++j) acc[i][j] = __builtin_amdgcn_mfma_i32_32x32x32_i8(fa[i], fb[j], acc[i][j], 0, 0, 0);
+                for (int kk = 0; kk < AT; ++kk) {
+                    const int piece = 2 * (k4 + kk) + lane / 32;
+#pragma unroll
+                    for (int t = 0; t < TM; ++t) {
+                        const int r = wm + 32 * t + lane % 32;
+                        fa[kk][t] = *reinterpret_cast<const i32x4*>(from + r * Q_STEP + 16 * (piece ^ (r & 7)));
+                    }
+#pragma unroll
+                    for (int t = 0; t < TN; ++t) {
+                        const int r = wn + 32 * t + lane % 32;
+                        fb[kk][t] = *reinterpret_cast<const i32x4*>(from + BM * Q_STEP + r * Q_STEP + 16 * (piece ^ (r & 7)));
+                    }
+                }
+                // The next step's requests go out between the products: in one go they would hold the wave up for as long as the
+                // products take.
+                __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                for (int kk = 0; kk < AT; ++kk) {
+                    if (request) load(k_ahead, buf ^ 1, (RA + RB) * (k4 + kk) / 4, (RA + RB) * (k4 + kk + 1) / 4);
+                    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                    for (int i = 0; i < TM; ++i)
+#pragma unroll
+                        for (int j = 0; j < TN; ++j) acc[i][j] = __builtin_amdgcn_mfma_i32_32x32x32_i8(fb[kk][j], fa[kk][i], acc[i][j], 0, 0, 0);
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+            }
         }
-    }
-    T* C = static_cast<T*>(a.C) + b * a.c_batch;
+        T* const C = static_cast<T*>(a.C) + cb * a.c_batch;
+        const float *sa = a.a_scale + cb * a.as_batch, *sb = a.b_scale + cb * a.bs_batch;
+        float ms[TM], mb[TM];
 #pragma unroll
-    for (int j = 0; j < 2; ++j) {
-        const int n = n0 + wn + 32 * j + lane % 32;
-        if (n >= a.N) continue;
-        const float sn = a.b_scale[b * a.bs_batch + n], bn = a.bias && !a.bias_m ? a.bias[n] : 0.0f;
+        for (int i = 0; i < TM; ++i) {
+            const int m = min(cm + 32 * i + lane % 32, a.M - 1);
+            ms[i] = sa[m];
+            mb[i] = a.bias && a.bias_m ? a.bias[m] : 0.0f;
+        }
 #pragma unroll
-        for (int i = 0; i < 2; ++i)
+        for (int j = 0; j < TN; ++j) {
+            float ns[16], nb[16];
 #pragma unroll
             for (int e = 0; e < 16; ++e) {
-                const int m = m0 + wm + 32 * i + 8 * (e / 4) + 4 * (lane / 32) + e % 4;
-                if (m >= a.M) continue;
-                const float bm = a.bias && a.bias_m ? a.bias[m] : bn;
-                C[(int64_t)m * a.N + n] = f32_to_io<T>(fmaf((float)acc[i][j][e], a.a_scale[b * a.as_batch + m] * sn, bm));
+                const int n = min(cn + 32 * j + 8 * (e / 4) + 4 * (lane / 32) + e % 4, a.N - 1);
+                ns[e] = sb[n];
+                nb[e] = a.bias && !a.bias_m ? a.bias[n] : 0.0f;
             }
+#pragma unroll
+            for (int i = 0; i < TM; ++i) {
+                float v[16];
+#pragma unroll
+                for (int e = 0; e < 16; ++e) v[e] = fmaf((float)acc[i][j][e], ms[i] * ns[e], mb[i] + nb[e]);
+                const int r = lane % 32;
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    if constexpr (sizeof(T) == 2) {
+                        *reinterpret_cast<uint2*>(strip + r * PITCH + 16 * q + 8 * (lane / 32)) =
+                            make_uint2(pack_bf16x2(v[4 * q], v[4 * q + 1]), pack_bf16x2(v[4 * q + 2], v[4 * q + 3]));
+                    } else {
+                        *reinterpret_cast<float4*>(strip + r * PITCH + 16 * ((2 * q + lane / 32) ^ (r & 7))) =
+                            make_float4(v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]);
+                    }
+                }
+                // the strip is this wave's: its LDS accesses are carried out in order
+                __builtin_amdgcn_wave_barrier();
+                constexpr int E = 16 / sizeof(T), LANES = 32 / E;   // results a lane stores at a time, lanes of a row
+#pragma unroll
+                for (int h = 0; h < 32 * LANES / WAVE; ++h) {
+                    const int row = h * (WAVE / LANES) + lane / LANES, c = lane % LANES;
+                    const u32x4 w = *reinterpret_cast<const u32x4*>(strip + row * PITCH + 16 * (sizeof(T) == 2 ? c : c ^ (row & 7)));
+                    const int m = cm + 32 * i + row, n = cn + 32 * j + E * c;
+                    if (m < a.M && n < a.N) {
+                        T* const to = C + (int64_t)m * a.N + n;
+                        if (n + E <= a.N) {
+                            if constexpr (sizeof(T) == 2) store_row16(to, w);
+                            else store_any(to, 0u, w);
+                        } else {
+#pragma unroll
+                            for (int e = 0; e < E; ++e)
+                                if (n + e < a.N) {
+                                    if constexpr (sizeof(T) == 2) to[e] = bf16_t(w[e / 2] >> (16 * (e % 2)));
+                                    else to[e] = __uint_as_float(w[e]);
+                                }
+                        }
+                    }
+                }
+                __builtin_amdgcn_wave_barrier();
+            }
+        }
+        if (!more) break;
+        id = next;
     }
 }
 
-template <typename T>
-void qgemm_launch(const QGemmArgs& a, int batch, hipStream_t st)
+// ---- few tokens ----------------------------------------------------------------------------------------
+// Up to 32 tokens: the weight's bytes bound it, so they go from memory to registers as operands, once each.  A workgroup takes 16
+// of the weight's rows, its waves share the contraction index out in turn (units of Q_STEP), and their sums, integers, are
+// added up through LDS.  v_mfma_i32_16x16x64_i8: lane l supplies row l % 16 (of the weight; a token of the other operand) at the 16
+// indices from 16 (l / 16), so a request takes 64 bytes of each of 16 rows; element e of lane l is row 4 (l / 16) + e, token l % 16.
+//
+// FUSED: every workgroup brings the tokens to 8 bits itself, from registers into LDS, while its first weights are under way (one
+// launch instead of two).
+struct QFewArgs {
+    int tokens, features, dim, pitch;
+    const void* x;                   // FUSED: (tokens, dim) io values
+    const int8_t* q;                 // else (tokens, pitch) and their scales
+    const float* q_scale;
+    const int8_t* w;
+    const float *scale, *bias;
+    void* out;                       // (tokens, features)
+};
+constexpr int FEW_SLICES = 4;        // FUSED: slices of 8 values of a thread, over all tokens
+constexpr int FEW_AHEAD = 4;         // units of a wave whose weights are requested together
+
+template <typename T, int GROUPS, int WAVES, bool FUSED>   // GROUPS of 16 tokens
+__global__ __launch_bounds__(WAVES* WAVE) void qfew_kernel(QFewArgs a)
 {
-    hipLaunchKernelGGL(qgemm_kernel<T>, dim3((unsigned)((a.N + 127) / 128), (unsigned)((a.M + 127) / 128), (unsigned)batch), dim3(256), 0, st, a);
+    constexpr int THREADS = WAVES * WAVE;
+    __shared__ __align__(16) int8_t lq[FUSED ? FEW_SLICES * THREADS * 8 : 16];
+    __shared__ uint32_t tops[16];
+    __shared__ float scales[GROUPS * 16];
+    __shared__ __align__(16) i32x4 sums[WAVES][GROUPS][WAVE];
+    const int lane = threadIdx.x % WAVE, wave = threadIdx.x / WAVE;
+    const int n0 = blockIdx.x * 16, units = a.pitch / Q_STEP;
+    const int8_t* const w = a.w + (int64_t)min(n0 + lane % 16, a.features - 1) * a.pitch + 16 * (lane / 16);
+    [[maybe_unused]] typename io8<T>::raw raw[FEW_SLICES];
+    const int per = a.pitch / 8;     // slices of a token; FUSED: a multiple of 64, so that a wave's are of one token
+    if constexpr (FUSED) {
+        if (threadIdx.x < 16) tops[threadIdx.x] = 0u;
+#pragma unroll
+        for (int v = 0; v < FEW_SLICES; ++v) {
+            const int s = v * THREADS + threadIdx.x, t = min(s / per, a.tokens - 1), at = min((s - s / per * per) * 8, (a.dim - 1) / 8 * 8);
+            raw[v] = slice_load<T>(static_cast<const T*>(a.x) + (int64_t)t * a.dim, at, a.dim, a.dim % 8 == 0 || t < a.tokens - 1);
+        }
+    }
+    i32x4 fw[FEW_AHEAD][2];
+    auto load = [&](int u0) {
+#pragma unroll
+        for (int k = 0; k < FEW_AHEAD; ++k) {
+            const int64_t at = (int64_t)min(u0 + k * WAVES, units - 1) * Q_STEP;   // past the end: the last unit again, not used
+            fw[k][0] = *reinterpret_cast<const i32x4*>(w + at);
+            fw[k][1] = *reinterpret_cast<const i32x4*>(w + at + 64);
+        }
+    };
+    load(wave);
+    if constexpr (FUSED) {
+        float f[FEW_SLICES][8];
+        __syncthreads();
+#pragma unroll
+        for (int v = 0; v < FEW_SLICES; ++v) {
+            const int s = v * THREADS + threadIdx.x, t = s / per, n = a.dim - (s - t * per) * 8;
+            io8<T>::unpack(raw[v], f[v]);
+            uint32_t top = 0u;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                f[v][j] = j < n ? f[v][j] : 0.0f;
+                top = max(top, magnitude(f[v][j]));
+            }
+#pragma unroll
+            for (int k = 1; k < WAVE; k *= 2) top = max(top, (uint32_t)__shfl_xor((int)top, k));
+            if (lane == 0 && t < a.tokens) atomicMax(&tops[t], top);
+        }
+        __syncthreads();
+#pragma unroll
+        for (int v = 0; v < FEW_SLICES; ++v) {
+            const int s = v * THREADS + threadIdx.x, t = s / per;
+            if (t < a.tokens) *reinterpret_cast<uint2*>(lq + 8 * s) = quantised8(f[v], row_scale(tops[t]).inv);
+        }
+        if (threadIdx.x < 16) scales[threadIdx.x] = row_scale(tops[threadIdx.x]).scale;
+        __syncthreads();
+    } else {
+        for (int t = threadIdx.x; t < GROUPS * 16; t += THREADS) scales[t] = a.q_scale[min(t, a.tokens - 1)];
+    }
+    i32x4 acc[GROUPS] = {};
+    for (int u0 = wave; u0 < units; u0 += FEW_AHEAD * WAVES) {
+        i32x4 cur[FEW_AHEAD][2];
+#pragma unroll
+        for (int k = 0; k < FEW_AHEAD; ++k) {
+            cur[k][0] = fw[k][0];
+            cur[k][1] = fw[k][1];
+        }
+        if (u0 + FEW_AHEAD * WAVES < units) load(u0 + FEW_AHEAD * WAVES);
+#pragma unroll
+        for (int k = 0; k < FEW_AHEAD; ++k) {
+            if (u0 + k * WAVES >= units) break;
+            const int at = (u0 + k * WAVES) * Q_STEP + 16 * (lane / 16);
+#pragma unroll
+            for (int g = 0; g < GROUPS; ++g) {
+                const int t = min(16 * g + lane % 16, a.tokens - 1);
+                i32x4 t0, t1;
+                if constexpr (FUSED) {
+                    t0 = *reinterpret_cast<const i32x4*>(lq + t * a.pitch + at);
+                    t1 = *reinterpret_cast<const i32x4*>(lq + t * a.pitch + at + 64);
+                } else {
+                    const int8_t* q = a.q + (int64_t)t * a.pitch + at;
+                    t0 = *reinterpret_cast<const i32x4*>(q);
+                    t1 = *reinterpret_cast<const i32x4*>(q + 64);
+                }
+                acc[g] = __builtin_amdgcn_mfma_i32_16x16x64_i8(cur[k][0], t0, acc[g], 0, 0, 0);
+                acc[g] = __builtin_amdgcn_mfma_i32_16x16x64_i8(cur[k][1], t1, acc[g], 0, 0, 0);
+            }
+        }
+    }
+#pragma unroll
+    for (int g = 0; g < GROUPS; ++g) sums[wave][g][lane] = acc[g];
+    __syncthreads();
+    for (int i = threadIdx.x; i < GROUPS * WAVE; i += THREADS) {
+        const int g = i / WAVE, l = i % WAVE, t = 16 * g + l % 16, n = n0 + 4 * (l / 16);
+        i32x4 v = sums[0][g][l];
+#pragma unroll
+        for (int k = 1; k < WAVES; ++k) v += sums[k][g][l];
+        if (t >= a.tokens) continue;
+        T* const to = static_cast<T*>(a.out) + (int64_t)t * a.features + n;
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (n + e < a.features) to[e] = f32_to_io<T>(fmaf((float)v[e], scales[t] * a.scale[n + e], a.bias ? a.bias[n + e] : 0.0f));
+    }
+}
+
+// Where the tiles begin to pay: products of 32 / 64 tokens take here / in tiles of 64 (us) 8.3 / 8.4 and 12.3 / 8.4 at 2048 x 8192,
+// 9.8 / 12.6 and 13.6 / 12.6 at 4096 x 2048, 10.8 / 14.9 and 15.5 / 14.9 at 5120 x 2560.
+constexpr int FEW_TOKENS = 32;
+// Waves of a workgroup: enough to fill the chip with (8 to a compute unit), while each has a unit.
+int few_waves(int features, int pitch)
+{
+    const int blocks = (features + 15) / 16;
+    return blocks >= 512 || pitch < 8 * Q_STEP ? 4 : (blocks >= 256 || pitch < 16 * Q_STEP ? 8 : 16);
+}
+bool few_fused(int tokens, int dim, int pitch, int waves)
+{
+    return tokens <= 16 && dim >= 8 && pitch % 512 == 0 && tokens * (pitch / 8) <= FEW_SLICES * waves * WAVE;
+}
+template <typename T>
+void qfew_launch(const QFewArgs& a, bool fused, hipStream_t st)
+{
+    const dim3 grid((unsigned)((a.features + 15) / 16));
+    auto with_waves = [&](auto w) {
+        constexpr int W = decltype(w)::value;
+        if (fused) hipLaunchKernelGGL((qfew_kernel<T, 1, W, true>), grid, dim3(W * WAVE), 0, st, a);
+        else if (a.tokens <= 16) hipLaunchKernelGGL((qfew_kernel<T, 1, W, false>), grid, dim3(W * WAVE), 0, st, a);
+        else hipLaunchKernelGGL((qfew_kernel<T, 2, W, false>), grid, dim3(W * WAVE), 0, st, a);
+    };
+    const int w = few_waves(a.features, a.pitch);
+    if (w == 4) with_waves(std::integral_constant<int, 4>{});
+    else if (w == 8) with_waves(std::integral_constant<int, 8>{});
+    else with_waves(std::integral_constant<int, 16>{});
+}
+
+// Tiles of 256, 128 or 64 by what a launch is modelled to take, in us: a start and an end, and steps that take as long as one
+// workgroup alone needs for each of its rounds (1, 2 or 4 workgroups share a compute unit), or as the chip needs for all of
+// them where that is more.  Fitted to 65 .. 16384 tokens at 2048 x 8192, 4096 x 2048, 768 x 3008 and 5120 x 2560 (dim x features).  us with 256 /
+// 128 / 64: 256 tokens at 2048 x 8192 27.1 / 15.5 / 10.9, 512 28.2 / 17.1 / 21.2, 1024 31.5 / 24.1 / 35.7, 4096 76.2 / 89.1 / 128.5;
+// 1024 at 4096 x 2048 49.6 / 31.3 / 19.2, 2048 52.0 / 33.8 / 41.2, 8192 69.6 / 80.5 / 122.9.
+template <typename T>
+void qgemm_launch(const QGemmArgs& a, hipStream_t st)
+{
+    auto tiles = [&](int t) { return (int64_t)((a.M + t - 1) / t) * ((a.N + t - 1) / t) * a.batch; };
+    auto us = [&](int64_t n, int at_once, double ends, double alone, double each) {
+        const double rounds = alone * (double)((n + at_once - 1) / at_once), all = each * (double)n;
+        return ends + a.K / Q_STEP * (rounds > all ? rounds : all);
+    };
+    const double t256 = us(tiles(256), 256, 10.0, 1.13, 0.0082), t128 = us(tiles(128), 512, 6.0, 0.56, 0.0023), t64 = us(tiles(64), 1024, 4.2, 0.27, 0.00098);
+    if (t256 <= t128 && t256 <= t64)
+        hipLaunchKernelGGL((qgemm_kernel<T, 4, 2, 2, 4, true>), dim3((unsigned)(tiles(256) < 256 ? tiles(256) : 256)), dim3(512), 0, st, a);
+    else if (t128 <= t64) hipLaunchKernelGGL((qgemm_kernel<T, 2, 2, 2, 2, false>), dim3((unsigned)tiles(128)), dim3(256), 0, st, a);
+    else hipLaunchKernelGGL((qgemm_kernel<T, 2, 2, 1, 1, false>), dim3((unsigned)tiles(64)), dim3(256), 0, st, a);
 }
 
 // ---- launches of the quantiser ------------------------------------------------------------------------
@@ -396,14 +682,15 @@ int ss_qlinear(const ss_qlinear_params* p, void* stream)
     if (p->features < 1) return SS_ERR_SHAPE;
     if (p->features > 0x7fffffff - 65536) return SS_ERR_UNSUPPORTED;
     if (p->flags & ~(uint32_t)(SS_Q_X_SEQ_LAST | SS_Q_OUT_SEQ_LAST | SS_Q_HAS_BIAS | SS_Q_X_QUANTISED)) return SS_ERR_UNSUPPORTED;
-    const bool x_last = p->flags & SS_Q_X_SEQ_LAST, out_last = p->flags & SS_Q_OUT_SEQ_LAST, done = p->flags & SS_Q_X_QUANTISED, hb = p->flags & SS_Q_HAS_BIAS;
+    bool x_last = p->flags & SS_Q_X_SEQ_LAST, out_last = p->flags & SS_Q_OUT_SEQ_LAST;
+    const bool done = p->flags & SS_Q_X_QUANTISED, hb = p->flags & SS_Q_HAS_BIAS;
     if (x_last && done) return SS_ERR_UNSUPPORTED;
     if (p->batch == 0 || p->seqlen == 0) return SS_OK;
     if ((x_last || out_last) && p->batch > 65535) return SS_ERR_UNSUPPORTED;
     const int64_t rows = (int64_t)p->batch * p->seqlen;
-    // tiles of the grid's second and third axes
-    if (x_last && chunks_of(p->dim) > 65535) return SS_ERR_UNSUPPORTED;
-    if ((out_last ? (int64_t)p->features : rows) > (int64_t)65535 * 128) return SS_ERR_UNSUPPORTED;
+    // the grid of the product is one-dimensional, of tiles of at least 64 x 64
+    const int64_t tm = ((out_last ? p->features : rows) + 63) / 64, tn = ((out_last ? p->seqlen : p->features) + 63) / 64;
+    if (tm * tn > 0x7fffffff / (out_last ? p->batch : 1)) return SS_ERR_UNSUPPORTED;
     if (!p->x || !p->weight || !p->scale || !p->out || (done && !p->x_scale) || (hb && !p->bias)) return SS_ERR_NULL;
     const size_t esz = p->io_dtype == SS_BF16 ? 2 : 4;
     if (!aligned_to(p->x, done ? 16 : esz) || !aligned_to(p->weight, 16) || !aligned_to(p->scale, 4) || !aligned_to(p->out, esz) ||
@@ -414,21 +701,30 @@ int ss_qlinear(const ss_qlinear_params* p, void* stream)
     if (s.total && (!ws || p->scratch_bytes < s.total)) return SS_ERR_WORKSPACE;
     if (s.total && !aligned_to(ws, 256)) return SS_ERR_ALIGN;
     hipStream_t st = static_cast<hipStream_t>(stream);
+    if (p->seqlen == 1) x_last = out_last = false;   // the two orders are one
     const int pitch = (int)ss_quant_pitch(p->dim);
     const int8_t* q = static_cast<const int8_t*>(p->x);
     const float* q_scale = p->x_scale;
-    if (!done) {
+    const bool few = rows <= ss::FEW_TOKENS && !out_last;
+    const bool fused = few && !done && !x_last && ss::few_fused((int)rows, p->dim, pitch, ss::few_waves(p->features, pitch));
+    if (!done && !fused) {
         const ss::QuantSizes z = {p->batch, p->seqlen, p->dim, pitch, chunks_of(p->dim)};
         quantise(z, x_last, p->io_dtype, p->x, reinterpret_cast<int8_t*>(ws + s.q), reinterpret_cast<float*>(ws + s.scale), ws + s.tops, st);
         q = reinterpret_cast<const int8_t*>(ws + s.q);
         q_scale = reinterpret_cast<const float*>(ws + s.scale);
+    }
+    if (few) {
+        const ss::QFewArgs f = {(int)rows, p->features, p->dim, pitch, p->x, q, q_scale, static_cast<const int8_t*>(p->weight), p->scale, hb ? p->bias : nullptr, p->out};
+        if (p->io_dtype == SS_BF16) ss::qfew_launch<ss::bf16_t>(f, fused, st);
+        else ss::qfew_launch<float>(f, fused, st);
+        return hipGetLastError() == hipSuccess ? SS_OK : SS_ERR_LAUNCH;
     }
     ss::QGemmArgs g{};
     g.K = pitch;
     g.bias = hb ? p->bias : nullptr;
     g.C = p->out;
     const int8_t* w = static_cast<const int8_t*>(p->weight);
-    int batch = 1;
+    g.batch = 1;
     if (out_last) {
         g.M = p->features; g.N = p->seqlen;
         g.A = w; g.a_scale = p->scale;
@@ -437,14 +733,14 @@ int ss_qlinear(const ss_qlinear_params* p, void* stream)
         g.bs_batch = p->seqlen;
         g.c_batch = (int64_t)p->features * p->seqlen;
         g.bias_m = 1;
-        batch = p->batch;
+        g.batch = p->batch;
     } else {
         g.M = (int)rows; g.N = p->features;
         g.A = q; g.a_scale = q_scale;
         g.B = w; g.b_scale = p->scale;
     }
-    if (p->io_dtype == SS_BF16) ss::qgemm_launch<ss::bf16_t>(g, batch, st);
-    else ss::qgemm_launch<float>(g, batch, st);
+    if (p->io_dtype == SS_BF16) ss::qgemm_launch<ss::bf16_t>(g, st);
+    else ss::qgemm_launch<float>(g, st);
     return hipGetLastError() == hipSuccess ? SS_OK : SS_ERR_LAUNCH;
 }
 
