@@ -209,7 +209,7 @@ struct QGemmArgs {
 // the 16 contraction indices from 16 (l / 32); accumulator element e of lane l is row 8 (e / 4) + 4 (l / 32) + e % 4, column l % 32).
 // B's rows are the instruction's rows, so that a lane holds four neighbours of a row of C.
 //
-// A step's 128 bytes of the tile's rows go straight from memory to LDS, one step ahead, in pieces of 16 bytes whose place in the
+// A step's 128 bytes of the tile's rows go straight from memory to LDS, STAGES - 1 steps ahead, in pieces of 16 bytes whose place in the
 // row is the piece's number XOR the row's last three bits, so that the lanes of a read, which take one piece of 32 rows, spread
 // over the banks.  Results are turned through a strip of LDS that each wave has to itself and leave in whole lines.
 //
@@ -223,17 +223,18 @@ struct QGemmArgs {
 // bytes of a wave's strip: 32 rows of 32 results; 16-bit rows are set 16 bytes apart, 32-bit ones swizzled like the tiles
 template <typename T> constexpr int strip_pitch() { return sizeof(T) == 2 ? 80 : 128; }
 
-template <typename T, int WM, int WN, int TM, int TN, bool PERSISTENT>
+template <typename T, int WM, int WN, int TM, int TN, int STAGES, bool PERSISTENT>
 __global__ __launch_bounds__(WM* WN* WAVE) void qgemm_kernel(QGemmArgs a)
 {
     constexpr int BM = WM * TM * 32, BN = WN * TN * 32, WAVES = WM * WN, RA = BM / 8 / WAVES, RB = BN / 8 / WAVES;
     constexpr int PITCH = strip_pitch<T>(), STRIP = 32 * PITCH, STAGE = (BM + BN) * Q_STEP;
-    __shared__ __align__(16) int8_t lds[2 * STAGE + WAVES * STRIP];
+    static_assert(!PERSISTENT || STAGES == 2, "a tile's last step requests the next one's first step alone");
+    __shared__ __align__(16) int8_t lds[STAGES * STAGE + WAVES * STRIP];
     const int lane = threadIdx.x % WAVE, wave = threadIdx.x / WAVE;
     const int nm = (a.M + BM - 1) / BM, nn = (a.N + BN - 1) / BN, tiles = nm * nn;
     const int64_t total = (int64_t)tiles * a.batch;
     const int wm = (wave / WN) * TM * 32, wn = (wave % WN) * TN * 32;
-    int8_t* const strip = lds + 2 * STAGE + wave * STRIP;
+    int8_t* const strip = lds + STAGES * STAGE + wave * STRIP;
     rsrc_t ra, rb;   // the tile's rows of both operands, and where in them a lane reads
     uint32_t oa[RA], ob[RB];
     int m0, n0, b;
@@ -269,18 +270,24 @@ __global__ __launch_bounds__(WM* WN* WAVE) void qgemm_kernel(QGemmArgs a)
                                                          16, (int)(r < RA ? oa[r < RA ? r : 0] : ob[r < RA ? 0 : r - RA]), k0, 0, 0);
     };
     int64_t id = blockIdx.x;
-    int buf = 0;   // of the step at hand; the other one gets the next step
+    int buf = 0;   // of the step at hand; the step before lay in the buffer that the one STAGES - 1 later gets
     place(id);
-    load(0, 0, 0, RA + RB);
+#pragma unroll
+    for (int k = 0; k < STAGES - 1; ++k)
+        if (k == 0 || k * Q_STEP < a.K) load(k * Q_STEP, k, 0, RA + RB);
     for (;;) {
         const int64_t next = id + gridDim.x;
         const bool more = PERSISTENT && next < total;
         const int cm = m0 + wm, cn = n0 + wn, cb = b;
         i32x16 acc[TM][TN] = {};
-        for (int k0 = 0; k0 < a.K; k0 += Q_STEP, buf ^= 1) {
-            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // this wave's requests of the step have arrived in LDS
-            __syncthreads();   // everybody's have, and the other buffer has been read
-            int k_ahead = k0 + Q_STEP;
+        for (int k0 = 0; k0 < a.K; k0 += Q_STEP, buf = buf + 1 == STAGES ? 0 : buf + 1) {
+            // this wave's requests of the step have arrived in LDS: all but those of the steps behind it that are under way
+            if (STAGES > 2 && k0 + (STAGES - 2) * Q_STEP < a.K) asm volatile("s_waitcnt vmcnt(%0)" ::"n"((STAGES - 2) * (RA + RB)) : "memory");
+            else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+            // everybody's have, and the buffer of the step before has been read (__syncthreads would wait for all requests)
+            asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+            const int ahead = buf == 0 ? STAGES - 1 : buf - 1;
+            int k_ahead = k0 + (STAGES - 1) * Q_STEP;
             bool request = k_ahead < a.K;
             if (!request && more) {
                 place(next);
@@ -313,7 +320,7 @@ __global__ __launch_bounds__(WM* WN* WAVE) void qgemm_kernel(QGemmArgs a)
                 __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
                 for (int kk = 0; kk < AT; ++kk) {
-                    if (request) load(k_ahead, buf ^ 1, (RA + RB) * (k4 + kk) / 4, (RA + RB) * (k4 + kk + 1) / 4);
+                    if (request) load(k_ahead, ahead, (RA + RB) * (k4 + kk) / 4, (RA + RB) * (k4 + kk + 1) / 4);
                     __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
                     for (int i = 0; i < TM; ++i)
@@ -405,26 +412,30 @@ struct QFewArgs {
     const float *scale, *bias;
     void* out;                       // (tokens, features)
 };
-constexpr int FEW_SLICES = 4;        // FUSED: slices of 8 values of a thread, over all tokens
+constexpr int FEW_SLICES = 4;        // most slices of 8 values of a thread, over all tokens, that a workgroup quantises itself
 constexpr int FEW_AHEAD = 4;         // units of a wave whose weights are requested together
 
-template <typename T, int GROUPS, int WAVES, bool FUSED>   // GROUPS of 16 tokens
+// Slices of 8 values that a token is dealt out in: whole waves of them, so that a wave's are of one token
+__host__ __device__ __forceinline__ int few_slices(int pitch) { return (pitch / 8 + WAVE - 1) / WAVE * WAVE; }
+
+template <typename T, int GROUPS, int WAVES, int SLICES>   // GROUPS of 16 tokens; SLICES of a thread where FUSED, else 0
 __global__ __launch_bounds__(WAVES* WAVE) void qfew_kernel(QFewArgs a)
 {
     constexpr int THREADS = WAVES * WAVE;
-    __shared__ __align__(16) int8_t lq[FUSED ? FEW_SLICES * THREADS * 8 : 16];
+    constexpr bool FUSED = SLICES > 0;
+    __shared__ __align__(16) int8_t lq[FUSED ? SLICES * THREADS * 8 : 16];
     __shared__ uint32_t tops[16];
     __shared__ float scales[GROUPS * 16];
     __shared__ __align__(16) i32x4 sums[WAVES][GROUPS][WAVE];
     const int lane = threadIdx.x % WAVE, wave = threadIdx.x / WAVE;
     const int n0 = blockIdx.x * 16, units = a.pitch / Q_STEP;
     const int8_t* const w = a.w + (int64_t)min(n0 + lane % 16, a.features - 1) * a.pitch + 16 * (lane / 16);
-    [[maybe_unused]] typename io8<T>::raw raw[FEW_SLICES];
-    const int per = a.pitch / 8;     // slices of a token; FUSED: a multiple of 64, so that a wave's are of one token
+    [[maybe_unused]] typename io8<T>::raw raw[FUSED ? SLICES : 1];
+    const int per = few_slices(a.pitch);
     if constexpr (FUSED) {
         if (threadIdx.x < 16) tops[threadIdx.x] = 0u;
 #pragma unroll
-        for (int v = 0; v < FEW_SLICES; ++v) {
+        for (int v = 0; v < SLICES; ++v) {
             const int s = v * THREADS + threadIdx.x, t = min(s / per, a.tokens - 1), at = min((s - s / per * per) * 8, (a.dim - 1) / 8 * 8);
             raw[v] = slice_load<T>(static_cast<const T*>(a.x) + (int64_t)t * a.dim, at, a.dim, a.dim % 8 == 0 || t < a.tokens - 1);
         }
@@ -440,10 +451,10 @@ __global__ __launch_bounds__(WAVES* WAVE) void qfew_kernel(QFewArgs a)
     };
     load(wave);
     if constexpr (FUSED) {
-        float f[FEW_SLICES][8];
+        float f[SLICES][8];
         __syncthreads();
 #pragma unroll
-        for (int v = 0; v < FEW_SLICES; ++v) {
+        for (int v = 0; v < SLICES; ++v) {
             const int s = v * THREADS + threadIdx.x, t = s / per, n = a.dim - (s - t * per) * 8;
             io8<T>::unpack(raw[v], f[v]);
             uint32_t top = 0u;
@@ -458,9 +469,10 @@ __global__ __launch_bounds__(WAVES* WAVE) void qfew_kernel(QFewArgs a)
         }
         __syncthreads();
 #pragma unroll
-        for (int v = 0; v < FEW_SLICES; ++v) {
+        for (int v = 0; v < SLICES; ++v) {
             const int s = v * THREADS + threadIdx.x, t = s / per;
-            if (t < a.tokens) *reinterpret_cast<uint2*>(lq + 8 * s) = quantised8(f[v], row_scale(tops[t]).inv);
+            const int at = (s - t * per) * 8;
+            if (t < a.tokens && at < a.pitch) *reinterpret_cast<uint2*>(lq + t * a.pitch + at) = quantised8(f[v], row_scale(tops[t]).inv);
         }
         if (threadIdx.x < 16) scales[threadIdx.x] = row_scale(tops[threadIdx.x]).scale;
         __syncthreads();
@@ -513,8 +525,8 @@ __global__ __launch_bounds__(WAVES* WAVE) void qfew_kernel(QFewArgs a)
     }
 }
 
-// Where the tiles begin to pay: products of 32 / 64 tokens take here / in tiles of 64 (us) 8.3 / 8.4 and 12.3 / 8.4 at 2048 x 8192,
-// 9.8 / 12.6 and 13.6 / 12.6 at 4096 x 2048, 10.8 / 14.9 and 15.5 / 14.9 at 5120 x 2560.
+// Where the tiles begin to pay: 33 tokens, weights and tokens not in a cache, the quantiser's launch included, would take here (four groups
+// of 16) / take in tiles of 64 (us) 13.4 / 11.9 at 2048 x 8192, 14.3 / 16.1 at 4096 x 2048, 8.1 / 7.4 at 768 x 3008, 9.5 / 9.4 at 1500 x 700.
 constexpr int FEW_TOKENS = 32;
 // Waves of a workgroup: enough to fill the chip with (8 to a compute unit), while each has a unit.
 int few_waves(int features, int pitch)
@@ -522,9 +534,12 @@ int few_waves(int features, int pitch)
     const int blocks = (features + 15) / 16;
     return blocks >= 512 || pitch < 8 * Q_STEP ? 4 : (blocks >= 256 || pitch < 16 * Q_STEP ? 8 : 16);
 }
+// Where a workgroup brings the tokens to 8 bits itself: two slices a thread at most, four for up to four tokens.  us, weights and tokens
+// not in a cache, fused / in two launches: one token 2048 x 8192 6.4 / 8.8, 4096 x 2048 7.4 / 9.7, 1500 x 700 5.8 / 7.3; four 8.1 / 9.3,
+// 9.0 / 10.2, 6.1 / 7.6; eight of 1024 x 1024 (two slices) 5.3 / 7.4, of 4096 x 2048 (four) 11.3 / 10.8, six of 1500 x 700 (three) 9.1 / 7.6.
 bool few_fused(int tokens, int dim, int pitch, int waves)
 {
-    return tokens <= 16 && dim >= 8 && pitch % 512 == 0 && tokens * (pitch / 8) <= FEW_SLICES * waves * WAVE;
+    return tokens <= 16 && dim >= 8 && tokens * few_slices(pitch) <= (tokens <= 4 ? FEW_SLICES : 2) * waves * WAVE;
 }
 template <typename T>
 void qfew_launch(const QFewArgs& a, bool fused, hipStream_t st)
@@ -532,9 +547,11 @@ void qfew_launch(const QFewArgs& a, bool fused, hipStream_t st)
     const dim3 grid((unsigned)((a.features + 15) / 16));
     auto with_waves = [&](auto w) {
         constexpr int W = decltype(w)::value;
-        if (fused) hipLaunchKernelGGL((qfew_kernel<T, 1, W, true>), grid, dim3(W * WAVE), 0, st, a);
-        else if (a.tokens <= 16) hipLaunchKernelGGL((qfew_kernel<T, 1, W, false>), grid, dim3(W * WAVE), 0, st, a);
-        else hipLaunchKernelGGL((qfew_kernel<T, 2, W, false>), grid, dim3(W * WAVE), 0, st, a);
+        if (fused && a.tokens * few_slices(a.pitch) <= W * WAVE) hipLaunchKernelGGL((qfew_kernel<T, 1, W, 1>), grid, dim3(W * WAVE), 0, st, a);
+        else if (fused && a.tokens * few_slices(a.pitch) <= 2 * W * WAVE) hipLaunchKernelGGL((qfew_kernel<T, 1, W, 2>), grid, dim3(W * WAVE), 0, st, a);
+        else if (fused) hipLaunchKernelGGL((qfew_kernel<T, 1, W, FEW_SLICES>), grid, dim3(W * WAVE), 0, st, a);
+        else if (a.tokens <= 16) hipLaunchKernelGGL((qfew_kernel<T, 1, W, 0>), grid, dim3(W * WAVE), 0, st, a);
+        else hipLaunchKernelGGL((qfew_kernel<T, 2, W, 0>), grid, dim3(W * WAVE), 0, st, a);
     };
     const int w = few_waves(a.features, a.pitch);
     if (w == 4) with_waves(std::integral_constant<int, 4>{});
@@ -543,10 +560,13 @@ void qfew_launch(const QFewArgs& a, bool fused, hipStream_t st)
 }
 
 // Tiles of 256, 128 or 64 by what a launch is modelled to take, in us: a start and an end, and steps that take as long as one
-// workgroup alone needs for each of its rounds (1, 2 or 4 workgroups share a compute unit), or as the chip needs for all of
-// them where that is more.  Fitted to 65 .. 16384 tokens at 2048 x 8192, 4096 x 2048, 768 x 3008 and 5120 x 2560 (dim x features).  us with 256 /
-// 128 / 64: 256 tokens at 2048 x 8192 27.1 / 15.5 / 10.9, 512 28.2 / 17.1 / 21.2, 1024 31.5 / 24.1 / 35.7, 4096 76.2 / 89.1 / 128.5;
-// 1024 at 4096 x 2048 49.6 / 31.3 / 19.2, 2048 52.0 / 33.8 / 41.2, 8192 69.6 / 80.5 / 122.9.
+// workgroup alone needs for each of its rounds (1, 2 and 2 workgroups share a compute unit), or as the chip needs for all of
+// them where that is more.  Fitted to 33 .. 16384 tokens at 2048 x 8192, 4096 x 2048, 768 x 3008 and 5120 x 2560 (dim x features).  us with 256 /
+// 128 / 64: 256 tokens at 2048 x 8192 27.1 / 15.5 / 10.7, 512 28.2 / 17.1 / 19.7, 1024 31.5 / 24.1 / 36.8, 4096 76.2 / 89.1 / 137.5;
+// 1024 at 4096 x 2048 49.6 / 25.5 / 17.4, 2048 52.0 / 28.7 / 33.4, 8192 69.6 / 80.5 / 122.0.
+// Few tiles are bound by the latency of their requests and look three steps ahead: with weights and tokens not in a cache, the
+// quantiser's launch included, 128 tokens at 4096 x 2048 16.2 us against 29.3 one step ahead (tiles of 64), 512 at 2048 x 8192 20.1
+// against 25.4 (tiles of 128, of which two of one step ahead share a unit: 1024 tokens 34.5 against 29.6).
 template <typename T>
 void qgemm_launch(const QGemmArgs& a, hipStream_t st)
 {
@@ -555,11 +575,12 @@ void qgemm_launch(const QGemmArgs& a, hipStream_t st)
         const double rounds = alone * (double)((n + at_once - 1) / at_once), all = each * (double)n;
         return ends + a.K / Q_STEP * (rounds > all ? rounds : all);
     };
-    const double t256 = us(tiles(256), 256, 10.0, 1.13, 0.0082), t128 = us(tiles(128), 512, 6.0, 0.56, 0.0023), t64 = us(tiles(64), 1024, 4.2, 0.27, 0.00098);
+    const double t256 = us(tiles(256), 256, 10.0, 1.13, 0.0082), t128 = us(tiles(128), 512, 6.0, 0.56, 0.0023), t64 = us(tiles(64), 512, 4.2, 0.27, 0.00095);
     if (t256 <= t128 && t256 <= t64)
-        hipLaunchKernelGGL((qgemm_kernel<T, 4, 2, 2, 4, true>), dim3((unsigned)(tiles(256) < 256 ? tiles(256) : 256)), dim3(512), 0, st, a);
-    else if (t128 <= t64) hipLaunchKernelGGL((qgemm_kernel<T, 2, 2, 2, 2, false>), dim3((unsigned)tiles(128)), dim3(256), 0, st, a);
-    else hipLaunchKernelGGL((qgemm_kernel<T, 2, 2, 1, 1, false>), dim3((unsigned)tiles(64)), dim3(256), 0, st, a);
+        hipLaunchKernelGGL((qgemm_kernel<T, 4, 2, 2, 4, 2, true>), dim3((unsigned)(tiles(256) < 256 ? tiles(256) : 256)), dim3(512), 0, st, a);
+    else if (t128 <= t64 && tiles(128) > 256) hipLaunchKernelGGL((qgemm_kernel<T, 2, 2, 2, 2, 2, false>), dim3((unsigned)tiles(128)), dim3(256), 0, st, a);
+    else if (t128 <= t64) hipLaunchKernelGGL((qgemm_kernel<T, 2, 2, 2, 2, 4, false>), dim3((unsigned)tiles(128)), dim3(256), 0, st, a);
+    else hipLaunchKernelGGL((qgemm_kernel<T, 2, 2, 1, 1, 4, false>), dim3((unsigned)tiles(64)), dim3(256), 0, st, a);
 }
 
 // ---- launches of the quantiser ------------------------------------------------------------------------
