@@ -25,12 +25,13 @@ namespace ss {
 
 constexpr int LANE_STEPS = 8;                       // steps of one lane
 constexpr int GATE_PIECE = WAVE * LANE_STEPS;       // steps of a whole wave: the distance of the checkpoints
-constexpr int GATE_WAVES = 4;                  // waves of a workgroup; they share nothing
+constexpr int GATE_WAVES = 4;                  // waves of a workgroup where each has rows of its own
 constexpr float GATE_LOG2E = 1.44269504088896340736f;
 
 struct GateArgs {
     int B, D, L, R;                            // R = B D rows
     int pieces, nseg, spp;                     // pieces of GATE_PIECE steps; segments and their pieces
+    int nmap, ppm;                             // maps that the segments are composed of, and their pieces
     unsigned flags;
     const void *x, *f, *i, *z;
     int64_t xb, fb, ib, zb;
@@ -39,7 +40,7 @@ struct GateArgs {
     void* out;
     float* h_last;
     float* ckpt;                               // (pieces, R): the state before each piece; or null
-    float2* agg;                               // (nseg, R): a segment's composed map
+    float2* agg;                               // (R, nmap): the composed maps of ppm pieces each
     float* carry;                              // (nseg, R): the state (backward: G) that enters a segment; null for one segment
     const void* dout;
     const float* dh_last;
@@ -92,37 +93,89 @@ __device__ __forceinline__ void scan_step(float& A, float& B, int gl)
         affine_after<RST>(A, B, A0, B0);
     }
 }
-// (A, B): a lane's slice as one map.  Returns the state before the slice (BACK: behind it, in time), given `c`, the one
-// before the piece; c becomes the one after the piece.
+// (A, B): a lane's slice as one map.  scan() composes those of the lanes before it (BACK: behind it, in time) onto it; apply() returns
+// the state before the slice, given `c`, the one before the piece, which becomes the one after it.
 template <int G, bool BACK, bool RST>
-__device__ __forceinline__ float scan_lanes(float A, float B, float& c, int lane)
-{
-    const int gl = lane & (G - 1);
-    scan_step<G, BACK, RST, 1>(A, B, gl);
-    scan_step<G, BACK, RST, 2>(A, B, gl);
-    scan_step<G, BACK, RST, 4>(A, B, gl);
-    scan_step<G, BACK, RST, 8>(A, B, gl);
-    constexpr int CTRL = BACK ? 0x101 : 0x111;
-    float Ae = dpp_or<CTRL>(A, 1.0f), Be = dpp_or<CTRL>(B, 0.0f);
-    float cin = c;
-    if constexpr (G == WAVE) {
-        const float c0 = c;
-        const float c1 = affine_of<RST>(lane_value(A, BACK ? 48 : 15), lane_value(B, BACK ? 48 : 15), c0);
-        const float c2 = affine_of<RST>(lane_value(A, BACK ? 32 : 31), lane_value(B, BACK ? 32 : 31), c1);
-        const float c3 = affine_of<RST>(lane_value(A, BACK ? 16 : 47), lane_value(B, BACK ? 16 : 47), c2);
-        c = affine_of<RST>(lane_value(A, BACK ? 0 : 63), lane_value(B, BACK ? 0 : 63), c3);
-        const int row = BACK ? 3 - (lane >> 4) : lane >> 4;
-        cin = row < 2 ? (row == 0 ? c0 : c1) : (row == 2 ? c2 : c3);
-    } else {
-        if constexpr (G < 16) {
-            const bool first = gl == (BACK ? G - 1 : 0);
-            Ae = first ? 1.0f : Ae;
-            Be = first ? 0.0f : Be;
+struct LaneScan {
+    float A, B;                  // through the lane, within its row of 16 lanes (its group, if smaller)
+    float rA[4], rB[4];          // G == 64: the rows of lanes, in time's order
+    __device__ __forceinline__ void scan(float A_, float B_, int lane)
+    {
+        A = A_;
+        B = B_;
+        const int gl = lane & (G - 1);
+        scan_step<G, BACK, RST, 1>(A, B, gl);
+        scan_step<G, BACK, RST, 2>(A, B, gl);
+        scan_step<G, BACK, RST, 4>(A, B, gl);
+        scan_step<G, BACK, RST, 8>(A, B, gl);
+        if constexpr (G == WAVE) {
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                rA[r] = lane_value(A, BACK ? 48 - 16 * r : 15 + 16 * r);
+                rB[r] = lane_value(B, BACK ? 48 - 16 * r : 15 + 16 * r);
+            }
         }
-        c = affine_of<RST>(A, B, c);   // valid in the group's last lane (BACK: first)
     }
-    return affine_of<RST>(Ae, Be, cin);
-}
+    __device__ __forceinline__ void whole(float& WA, float& WB) const   // the wave's map
+    {
+        WA = rA[0];
+        WB = rB[0];
+#pragma unroll
+        for (int r = 1; r < 4; ++r) {
+            float A1 = rA[r], B1 = rB[r];
+            affine_after<RST>(A1, B1, WA, WB);
+            WA = A1;
+            WB = B1;
+        }
+    }
+    __device__ __forceinline__ float apply(float& c, int lane) const
+    {
+        const int gl = lane & (G - 1);
+        constexpr int CTRL = BACK ? 0x101 : 0x111;
+        float Ae = dpp_or<CTRL>(A, 1.0f), Be = dpp_or<CTRL>(B, 0.0f);
+        float cin = c;
+        if constexpr (G == WAVE) {
+            const float c0 = c, c1 = affine_of<RST>(rA[0], rB[0], c0), c2 = affine_of<RST>(rA[1], rB[1], c1), c3 = affine_of<RST>(rA[2], rB[2], c2);
+            c = affine_of<RST>(rA[3], rB[3], c3);
+            const int row = BACK ? 3 - (lane >> 4) : lane >> 4;
+            cin = row < 2 ? (row == 0 ? c0 : c1) : (row == 2 ? c2 : c3);
+        } else {
+            if constexpr (G < 16) {
+                const bool first = gl == (BACK ? G - 1 : 0);
+                Ae = first ? 1.0f : Ae;
+                Be = first ? 0.0f : Be;
+            }
+            c = affine_of<RST>(A, B, c);   // valid in the group's last lane (BACK: first)
+        }
+        return affine_of<RST>(Ae, Be, cin);
+    }
+};
+
+// TEAM waves work on neighbouring pieces of one row at a time: from their pieces' maps and the state `c` before all of them each
+// gets the state before its own; c becomes the one behind all.  The two halves of LDS are used in turn, so one barrier a time.
+template <int TEAM, bool BACK, bool RST>
+struct TeamScan {
+    float2 (*lds)[TEAM];
+    int turn = 0;
+    __device__ __forceinline__ float operator()(float A, float B, float& c, int wave, int lane)
+    {
+        const int pos = BACK ? TEAM - 1 - wave : wave;
+        if (lane == 0) lds[turn][pos] = make_float2(A, B);
+        __syncthreads();
+        const float2 m = lds[turn][lane & (TEAM - 1)];
+        turn ^= 1;
+        float A1 = m.x, B1 = m.y;   // lanes of a row of 16: the maps in time's order
+        const int gl = lane & (TEAM - 1);
+        scan_step<TEAM, false, RST, 1>(A1, B1, gl);
+        scan_step<TEAM, false, RST, 2>(A1, B1, gl);
+        scan_step<TEAM, false, RST, 4>(A1, B1, gl);
+        scan_step<TEAM, false, RST, 8>(A1, B1, gl);
+        const float h = affine_of<RST>(A1, B1, c);
+        const float before = pos == 0 ? c : lane_value(h, pos - 1);
+        c = lane_value(h, TEAM - 1);
+        return before;
+    }
+};
 
 // ---- reset marks ---------------------------------------------------------------------------
 __device__ __forceinline__ uint2 marks_load(const uint8_t* row, int t0, int L)   // eight reset marks, zeros past the row
@@ -166,15 +219,17 @@ __device__ __forceinline__ Channel channel_of(const GateArgs& a, int d)
 }
 
 // Where a lane works: its row, and what is common to the row's slices.
-template <int G>
+template <int G, int TEAM>
 struct Place {
     int lane, gl, row, b, d, last;   // last: the start of the row's last slice
+    int member;                      // of the team
     bool valid, whole;
     __device__ __forceinline__ Place(const GateArgs& a)
     {
         lane = threadIdx.x & (WAVE - 1);
         gl = lane & (G - 1);
-        const int wave = (int)blockIdx.x * GATE_WAVES + (int)(threadIdx.x / WAVE);
+        member = TEAM > 1 ? __builtin_amdgcn_readfirstlane((int)(threadIdx.x / WAVE)) : 0;
+        const int wave = TEAM > 1 ? (int)blockIdx.x : (int)blockIdx.x * GATE_WAVES + (int)(threadIdx.x / WAVE);
         row = wave * (WAVE / G) + lane / G;
         if constexpr (G == WAVE) row = __builtin_amdgcn_readfirstlane(row);
         valid = row < a.R;
@@ -239,10 +294,12 @@ __device__ __forceinline__ void slice_map(const float (&av)[8], const float (&bv
     }
 }
 
-template <typename T, int G, bool HI, bool HZ, bool RST>
-__global__ __launch_bounds__(GATE_WAVES* WAVE) void gate_fwd_kernel(GateArgs a)
+template <int TEAM> constexpr int gate_threads() { return (TEAM > 1 ? TEAM : GATE_WAVES) * WAVE; }
+
+template <typename T, int G, int TEAM, bool HI, bool HZ, bool RST>
+__global__ __launch_bounds__(gate_threads<TEAM>()) void gate_fwd_kernel(GateArgs a)
 {
-    const Place<G> at(a);
+    const Place<G, TEAM> at(a);
     const Channel ch = channel_of(a, at.d);
     const T *x = at.template in<T>(a.x, a.xb, a.L), *f = at.template in<T>(a.f, a.fb, a.L);
     const T* iv = HI ? at.template in<T>(a.i, a.ib, a.L) : nullptr;
@@ -250,9 +307,11 @@ __global__ __launch_bounds__(GATE_WAVES* WAVE) void gate_fwd_kernel(GateArgs a)
     T* out = static_cast<T*>(a.out) + (int64_t)at.row * a.L;
     const uint8_t* reset = RST ? a.reset + (int64_t)at.b * a.L : nullptr;
     const int seg = blockIdx.y, p0 = seg * a.spp, p1 = min(p0 + a.spp, a.pieces);
-    float c = 0.0f;
+    float c = 0.0f;   // the state before what the team has at hand
     if (seg > 0) c = a.carry[(int64_t)seg * a.R + at.row];
     else if (a.flags & SS_GATE_HAS_H0) c = a.h0[at.row];
+    __shared__ float2 maps[2][TEAM];
+    TeamScan<TEAM, false, RST> team{maps};
 
     fwd_raw<T, HI> r;
     typename io8<T>::raw rz;
@@ -264,17 +323,26 @@ __global__ __launch_bounds__(GATE_WAVES* WAVE) void gate_fwd_kernel(GateArgs a)
         if constexpr (HZ) rz = slice_load<T>(z, t, a.L, at.whole);
         if constexpr (RST) r.m = marks_load(reset, t0, a.L);
     };
-    load(p0);
-    for (int p = p0; p < p1; ++p) {
-        const int t0 = p * GATE_PIECE + at.gl * LANE_STEPS, n = a.L - t0;
-        if (a.ckpt && at.valid && at.gl == 0) a.ckpt[(int64_t)p * a.R + at.row] = c;
+    // a team's members that have no piece left take part with maps that change nothing
+    load(min(p0 + at.member, a.pieces - 1));
+    for (int q = p0; q < p1; q += TEAM) {
+        const int p = q + at.member, t0 = p * GATE_PIECE + at.gl * LANE_STEPS, n = p < p1 ? a.L - t0 : 0;
         float av[8], bv[8], zv[8], y[8];
         steps_of<T, HI, RST>(r, ch, n, av, bv);
         if constexpr (HZ) io8<T>::unpack(rz, zv);
-        if (p + 1 < p1) load(p + 1);
+        if (q + TEAM < p1) load(min(p + TEAM, a.pieces - 1));
         float A, B;
         slice_map<RST>(av, bv, A, B);
-        float h = scan_lanes<G, false, RST>(A, B, c, at.lane);
+        LaneScan<G, false, RST> lanes;
+        lanes.scan(A, B, at.lane);
+        float own = c;
+        if constexpr (TEAM > 1) {
+            lanes.whole(A, B);
+            own = team(A, B, c, at.member, at.lane);
+        }
+        if (a.ckpt && at.valid && at.gl == 0 && p < p1) a.ckpt[(int64_t)p * a.R + at.row] = own;
+        float h = lanes.apply(own, at.lane);
+        if constexpr (TEAM == 1) c = own;
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
             h = affine_of<RST>(av[j], bv[j], h);
@@ -282,61 +350,78 @@ __global__ __launch_bounds__(GATE_WAVES* WAVE) void gate_fwd_kernel(GateArgs a)
         }
         if (at.valid) slice_store<T>(out, t0, n, y);
     }
-    if (a.h_last && at.valid && seg == a.nseg - 1 && at.gl == (G == WAVE ? 0 : G - 1)) a.h_last[at.row] = c;
+    if (a.h_last && at.valid && seg == a.nseg - 1 && at.member == 0 && at.gl == (G == WAVE ? 0 : G - 1)) a.h_last[at.row] = c;
 }
 
-// A segment as one map (all but the last one).
+// ppm pieces as one map: one wave each (a segment is a whole number of them).
 template <typename T, bool HI, bool RST>
 __global__ __launch_bounds__(GATE_WAVES* WAVE) void gate_fwd_map_kernel(GateArgs a)
 {
-    const Place<WAVE> at(a);
+    const Place<WAVE, 1> at(a);
     const Channel ch = channel_of(a, at.d);
     const T *x = at.template in<T>(a.x, a.xb, a.L), *f = at.template in<T>(a.f, a.fb, a.L);
     const T* iv = HI ? at.template in<T>(a.i, a.ib, a.L) : nullptr;
     const uint8_t* reset = RST ? a.reset + (int64_t)at.b * a.L : nullptr;
-    const int seg = blockIdx.y, p0 = seg * a.spp, p1 = min(p0 + a.spp, a.pieces);
-    float sA = 1.0f, sB = 0.0f;
-    for (int p = p0; p < p1; ++p) {
-        const int t0 = p * GATE_PIECE + at.gl * LANE_STEPS, n = a.L - t0, t = min(t0, at.last);
-        fwd_raw<T, HI> r;
+    const int map = blockIdx.y, p0 = map * a.ppm, p1 = min(p0 + a.ppm, a.pieces);
+    fwd_raw<T, HI> r;
+    auto load = [&](int p) {
+        const int t0 = p * GATE_PIECE + at.gl * LANE_STEPS, t = min(t0, at.last);
         r.x = slice_load<T>(x, t, a.L, at.whole);
         r.f = slice_load<T>(f, t, a.L, at.whole);
         if constexpr (HI) r.i = slice_load<T>(iv, t, a.L, at.whole);
         if constexpr (RST) r.m = marks_load(reset, t0, a.L);
+    };
+    float sA = 1.0f, sB = 0.0f;
+    load(p0);
+    for (int p = p0; p < p1; ++p) {
         float av[8], bv[8], A, B;
-        steps_of<T, HI, RST>(r, ch, n, av, bv);
+        steps_of<T, HI, RST>(r, ch, a.L - (p * GATE_PIECE + at.gl * LANE_STEPS), av, bv);
+        if (p + 1 < p1) load(p + 1);
         slice_map<RST>(av, bv, A, B);
-        // the lanes' maps in order: lane l's after those of the lanes below
-#pragma unroll
-        for (int k = 1; k < WAVE; k *= 2) {
-            float A1 = __shfl_down(A, k), B1 = __shfl_down(B, k);   // of the half behind
-            affine_after<RST>(A1, B1, A, B);
-            A = A1;
-            B = B1;
-        }
+        LaneScan<WAVE, false, RST> lanes;
+        lanes.scan(A, B, at.lane);
+        lanes.whole(A, B);
         affine_after<RST>(A, B, sA, sB);
         sA = A;
         sB = B;
     }
-    if (at.valid && at.lane == 0) a.agg[(int64_t)seg * a.R + at.row] = make_float2(sA, sB);
+    if (at.valid && at.lane == 0) a.agg[(int64_t)at.row * a.nmap + map] = make_float2(sA, sB);
 }
 
-// The state that enters each segment, from the segments' maps; BACK: the adjoint, from the last segment on.
+// The state that enters each segment, from the maps: a wave a row, whose lanes have neighbouring segments; BACK: the adjoint, from the
+// last segment on.  per: maps of a segment.
 template <bool RST, bool BACK>
-__global__ __launch_bounds__(256) void gate_carry_kernel(GateArgs a)
+__global__ __launch_bounds__(WAVE) void gate_carry_kernel(GateArgs a)
 {
-    const int row = blockIdx.x * 256 + threadIdx.x;
-    if (row >= a.R) return;
+    const int row = blockIdx.x, lane = threadIdx.x, per = a.spp / a.ppm, share = (a.nseg + WAVE - 1) / WAVE;
+    const float2* const maps = a.agg + (int64_t)row * a.nmap;
     float c = 0.0f;
     if (BACK) { if (a.dh_last) c = a.dh_last[row]; }
     else if (a.flags & SS_GATE_HAS_H0) c = a.h0[row];
-    for (int k = 0; k < a.nseg; ++k) {
-        const int64_t e = (int64_t)(BACK ? a.nseg - 1 - k : k) * a.R + row;
-        a.carry[e] = c;
-        if (k + 1 < a.nseg) {
-            const float2 m = a.agg[e];
-            c = affine_of<RST>(m.x, m.y, c);
+    // the lane's segments in time's order (BACK: against it) from s0 on
+    const int s0 = lane * share, s1 = min(s0 + share, a.nseg);
+    auto segment = [&](int s, float& A, float& B) {   // composed onto (A, B)
+        const int first = (BACK ? a.nseg - 1 - s : s) * per;
+        for (int k = 0; k < per; ++k) {
+            const int m = first + (BACK ? per - 1 - k : k);
+            if (m >= a.nmap) continue;
+            float2 v = maps[m];
+            affine_after<RST>(v.x, v.y, A, B);
+            A = v.x;
+            B = v.y;
         }
+    };
+    float A = 1.0f, B = 0.0f;
+    for (int s = s0; s < s1; ++s) segment(s, A, B);
+    LaneScan<WAVE, false, RST> lanes;
+    lanes.scan(A, B, lane);
+    float h = lanes.apply(c, lane);
+    for (int s = s0; s < s1; ++s) {
+        a.carry[(int64_t)(BACK ? a.nseg - 1 - s : s) * a.R + row] = h;
+        A = 1.0f;
+        B = 0.0f;
+        segment(s, A, B);
+        h = affine_of<RST>(A, B, h);
     }
 }
 
@@ -345,10 +430,10 @@ __global__ __launch_bounds__(256) void gate_carry_kernel(GateArgs a)
 //     dx = lam m g,   di = lam v (1 - g),   d(log a) = lam (a h_{t-1} - (g x) a^2 / m) = lam a (h_{t-1} - g x a / m)
 //     log a = -rate s:   df = -d(log a) rate s (1 - s),   drate = -sum d(log a) s
 //     dz = dout h (sz + z sz (1 - sz)),   dy = dout z sz
-template <typename T, int G, bool HI, bool HZ, bool RST>
-__global__ __launch_bounds__(GATE_WAVES* WAVE) void gate_bwd_kernel(GateArgs a)
+template <typename T, int G, int TEAM, bool HI, bool HZ, bool RST>
+__global__ __launch_bounds__(gate_threads<TEAM>()) void gate_bwd_kernel(GateArgs a)
 {
-    const Place<G> at(a);
+    const Place<G, TEAM> at(a);
     const Channel ch = channel_of(a, at.d);
     const T *x = at.template in<T>(a.x, a.xb, a.L), *f = at.template in<T>(a.f, a.fb, a.L);
     const T* iv = HI ? at.template in<T>(a.i, a.ib, a.L) : nullptr;
@@ -364,6 +449,8 @@ __global__ __launch_bounds__(GATE_WAVES* WAVE) void gate_bwd_kernel(GateArgs a)
     else if (a.dh_last) c = a.dh_last[at.row];
     const float k = -GATE_LOG2E * ch.rate, rate2 = 2.0f * ch.rate;
     float sum_q = 0.0f, sum_f = 0.0f, sum_i = 0.0f;
+    __shared__ float2 maps[2][TEAM];
+    TeamScan<TEAM, true, RST> team{maps};
 
     fwd_raw<T, HI> r;
     typename io8<T>::raw rz, rd;
@@ -376,10 +463,12 @@ __global__ __launch_bounds__(GATE_WAVES* WAVE) void gate_bwd_kernel(GateArgs a)
         if constexpr (HZ) rz = slice_load<T>(z, t, a.L, at.whole);
         if constexpr (RST) r.m = marks_load(reset, t0, a.L);
     };
-    load(p1 - 1);
-    for (int p = p1 - 1; p >= p0; --p) {
-        const int t0 = p * GATE_PIECE + at.gl * LANE_STEPS, n = a.L - t0;
-        float start = a.ckpt[(int64_t)p * a.R + at.row];
+    // the team's pieces from the last ones on, the first time as many as are left over
+    const int top = p0 + (p1 - 1 - p0) / TEAM * TEAM;
+    load(min(top + at.member, a.pieces - 1));
+    for (int q = top; q >= p0; q -= TEAM) {
+        const int p = q + at.member, t0 = p * GATE_PIECE + at.gl * LANE_STEPS, n = p < p1 ? a.L - t0 : 0;
+        float start = a.ckpt[(int64_t)min(p, a.pieces - 1) * a.R + at.row];
         float av[8], bv[8], sv[8], gx[8], gv[8], iq[8], hp[8], dy[8], o[8], zv[8];   // iq: 1 / m
         uint2 marks = r.m;
         {
@@ -389,20 +478,20 @@ __global__ __launch_bounds__(GATE_WAVES* WAVE) void gate_bwd_kernel(GateArgs a)
             io8<T>::unpack(rd, dy);
             if constexpr (HI) io8<T>::unpack(r.i, ivv);
             if constexpr (HZ) io8<T>::unpack(rz, zv);
-            if (p > p0) load(p - 1);
+            if (q > p0) load(p - TEAM);
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
                 const bool in = j < n, mk = RST && marked(marks, j);
                 const float s = gate_sigmoid(fv[j] + ch.f_bias);
                 const float aa = exp2_fast(k * s);
                 const float m2 = one_minus_square(rate2 * s, aa);
-                float q = __builtin_amdgcn_rsqf(m2);
-                q = m2 == 0.0f ? 0.0f : q;
+                float rm = __builtin_amdgcn_rsqf(m2);
+                rm = m2 == 0.0f ? 0.0f : rm;
                 const float g = HI ? gate_sigmoid(ivv[j] + ch.i_bias) : 1.0f;
-                const float m = mk ? 1.0f : m2 * q;
+                const float m = mk ? 1.0f : m2 * rm;
                 sv[j] = s;
                 gv[j] = g;
-                iq[j] = q;
+                iq[j] = rm;
                 gx[j] = in ? g * xv[j] : 0.0f;
                 av[j] = in ? (mk ? -1.0f : aa) : 1.0f;
                 bv[j] = in ? m * gx[j] : 0.0f;
@@ -411,7 +500,9 @@ __global__ __launch_bounds__(GATE_WAVES* WAVE) void gate_bwd_kernel(GateArgs a)
         }
         float A, B;
         slice_map<RST>(av, bv, A, B);
-        float h = scan_lanes<G, false, RST>(A, B, start, at.lane);
+        LaneScan<G, false, RST> lanes;
+        lanes.scan(A, B, at.lane);
+        float h = lanes.apply(start, at.lane);
         float gz[8];
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
@@ -439,7 +530,15 @@ __global__ __launch_bounds__(GATE_WAVES* WAVE) void gate_bwd_kernel(GateArgs a)
                 B = B1;
             }
         }
-        float gn = scan_lanes<G, true, RST>(A, B, c, at.lane);
+        LaneScan<G, true, RST> back;
+        back.scan(A, B, at.lane);
+        float own = c;
+        if constexpr (TEAM > 1) {
+            back.whole(A, B);
+            own = team(A, B, c, at.member, at.lane);
+        }
+        float gn = back.apply(own, at.lane);
+        if constexpr (TEAM == 1) c = own;
         float sq = 0.0f, sf = 0.0f, si = 0.0f;
         float o2[8];
 #pragma unroll
@@ -452,9 +551,9 @@ __global__ __launch_bounds__(GATE_WAVES* WAVE) void gate_bwd_kernel(GateArgs a)
                 o[j] = in ? lam * bv[j] * (1.0f - gv[j]) : 0.0f;
                 si += o[j];
             }
-            const float q = mk || !in ? 0.0f : lam * av[j] * (hp[j] - gx[j] * av[j] * iq[j]) * sv[j];
-            sq -= q;
-            o2[j] = -ch.rate * q * (1.0f - sv[j]);
+            const float dr = mk || !in ? 0.0f : lam * av[j] * (hp[j] - gx[j] * av[j] * iq[j]) * sv[j];
+            sq -= dr;
+            o2[j] = -ch.rate * dr * (1.0f - sv[j]);
             sf += o2[j];
             gn = mk ? 0.0f : (in ? av[j] * lam : gn);
         }
@@ -467,14 +566,30 @@ __global__ __launch_bounds__(GATE_WAVES* WAVE) void gate_bwd_kernel(GateArgs a)
             if constexpr (HI) slice_store<T>(di, t0, n, o);
         }
     }
-    if (a.dh0 && at.valid && seg == 0 && at.gl == 0) a.dh0[at.row] = c;
+    if (a.dh0 && at.valid && seg == 0 && at.member == 0 && at.gl == 0) a.dh0[at.row] = c;
 #pragma unroll
     for (int s = 1; s < G; s *= 2) {
         sum_q += __shfl_xor(sum_q, s);
         sum_f += __shfl_xor(sum_f, s);
         if constexpr (HI) sum_i += __shfl_xor(sum_i, s);
     }
-    if (at.valid && at.gl == 0) {
+    if constexpr (TEAM > 1) {
+        __shared__ float sums[3][TEAM];
+        if (at.lane == 0) {
+            sums[0][at.member] = sum_q;
+            sums[1][at.member] = sum_f;
+            sums[2][at.member] = sum_i;
+        }
+        __syncthreads();
+        sum_q = sum_f = sum_i = 0.0f;
+#pragma unroll
+        for (int k = 0; k < TEAM; ++k) {
+            sum_q += sums[0][k];
+            sum_f += sums[1][k];
+            sum_i += sums[2][k];
+        }
+    }
+    if (at.valid && at.member == 0 && at.gl == 0) {
         const int64_t e = (int64_t)seg * a.R + at.row;
         a.part_rate[e] = sum_q;
         if (a.part_f) a.part_f[e] = sum_f;
@@ -482,32 +597,41 @@ __global__ __launch_bounds__(GATE_WAVES* WAVE) void gate_bwd_kernel(GateArgs a)
     }
 }
 
-// A segment's adjoint as one map of G (all but the first one, whose result is dh0's and comes from the main kernel).
+// ppm pieces' adjoint as one map of G.
 template <typename T, bool HZ, bool RST>
 __global__ __launch_bounds__(GATE_WAVES* WAVE) void gate_bwd_map_kernel(GateArgs a)
 {
-    const Place<WAVE> at(a);
+    const Place<WAVE, 1> at(a);
     const Channel ch = channel_of(a, at.d);
     const T* f = at.template in<T>(a.f, a.fb, a.L);
     const T* z = HZ ? at.template in<T>(a.z, a.zb, a.L) : nullptr;
     const T* dout = static_cast<const T*>(a.dout) + (int64_t)at.row * a.L;
     const uint8_t* reset = RST ? a.reset + (int64_t)at.b * a.L : nullptr;
-    const int seg = blockIdx.y + 1, p0 = seg * a.spp, p1 = min(p0 + a.spp, a.pieces);
+    const int map = blockIdx.y, p0 = map * a.ppm, p1 = min(p0 + a.ppm, a.pieces);
     const float k = -GATE_LOG2E * ch.rate;
-    float sA = 1.0f, sB = 0.0f;
-    for (int p = p1 - 1; p >= p0; --p) {
-        const int t0 = p * GATE_PIECE + at.gl * LANE_STEPS, n = a.L - t0, t = min(t0, at.last);
-        const typename io8<T>::raw rf = slice_load<T>(f, t, a.L, at.whole), rd = slice_load<T>(dout, t, a.L, at.whole);
-        float fv[8], dy[8], zv[8];
-        if constexpr (HZ) io8<T>::unpack(slice_load<T>(z, t, a.L, at.whole), zv);
-        uint2 marks = make_uint2(0u, 0u);
+    typename io8<T>::raw rf, rd, rz;
+    uint2 marks = make_uint2(0u, 0u);
+    auto load = [&](int p) {
+        const int t0 = p * GATE_PIECE + at.gl * LANE_STEPS, t = min(t0, at.last);
+        rf = slice_load<T>(f, t, a.L, at.whole);
+        rd = slice_load<T>(dout, t, a.L, at.whole);
+        if constexpr (HZ) rz = slice_load<T>(z, t, a.L, at.whole);
         if constexpr (RST) marks = marks_load(reset, t0, a.L);
+    };
+    float sA = 1.0f, sB = 0.0f;
+    load(p1 - 1);
+    for (int p = p1 - 1; p >= p0; --p) {
+        const int n = a.L - (p * GATE_PIECE + at.gl * LANE_STEPS);
+        float fv[8], dy[8], zv[8];
         io8<T>::unpack(rf, fv);
         io8<T>::unpack(rd, dy);
+        if constexpr (HZ) io8<T>::unpack(rz, zv);
+        const uint2 m = marks;
+        if (p > p0) load(p - 1);
         float A = 1.0f, B = 0.0f;
 #pragma unroll
         for (int j = 7; j >= 0; --j) {
-            const bool in = j < n, mk = RST && marked(marks, j);
+            const bool in = j < n, mk = RST && marked(m, j);
             const float aa = exp2_fast(k * gate_sigmoid(fv[j] + ch.f_bias));
             const float d = HZ ? dy[j] * zv[j] * gate_sigmoid(zv[j]) : dy[j];
             float A1 = in ? (mk ? -1.0f : aa) : 1.0f, B1 = in && !mk ? aa * d : 0.0f;
@@ -515,16 +639,14 @@ __global__ __launch_bounds__(GATE_WAVES* WAVE) void gate_bwd_map_kernel(GateArgs
             A = A1;
             B = B1;
         }
-#pragma unroll
-        for (int s = 1; s < WAVE; s *= 2) {   // lane l's map after (earlier in time) those of the lanes above
-            const float A0 = __shfl_down(A, s), B0 = __shfl_down(B, s);
-            affine_after<RST>(A, B, A0, B0);
-        }
+        LaneScan<WAVE, true, RST> lanes;
+        lanes.scan(A, B, at.lane);
+        lanes.whole(A, B);
         affine_after<RST>(A, B, sA, sB);
         sA = A;
         sB = B;
     }
-    if (at.valid && at.lane == 0) a.agg[(int64_t)seg * a.R + at.row] = make_float2(sA, sB);
+    if (at.valid && at.lane == 0) a.agg[(int64_t)at.row * a.nmap + map] = make_float2(sA, sB);
 }
 
 // Sums of the rows' partial sums over batch entries and segments, in a fixed order: 16 channels of one of the three
@@ -581,7 +703,7 @@ __global__ __launch_bounds__(256) void gate_step_kernel(ss_gate_step_params p)
 }
 
 // ---- launches --------------------------------------------------------------------------------------
-template <int G, typename F>
+template <typename F>
 void with_flags(unsigned flags, F f)
 {
     auto rst = [&](auto i, auto z) { (flags & SS_GATE_HAS_RESET) ? f(i, z, std::true_type{}) : f(i, z, std::false_type{}); };
@@ -592,37 +714,38 @@ void with_flags(unsigned flags, F f)
 // Lanes of a row: all 64 from 128 steps on; below, as many as a power of four (one piece then holds the row)
 int lanes_for(int L) { return L > 16 * LANE_STEPS ? WAVE : (L > 4 * LANE_STEPS ? 16 : 4); }
 
-template <typename T, int G>
+template <typename T, int G, int TEAM>
 void launch_main(const GateArgs& a, bool bwd, hipStream_t st)
 {
-    const int rows = GATE_WAVES * (WAVE / G);
-    const dim3 grid((unsigned)((a.R + rows - 1) / rows), (unsigned)a.nseg), block(GATE_WAVES * WAVE);
-    with_flags<G>(a.flags, [&](auto i, auto z, auto rst) {
-        if (bwd) hipLaunchKernelGGL((gate_bwd_kernel<T, G, decltype(i)::value, decltype(z)::value, decltype(rst)::value>), grid, block, 0, st, a);
-        else hipLaunchKernelGGL((gate_fwd_kernel<T, G, decltype(i)::value, decltype(z)::value, decltype(rst)::value>), grid, block, 0, st, a);
+    const int rows = TEAM > 1 ? 1 : GATE_WAVES * (WAVE / G);
+    const dim3 grid((unsigned)((a.R + rows - 1) / rows), (unsigned)a.nseg), block(gate_threads<TEAM>());
+    with_flags(a.flags, [&](auto i, auto z, auto rst) {
+        if (bwd) hipLaunchKernelGGL((gate_bwd_kernel<T, G, TEAM, decltype(i)::value, decltype(z)::value, decltype(rst)::value>), grid, block, 0, st, a);
+        else hipLaunchKernelGGL((gate_fwd_kernel<T, G, TEAM, decltype(i)::value, decltype(z)::value, decltype(rst)::value>), grid, block, 0, st, a);
     });
 }
 template <typename T>
-void launch_all(const GateArgs& a, bool bwd, hipStream_t st)
+void launch_all(const GateArgs& a, int team, bool bwd, hipStream_t st)
 {
     if (a.nseg > 1) {
-        const dim3 grid((unsigned)((a.R + GATE_WAVES - 1) / GATE_WAVES), (unsigned)(a.nseg - 1)), block(GATE_WAVES * WAVE);
-        const dim3 rows((unsigned)((a.R + 255) / 256));
-        with_flags<WAVE>(a.flags, [&](auto i, auto z, auto rst) {
+        const dim3 grid((unsigned)((a.R + GATE_WAVES - 1) / GATE_WAVES), (unsigned)a.nmap), block(GATE_WAVES * WAVE);
+        with_flags(a.flags, [&](auto i, auto z, auto rst) {
             constexpr bool I = decltype(i)::value, Z = decltype(z)::value, S = decltype(rst)::value;
             if (bwd) {
                 hipLaunchKernelGGL((gate_bwd_map_kernel<T, Z, S>), grid, block, 0, st, a);
-                hipLaunchKernelGGL((gate_carry_kernel<S, true>), rows, dim3(256), 0, st, a);
+                hipLaunchKernelGGL((gate_carry_kernel<S, true>), dim3((unsigned)a.R), dim3(WAVE), 0, st, a);
             } else {
                 hipLaunchKernelGGL((gate_fwd_map_kernel<T, I, S>), grid, block, 0, st, a);
-                hipLaunchKernelGGL((gate_carry_kernel<S, false>), rows, dim3(256), 0, st, a);
+                hipLaunchKernelGGL((gate_carry_kernel<S, false>), dim3((unsigned)a.R), dim3(WAVE), 0, st, a);
             }
         });
     }
     const int g = lanes_for(a.L);
-    if (g == WAVE) launch_main<T, WAVE>(a, bwd, st);
-    else if (g == 16) launch_main<T, 16>(a, bwd, st);
-    else launch_main<T, 4>(a, bwd, st);
+    if (g == 4) launch_main<T, 4, 1>(a, bwd, st);
+    else if (g == 16) launch_main<T, 16, 1>(a, bwd, st);
+    else if (team == 1) launch_main<T, WAVE, 1>(a, bwd, st);
+    else if (team == 4) launch_main<T, WAVE, 4>(a, bwd, st);
+    else launch_main<T, WAVE, 8>(a, bwd, st);
 }
 
 }  // namespace ss
@@ -636,24 +759,29 @@ constexpr uint32_t kGateStepFlags = SS_GATE_HAS_I | SS_GATE_HAS_Z | SS_GATE_HAS_
 inline bool aligned_to(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) % a) == 0; }
 inline size_t round_up(size_t v, size_t a) { return (v + a - 1) / a * a; }
 
-// Segments of a sequence: a chip full of waves where the rows alone are too few.
+// How a sequence is dealt out: the waves that share a row, and segments where the rows with their teams are still too few.
 struct GatePlan {
-    int pieces, nseg, spp;
+    int pieces, team, nseg, spp, nmap, ppm;
 };
 GatePlan gate_plan(long rows, int L)
 {
     GatePlan g;
     g.pieces = (L + ss::GATE_PIECE - 1) / ss::GATE_PIECE;
-    long n = rows >= 2048 ? 1 : (4096 + rows - 1) / rows;
-    if (n > g.pieces) n = g.pieces;
+    g.team = rows >= 4096 || g.pieces < 3 ? 1 : (rows >= 1024 || g.pieces < 6 ? 4 : 8);
+    long n = rows >= 192 || g.team < 8 ? 1 : (512 + rows - 1) / rows;
+    const long most = (g.pieces + 15) / 16;   // a segment has two rounds of its team's at least
+    if (n > most) n = most;
     if (n < 1) n = 1;
     g.spp = (int)((g.pieces + n - 1) / n);
+    if (n > 1) g.spp = (g.spp + g.team - 1) / g.team * g.team;
     if (g.spp < 1) g.spp = 1;
     g.nseg = g.pieces > 0 ? (g.pieces + g.spp - 1) / g.spp : 1;
+    g.ppm = g.nseg > 1 ? g.spp / g.team : g.spp;   // the maps are made by single waves
+    g.nmap = g.pieces > 0 ? (g.pieces + g.ppm - 1) / g.ppm : 1;
     return g;
 }
 
-// Parts of the workspace: checkpoints (pieces, R), maps (nseg, R) pairs, carries (nseg, R), and for the backward call
+// Parts of the workspace: checkpoints (pieces, R), maps (R, nmap) pairs, carries (nseg, R), and for the backward call
 // the rows' sums, three planes of (nseg, R).
 struct GateSpace {
     size_t ckpt, agg, carry, part, total;
@@ -666,7 +794,7 @@ GateSpace gate_space(long rows, const GatePlan& g, bool for_backward)
     s.ckpt = at;
     if (for_backward) at = round_up(at + one * g.pieces, 256);
     s.agg = at;
-    if (g.nseg > 1) at = round_up(at + 2 * one * g.nseg, 256);
+    if (g.nseg > 1) at = round_up(at + 2 * one * g.nmap, 256);
     s.carry = at;
     if (g.nseg > 1) at = round_up(at + one * g.nseg, 256);
     s.part = at;
@@ -705,7 +833,7 @@ GateArgs gate_args(const ss_gate_params* p, const GatePlan& g)
 {
     GateArgs a{};
     a.B = p->batch; a.D = p->dim; a.L = p->seqlen; a.R = p->batch * p->dim;
-    a.pieces = g.pieces; a.nseg = g.nseg; a.spp = g.spp;
+    a.pieces = g.pieces; a.nseg = g.nseg; a.spp = g.spp; a.nmap = g.nmap; a.ppm = g.ppm;
     a.flags = p->flags;
     a.x = p->x; a.f = p->f; a.i = p->i; a.z = p->z;
     a.xb = p->x_batch; a.fb = p->f_batch; a.ib = p->i_batch; a.zb = p->z_batch;
@@ -741,8 +869,8 @@ int ss_gate_fwd(const ss_gate_params* p, void* stream)
     const bool have = ws && p->workspace_bytes >= s.total;
     if (save && s.total > 0 && !have) return SS_ERR_WORKSPACE;
     if (!have) {
-        g.nseg = 1;
-        g.spp = g.pieces;
+        g.nseg = g.nmap = 1;
+        g.spp = g.ppm = g.pieces;
     }
     hipStream_t st = static_cast<hipStream_t>(stream);
     GateArgs a = gate_args(p, g);
@@ -757,8 +885,8 @@ int ss_gate_fwd(const ss_gate_params* p, void* stream)
         a.agg = reinterpret_cast<float2*>(ws + s.agg);
         a.carry = reinterpret_cast<float*>(ws + s.carry);
     }
-    if (p->io_dtype == SS_BF16) ss::launch_all<ss::bf16_t>(a, false, st);
-    else ss::launch_all<float>(a, false, st);
+    if (p->io_dtype == SS_BF16) ss::launch_all<ss::bf16_t>(a, g.team, false, st);
+    else ss::launch_all<float>(a, g.team, false, st);
     return hipGetLastError() == hipSuccess ? SS_OK : SS_ERR_LAUNCH;
 }
 
@@ -810,8 +938,8 @@ int ss_gate_bwd(const ss_gate_bwd_params* p, void* stream)
     a.part_rate = direct ? p->drate : part;
     a.part_f = fb ? (direct ? p->df_bias : part + plane) : nullptr;
     a.part_i = ib ? (direct ? p->di_bias : part + 2 * plane) : nullptr;
-    if (q->io_dtype == SS_BF16) ss::launch_all<ss::bf16_t>(a, true, st);
-    else ss::launch_all<float>(a, true, st);
+    if (q->io_dtype == SS_BF16) ss::launch_all<ss::bf16_t>(a, g.team, true, st);
+    else ss::launch_all<float>(a, g.team, true, st);
     if (!direct)
         hipLaunchKernelGGL(ss::gate_sums_kernel, dim3((unsigned)((q->dim + 15) / 16), ib ? 3u : (fb ? 2u : 1u)), dim3(256), 0, st, part, p->drate,
                            fb ? p->df_bias : nullptr, ib ? p->di_bias : nullptr, plane, q->dim, g.nseg * q->batch);
