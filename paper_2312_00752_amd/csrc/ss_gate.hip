@@ -221,7 +221,7 @@ __device__ __forceinline__ Channel channel_of(const GateArgs& a, int d)
 // Where a lane works: its row, and what is common to the row's slices.
 template <int G, int TEAM>
 struct Place {
-    int lane, gl, row, b, d, last;   // last: the start of the row's last slice
+    int lane, gl, row, b, d, limit;   // limit: slice_limit of the row
     int member;                      // of the team
     bool valid, whole;
     __device__ __forceinline__ Place(const GateArgs& a)
@@ -236,12 +236,15 @@ struct Place {
         row = min(row, a.R - 1);
         b = row / a.D;
         d = row - b * a.D;
-        last = (a.L - 1) / LANE_STEPS * LANE_STEPS;
-        // the tensor's last row is in the last wave only
-        whole = a.L % LANE_STEPS == 0 || (a.L >= LANE_STEPS && (wave + 1) * (WAVE / G) < a.R);
+        whole = slice_whole(a.L, (wave + 1) * (WAVE / G) >= a.R);   // the tensor's last row is in the last wave only
+        limit = slice_limit(a.L, whole);
     }
     template <typename T>
     __device__ __forceinline__ const T* in(const void* p, int64_t batch, int L) const { return static_cast<const T*>(p) + b * batch + (int64_t)d * L; }
+    template <typename T>
+    __device__ __forceinline__ typename io8<T>::raw request(const T* row, int t0, int L) const { return slice_request<T, G == 4>(row, t0, L, limit); }
+    template <typename T>
+    __device__ __forceinline__ void settle(typename io8<T>::raw& r, int t0, int L) const { slice_settle<T>(r, t0, L, limit, whole); }
     template <typename T>
     __device__ __forceinline__ T* to(void* p, int64_t batch, int L) const { return static_cast<T*>(p) + b * batch + (int64_t)d * L; }
 };
@@ -316,11 +319,11 @@ __global__ __launch_bounds__(gate_threads<TEAM>()) void gate_fwd_kernel(GateArgs
     fwd_raw<T, HI> r;
     typename io8<T>::raw rz;
     auto load = [&](int p) {
-        const int t0 = p * GATE_PIECE + at.gl * LANE_STEPS, t = min(t0, at.last);
-        r.x = slice_load<T>(x, t, a.L, at.whole);
-        r.f = slice_load<T>(f, t, a.L, at.whole);
-        if constexpr (HI) r.i = slice_load<T>(iv, t, a.L, at.whole);
-        if constexpr (HZ) rz = slice_load<T>(z, t, a.L, at.whole);
+        const int t0 = p * GATE_PIECE + at.gl * LANE_STEPS;
+        r.x = at.template request<T>(x, t0, a.L);
+        r.f = at.template request<T>(f, t0, a.L);
+        if constexpr (HI) r.i = at.template request<T>(iv, t0, a.L);
+        if constexpr (HZ) rz = at.template request<T>(z, t0, a.L);
         if constexpr (RST) r.m = marks_load(reset, t0, a.L);
     };
     // a team's members that have no piece left take part with maps that change nothing
@@ -328,6 +331,12 @@ __global__ __launch_bounds__(gate_threads<TEAM>()) void gate_fwd_kernel(GateArgs
     for (int q = p0; q < p1; q += TEAM) {
         const int p = q + at.member, t0 = p * GATE_PIECE + at.gl * LANE_STEPS, n = p < p1 ? a.L - t0 : 0;
         float av[8], bv[8], zv[8], y[8];
+        if (!at.whole) {
+            at.template settle<T>(r.x, t0, a.L);
+            at.template settle<T>(r.f, t0, a.L);
+            if constexpr (HI) at.template settle<T>(r.i, t0, a.L);
+            if constexpr (HZ) at.template settle<T>(rz, t0, a.L);
+        }
         steps_of<T, HI, RST>(r, ch, n, av, bv);
         if constexpr (HZ) io8<T>::unpack(rz, zv);
         if (q + TEAM < p1) load(min(p + TEAM, a.pieces - 1));
@@ -365,17 +374,23 @@ __global__ __launch_bounds__(GATE_WAVES* WAVE) void gate_fwd_map_kernel(GateArgs
     const int map = blockIdx.y, p0 = map * a.ppm, p1 = min(p0 + a.ppm, a.pieces);
     fwd_raw<T, HI> r;
     auto load = [&](int p) {
-        const int t0 = p * GATE_PIECE + at.gl * LANE_STEPS, t = min(t0, at.last);
-        r.x = slice_load<T>(x, t, a.L, at.whole);
-        r.f = slice_load<T>(f, t, a.L, at.whole);
-        if constexpr (HI) r.i = slice_load<T>(iv, t, a.L, at.whole);
+        const int t0 = p * GATE_PIECE + at.gl * LANE_STEPS;
+        r.x = at.template request<T>(x, t0, a.L);
+        r.f = at.template request<T>(f, t0, a.L);
+        if constexpr (HI) r.i = at.template request<T>(iv, t0, a.L);
         if constexpr (RST) r.m = marks_load(reset, t0, a.L);
     };
     float sA = 1.0f, sB = 0.0f;
     load(p0);
     for (int p = p0; p < p1; ++p) {
+        const int t0 = p * GATE_PIECE + at.gl * LANE_STEPS;
+        if (!at.whole) {
+            at.template settle<T>(r.x, t0, a.L);
+            at.template settle<T>(r.f, t0, a.L);
+            if constexpr (HI) at.template settle<T>(r.i, t0, a.L);
+        }
         float av[8], bv[8], A, B;
-        steps_of<T, HI, RST>(r, ch, a.L - (p * GATE_PIECE + at.gl * LANE_STEPS), av, bv);
+        steps_of<T, HI, RST>(r, ch, a.L - t0, av, bv);
         if (p + 1 < p1) load(p + 1);
         slice_map<RST>(av, bv, A, B);
         LaneScan<WAVE, false, RST> lanes;
@@ -455,12 +470,12 @@ __global__ __launch_bounds__(gate_threads<TEAM>()) void gate_bwd_kernel(GateArgs
     fwd_raw<T, HI> r;
     typename io8<T>::raw rz, rd;
     auto load = [&](int p) {
-        const int t0 = p * GATE_PIECE + at.gl * LANE_STEPS, t = min(t0, at.last);
-        r.x = slice_load<T>(x, t, a.L, at.whole);
-        r.f = slice_load<T>(f, t, a.L, at.whole);
-        rd = slice_load<T>(dout, t, a.L, at.whole);
-        if constexpr (HI) r.i = slice_load<T>(iv, t, a.L, at.whole);
-        if constexpr (HZ) rz = slice_load<T>(z, t, a.L, at.whole);
+        const int t0 = p * GATE_PIECE + at.gl * LANE_STEPS;
+        r.x = at.template request<T>(x, t0, a.L);
+        r.f = at.template request<T>(f, t0, a.L);
+        rd = at.template request<T>(dout, t0, a.L);
+        if constexpr (HI) r.i = at.template request<T>(iv, t0, a.L);
+        if constexpr (HZ) rz = at.template request<T>(z, t0, a.L);
         if constexpr (RST) r.m = marks_load(reset, t0, a.L);
     };
     // the team's pieces from the last ones on, the first time as many as are left over
@@ -471,6 +486,13 @@ __global__ __launch_bounds__(gate_threads<TEAM>()) void gate_bwd_kernel(GateArgs
         float start = a.ckpt[(int64_t)min(p, a.pieces - 1) * a.R + at.row];
         float av[8], bv[8], sv[8], gx[8], gv[8], iq[8], hp[8], dy[8], o[8], zv[8];   // iq: 1 / m
         uint2 marks = r.m;
+        if (!at.whole) {
+            at.template settle<T>(r.x, t0, a.L);
+            at.template settle<T>(r.f, t0, a.L);
+            at.template settle<T>(rd, t0, a.L);
+            if constexpr (HI) at.template settle<T>(r.i, t0, a.L);
+            if constexpr (HZ) at.template settle<T>(rz, t0, a.L);
+        }
         {
             float xv[8], fv[8], ivv[8];
             io8<T>::unpack(r.x, xv);
@@ -612,16 +634,21 @@ __global__ __launch_bounds__(GATE_WAVES* WAVE) void gate_bwd_map_kernel(GateArgs
     typename io8<T>::raw rf, rd, rz;
     uint2 marks = make_uint2(0u, 0u);
     auto load = [&](int p) {
-        const int t0 = p * GATE_PIECE + at.gl * LANE_STEPS, t = min(t0, at.last);
-        rf = slice_load<T>(f, t, a.L, at.whole);
-        rd = slice_load<T>(dout, t, a.L, at.whole);
-        if constexpr (HZ) rz = slice_load<T>(z, t, a.L, at.whole);
+        const int t0 = p * GATE_PIECE + at.gl * LANE_STEPS;
+        rf = at.template request<T>(f, t0, a.L);
+        rd = at.template request<T>(dout, t0, a.L);
+        if constexpr (HZ) rz = at.template request<T>(z, t0, a.L);
         if constexpr (RST) marks = marks_load(reset, t0, a.L);
     };
     float sA = 1.0f, sB = 0.0f;
     load(p1 - 1);
     for (int p = p1 - 1; p >= p0; --p) {
-        const int n = a.L - (p * GATE_PIECE + at.gl * LANE_STEPS);
+        const int t0 = p * GATE_PIECE + at.gl * LANE_STEPS, n = a.L - t0;
+        if (!at.whole) {
+            at.template settle<T>(rf, t0, a.L);
+            at.template settle<T>(rd, t0, a.L);
+            if constexpr (HZ) at.template settle<T>(rz, t0, a.L);
+        }
         float fv[8], dy[8], zv[8];
         io8<T>::unpack(rf, fv);
         io8<T>::unpack(rd, dy);

@@ -84,7 +84,7 @@ __global__ __launch_bounds__(norm_threads<G>(false)) void norm_fwd_kernel(NormAr
     constexpr int THREADS = norm_threads<G>(false), SIDE = THREADS / G;
     __shared__ float lds[2][1][RowSum<G, 1>::WAVES];
     RowSum<G, 1> sum{lds};
-    const int gl = threadIdx.x % G, W = a.width, last = (W - 1) / 8 * 8;
+    const int gl = threadIdx.x % G, W = a.width;
     float w[V][8], b[V][8];
 #pragma unroll
     for (int v = 0; v < V; ++v) {
@@ -98,14 +98,14 @@ __global__ __launch_bounds__(norm_threads<G>(false)) void norm_fwd_kernel(NormAr
     typename io8<S>::raw rr[V];
     auto load = [&](int row) {
         row = min(row, a.rows - 1);
-        const bool whole = W % 8 == 0 || (W >= 8 && row < a.rows - 1);
+        const int limit = slice_limit(W, slice_whole(W, row == a.rows - 1));
         const T* x = static_cast<const T*>(a.x) + (int64_t)row * W;
         const S* r = static_cast<const S*>(a.residual) + (int64_t)row * W;
 #pragma unroll
         for (int v = 0; v < V; ++v) {
-            const int at = min((v * G + gl) * 8, last);
-            rx[v] = slice_load<T>(x, at, W, whole);
-            if constexpr (RES) rr[v] = slice_load<S>(r, at, W, whole);
+            const int at = (v * G + gl) * 8;
+            rx[v] = slice_request<T, G == 16>(x, at, W, limit);
+            if constexpr (RES) rr[v] = slice_request<S, G == 16>(r, at, W, limit);
         }
     };
     // G > 64: all lanes of the workgroup share the row, so they leave the loop together (the sums hold barriers); else rows
@@ -115,7 +115,15 @@ __global__ __launch_bounds__(norm_threads<G>(false)) void norm_fwd_kernel(NormAr
     for (int row = first; row - (int)(threadIdx.x / G) < a.rows; row += step) {
         if constexpr (!norm_ahead<G>()) load(row);
         float s[V][8];
-        const bool valid = row < a.rows;
+        const bool valid = row < a.rows, whole = slice_whole(W, row >= a.rows - 1);
+        if (!whole) {
+            const int limit = slice_limit(W, false);
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                slice_settle<T>(rx[v], (v * G + gl) * 8, W, limit, false);
+                if constexpr (RES) slice_settle<S>(rr[v], (v * G + gl) * 8, W, limit, false);
+            }
+        }
 #pragma unroll
         for (int v = 0; v < V; ++v) {
             io8<T>::unpack(rx[v], s[v]);
@@ -186,7 +194,7 @@ __global__ __launch_bounds__(norm_threads<G>(true)) void norm_bwd_kernel(NormArg
     constexpr int THREADS = norm_threads<G>(true), SIDE = THREADS / G;
     __shared__ float lds[2][2][RowSum<G, 2>::WAVES];
     RowSum<G, 2> sum{lds};
-    const int gl = threadIdx.x % G, W = a.width, last = (W - 1) / 8 * 8;
+    const int gl = threadIdx.x % G, W = a.width;
     float w[V][8], dw[V][8], db[V][8];
 #pragma unroll
     for (int v = 0; v < V; ++v) {
@@ -202,15 +210,15 @@ __global__ __launch_bounds__(norm_threads<G>(true)) void norm_bwd_kernel(NormArg
     float mean_next, rstd_next;
     auto load = [&](int row) {
         row = min(row, a.rows - 1);
-        const bool whole = W % 8 == 0 || (W >= 8 && row < a.rows - 1);
+        const int limit = slice_limit(W, slice_whole(W, row == a.rows - 1));
         const int64_t off = (int64_t)row * W;
 #pragma unroll
         for (int v = 0; v < V; ++v) {
-            const int at = min((v * G + gl) * 8, last);
-            rs[v] = slice_load<S>(static_cast<const S*>(a.s) + off, at, W, whole);
-            rd[v] = slice_load<T>(static_cast<const T*>(a.dout) + off, at, W, whole);
+            const int at = (v * G + gl) * 8;
+            rs[v] = slice_request<S, G == 16>(static_cast<const S*>(a.s) + off, at, W, limit);
+            rd[v] = slice_request<T, G == 16>(static_cast<const T*>(a.dout) + off, at, W, limit);
             if constexpr (RES && norm_ahead<G>())
-                if (more) rm[v] = slice_load<S>(static_cast<const S*>(a.dsummed) + off, at, W, whole);
+                if (more) rm[v] = slice_request<S, G == 16>(static_cast<const S*>(a.dsummed) + off, at, W, limit);
         }
         mean_next = a.mean[row];
         rstd_next = a.rstd[row];
@@ -223,6 +231,16 @@ __global__ __launch_bounds__(norm_threads<G>(true)) void norm_bwd_kernel(NormArg
         const float mean = mean_next, rstd = rstd_next;
         float x[V][8], g[V][8], m[V][8];
         float t[2] = {0.0f, 0.0f};
+        if (!slice_whole(W, row >= a.rows - 1)) {
+            const int limit = slice_limit(W, false);
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                slice_settle<S>(rs[v], (v * G + gl) * 8, W, limit, false);
+                slice_settle<T>(rd[v], (v * G + gl) * 8, W, limit, false);
+                if constexpr (RES && norm_ahead<G>())
+                    if (more) slice_settle<S>(rm[v], (v * G + gl) * 8, W, limit, false);
+            }
+        }
 #pragma unroll
         for (int v = 0; v < V; ++v) {
             io8<S>::unpack(rs[v], x[v]);
@@ -272,8 +290,10 @@ __global__ __launch_bounds__(norm_threads<G>(true)) void norm_bwd_kernel(NormArg
                 if constexpr (RES && !norm_ahead<G>()) {
                     if (more) {
                         float mv[8];
-                        const bool whole = W % 8 == 0 || (W >= 8 && row < a.rows - 1);
-                        io8<S>::unpack(slice_load<S>(static_cast<const S*>(a.dsummed) + off, min(at, last), W, whole), mv);
+                        const bool whole = slice_whole(W, row == a.rows - 1);
+                        typename io8<S>::raw r = slice_request<S, false>(static_cast<const S*>(a.dsummed) + off, at, W, slice_limit(W, whole));
+                        slice_settle<S>(r, at, W, slice_limit(W, whole), whole);
+                        io8<S>::unpack(r, mv);
 #pragma unroll
                         for (int j = 0; j < 8; ++j) o[j] += mv[j];
                     }

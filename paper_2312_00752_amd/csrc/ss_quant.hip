@@ -66,15 +66,20 @@ __global__ __launch_bounds__(G > 256 ? G : 256) void quant_rows_kernel(const T* 
 {
     constexpr int THREADS = G > 256 ? G : 256, SIDE = THREADS / G, WAVES = G > WAVE ? G / WAVE : 1;
     __shared__ uint32_t lds[WAVES];
-    const int gl = threadIdx.x % G, last = (dim - 1) / 8 * 8;
+    const int gl = threadIdx.x % G;
     const int row0 = blockIdx.x * SIDE + threadIdx.x / G;
     const bool valid = row0 < rows;
     const int row = min(row0, rows - 1);
-    const bool whole = dim % 8 == 0 || (dim >= 8 && row < rows - 1);
+    const bool whole = slice_whole(dim, row == rows - 1);
+    const int limit = slice_limit(dim, whole);
     const T* r = x + (int64_t)row * dim;
     typename io8<T>::raw raw[V];
 #pragma unroll
-    for (int v = 0; v < V; ++v) raw[v] = slice_load<T>(r, min((v * G + gl) * 8, last), dim, whole);
+    for (int v = 0; v < V; ++v) raw[v] = slice_request<T, G == 64 && V == 1>(r, (v * G + gl) * 8, dim, limit);
+    if (!whole) {
+#pragma unroll
+        for (int v = 0; v < V; ++v) slice_settle<T>(raw[v], (v * G + gl) * 8, dim, limit, false);
+    }
     float f[V][8];
     uint32_t top = 0u;
 #pragma unroll
@@ -133,12 +138,14 @@ __global__ __launch_bounds__(256) void quant_tops_kernel(const T* x, uint32_t* t
     // thread: 8 tokens, every 8th channel of the chunk; 32 threads side by side
     __shared__ uint32_t lds[8][32][9];
     const int t0 = blockIdx.x * 256 + (threadIdx.x % 32) * 8, kk = threadIdx.x / 32, b = blockIdx.z, k0 = blockIdx.y * Q_CHUNK;
-    const int last = (L - 1) / 8 * 8, at = min(t0, last);
     uint32_t top[8] = {0u, 0u, 0u, 0u, 0u, 0u, 0u, 0u};
     for (int k = k0 + kk; k < min(k0 + Q_CHUNK, dim); k += 8) {
-        const bool whole = L % 8 == 0 || (L >= 8 && !(b == batch - 1 && k == dim - 1));
+        const bool whole = slice_whole(L, b == batch - 1 && k == dim - 1);
+        const int limit = slice_limit(L, whole);
+        typename io8<T>::raw r = slice_request<T, true>(x + ((int64_t)b * dim + k) * L, t0, L, limit);
+        slice_settle<T>(r, t0, L, limit, whole);
         float v[8];
-        io8<T>::unpack(slice_load<T>(x + ((int64_t)b * dim + k) * L, at, L, whole), v);
+        io8<T>::unpack(r, v);
 #pragma unroll
         for (int j = 0; j < 8; ++j) top[j] = max(top[j], magnitude(v[j]));
     }
@@ -168,7 +175,7 @@ __global__ __launch_bounds__(256) void quant_turn_kernel(const T* x, const uint3
         if (blockIdx.y == 0 && t < L) scale[(int64_t)b * L + t] = s.scale;
     }
     __syncthreads();
-    const int last = (L - 1) / 8 * 8, i = threadIdx.x % 8, at = min(t0 + 8 * i, last);
+    const int i = threadIdx.x % 8;
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
         const int kl = r * 32 + threadIdx.x / 8, k = k0 + kl;
@@ -176,8 +183,11 @@ __global__ __launch_bounds__(256) void quant_turn_kernel(const T* x, const uint3
 #pragma unroll
         for (int j = 0; j < 8; ++j) v[j] = 0.0f;
         if (k < dim) {
-            const bool whole = L % 8 == 0 || (L >= 8 && !(b == batch - 1 && k == dim - 1));
-            io8<T>::unpack(slice_load<T>(x + ((int64_t)b * dim + k) * L, at, L, whole), v);
+            const bool whole = slice_whole(L, b == batch - 1 && k == dim - 1);
+            const int limit = slice_limit(L, whole);
+            typename io8<T>::raw raw = slice_request<T, true>(x + ((int64_t)b * dim + k) * L, t0 + 8 * i, L, limit);
+            slice_settle<T>(raw, t0 + 8 * i, L, limit, whole);
+            io8<T>::unpack(raw, v);
         }
 #pragma unroll
         for (int j = 0; j < 8; ++j) tile[8 * i + j][kl] = (int8_t)quantised(v[j], inv[8 * i + j]);
@@ -436,8 +446,8 @@ __global__ __launch_bounds__(WAVES* WAVE) void qfew_kernel(QFewArgs a)
         if (threadIdx.x < 16) tops[threadIdx.x] = 0u;
 #pragma unroll
         for (int v = 0; v < SLICES; ++v) {
-            const int s = v * THREADS + threadIdx.x, t = min(s / per, a.tokens - 1), at = min((s - s / per * per) * 8, (a.dim - 1) / 8 * 8);
-            raw[v] = slice_load<T>(static_cast<const T*>(a.x) + (int64_t)t * a.dim, at, a.dim, a.dim % 8 == 0 || t < a.tokens - 1);
+            const int s = v * THREADS + threadIdx.x, t = min(s / per, a.tokens - 1), at = (s - s / per * per) * 8;
+            raw[v] = slice_request<T, false>(static_cast<const T*>(a.x) + (int64_t)t * a.dim, at, a.dim, slice_limit(a.dim, slice_whole(a.dim, t == a.tokens - 1)));
         }
     }
     i32x4 fw[FEW_AHEAD][2];
@@ -456,6 +466,7 @@ __global__ __launch_bounds__(WAVES* WAVE) void qfew_kernel(QFewArgs a)
 #pragma unroll
         for (int v = 0; v < SLICES; ++v) {
             const int s = v * THREADS + threadIdx.x, t = s / per, n = a.dim - (s - t * per) * 8;
+            if (!slice_whole(a.dim, t >= a.tokens - 1)) slice_settle<T>(raw[v], a.dim - n, a.dim, slice_limit(a.dim, false), false);
             io8<T>::unpack(raw[v], f[v]);
             uint32_t top = 0u;
 #pragma unroll
