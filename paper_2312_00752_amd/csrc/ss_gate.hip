@@ -95,10 +95,11 @@ __device__ __forceinline__ void scan_step(float& A, float& B, int gl)
 }
 // (A, B): a lane's slice as one map.  scan() composes those of the lanes before it (BACK: behind it, in time) onto it; apply() returns
 // the state before the slice, given `c`, the one before the piece, which becomes the one after it.
-template <int G, bool BACK, bool RST>
+template <int G, bool BACK>
 struct LaneScan {
     float A, B;                  // through the lane, within its row of 16 lanes (its group, if smaller)
     float rA[4], rB[4];          // G == 64: the rows of lanes, in time's order
+    template <bool RST>
     __device__ __forceinline__ void scan(float A_, float B_, int lane)
     {
         A = A_;
@@ -116,6 +117,7 @@ struct LaneScan {
             }
         }
     }
+    template <bool RST>
     __device__ __forceinline__ void whole(float& WA, float& WB) const   // the wave's map
     {
         WA = rA[0];
@@ -128,6 +130,7 @@ struct LaneScan {
             WB = B1;
         }
     }
+    template <bool RST>
     __device__ __forceinline__ float apply(float& c, int lane) const
     {
         const int gl = lane & (G - 1);
@@ -178,20 +181,39 @@ struct TeamScan {
 };
 
 // ---- reset marks ---------------------------------------------------------------------------
-__device__ __forceinline__ uint2 marks_load(const uint8_t* row, int t0, int L)   // eight reset marks, zeros past the row
+// Eight reset marks, asked for like a slice (nothing waits between the request and the use) and shifted into place when they are
+// used, zeros past the row.
+template <bool TINY>
+__device__ __forceinline__ uint2 marks_request(const uint8_t* row, int t0, int L)
 {
-    if (L >= 8) {
-        const int t = min(t0, L - 8);
-        typedef uint32_t u2 __attribute__((ext_vector_type(2)));
-        const u2 v = load_any<u2>(row + t, 0u);
-        const int s = 8 * (t0 - t);
-        const uint64_t w = s < 64 ? ((uint64_t(v[1]) << 32) | v[0]) >> s : 0;
-        return make_uint2((uint32_t)w, (uint32_t)(w >> 32));
+    if constexpr (TINY)
+        if (L < 8) {
+            uint32_t w[2] = {0u, 0u};
+            for (int j = 0; j < 8; ++j)
+                if (t0 + j < L) w[j >> 2] |= uint32_t(row[t0 + j]) << (8 * (j & 3));
+            return make_uint2(w[0], w[1]);
+        }
+    typedef uint32_t u2 __attribute__((ext_vector_type(2)));
+    const u2 v = load_any<u2>(row + min(t0, L - 8), 0u);
+    return make_uint2(v[0], v[1]);
+}
+__device__ __forceinline__ uint2 marks_settle(uint2 m, int t0, int L)
+{
+    const int s = 8 * (t0 - (L - 8));   // L < 8: the marks are in place
+    if (s <= 0 || L < 8) return m;
+    const uint64_t w = s < 64 ? ((uint64_t(m.y) << 32) | m.x) >> s : 0;
+    return make_uint2((uint32_t)w, (uint32_t)(w >> 32));
+}
+// f with true where a lane of the wave has a mark, else with false: most pieces have none, and do without the selects
+template <bool RST, typename F>
+__device__ __forceinline__ void with_marks(bool any, F f)
+{
+    if constexpr (RST) {
+        if (any) f(std::true_type{});
+        else f(std::false_type{});
+    } else {
+        f(std::false_type{});
     }
-    uint32_t w[2] = {0u, 0u};
-    for (int j = 0; j < 8; ++j)
-        if (t0 + j < L) w[j >> 2] |= uint32_t(row[t0 + j]) << (8 * (j & 3));
-    return make_uint2(w[0], w[1]);
 }
 __device__ __forceinline__ bool marked(uint2 m, int j) { return ((j < 4 ? m.x : m.y) & (0xffu << (8 * (j & 3)))) != 0; }
 
@@ -324,7 +346,7 @@ __global__ __launch_bounds__(gate_threads<TEAM>()) void gate_fwd_kernel(GateArgs
         r.f = at.template request<T>(f, t0, a.L);
         if constexpr (HI) r.i = at.template request<T>(iv, t0, a.L);
         if constexpr (HZ) rz = at.template request<T>(z, t0, a.L);
-        if constexpr (RST) r.m = marks_load(reset, t0, a.L);
+        if constexpr (RST) r.m = marks_request<G == 4>(reset, t0, a.L);
     };
     // a team's members that have no piece left take part with maps that change nothing
     load(min(p0 + at.member, a.pieces - 1));
@@ -337,26 +359,32 @@ __global__ __launch_bounds__(gate_threads<TEAM>()) void gate_fwd_kernel(GateArgs
             if constexpr (HI) at.template settle<T>(r.i, t0, a.L);
             if constexpr (HZ) at.template settle<T>(rz, t0, a.L);
         }
-        steps_of<T, HI, RST>(r, ch, n, av, bv);
-        if constexpr (HZ) io8<T>::unpack(rz, zv);
-        if (q + TEAM < p1) load(min(p + TEAM, a.pieces - 1));
+        if constexpr (RST) r.m = marks_settle(r.m, t0, a.L);
+        const bool any = RST && __any((r.m.x | r.m.y) != 0u);
+        LaneScan<G, false> lanes;
         float A, B;
-        slice_map<RST>(av, bv, A, B);
-        LaneScan<G, false, RST> lanes;
-        lanes.scan(A, B, at.lane);
+        with_marks<RST>(any, [&](auto marks) {
+            constexpr bool S = decltype(marks)::value;
+            steps_of<T, HI, S>(r, ch, n, av, bv);
+            if constexpr (HZ) io8<T>::unpack(rz, zv);
+            if (q + TEAM < p1) load(min(p + TEAM, a.pieces - 1));
+            slice_map<S>(av, bv, A, B);
+            lanes.template scan<S>(A, B, at.lane);
+            if constexpr (TEAM > 1) lanes.template whole<S>(A, B);
+        });
         float own = c;
-        if constexpr (TEAM > 1) {
-            lanes.whole(A, B);
-            own = team(A, B, c, at.member, at.lane);
-        }
+        if constexpr (TEAM > 1) own = team(A, B, c, at.member, at.lane);
         if (a.ckpt && at.valid && at.gl == 0 && p < p1) a.ckpt[(int64_t)p * a.R + at.row] = own;
-        float h = lanes.apply(own, at.lane);
-        if constexpr (TEAM == 1) c = own;
+        with_marks<RST>(any, [&](auto marks) {
+            constexpr bool S = decltype(marks)::value;
+            float h = lanes.template apply<S>(own, at.lane);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            h = affine_of<RST>(av[j], bv[j], h);
-            y[j] = HZ ? h * zv[j] * gate_sigmoid(zv[j]) : h;
-        }
+            for (int j = 0; j < 8; ++j) {
+                h = affine_of<S>(av[j], bv[j], h);
+                y[j] = HZ ? h * zv[j] * gate_sigmoid(zv[j]) : h;
+            }
+        });
+        if constexpr (TEAM == 1) c = own;
         if (at.valid) slice_store<T>(out, t0, n, y);
     }
     if (a.h_last && at.valid && seg == a.nseg - 1 && at.member == 0 && at.gl == (G == WAVE ? 0 : G - 1)) a.h_last[at.row] = c;
@@ -378,7 +406,7 @@ __global__ __launch_bounds__(GATE_WAVES* WAVE) void gate_fwd_map_kernel(GateArgs
         r.x = at.template request<T>(x, t0, a.L);
         r.f = at.template request<T>(f, t0, a.L);
         if constexpr (HI) r.i = at.template request<T>(iv, t0, a.L);
-        if constexpr (RST) r.m = marks_load(reset, t0, a.L);
+        if constexpr (RST) r.m = marks_request<false>(reset, t0, a.L);
     };
     float sA = 1.0f, sB = 0.0f;
     load(p0);
@@ -389,13 +417,14 @@ __global__ __launch_bounds__(GATE_WAVES* WAVE) void gate_fwd_map_kernel(GateArgs
             at.template settle<T>(r.f, t0, a.L);
             if constexpr (HI) at.template settle<T>(r.i, t0, a.L);
         }
+        if constexpr (RST) r.m = marks_settle(r.m, t0, a.L);
         float av[8], bv[8], A, B;
         steps_of<T, HI, RST>(r, ch, a.L - t0, av, bv);
         if (p + 1 < p1) load(p + 1);
         slice_map<RST>(av, bv, A, B);
-        LaneScan<WAVE, false, RST> lanes;
-        lanes.scan(A, B, at.lane);
-        lanes.whole(A, B);
+        LaneScan<WAVE, false> lanes;
+        lanes.template scan<RST>(A, B, at.lane);
+        lanes.template whole<RST>(A, B);
         affine_after<RST>(A, B, sA, sB);
         sA = A;
         sB = B;
@@ -428,9 +457,9 @@ __global__ __launch_bounds__(WAVE) void gate_carry_kernel(GateArgs a)
     };
     float A = 1.0f, B = 0.0f;
     for (int s = s0; s < s1; ++s) segment(s, A, B);
-    LaneScan<WAVE, false, RST> lanes;
-    lanes.scan(A, B, lane);
-    float h = lanes.apply(c, lane);
+    LaneScan<WAVE, false> lanes;
+    lanes.template scan<RST>(A, B, lane);
+    float h = lanes.template apply<RST>(c, lane);
     for (int s = s0; s < s1; ++s) {
         a.carry[(int64_t)(BACK ? a.nseg - 1 - s : s) * a.R + row] = h;
         A = 1.0f;
@@ -476,7 +505,7 @@ __global__ __launch_bounds__(gate_threads<TEAM>()) void gate_bwd_kernel(GateArgs
         rd = at.template request<T>(dout, t0, a.L);
         if constexpr (HI) r.i = at.template request<T>(iv, t0, a.L);
         if constexpr (HZ) rz = at.template request<T>(z, t0, a.L);
-        if constexpr (RST) r.m = marks_load(reset, t0, a.L);
+        if constexpr (RST) r.m = marks_request<G == 4>(reset, t0, a.L);
     };
     // the team's pieces from the last ones on, the first time as many as are left over
     const int top = p0 + (p1 - 1 - p0) / TEAM * TEAM;
@@ -485,7 +514,8 @@ __global__ __launch_bounds__(gate_threads<TEAM>()) void gate_bwd_kernel(GateArgs
         const int p = q + at.member, t0 = p * GATE_PIECE + at.gl * LANE_STEPS, n = p < p1 ? a.L - t0 : 0;
         float start = a.ckpt[(int64_t)min(p, a.pieces - 1) * a.R + at.row];
         float av[8], bv[8], sv[8], gx[8], gv[8], iq[8], hp[8], dy[8], o[8], zv[8];   // iq: 1 / m
-        uint2 marks = r.m;
+        const uint2 marks = RST ? marks_settle(r.m, t0, a.L) : r.m;
+        const bool any = RST && __any((marks.x | marks.y) != 0u);
         if (!at.whole) {
             at.template settle<T>(r.x, t0, a.L);
             at.template settle<T>(r.f, t0, a.L);
@@ -493,92 +523,92 @@ __global__ __launch_bounds__(gate_threads<TEAM>()) void gate_bwd_kernel(GateArgs
             if constexpr (HI) at.template settle<T>(r.i, t0, a.L);
             if constexpr (HZ) at.template settle<T>(rz, t0, a.L);
         }
-        {
-            float xv[8], fv[8], ivv[8];
-            io8<T>::unpack(r.x, xv);
-            io8<T>::unpack(r.f, fv);
-            io8<T>::unpack(rd, dy);
-            if constexpr (HI) io8<T>::unpack(r.i, ivv);
-            if constexpr (HZ) io8<T>::unpack(rz, zv);
-            if (q > p0) load(p - TEAM);
+        LaneScan<G, true> back;
+        float A, B;
+        with_marks<RST>(any, [&](auto have) {
+            constexpr bool S = decltype(have)::value;
+            {
+                float xv[8], fv[8], ivv[8];
+                io8<T>::unpack(r.x, xv);
+                io8<T>::unpack(r.f, fv);
+                io8<T>::unpack(rd, dy);
+                if constexpr (HI) io8<T>::unpack(r.i, ivv);
+                if constexpr (HZ) io8<T>::unpack(rz, zv);
+                if (q > p0) load(p - TEAM);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    const bool in = j < n, mk = S && marked(marks, j);
+                    const float s = gate_sigmoid(fv[j] + ch.f_bias);
+                    const float aa = exp2_fast(k * s);
+                    const float m2 = one_minus_square(rate2 * s, aa);
+                    float rm = __builtin_amdgcn_rsqf(m2);
+                    rm = m2 == 0.0f ? 0.0f : rm;
+                    const float g = HI ? gate_sigmoid(ivv[j] + ch.i_bias) : 1.0f;
+                    const float m = mk ? 1.0f : m2 * rm;
+                    sv[j] = s;
+                    gv[j] = g;
+                    iq[j] = rm;
+                    gx[j] = in ? g * xv[j] : 0.0f;
+                    av[j] = in ? (mk ? -1.0f : aa) : 1.0f;
+                    bv[j] = in ? m * gx[j] : 0.0f;
+                    dy[j] = in ? dy[j] : 0.0f;
+                }
+            }
+            slice_map<S>(av, bv, A, B);
+            LaneScan<G, false> lanes;
+            lanes.template scan<S>(A, B, at.lane);
+            float h = lanes.template apply<S>(start, at.lane);
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-                const bool in = j < n, mk = RST && marked(marks, j);
-                const float s = gate_sigmoid(fv[j] + ch.f_bias);
-                const float aa = exp2_fast(k * s);
-                const float m2 = one_minus_square(rate2 * s, aa);
-                float rm = __builtin_amdgcn_rsqf(m2);
-                rm = m2 == 0.0f ? 0.0f : rm;
-                const float g = HI ? gate_sigmoid(ivv[j] + ch.i_bias) : 1.0f;
-                const float m = mk ? 1.0f : m2 * rm;
-                sv[j] = s;
-                gv[j] = g;
-                iq[j] = rm;
-                gx[j] = in ? g * xv[j] : 0.0f;
-                av[j] = in ? (mk ? -1.0f : aa) : 1.0f;
-                bv[j] = in ? m * gx[j] : 0.0f;
-                dy[j] = in ? dy[j] : 0.0f;
+                hp[j] = h;
+                h = affine_of<S>(av[j], bv[j], h);
+                if constexpr (HZ) {
+                    const float sz = gate_sigmoid(zv[j]);
+                    o[j] = dy[j] * h * fmaf(zv[j] * sz, 1.0f - sz, sz);
+                    dy[j] = j < n ? dy[j] * zv[j] * sz : 0.0f;
+                }
             }
-        }
-        float A, B;
-        slice_map<RST>(av, bv, A, B);
-        LaneScan<G, false, RST> lanes;
-        lanes.scan(A, B, at.lane);
-        float h = lanes.apply(start, at.lane);
-        float gz[8];
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            hp[j] = h;
-            h = affine_of<RST>(av[j], bv[j], h);
-            if constexpr (HZ) {
-                const float sz = gate_sigmoid(zv[j]);
-                o[j] = dy[j] * h * fmaf(zv[j] * sz, 1.0f - sz, sz);
-                dy[j] = j < n ? dy[j] * zv[j] * sz : 0.0f;
-            }
-        }
-        if constexpr (HZ)
-            if (at.valid) slice_store<T>(dz, t0, n, o);
-        // G of the slice as one map, from its last step to its first
-        {
+            // G of the slice as one map, from its last step to its first: G_t = a (dy + G_{t+1}), 0 at a reset
             A = 1.0f;
             B = 0.0f;
 #pragma unroll
             for (int j = 7; j >= 0; --j) {
-                // G_t = a (dy + G_{t+1}); 0 at a reset
                 float A1 = av[j], B1 = av[j] * dy[j];
-                if (RST && A1 < 0.0f) B1 = 0.0f;
-                affine_after<RST>(A1, B1, A, B);
+                if (S && A1 < 0.0f) B1 = 0.0f;
+                affine_after<S>(A1, B1, A, B);
                 A = A1;
                 B = B1;
             }
-        }
-        LaneScan<G, true, RST> back;
-        back.scan(A, B, at.lane);
+            back.template scan<S>(A, B, at.lane);
+            if constexpr (TEAM > 1) back.template whole<S>(A, B);
+        });
+        if constexpr (HZ)
+            if (at.valid) slice_store<T>(dz, t0, n, o);
         float own = c;
-        if constexpr (TEAM > 1) {
-            back.whole(A, B);
-            own = team(A, B, c, at.member, at.lane);
-        }
-        float gn = back.apply(own, at.lane);
-        if constexpr (TEAM == 1) c = own;
+        if constexpr (TEAM > 1) own = team(A, B, c, at.member, at.lane);
         float sq = 0.0f, sf = 0.0f, si = 0.0f;
-        float o2[8];
+        float gz[8], o2[8];
+        with_marks<RST>(any, [&](auto have) {
+            constexpr bool S = decltype(have)::value;
+            float gn = back.template apply<S>(own, at.lane);
 #pragma unroll
-        for (int j = 7; j >= 0; --j) {
-            const bool in = j < n, mk = RST && av[j] < 0.0f;
-            const float lam = dy[j] + gn;
-            const float m = mk ? 1.0f : iq[j] * one_minus_square(rate2 * sv[j], av[j]);
-            gz[j] = lam * m * gv[j];                      // dx
-            if constexpr (HI) {
-                o[j] = in ? lam * bv[j] * (1.0f - gv[j]) : 0.0f;
-                si += o[j];
+            for (int j = 7; j >= 0; --j) {
+                const bool in = j < n, mk = S && av[j] < 0.0f;
+                const float lam = dy[j] + gn;
+                const float m = mk ? 1.0f : (iq[j] == 0.0f ? 0.0f : rcp_fast(iq[j]));
+                gz[j] = lam * m * gv[j];                      // dx
+                if constexpr (HI) {
+                    o[j] = in ? lam * bv[j] * (1.0f - gv[j]) : 0.0f;
+                    si += o[j];
+                }
+                const float dr = mk || !in ? 0.0f : lam * av[j] * (hp[j] - gx[j] * av[j] * iq[j]) * sv[j];
+                sq -= dr;
+                o2[j] = -ch.rate * dr * (1.0f - sv[j]);
+                sf += o2[j];
+                gn = mk ? 0.0f : (in ? av[j] * lam : gn);
             }
-            const float dr = mk || !in ? 0.0f : lam * av[j] * (hp[j] - gx[j] * av[j] * iq[j]) * sv[j];
-            sq -= dr;
-            o2[j] = -ch.rate * dr * (1.0f - sv[j]);
-            sf += o2[j];
-            gn = mk ? 0.0f : (in ? av[j] * lam : gn);
-        }
+        });
+        if constexpr (TEAM == 1) c = own;
         sum_q += sq;
         sum_f += sf;
         sum_i += si;
@@ -638,7 +668,7 @@ __global__ __launch_bounds__(GATE_WAVES* WAVE) void gate_bwd_map_kernel(GateArgs
         rf = at.template request<T>(f, t0, a.L);
         rd = at.template request<T>(dout, t0, a.L);
         if constexpr (HZ) rz = at.template request<T>(z, t0, a.L);
-        if constexpr (RST) marks = marks_load(reset, t0, a.L);
+        if constexpr (RST) marks = marks_request<false>(reset, t0, a.L);
     };
     float sA = 1.0f, sB = 0.0f;
     load(p1 - 1);
@@ -653,7 +683,7 @@ __global__ __launch_bounds__(GATE_WAVES* WAVE) void gate_bwd_map_kernel(GateArgs
         io8<T>::unpack(rf, fv);
         io8<T>::unpack(rd, dy);
         if constexpr (HZ) io8<T>::unpack(rz, zv);
-        const uint2 m = marks;
+        const uint2 m = marks_settle(marks, t0, a.L);
         if (p > p0) load(p - 1);
         float A = 1.0f, B = 0.0f;
 #pragma unroll
@@ -666,9 +696,9 @@ __global__ __launch_bounds__(GATE_WAVES* WAVE) void gate_bwd_map_kernel(GateArgs
             A = A1;
             B = B1;
         }
-        LaneScan<WAVE, true, RST> lanes;
-        lanes.scan(A, B, at.lane);
-        lanes.whole(A, B);
+        LaneScan<WAVE, true> lanes;
+        lanes.template scan<RST>(A, B, at.lane);
+        lanes.template whole<RST>(A, B);
         affine_after<RST>(A, B, sA, sB);
         sA = A;
         sB = B;
@@ -771,8 +801,7 @@ void launch_all(const GateArgs& a, int team, bool bwd, hipStream_t st)
     if (g == 4) launch_main<T, 4, 1>(a, bwd, st);
     else if (g == 16) launch_main<T, 16, 1>(a, bwd, st);
     else if (team == 1) launch_main<T, WAVE, 1>(a, bwd, st);
-    else if (team == 4) launch_main<T, WAVE, 4>(a, bwd, st);
-    else launch_main<T, WAVE, 8>(a, bwd, st);
+    else launch_main<T, WAVE, 4>(a, bwd, st);
 }
 
 }  // namespace ss
@@ -786,17 +815,24 @@ constexpr uint32_t kGateStepFlags = SS_GATE_HAS_I | SS_GATE_HAS_Z | SS_GATE_HAS_
 inline bool aligned_to(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) % a) == 0; }
 inline size_t round_up(size_t v, size_t a) { return (v + a - 1) / a * a; }
 
-// How a sequence is dealt out: the waves that share a row, and segments where the rows with their teams are still too few.
+// How a sequence is dealt out: one wave or four share a row, and segments where the rows with their teams are still too few.
+// us forward / backward with one wave / four, input gate and z, rows x steps: bf16 4096 x 1030 15.6 26.5 / 18.9 38.3, 2048 x 4096
+// 22.5 34.9 / 21.0 37.8, 1024 x 16384 47.7 72.7 / 35.5 64.4, 512 x 2048 7.2 11.6 / 5.6 9.0; float32, whose requests are twice as
+// wide, gains more often, and wherever the team's rounds come out even: 1536 x 4097 29.8 50.9 / 27.4 46.6, 6144 x 2048 47.5 97.9 / 41.8 86.8, 3000 x 2048 27.9 48.7 / 23.8 42.0, but 4096 x 1030
+// 19.8 36.4 / 20.8 42.5.  (Teams of 8 and 16 bring up to a fifth at 256 rows and lose as much or more elsewhere.)
+// In segments (two more launches and a second reading of most inputs) / whole: bf16 128 x 16384 16.0 23.1 / 12.7 21.2, 64 x 8192 12.3 16.6 / 7.5
+// 12.1, 200 x 30000 29.8 43.6 / 24.4 39.2; but 128 x 65536 35.6 52.6 / 46.1 74.6, 64 x 100000 30.8 45.0 / 65.5 103.9, 1 x 1000000 19.0 25.0 / 558 944.
 struct GatePlan {
     int pieces, team, nseg, spp, nmap, ppm;
 };
-GatePlan gate_plan(long rows, int L)
+GatePlan gate_plan(long rows, int L, int io)
 {
     GatePlan g;
     g.pieces = (L + ss::GATE_PIECE - 1) / ss::GATE_PIECE;
-    g.team = rows >= 4096 || g.pieces < 3 ? 1 : (rows >= 1024 || g.pieces < 6 ? 4 : 8);
-    long n = rows >= 192 || g.team < 8 ? 1 : (512 + rows - 1) / rows;
-    const long most = (g.pieces + 15) / 16;   // a segment has two rounds of its team's at least
+    const bool fill = 10 * g.pieces >= 9 * ((g.pieces + 3) / 4 * 4);
+    g.team = g.pieces >= 3 && (rows < (io == SS_F32 ? 2048 : 1536) || (io == SS_F32 && fill)) ? 4 : 1;
+    long n = rows > 160 || g.pieces < 48 ? 1 : (768 + rows - 1) / rows;
+    const long most = (g.pieces + 7) / 8;   // a segment has two rounds of its team's at least
     if (n > most) n = most;
     if (n < 1) n = 1;
     g.spp = (int)((g.pieces + n - 1) / n);
@@ -880,7 +916,8 @@ size_t ss_gate_workspace_bytes(const ss_gate_params* p, int for_backward)
 {
     if (!p || p->batch < 1 || p->dim < 1 || p->seqlen < 0) return 0;
     const long rows = (long)p->batch * p->dim;
-    return gate_space(rows, gate_plan(rows, p->seqlen), for_backward != 0).total;
+    // the plan's io_dtype decides on the team's size alone, and where a row is split that is four either way
+    return gate_space(rows, gate_plan(rows, p->seqlen, SS_F32), for_backward != 0).total;
 }
 
 int ss_gate_fwd(const ss_gate_params* p, void* stream)
@@ -889,7 +926,7 @@ int ss_gate_fwd(const ss_gate_params* p, void* stream)
     if (rc != SS_OK) return rc;
     const long rows = (long)p->batch * p->dim;
     const bool save = p->flags & SS_GATE_SAVE_FOR_BWD;
-    GatePlan g = gate_plan(rows, p->seqlen);
+    GatePlan g = gate_plan(rows, p->seqlen, p->io_dtype);
     const GateSpace s = gate_space(rows, g, save);
     char* const ws = static_cast<char*>(p->workspace);
     if (ws && !aligned_to(ws, 256)) return SS_ERR_ALIGN;
@@ -935,7 +972,7 @@ int ss_gate_bwd(const ss_gate_bwd_params* p, void* stream)
         (ib && !aligned_to(p->di_bias, 4)) || !aligned_to(p->dh0, 4))
         return SS_ERR_ALIGN;
     const long rows = (long)q->batch * q->dim;
-    const GatePlan g = gate_plan(rows, q->seqlen);
+    const GatePlan g = gate_plan(rows, q->seqlen, q->io_dtype);
     const GateSpace s = gate_space(rows, g, true);
     char* const ws = static_cast<char*>(q->workspace);
     if (!empty && (!ws || q->workspace_bytes < s.total)) return SS_ERR_WORKSPACE;
