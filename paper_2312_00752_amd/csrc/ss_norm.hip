@@ -346,23 +346,26 @@ __global__ __launch_bounds__(norm_threads<G>(true)) void norm_bwd_kernel(NormArg
     }
 }
 
-// dweight and dbias from the parts: 64 columns of one of the two per workgroup, 16 threads a column.
+// dweight and dbias from the parts: 32 columns of one of the two per workgroup, 32 threads a column.
 __global__ __launch_bounds__(1024) void norm_parts_kernel(const float* part, float* dweight, float* dbias, int W, int parts)
 {
     float* const to = blockIdx.y == 0 ? dweight : dbias;
     if (!to) return;
-    __shared__ float s[16][64];
-    const int c = blockIdx.x * 64 + threadIdx.x % 64, k0 = threadIdx.x / 64;
+    __shared__ float s[32][33];
+    const int c = blockIdx.x * 32 + threadIdx.x % 32, k0 = threadIdx.x / 32;
     float v = 0.0f;
-    if (c < W)
-        for (int k = k0; k < parts; k += 16) v += part[((int64_t)k * 2 + blockIdx.y) * W + c];
-    s[k0][threadIdx.x % 64] = v;
-    __syncthreads();
-    if (threadIdx.x < 64 && c < W) {
-        float t = 0.0f;
-        for (int k = 0; k < 16; ++k) t += s[k][threadIdx.x];
-        to[c] = t;
+    if (c < W) {
+#pragma unroll 8
+        for (int k = k0; k < parts; k += 32) v += part[((int64_t)k * 2 + blockIdx.y) * W + c];
     }
+    s[threadIdx.x % 32][k0] = v;
+    __syncthreads();
+    // a column's 32 sums in the lanes of half a wave
+    float t = s[threadIdx.x / 32][threadIdx.x % 32];
+#pragma unroll
+    for (int k = 1; k < 32; k *= 2) t += __shfl_xor(t, k);
+    const int col = blockIdx.x * 32 + threadIdx.x / 32;
+    if (threadIdx.x % 32 == 0 && col < W) to[col] = t;
 }
 
 // ---- rows that do not fit the registers of a workgroup ------------------------------------------
@@ -630,7 +633,7 @@ int ss_norm_bwd(const ss_norm_bwd_params* p, void* stream)
         ss::norm_dispatch(a, q->io_dtype, q->flags, true, st);
     }
     if (hw || hb)
-        hipLaunchKernelGGL(ss::norm_parts_kernel, dim3((unsigned)((q->width + 63) / 64), hb ? 2u : 1u), dim3(1024), 0, st, a.part, hw ? p->dweight : nullptr,
+        hipLaunchKernelGGL(ss::norm_parts_kernel, dim3((unsigned)((q->width + 31) / 32), hb ? 2u : 1u), dim3(1024), 0, st, a.part, hw ? p->dweight : nullptr,
                            hb ? p->dbias : nullptr, q->width, q->rows > 0 ? ss::norm_parts(q->rows, q->width) : 0);
     return hipGetLastError() == hipSuccess ? SS_OK : SS_ERR_LAUNCH;
 }
