@@ -109,6 +109,10 @@ class _LayerNorm(torch.autograd.Function):
 def layer_norm(x, weight=None, bias=None, residual=None, eps=1e-5):
     """Differentiable layer norm over the last axis.  With ``residual`` (float32 or x's dtype) the sum of the two is normalised
     and returned as well, in residual's dtype: (out, summed), the residual stream that the next block continues."""
+    if x.is_cuda:
+        r = B.layer_norm_node(x, weight, bias, residual, eps)
+        if r is not None:
+            return r if residual is not None else r[0]
     return _LayerNorm.apply(x, weight, bias, residual, eps)
 
 
@@ -132,4 +136,8 @@ class _GatedRecurrence(torch.autograd.Function):
 def gated_recurrence(x, f, rate, i=None, z=None, f_bias=None, i_bias=None, reset=None, h0=None, return_last_state=False):
     """Differentiable gated linear recurrence (include/ss_gate.h): h <- a h + sqrt(1 - a^2) sigmoid(i) x with
     a = exp(-rate sigmoid(f)), gated by SiLU(z).  Returns out, or (out, h_last) with ``return_last_state``."""
+    if x.is_cuda:
+        r = B.gated_recurrence_node(x, f, i, z, rate, f_bias, i_bias, reset, h0, return_last_state)
+        if r is not None:
+            return r if return_last_state else r[0]
     return _GatedRecurrence.apply(x, f, rate, i, z, f_bias, i_bias, reset, h0, return_last_state)

@@ -237,7 +237,7 @@ class _NoMarshal:
         return None
 
     step = layer_step = scan_fwd = scan_bwd = layer_fwd = layer_bwd = staticmethod(_none)
-    norm_fwd = norm_bwd = gate_fwd = gate_bwd = gate_step = qlinear = staticmethod(_none)
+    norm_fwd = norm_bwd = gate_fwd = gate_bwd = gate_step = qlinear = layer_norm = gated_recurrence = staticmethod(_none)
 
 
 def _marshal():
@@ -1202,3 +1202,16 @@ def ss_qlinear(x, weight, scale, bias=None, x_seq_last=False, out_seq_last=False
         p.scratch, p.scratch_bytes = _lend(scratch, need, x.device, "scratch")
     _check(lib().ss_qlinear(ctypes.byref(p), _stream(stream)))
     return out
+
+
+# ---------------------------------------------------------------- gradient functions of the compiled module
+def layer_norm_node(x, weight, bias, residual, eps):
+    """(out,) or (out, summed) of autograd.layer_norm from the compiled module, or None where it does not serve the call."""
+    r = (_native or _marshal()).layer_norm(x, weight, bias, residual, eps, _stream(None))
+    return r if r is None else _result(r)
+
+
+def gated_recurrence_node(x, f, i, z, rate, f_bias, i_bias, reset, h0, return_last_state):
+    """The same for autograd.gated_recurrence."""
+    r = (_native or _marshal()).gated_recurrence(x, f, i, z, rate, f_bias, i_bias, reset, h0, bool(return_last_state), _stream(None))
+    return r if r is None else _result(r)

@@ -9,9 +9,11 @@
 #include <Python.h>
 
 #include <initializer_list>
+#include <optional>
 
 #include <ATen/ATen.h>
 #include <torch/csrc/Exceptions.h>
+#include <torch/csrc/autograd/custom_function.h>
 #include <torch/csrc/autograd/python_variable.h>
 
 #include "ss_gate.h"
@@ -461,40 +463,125 @@ const at::Tensor* held(Args& a, int i, const at::Tensor& x)
     return t;
 }
 
+// The calls themselves, on tensors that have been looked at.  They hold no lock and are also what the gradient functions call.
+struct Norm {
+    at::Tensor out, summed, stats;
+    int fwd(const at::Tensor& x, const at::Tensor& weight, const at::Tensor& bias, const at::Tensor& residual, double eps, bool save, void* stream)
+    {
+        ss_norm_params p{};
+        if (!norm_sizes(x, p)) return SS_ERR_SHAPE;
+        p.eps = (float)eps;
+        p.x = x.data_ptr();
+        p.weight = data<const float>(weight);
+        p.bias = data<const float>(bias);
+        p.flags = (weight.defined() ? SS_NORM_HAS_WEIGHT : 0u) | (bias.defined() ? SS_NORM_HAS_BIAS : 0u);
+        out = empty_io(x);
+        p.out = out.data_ptr();
+        if (residual.defined()) {
+            p.flags |= SS_NORM_HAS_RESIDUAL | (residual.scalar_type() == at::kFloat ? SS_NORM_RESIDUAL_F32 : 0u);
+            p.residual = residual.data_ptr();
+            summed = empty_io(residual);
+            p.summed = summed.data_ptr();
+        }
+        if (save) {
+            p.flags |= SS_NORM_SAVE_STATS;
+            stats = empty_f32({2, p.rows}, x);
+            p.stats = data<float>(stats);
+        }
+        return ss_norm_fwd(&p, stream);
+    }
+};
+struct NormGrads {
+    at::Tensor dx, dresidual, dweight, dbias;
+    int bwd(const at::Tensor& dout, const at::Tensor& s, const at::Tensor& stats, const at::Tensor& weight, bool has_bias, bool res, const at::Tensor& more,
+            double eps, void* stream)
+    {
+        ss_norm_bwd_params q{};
+        ss_norm_params& p = q.fwd;
+        if (!norm_sizes(dout, p)) return SS_ERR_SHAPE;
+        p.eps = (float)eps;
+        p.stats = data<float>(stats);
+        p.weight = data<const float>(weight);
+        dx = empty_io(dout);
+        const bool two = res && s.scalar_type() != dout.scalar_type();
+        if (res) {
+            p.flags |= SS_NORM_HAS_RESIDUAL | (s.scalar_type() == at::kFloat ? SS_NORM_RESIDUAL_F32 : 0u);
+            p.summed = s.data_ptr();
+            dresidual = two ? empty_io(s) : dx;
+        } else {
+            p.x = s.data_ptr();
+        }
+        if (weight.defined()) {
+            p.flags |= SS_NORM_HAS_WEIGHT;
+            dweight = empty_f32({p.width}, dout);
+        }
+        if (has_bias) {
+            p.flags |= SS_NORM_HAS_BIAS;
+            dbias = empty_f32({p.width}, dout);
+        }
+        q.dout = dout.data_ptr();
+        q.dsummed = data<const void>(more);
+        q.dx = dx.data_ptr();
+        q.dresidual = two ? dresidual.data_ptr() : nullptr;
+        q.dweight = data<float>(dweight);
+        q.dbias = data<float>(dbias);
+        const at::Tensor ws = empty_bytes(ss_norm_workspace_bytes(&p), dout);
+        q.workspace = ws.data_ptr();
+        q.workspace_bytes = (size_t)ws.numel();
+        return ss_norm_bwd(&q, stream);
+    }
+};
+// Whether the forward call's tensors are the plain case; they are left in `t` (x, weight, bias, residual).
+bool norm_tensors(Args& a, int at, at::Tensor (&t)[4])
+{
+    const at::Tensor* x = a.tensor(at);
+    ss_norm_params p{};
+    if (!x || !norm_sizes(*x, p)) return false;
+    a.ptr(at + 1, at::kFloat, {p.width}, true);
+    a.ptr(at + 2, at::kFloat, {p.width}, true);
+    if (a.ok && !a.none(at + 3)) held(a, at + 3, *x);
+    if (!a.ok) return false;
+    for (int i = 0; i < 4; ++i)
+        if (!a.none(at + i)) t[i] = THPVariable_Unpack(a.a[at + i]);
+    return true;
+}
+bool real_number(PyObject* o, double& v)
+{
+    if (!PyFloat_CheckExact(o)) return false;
+    v = PyFloat_AS_DOUBLE(o);
+    return true;
+}
+struct Unlocked {   // without the interpreter's lock, also where an exception passes
+    PyThreadState* state = PyEval_SaveThread();
+    ~Unlocked() { PyEval_RestoreThread(state); }
+};
+struct Refused {    // the library's code on its way out of a gradient function's forward call
+    int rc;
+};
+typedef std::optional<at::Tensor> Optional;   // what an input of a gradient function is that may be missing
+at::Tensor given(const Optional& t) { return t.has_value() ? *t : at::Tensor(); }
+Optional optional(const at::Tensor& t) { return t.defined() ? Optional(t) : Optional(); }
+void backward_check(int rc) { TORCH_CHECK(rc == SS_OK, "ss_scan error ", rc, ": ", ss_strerror(rc)); }
+
 // norm_fwd(x, weight, bias, residual, eps, save, stream) -> (out, summed or None, stats or None)
 PyObject* py_norm_fwd(PyObject*, PyObject* const* argv, Py_ssize_t n)
 {
     HANDLE_TH_ERRORS
     if (n != 7) Py_RETURN_NONE;
     Args a{argv};
-    ss_norm_params p{};
-    const at::Tensor* x = a.tensor(0);
-    if (!x || !norm_sizes(*x, p) || !PyFloat_CheckExact(argv[4])) Py_RETURN_NONE;
-    p.eps = (float)PyFloat_AS_DOUBLE(argv[4]);
-    p.x = x->data_ptr();
-    p.weight = static_cast<const float*>(a.ptr(1, at::kFloat, {p.width}, true));
-    p.bias = static_cast<const float*>(a.ptr(2, at::kFloat, {p.width}, true));
-    const at::Tensor* r = a.ok && !a.none(3) ? held(a, 3, *x) : nullptr;
+    at::Tensor t[4];
+    double eps;
+    if (!norm_tensors(a, 0, t) || !real_number(argv[4], eps)) Py_RETURN_NONE;
     void* stream = a.stream(6);
     if (!a.ok) Py_RETURN_NONE;
-    if (p.weight) p.flags |= SS_NORM_HAS_WEIGHT;
-    if (p.bias) p.flags |= SS_NORM_HAS_BIAS;
-    at::Tensor out = empty_io(*x), summed, stats;
-    p.out = out.data_ptr();
-    if (r) {
-        p.flags |= SS_NORM_HAS_RESIDUAL | (r->scalar_type() == at::kFloat ? SS_NORM_RESIDUAL_F32 : 0u);
-        p.residual = r->data_ptr();
-        summed = empty_io(*r);
-        p.summed = summed.data_ptr();
+    Norm c;
+    int rc;
+    {
+        Unlocked u;
+        rc = c.fwd(t[0], t[1], t[2], t[3], eps, argv[5] == Py_True, stream);
     }
-    if (argv[5] == Py_True) {
-        p.flags |= SS_NORM_SAVE_STATS;
-        stats = empty_f32({2, p.rows}, *x);
-        p.stats = data<float>(stats);
-    }
-    const int rc = call(ss_norm_fwd, p, stream);
     if (rc != SS_OK) return PyLong_FromLong(rc);
-    return tuple_of({out, summed, stats});
+    return tuple_of({c.out, c.summed, c.stats});
     END_HANDLE_TH_ERRORS
 }
 
@@ -504,48 +591,85 @@ PyObject* py_norm_bwd(PyObject*, PyObject* const* argv, Py_ssize_t n)
     HANDLE_TH_ERRORS
     if (n != 9) Py_RETURN_NONE;
     Args a{argv};
-    ss_norm_bwd_params q{};
-    ss_norm_params& p = q.fwd;
+    ss_norm_params p{};
     const at::Tensor* dout = a.tensor(0);
-    if (!dout || !norm_sizes(*dout, p) || !PyFloat_CheckExact(argv[7])) Py_RETURN_NONE;
+    double eps;
+    if (!dout || !norm_sizes(*dout, p) || !real_number(argv[7], eps)) Py_RETURN_NONE;
     const bool res = argv[5] == Py_True;
     const at::Tensor* s = held(a, 1, *dout);
     if (!s || (!res && (s->scalar_type() != dout->scalar_type() || !a.none(6)))) Py_RETURN_NONE;
-    p.eps = (float)PyFloat_AS_DOUBLE(argv[7]);
-    p.stats = static_cast<float*>(a.ptr(2, at::kFloat, {2, p.rows}));
-    p.weight = static_cast<const float*>(a.ptr(3, at::kFloat, {p.width}, true));
+    a.ptr(2, at::kFloat, {2, p.rows});
+    a.ptr(3, at::kFloat, {p.width}, true);
     const at::Tensor* more = a.ok && !a.none(6) ? held(a, 6, *dout) : nullptr;
     void* stream = a.stream(8);
     if (!a.ok || (more && more->scalar_type() != s->scalar_type())) Py_RETURN_NONE;
-    at::Tensor dx = empty_io(*dout), dresidual, dweight, dbias;
-    const bool two = res && s->scalar_type() != dout->scalar_type();
-    if (res) {
-        p.flags |= SS_NORM_HAS_RESIDUAL | (s->scalar_type() == at::kFloat ? SS_NORM_RESIDUAL_F32 : 0u);
-        p.summed = s->data_ptr();
-        dresidual = two ? empty_io(*s) : dx;
-    } else {
-        p.x = s->data_ptr();
+    const at::Tensor& stats = THPVariable_Unpack(argv[2]);
+    const at::Tensor weight = a.none(3) ? at::Tensor() : THPVariable_Unpack(argv[3]), dsummed = more ? *more : at::Tensor();
+    NormGrads g;
+    int rc;
+    {
+        Unlocked u;
+        rc = g.bwd(*dout, *s, stats, weight, argv[4] == Py_True, res, dsummed, eps, stream);
     }
-    if (p.weight) {
-        p.flags |= SS_NORM_HAS_WEIGHT;
-        dweight = empty_f32({p.width}, *dout);
-    }
-    if (argv[4] == Py_True) {
-        p.flags |= SS_NORM_HAS_BIAS;
-        dbias = empty_f32({p.width}, *dout);
-    }
-    q.dout = dout->data_ptr();
-    q.dsummed = more ? more->data_ptr() : nullptr;
-    q.dx = dx.data_ptr();
-    q.dresidual = two ? dresidual.data_ptr() : nullptr;
-    q.dweight = data<float>(dweight);
-    q.dbias = data<float>(dbias);
-    const at::Tensor ws = empty_bytes(ss_norm_workspace_bytes(&p), *dout);
-    q.workspace = ws.data_ptr();
-    q.workspace_bytes = (size_t)ws.numel();
-    const int rc = call(ss_norm_bwd, q, stream);
     if (rc != SS_OK) return PyLong_FromLong(rc);
-    return dict_of({{"dx", dx}, {"dresidual", dresidual}, {"dweight", dweight}, {"dbias", dbias}});
+    return dict_of({{"dx", g.dx}, {"dresidual", g.dresidual}, {"dweight", g.dweight}, {"dbias", g.dbias}});
+    END_HANDLE_TH_ERRORS
+}
+
+// Layer norm as a node of torch's graph (what autograd._LayerNorm is in Python): the backward pass runs on the stream of the forward pass,
+// which is also the one that torch makes current for it.
+struct NormFunction : torch::autograd::Function<NormFunction> {
+    static torch::autograd::variable_list forward(torch::autograd::AutogradContext* ctx, const at::Tensor& x, const Optional& weight_, const Optional& bias_,
+                                                  const Optional& residual_, double eps, int64_t stream)
+    {
+        const at::Tensor weight = given(weight_), bias = given(bias_), residual = given(residual_);
+        Norm c;
+        const int rc = c.fwd(x, weight, bias, residual, eps, true, reinterpret_cast<void*>(stream));
+        if (rc != SS_OK) throw Refused{rc};
+        ctx->set_materialize_grads(false);
+        ctx->save_for_backward({residual.defined() ? c.summed : x, weight, c.stats});
+        ctx->saved_data["bias"] = bias.defined();
+        ctx->saved_data["residual"] = residual.defined();
+        ctx->saved_data["eps"] = eps;
+        ctx->saved_data["stream"] = stream;
+        ctx->saved_data["io"] = (int64_t)x.scalar_type();
+        if (residual.defined()) return {c.out, c.summed};
+        return {c.out};
+    }
+    static torch::autograd::variable_list backward(torch::autograd::AutogradContext* ctx, torch::autograd::variable_list grads)
+    {
+        const bool res = ctx->saved_data["residual"].toBool();
+        const at::Tensor more = res && grads[1].defined() ? grads[1].contiguous() : at::Tensor();
+        if (!grads[0].defined()) {   // only the sum was used
+            const auto io = (at::ScalarType)ctx->saved_data["io"].toInt();
+            return {more.defined() ? more.to(io) : at::Tensor(), at::Tensor(), at::Tensor(), more, at::Tensor(), at::Tensor()};
+        }
+        const auto saved = ctx->get_saved_variables();
+        NormGrads g;
+        backward_check(g.bwd(grads[0].contiguous(), saved[0], saved[2], saved[1], ctx->saved_data["bias"].toBool(), res, more,
+                             ctx->saved_data["eps"].toDouble(), reinterpret_cast<void*>(ctx->saved_data["stream"].toInt())));
+        return {g.dx, g.dweight, g.dbias, g.dresidual, at::Tensor(), at::Tensor()};
+    }
+};
+// layer_norm(x, weight, bias, residual, eps, stream) -> (out,) or (out, summed), with gradients
+PyObject* py_layer_norm(PyObject*, PyObject* const* argv, Py_ssize_t n)
+{
+    HANDLE_TH_ERRORS
+    if (n != 6) Py_RETURN_NONE;
+    Args a{argv};
+    at::Tensor t[4];
+    double eps;
+    if (!norm_tensors(a, 0, t) || !real_number(argv[4], eps)) Py_RETURN_NONE;
+    void* stream = a.stream(5);
+    if (!a.ok) Py_RETURN_NONE;
+    torch::autograd::variable_list r;
+    try {
+        Unlocked u;
+        r = NormFunction::apply(t[0], optional(t[1]), optional(t[2]), optional(t[3]), eps, reinterpret_cast<int64_t>(stream));
+    } catch (const Refused& e) {
+        return PyLong_FromLong(e.rc);
+    }
+    return r.size() == 2 ? tuple_of({r[0], r[1]}) : tuple_of({r[0]});
     END_HANDLE_TH_ERRORS
 }
 
@@ -614,6 +738,52 @@ bool gate_all(Args& a, int at, const at::Tensor& x, ss_gate_params& p)
     return a.ok;
 }
 
+// The recurrence's calls, with the struct filled by gate_all or by gate_refill.
+struct Gate {
+    at::Tensor out, h_last;
+    int fwd(const at::Tensor& x, ss_gate_params p, const at::Tensor& ws, bool save, bool want_last, void* stream)
+    {
+        if (ws.defined()) {
+            p.workspace = ws.data_ptr();
+            p.workspace_bytes = (size_t)ws.numel();
+        }
+        if (save) p.flags |= SS_GATE_SAVE_FOR_BWD;
+        out = at::empty(x.sizes(), x.options().requires_grad(false));
+        p.out = out.data_ptr();
+        if (want_last) {
+            h_last = empty_f32({p.batch, p.dim}, x);
+            p.h_last = data<float>(h_last);
+            p.flags |= SS_GATE_WRITE_H_LAST;
+        }
+        return ss_gate_fwd(&p, stream);
+    }
+};
+struct GateGrads {
+    at::Tensor dx, df, di, dz, drate, df_bias, di_bias, dh0;
+    int bwd(const at::Tensor& x, const ss_gate_params& p, const at::Tensor& ws, const at::Tensor& dout, const at::Tensor& dh_last, bool want_dh0, void* stream)
+    {
+        ss_gate_bwd_params q{};
+        q.fwd = p;
+        q.fwd.workspace = ws.data_ptr();
+        q.fwd.workspace_bytes = (size_t)ws.numel();
+        q.dout = dout.data_ptr();
+        q.dh_last = data<const float>(dh_last);
+        const int64_t nd = p.dim;
+        dx = empty_io(x);
+        df = empty_io(x);
+        drate = empty_f32({nd}, x);
+        if (p.flags & SS_GATE_HAS_I) di = empty_io(x);
+        if (p.flags & SS_GATE_HAS_Z) dz = empty_io(x);
+        if (p.flags & SS_GATE_HAS_F_BIAS) df_bias = empty_f32({nd}, x);
+        if (p.flags & SS_GATE_HAS_I_BIAS) di_bias = empty_f32({nd}, x);
+        if (want_dh0) dh0 = empty_f32({p.batch, nd}, x);
+        q.dx = dx.data_ptr(); q.df = df.data_ptr(); q.di = data(di); q.dz = data(dz);
+        q.dx_batch = q.df_batch = q.di_batch = q.dz_batch = nd * p.seqlen;
+        q.drate = data<float>(drate); q.df_bias = data<float>(df_bias); q.di_bias = data<float>(di_bias); q.dh0 = data<float>(dh0);
+        return ss_gate_bwd(&q, stream);
+    }
+};
+
 // gate_fwd(x, f, i, z, rate, f_bias, i_bias, reset, h0, workspace, save, want_last, stream) -> (out, h_last or None)
 PyObject* py_gate_fwd(PyObject*, PyObject* const* argv, Py_ssize_t n)
 {
@@ -636,21 +806,14 @@ PyObject* py_gate_fwd(PyObject*, PyObject* const* argv, Py_ssize_t n)
         const size_t need = ss_gate_workspace_bytes(&p, 0);
         if (need) ws = empty_bytes(need, *x);
     }
-    if (ws.defined()) {
-        p.workspace = ws.data_ptr();
-        p.workspace_bytes = (size_t)ws.numel();
+    Gate g;
+    int rc;
+    {
+        Unlocked u;
+        rc = g.fwd(*x, p, ws, save, argv[11] == Py_True, stream);
     }
-    if (save) p.flags |= SS_GATE_SAVE_FOR_BWD;
-    at::Tensor out = empty_io(*x), h_last;
-    p.out = out.data_ptr();
-    if (argv[11] == Py_True) {
-        h_last = empty_f32({p.batch, p.dim}, *x);
-        p.h_last = data<float>(h_last);
-        p.flags |= SS_GATE_WRITE_H_LAST;
-    }
-    const int rc = call(ss_gate_fwd, p, stream);
     if (rc != SS_OK) return PyLong_FromLong(rc);
-    return tuple_of({out, h_last});
+    return tuple_of({g.out, g.h_last});
     END_HANDLE_TH_ERRORS
 }
 
@@ -660,31 +823,86 @@ PyObject* py_gate_bwd(PyObject*, PyObject* const* argv, Py_ssize_t n)
     HANDLE_TH_ERRORS
     if (n != 14) Py_RETURN_NONE;
     Args a{argv};
-    ss_gate_bwd_params q{};
+    ss_gate_params p{};
     const at::Tensor* x = gate_x(a, 0, 3);
     void* stream = a.stream(13);
-    if (!x || !a.ok || !gate_all(a, 0, *x, q.fwd)) Py_RETURN_NONE;
+    if (!x || !a.ok || !gate_all(a, 0, *x, p)) Py_RETURN_NONE;
     const at::Tensor* ws = a.tensor(9);
     if (!ws || ws->scalar_type() != at::kByte) Py_RETURN_NONE;
-    q.fwd.workspace = ws->data_ptr();
-    q.fwd.workspace_bytes = (size_t)ws->numel();
-    q.dout = a.ptr(10, x->scalar_type(), {q.fwd.batch, q.fwd.dim, q.fwd.seqlen});
-    q.dh_last = static_cast<const float*>(a.ptr(11, at::kFloat, {q.fwd.batch, q.fwd.dim}, true));
+    a.ptr(10, x->scalar_type(), {p.batch, p.dim, p.seqlen});
+    a.ptr(11, at::kFloat, {p.batch, p.dim}, true);
     if (!a.ok) Py_RETURN_NONE;
-    const int64_t nd = q.fwd.dim;
-    const uint32_t flags = q.fwd.flags;
-    at::Tensor dx = empty_io(*x), df = empty_io(*x), di, dz, drate = empty_f32({nd}, *x), dfb, dib, dh0;
-    if (flags & SS_GATE_HAS_I) di = empty_io(*x);
-    if (flags & SS_GATE_HAS_Z) dz = empty_io(*x);
-    if (flags & SS_GATE_HAS_F_BIAS) dfb = empty_f32({nd}, *x);
-    if (flags & SS_GATE_HAS_I_BIAS) dib = empty_f32({nd}, *x);
-    if (argv[12] == Py_True) dh0 = empty_f32({q.fwd.batch, nd}, *x);
-    q.dx = dx.data_ptr(); q.df = df.data_ptr(); q.di = data(di); q.dz = data(dz);
-    q.dx_batch = q.df_batch = q.di_batch = q.dz_batch = nd * q.fwd.seqlen;
-    q.drate = data<float>(drate); q.df_bias = data<float>(dfb); q.di_bias = data<float>(dib); q.dh0 = data<float>(dh0);
-    const int rc = call(ss_gate_bwd, q, stream);
+    const at::Tensor dh_last = a.none(11) ? at::Tensor() : THPVariable_Unpack(argv[11]);
+    GateGrads g;
+    int rc;
+    {
+        Unlocked u;
+        rc = g.bwd(*x, p, *ws, THPVariable_Unpack(argv[10]), dh_last, argv[12] == Py_True, stream);
+    }
     if (rc != SS_OK) return PyLong_FromLong(rc);
-    return dict_of({{"dx", dx}, {"df", df}, {"di", di}, {"dz", dz}, {"drate", drate}, {"df_bias", dfb}, {"di_bias", dib}, {"dh0", dh0}});
+    return dict_of({{"dx", g.dx}, {"df", g.df}, {"di", g.di}, {"dz", g.dz}, {"drate", g.drate}, {"df_bias", g.df_bias}, {"di_bias", g.di_bias}, {"dh0", g.dh0}});
+    END_HANDLE_TH_ERRORS
+}
+
+// The recurrence as a node of torch's graph (what autograd._GatedRecurrence is in Python).
+struct GateFunction : torch::autograd::Function<GateFunction> {
+    static torch::autograd::variable_list forward(torch::autograd::AutogradContext* ctx, const at::Tensor& x, const at::Tensor& f, const Optional& i,
+                                                  const Optional& z, const at::Tensor& rate, const Optional& f_bias, const Optional& i_bias,
+                                                  const Optional& reset, const Optional& h0, bool want_last, const ss_gate_params* p, int64_t stream)
+    {
+        const at::Tensor ws = empty_bytes(ss_gate_workspace_bytes(p, 1), x);
+        Gate g;
+        const int rc = g.fwd(x, *p, ws, true, want_last, reinterpret_cast<void*>(stream));
+        if (rc != SS_OK) throw Refused{rc};
+        ctx->save_for_backward({x, f, given(i), given(z), rate, given(f_bias), given(i_bias), given(reset), given(h0), ws});
+        ctx->saved_data["flags"] = (int64_t)p->flags;
+        ctx->saved_data["stream"] = stream;
+        if (want_last) return {g.out, g.h_last};
+        return {g.out};
+    }
+    static torch::autograd::variable_list backward(torch::autograd::AutogradContext* ctx, torch::autograd::variable_list grads)
+    {
+        const auto t = ctx->get_saved_variables();
+        const at::Tensor& x = t[0];
+        ss_gate_params p{};
+        io_type(x, p.io_dtype);
+        p.batch = (int32_t)x.size(0); p.dim = (int32_t)x.size(1); p.seqlen = (int32_t)x.size(2);
+        p.flags = (uint32_t)ctx->saved_data["flags"].toInt();
+        const int64_t dense = x.size(1) * x.size(2);
+        auto rows = [&](const at::Tensor& v, int64_t& batch) {
+            batch = v.defined() && x.size(0) > 1 ? v.stride(0) : dense;
+            return data<const void>(v);
+        };
+        p.x = rows(t[0], p.x_batch); p.f = rows(t[1], p.f_batch); p.i = rows(t[2], p.i_batch); p.z = rows(t[3], p.z_batch);
+        p.rate = data<const float>(t[4]); p.f_bias = data<const float>(t[5]); p.i_bias = data<const float>(t[6]);
+        p.reset = data<const uint8_t>(t[7]); p.h0 = data<const float>(t[8]);
+        GateGrads g;
+        backward_check(g.bwd(x, p, t[9], grads[0].contiguous(), grads.size() > 1 ? grads[1].contiguous() : at::Tensor(), t[8].defined(),
+                             reinterpret_cast<void*>(ctx->saved_data["stream"].toInt())));
+        return {g.dx, g.df, g.di, g.dz, g.drate, g.df_bias, g.di_bias, at::Tensor(), g.dh0, at::Tensor(), at::Tensor(), at::Tensor()};
+    }
+};
+// gated_recurrence(x, f, i, z, rate, f_bias, i_bias, reset, h0, want_last, stream) -> (out,) or (out, h_last), with gradients
+PyObject* py_gated_recurrence(PyObject*, PyObject* const* argv, Py_ssize_t n)
+{
+    HANDLE_TH_ERRORS
+    if (n != 11) Py_RETURN_NONE;
+    Args a{argv};
+    ss_gate_params p{};
+    const at::Tensor* x = gate_x(a, 0, 3);
+    void* stream = a.stream(10);
+    if (!x || !a.ok || !gate_all(a, 0, *x, p)) Py_RETURN_NONE;
+    at::Tensor t[9];
+    for (int i = 0; i < 9; ++i)
+        if (!a.none(i)) t[i] = THPVariable_Unpack(argv[i]);
+    torch::autograd::variable_list r;
+    try {
+        Unlocked u;
+        r = GateFunction::apply(t[0], t[1], optional(t[2]), optional(t[3]), t[4], optional(t[5]), optional(t[6]), optional(t[7]), optional(t[8]), argv[9] == Py_True, &p, reinterpret_cast<int64_t>(stream));
+    } catch (const Refused& e) {
+        return PyLong_FromLong(e.rc);
+    }
+    return r.size() == 2 ? tuple_of({r[0], r[1]}) : tuple_of({r[0]});
     END_HANDLE_TH_ERRORS
 }
 
@@ -763,7 +981,7 @@ PyObject* py_qlinear(PyObject*, PyObject* const* argv, Py_ssize_t n)
 #define SS_METHOD(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)(void)>(py_##name)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {SS_METHOD(step), SS_METHOD(layer_step), SS_METHOD(scan_fwd), SS_METHOD(scan_bwd),
                          SS_METHOD(layer_fwd), SS_METHOD(layer_bwd), SS_METHOD(norm_fwd), SS_METHOD(norm_bwd), SS_METHOD(gate_fwd),
-                         SS_METHOD(gate_bwd), SS_METHOD(gate_step), SS_METHOD(qlinear), {nullptr, nullptr, 0, nullptr}};
+                         SS_METHOD(gate_bwd), SS_METHOD(gate_step), SS_METHOD(qlinear), SS_METHOD(layer_norm), SS_METHOD(gated_recurrence), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_marshal", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace
