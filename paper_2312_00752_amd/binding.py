@@ -844,6 +844,14 @@ def _bytes(n, device):
     return torch.empty(max(256, n), dtype=torch.uint8, device=device)
 
 
+def _current(stream):
+    """Context in which ``stream`` (a torch.cuda.Stream or a raw handle) is torch's current stream.  The calls below take memory of their
+    own (results, scratch): it has to belong to the stream that they run on, or torch may hand it out again while they run."""
+    if isinstance(stream, int):
+        stream = torch.cuda.ExternalStream(stream) if stream else torch.cuda.default_stream()
+    return torch.cuda.stream(stream)
+
+
 def _lend(given, need, device, name):
     """The caller's scratch tensor, or one of our own."""
     if given is None:
@@ -853,6 +861,8 @@ def _lend(given, need, device, name):
 
 def _norm_params(x, weight, bias, residual, eps):
     f32 = torch.float32
+    if x.dim() < 1:
+        raise ValueError("a tensor without axes cannot be normalised")
     p = NormParams()
     width = x.shape[-1]
     p.rows, p.width = (x.numel() // width if width else 0), width
@@ -874,6 +884,9 @@ def ss_norm_fwd(x, weight=None, bias=None, residual=None, eps=1e-5, out=None, su
     """Enqueue layer norm over the last axis, of ``x`` or of ``x + residual`` (float32 or of x's dtype; the sum is held in its
     dtype and normalised as held).  Returns (out, summed or None, stats or None); ``summed`` may be given as ``residual`` itself,
     ``stats`` (2, rows) is what ``ss_norm_bwd`` needs."""
+    if stream is not None:
+        with _current(stream):
+            return ss_norm_fwd(x, weight, bias, residual, eps, out, summed, save_stats)
     if out is None and summed is None and x.is_cuda:
         r = (_native or _marshal()).norm_fwd(x, weight, bias, residual, eps, bool(save_stats), _stream(stream))
         if r is not None:
@@ -910,6 +923,9 @@ def ss_norm_bwd(dout, s, stats, weight=None, has_bias=False, residual_dtype=None
     """Enqueue the backward pass.  ``s`` is what was normalised (``summed``, or ``x`` of a call without a residual, with
     ``residual_dtype`` None) and ``dsummed`` the gradient that reaches the sum from behind, or None.  Returns a dict with dx,
     dresidual (dx itself where the dtypes agree), dweight and dbias."""
+    if stream is not None:
+        with _current(stream):
+            return ss_norm_bwd(dout, s, stats, weight, has_bias, residual_dtype, dsummed, eps, workspace)
     if workspace is None and dout.is_cuda and (residual_dtype is None or s.dtype == residual_dtype):
         r = (_native or _marshal()).norm_bwd(dout, s, stats, weight, bool(has_bias), residual_dtype is not None, dsummed, eps, _stream(stream))
         if r is not None:
@@ -971,6 +987,8 @@ def _rows_of(t, io, shape, name):
 
 def _gate_inputs(p, x, f, i, z, rate, f_bias, i_bias, names=("x", "f", "i", "z")):
     f32, shape, io = torch.float32, x.shape, x.dtype
+    if len(shape) != (3 if names[0] == "x" else 2):
+        raise ValueError("%s must have %s axes" % (names[0], "three" if names[0] == "x" else "two"))
     p.batch, p.dim = shape[0], shape[1]
     p.io_dtype = _io_code(x)
     for name, t in zip(names, (x, f, i, z)):
@@ -1024,6 +1042,9 @@ def ss_gate_fwd(x, f, rate, i=None, z=None, f_bias=None, i_bias=None, reset=None
     bool or uint8, not 0 where a sequence begins; h0 (B,D) float32.  ``workspace``: a uint8 tensor of
     ``ss_gate_workspace_bytes`` bytes; with ``save_for_bwd`` it is filled for ``ss_gate_bwd``, without it serves as
     scratch (one of the call's own if not given)."""
+    if stream is not None:
+        with _current(stream):
+            return ss_gate_fwd(x, f, rate, i, z, f_bias, i_bias, reset, h0, out, h_last, return_last_state, workspace, save_for_bwd)
     if out is None and h_last is None and x.is_cuda:
         r = (_native or _marshal()).gate_fwd(x, f, i, z, rate, f_bias, i_bias, reset, h0, workspace, bool(save_for_bwd), bool(return_last_state),
                                              _stream(stream))
@@ -1054,6 +1075,9 @@ def ss_gate_bwd(dout, x, f, rate, workspace, i=None, z=None, f_bias=None, i_bias
     """Enqueue the backward pass after a forward call that filled ``workspace``.  Returns a dict with dx, df, di, dz, drate,
     df_bias, di_bias, dh0 (None where the input was not given).  ``grads``: tensors under these names to write into
     instead of new ones; dx, df, di and dz may be slices along dim 1 of a wider tensor."""
+    if stream is not None:
+        with _current(stream):
+            return ss_gate_bwd(dout, x, f, rate, workspace, i, z, f_bias, i_bias, reset, h0, dh_last, want_dh0, grads)
     if grads is None and x.is_cuda:
         r = (_native or _marshal()).gate_bwd(x, f, i, z, rate, f_bias, i_bias, reset, h0, workspace, dout, dh_last, bool(want_dh0), _stream(stream))
         if r is not None:
@@ -1092,6 +1116,9 @@ def ss_gate_bwd(dout, x, f, rate, workspace, i=None, z=None, f_bias=None, i_bias
 def ss_gate_step(h, x_t, f_t, rate, i_t=None, z_t=None, f_bias=None, i_bias=None, reset_t=None, out_t=None, stream=None):
     """Enqueue one token of the recurrence; ``h`` (B,D) float32 is updated in place.  x_t, f_t, i_t, z_t are (B,D), each dense or
     a slice along dim 1; ``reset_t`` (B) marks entries whose sequence begins with this token.  Returns out_t."""
+    if stream is not None:
+        with _current(stream):
+            return ss_gate_step(h, x_t, f_t, rate, i_t, z_t, f_bias, i_bias, reset_t, out_t)
     if x_t.is_cuda:
         r = (_native or _marshal()).gate_step(x_t, f_t, i_t, z_t, rate, f_bias, i_bias, reset_t, h, out_t, _stream(stream))
         if r is not None:
@@ -1117,6 +1144,11 @@ def ss_quant_pitch(dim):
 def ss_quant_rows(x, seq_last=False, scratch=None, stream=None):
     """Enqueue the quantiser: (q, scale) of the rows of ``x`` (..., K), or with ``seq_last`` of the tokens of ``x`` (B,K,L).
     q is (rows, ss_quant_pitch(K)) int8, scale (rows) float32; a weight (features, K) is brought to 8 bits the same way."""
+    if stream is not None:
+        with _current(stream):
+            return ss_quant_rows(x, seq_last, scratch)
+    if x.dim() != 3 if seq_last else x.dim() < 1:
+        raise ValueError("x must have %s" % ("three axes" if seq_last else "an axis to quantise"))
     p = QuantParams()
     if seq_last:
         p.batch, p.dim, p.seqlen = x.shape
@@ -1156,13 +1188,16 @@ def ss_qlinear(x, weight, scale, bias=None, x_seq_last=False, out_seq_last=False
     the result (..., features), with ``out_seq_last`` (B,features,L), which takes x of three axes.  With ``x_scale`` x is itself
     quantised, (rows, pitch) int8 or (B, L, pitch), of ``dim`` values each, and the result has ``out_dtype`` (bfloat16 unless
     given).  ``scratch``: uint8 tensor of ``ss_qlinear_scratch_bytes`` bytes, or None: the call takes its own."""
+    if stream is not None:
+        with _current(stream):
+            return ss_qlinear(x, weight, scale, bias, x_seq_last, out_seq_last, x_scale, dim, out_dtype, out, scratch)
     if x_scale is None and out is None and scratch is None and out_dtype is None and x.is_cuda:
         r = (_native or _marshal()).qlinear(x, weight, scale, bias, (SS_Q_X_SEQ_LAST if x_seq_last else 0) | (SS_Q_OUT_SEQ_LAST if out_seq_last else 0),
                                             _stream(stream))
         if r is not None:
             return _result(r)
-    if weight.dim() != 2:
-        raise ValueError("weight must have two axes")
+    if weight.dim() != 2 or x.dim() < 1:
+        raise ValueError("weight must have two axes, x one at least")
     quantised = x_scale is not None
     lead = tuple(x.shape[:-1])
     if x_seq_last or out_seq_last:

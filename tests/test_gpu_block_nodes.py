@@ -99,3 +99,41 @@ def test_refused_calls():
         x.add_(1.0)
     with pytest.raises(RuntimeError):   # x is needed as it was
         out.sum().backward()
+
+
+def test_memory_of_a_call_belongs_to_its_stream():
+    """A call's own scratch and results on a side stream are not handed out again while it runs: current-stream work that
+    allocates and writes at once after each call leaves its results alone."""
+    side = torch.cuda.Stream()
+    x = torch.randn(1, 700, 1500, device="cuda").bfloat16()
+    w, s = B.ss_quant_rows(torch.randn(600, 1500, device="cuda"))
+    res = torch.randn(3000, 1100, device="cuda")
+    long = torch.randn(1, 8, 60000, device="cuda")
+    rate = torch.ones(8, device="cuda")
+    _, _, stats = B.ss_norm_fwd(res, save_stats=True)
+    wn = torch.ones(1100, device="cuda")
+    calls = [lambda st: B.ss_qlinear(x, w, s, out_seq_last=True, stream=st), lambda st: B.ss_gate_fwd(long, long, rate, stream=st)[0],
+             lambda st: B.ss_norm_bwd(res, res, stats, wn, stream=st)["dweight"], lambda st: B.ss_norm_fwd(res, stream=st)[0],
+             lambda st: B.ss_quant_rows(x, seq_last=True, stream=st)[0]]
+    want = [c(None) for c in calls]
+    torch.cuda.synchronize()
+    for c, ref in zip(calls, want):
+        for stream in (side, side.cuda_stream):
+            got = []
+            for _ in range(5):
+                got.append(c(stream))
+                for _ in range(4):
+                    torch.full((4 << 20,), 7, dtype=torch.uint8, device="cuda")
+            torch.cuda.synchronize()
+            assert all(torch.equal(g, ref) for g in got)
+    assert torch.equal(B.ss_norm_fwd(res, stream=0)[0], want[3])
+
+
+def test_axes():
+    one = torch.tensor(1.0, device="cuda")
+    rate = torch.ones(3, device="cuda")
+    for call in (lambda: B.ss_norm_fwd(one), lambda: B.ss_quant_rows(one), lambda: B.ss_quant_rows(rate, seq_last=True),
+                 lambda: B.ss_gate_fwd(rate, rate, rate), lambda: B.ss_gate_step(one, rate, rate, rate),
+                 lambda: B.ss_qlinear(one, *B.ss_quant_rows(torch.ones(2, 3, device="cuda")))):
+        with pytest.raises(ValueError):
+            call()
