@@ -42,25 +42,24 @@ __device__ __forceinline__ RowScale row_scale(uint32_t top)
     }
     return r;
 }
-// round(v inv), ties to even; a value without a number (its row comes out as NaN) gives 0
-__device__ __forceinline__ int quantised(float v, float inv)
+// round(v inv) of four values, ties to even, as the bytes of a word: 1.5 2^23 added to the rounded product leaves the whole number in the
+// low byte.  inv is 0 in rows that come out as zeros or NaN; their bytes are 0 whatever stands in them.
+__device__ __forceinline__ uint32_t quantised4(float v0, float v1, float v2, float v3, float inv)
 {
-    const float p = v * inv;
-    return p == p ? (int)rintf(p) : 0;
+#pragma clang fp contract(off)
+    constexpr float up = 12582912.0f;
+    const float p0 = v0 * inv, p1 = v1 * inv, p2 = v2 * inv, p3 = v3 * inv;
+    const uint32_t low = __builtin_amdgcn_perm(__float_as_uint(p1 + up), __float_as_uint(p0 + up), 0x0c0c0400u);
+    const uint32_t high = __builtin_amdgcn_perm(__float_as_uint(p3 + up), __float_as_uint(p2 + up), 0x04000c0cu);
+    return inv == 0.0f ? 0u : low | high;
 }
 __device__ __forceinline__ uint2 quantised8(const float (&v)[8], float inv)
 {
-    uint32_t w[2];
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-        w[h] = 0u;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) w[h] |= (uint32_t(quantised(v[4 * h + j], inv)) & 0xffu) << (8 * j);
-    }
-    return make_uint2(w[0], w[1]);
+    return make_uint2(quantised4(v[0], v[1], v[2], v[3], inv), quantised4(v[4], v[5], v[6], v[7], inv));
 }
 
-// Rows contiguous along dim: G lanes hold a row in registers, V slices of 8 each.
+// Rows contiguous along dim: G lanes hold a row in registers, V slices of 8 each, so it is read once.  Bound by HBM: 16384 x 2048 bf16
+// (67 MB in, 34 MB out) 24 us when not in a cache, 4.2 TB/s.
 template <typename T, int G, int V>
 __global__ __launch_bounds__(G > 256 ? G : 256) void quant_rows_kernel(const T* x, int8_t* q, float* scale, int rows, int dim, int pitch)
 {
@@ -110,7 +109,7 @@ __global__ __launch_bounds__(G > 256 ? G : 256) void quant_rows_kernel(const T* 
     }
     if (gl == 0) scale[row] = s.scale;
 }
-// Rows that do not fit: a workgroup a row, read twice.
+// Rows that do not fit: a workgroup a row, read twice, the second time from the caches.  2048 x 20000 bf16 57 us.
 template <typename T>
 __global__ __launch_bounds__(1024) void quant_rows_wide_kernel(const T* x, int8_t* q, float* scale, int dim, int pitch)
 {
@@ -126,11 +125,33 @@ __global__ __launch_bounds__(1024) void quant_rows_wide_kernel(const T* x, int8_
     for (int w = 0; w < 16; ++w) top = max(top, lds[w]);
     const RowScale s = row_scale(top);
     for (int k = threadIdx.x; k < pitch; k += 1024)
-        q[(int64_t)blockIdx.x * pitch + k] = k < dim ? (int8_t)quantised(io_to_f32<T>(r[k]), s.inv) : (int8_t)0;
+        q[(int64_t)blockIdx.x * pitch + k] = k < dim ? (int8_t)quantised4(io_to_f32<T>(r[k]), 0.0f, 0.0f, 0.0f, s.inv) : (int8_t)0;
     if (threadIdx.x == 0) scale[blockIdx.x] = s.scale;
 }
 
-// Sequence last, x (batch, dim, L).  First the largest magnitudes of Q_CHUNK channels at a time, (chunks, batch L); ...
+// Slices of eight tokens with the sequence last, x (batch, dim, L): of channel k, the last one's for those past it, ...
+template <typename T>
+__device__ __forceinline__ typename io8<T>::raw request_channel(const T* x, int b, bool last_entry, int k, int dim, int t0, int L)
+{
+    const int kk = min(k, dim - 1);
+    return slice_request<T, true>(x + ((int64_t)b * dim + kk) * L, t0, L, slice_limit(L, slice_whole(L, last_entry && kk == dim - 1)));
+}
+// ... and of four channels as floats, zeros for those past the last.
+template <typename T>
+__device__ __forceinline__ void settle4(typename io8<T>::raw (&raw)[4], bool last_entry, int k0, int dim, int t0, int L, float (&v)[4][8])
+{
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        const bool whole = slice_whole(L, last_entry && k0 + e >= dim - 1);
+        slice_settle<T>(raw[e], t0, L, slice_limit(L, whole), whole);
+        io8<T>::unpack(raw[e], v[e]);
+        if (k0 + e >= dim)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[e][j] = 0.0f;
+    }
+}
+// In two launches, where registers do not hold the channels.  First the largest magnitudes of Q_CHUNK channels at a time, (chunks, batch L); ...
+// (2 x 8192 x 4096 bf16, 134 MB, 30 us)
 constexpr int Q_CHUNK = 128;
 template <typename T>
 __global__ __launch_bounds__(256) void quant_tops_kernel(const T* x, uint32_t* tops, int batch, int dim, int L)
@@ -159,7 +180,8 @@ __global__ __launch_bounds__(256) void quant_tops_kernel(const T* x, uint32_t* t
     if (t < L) tops[(int64_t)blockIdx.y * batch * L + (int64_t)b * L + t] = m;
 }
 // ... then tiles of 128 tokens and 128 channels, turned through LDS: a thread takes 8 tokens of four channels and puts each token's four
-// bytes down as a word; rows of 132 bytes spread those of a wave over all banks.  4 x 4096 x 1531 bf16 (75 MB) 19.8 us (64 tokens, bytes put down one by one: 35).
+// bytes down as a word; rows of 132 bytes spread those of a wave over all banks.  2 x 8192 x 4096 bf16 35 us, 5.8 TB/s (64 tokens, bytes put down one
+// by one: 1.8 times as long).
 constexpr int TURN_TOKENS = 128;
 template <typename T>
 __global__ __launch_bounds__(256) void quant_turn_kernel(const T* x, const uint32_t* tops, int8_t* q, float* scale, int batch, int dim, int L, int pitch, int chunks)
@@ -185,11 +207,7 @@ __global__ __launch_bounds__(256) void quant_turn_kernel(const T* x, const uint3
 #pragma unroll
     for (int r = 0; r < 2; ++r)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            const int k = min(k0 + 64 * r + 4 * kq + e, dim - 1);
-            const int limit = slice_limit(L, slice_whole(L, b == batch - 1 && k == dim - 1));
-            raw[r][e] = slice_request<T, true>(x + ((int64_t)b * dim + k) * L, t0 + 8 * i, L, limit);
-        }
+        for (int e = 0; e < 4; ++e) raw[r][e] = request_channel<T>(x, b, b == batch - 1, k0 + 64 * r + 4 * kq + e, dim, t0 + 8 * i, L);
     __syncthreads();
     if (threadIdx.x < TURN_TOKENS) {
         const RowScale s = row_scale(max(half[0][threadIdx.x], half[1][threadIdx.x]));
@@ -199,19 +217,10 @@ __global__ __launch_bounds__(256) void quant_turn_kernel(const T* x, const uint3
     __syncthreads();
 #pragma unroll
     for (int r = 0; r < 2; ++r) {
-        uint32_t w[8] = {0u, 0u, 0u, 0u, 0u, 0u, 0u, 0u};
+        float v[4][8];
+        settle4<T>(raw[r], b == batch - 1, k0 + 64 * r + 4 * kq, dim, t0 + 8 * i, L, v);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            const int k = k0 + 64 * r + 4 * kq + e;
-            const bool whole = slice_whole(L, b == batch - 1 && k >= dim - 1);
-            slice_settle<T>(raw[r][e], t0 + 8 * i, L, slice_limit(L, whole), whole);
-            float v[8];
-            io8<T>::unpack(raw[r][e], v);
-#pragma unroll
-            for (int j = 0; j < 8; ++j) w[j] |= k < dim ? (uint32_t(quantised(v[j], inv[8 * i + j])) & 0xffu) << (8 * e) : 0u;
-        }
-#pragma unroll
-        for (int j = 0; j < 8; ++j) tile[(8 * i + j) * ROW + 16 * r + kq] = w[j];
+        for (int j = 0; j < 8; ++j) tile[(8 * i + j) * ROW + 16 * r + kq] = quantised4(v[0][j], v[1][j], v[2][j], v[3][j], inv[8 * i + j]);
     }
     __syncthreads();
 #pragma unroll
@@ -221,6 +230,119 @@ __global__ __launch_bounds__(256) void quant_turn_kernel(const T* x, const uint3
             const uint32_t* p = &tile[tl * ROW + 4 * c];
             *reinterpret_cast<uint4*>(q + ((int64_t)b * L + t) * pitch + k0 + 16 * c) = make_uint4(p[0], p[1], p[2], p[3]);
         }
+    }
+}
+
+// The largest magnitudes of eight values each lane has seen, and their exchange over LDS: 16-bit ones in pairs.
+template <typename T>
+struct Tops {
+    uint32_t w[8] = {0u, 0u, 0u, 0u, 0u, 0u, 0u, 0u};
+    static constexpr int N = 8;
+    static __device__ __forceinline__ uint32_t larger(uint32_t a, uint32_t b) { return max(a, b); }
+    __device__ __forceinline__ void see(const typename io8<T>::raw& r)
+    {
+        float v[8];
+        io8<T>::unpack(r, v);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) w[j] = max(w[j], magnitude(v[j]));
+    }
+    static __device__ __forceinline__ void put(uint32_t* to, int i, uint32_t v) { to[i] = v; }
+};
+template <>
+struct Tops<bf16_t> {
+    typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+    uint32_t w[4] = {0u, 0u, 0u, 0u};
+    static constexpr int N = 4;
+    static __device__ __forceinline__ uint32_t larger(uint32_t a, uint32_t b)
+    {
+        return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(u16x2, a), __builtin_bit_cast(u16x2, b)));
+    }
+    __device__ __forceinline__ void see(const io8<bf16_t>::raw& r)
+    {
+        const uint32_t v[4] = {r.w.x, r.w.y, r.w.z, r.w.w};
+#pragma unroll
+        for (int j = 0; j < 4; ++j) w[j] = larger(w[j], v[j] & 0x7fff7fffu);
+    }
+    static __device__ __forceinline__ void put(uint32_t* to, int i, uint32_t v)
+    {
+        to[2 * i] = v << 16;
+        to[2 * i + 1] = v & 0xffff0000u;
+    }
+};
+
+// Where a workgroup's registers hold all channels of 8 WIDE tokens, one pass: a thread has 8 tokens of four channels R times, the tokens' scales
+// come from an exchange over the workgroup, and a thread's four bytes of a token are a word of its row, of which a wave writes
+// whole lines.  Bound by the pieces in which rows are read, 16 WIDE bytes of bf16: 4 x 4096 x 1531 bf16 (75 MB in, 25 MB out) takes 18 us at
+// 64 bytes, 27 at 32; in two launches 11 + 20.  Up to 64 registers a thread where they do without spilling, so that two
+// workgroups of 1024 share a unit.
+template <typename T, int THREADS, int WIDE, int R>
+__global__ __launch_bounds__(THREADS, R * sizeof(T) <= 4 && THREADS * R < 2048 * WIDE ? 8 : 4) void quant_held_kernel(const T* x, int8_t* q, float* scale, int batch, int dim, int L, int pitch, int tiles)
+{
+    constexpr int WAVES = THREADS / WAVE, TOKENS = 8 * WIDE, SIDE = THREADS / WIDE;
+    __shared__ uint32_t lds[WAVES][TOKENS];
+    __shared__ float inv[TOKENS];
+    // the XCDs get neighbouring tiles, which share lines
+    const int share = gridDim.x / 8, id = blockIdx.x < 8 * share ? (blockIdx.x % 8) * share + blockIdx.x / 8 : blockIdx.x;
+    const int b = id / tiles, t0 = (id - b * tiles) * TOKENS, i = threadIdx.x % WIDE, kq = 4 * (threadIdx.x / WIDE);
+    const bool last = b == batch - 1;
+    typename io8<T>::raw raw[R][4];
+#pragma unroll
+    for (int r = 0; r < R; ++r)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) raw[r][e] = request_channel<T>(x, b, last, r * 4 * SIDE + kq + e, dim, t0 + 8 * i, L);
+    Tops<T> top;
+#pragma unroll
+    for (int r = 0; r < R; ++r)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const bool whole = slice_whole(L, last && r * 4 * SIDE + kq + e >= dim - 1);
+            slice_settle<T>(raw[r][e], t0 + 8 * i, L, slice_limit(L, whole), whole);
+            top.see(raw[r][e]);
+        }
+    // lanes of the same tokens halve the words between them, then take the larger
+    int word = 0, lanes = WIDE;
+#pragma unroll
+    for (int n = Tops<T>::N / 2; n >= 1; n /= 2, lanes *= 2) {
+        const bool up = threadIdx.x & lanes;
+#pragma unroll
+        for (int j = 0; j < n; ++j) {
+            const uint32_t mine = up ? top.w[j + n] : top.w[j], other = up ? top.w[j] : top.w[j + n];
+            top.w[j] = Tops<T>::larger(mine, (uint32_t)__shfl_xor((int)other, lanes));
+        }
+        word += up ? n : 0;
+    }
+#pragma unroll
+    for (; lanes < WAVE; lanes *= 2) top.w[0] = Tops<T>::larger(top.w[0], (uint32_t)__shfl_xor((int)top.w[0], lanes));
+    if (threadIdx.x % WAVE < WIDE * Tops<T>::N) Tops<T>::put(&lds[threadIdx.x / WAVE][8 * i], word, top.w[0]);
+    __syncthreads();
+    if (threadIdx.x < TOKENS) {
+        uint32_t m = 0u;
+#pragma unroll
+        for (int w = 0; w < WAVES; ++w) m = max(m, lds[w][threadIdx.x]);
+        const RowScale s = row_scale(m);
+        inv[threadIdx.x] = s.inv;
+        if (t0 + (int)threadIdx.x < L) scale[(int64_t)b * L + t0 + threadIdx.x] = s.scale;
+    }
+    __syncthreads();
+    int8_t* const to = q + ((int64_t)b * L + t0 + 8 * i) * pitch;
+    float by[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) by[j] = inv[8 * i + j];
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+        const int k = r * 4 * SIDE + kq;
+        if (k >= pitch) break;
+        float v[4][8];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            io8<T>::unpack(raw[r][e], v[e]);
+            if (k + e >= dim)
+#pragma unroll
+                for (int j = 0; j < 8; ++j) v[e][j] = 0.0f;
+        }
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            if (t0 + 8 * i + j < L) *reinterpret_cast<uint32_t*>(to + (int64_t)j * pitch + k) = quantised4(v[0][j], v[1][j], v[2][j], v[3][j], by[j]);
     }
 }
 
@@ -621,11 +743,45 @@ struct QuantSizes {
     int batch, L, dim, pitch;
     int chunks;   // of channels, sequence last
 };
+// One pass over tokens with the sequence last, where that is faster.  us, not in a cache, one pass / two: bf16, 70, 1000, 4100 and 16384 tokens of
+// 2048 channels 4.7 7.0 9.8 34.2 / 9.7 13.7 17.3 33.3, of 4096 9.5 9.8 21.1 58.4 / 10.2 15.1 27.5 71.3; 1000 of 5120 11.8 / 16.6; float32 of
+// 2048 8.7 8.8 15.4 38.4 / 9.2 13.8 23.7 55.2, of 4096 11.6 11.4 27.7 89.7 / 9.5 15.9 35.2 114; but 4100 of 5120 31.4 / 31.7 (float32 45.4 / 41.3) and
+// 70 of 8192 15.7 / 10.8.  Wide tiles read longer pieces of rows, and take many tokens to fill the chip: tiles of 8 (or 16) and of 32 tokens (float32: 16 of
+// 4096), bf16 4096 channels 1000 tokens 9.8 / 14.1, 6000 28.2 / 21.3, float32 2048 1000 8.8 / 10.2, 8192 28.9 / 20.3.
+template <typename T>
+bool quant_held(const QuantSizes& z, const T* x, int8_t* q, float* scale, hipStream_t st)
+{
+    constexpr bool NARROW = sizeof(T) == 2;
+    const int tokens = z.batch * z.L;
+    auto go = [&](auto threads, auto wide, auto r) {
+        constexpr int THREADS = decltype(threads)::value, WIDE = decltype(wide)::value, R = decltype(r)::value;
+        if (z.pitch > 4 * (THREADS / WIDE) * R) return false;
+        const int tiles = (z.L + 8 * WIDE - 1) / (8 * WIDE);
+        hipLaunchKernelGGL((quant_held_kernel<T, THREADS, WIDE, R>), dim3((unsigned)(tiles * z.batch)), dim3(THREADS), 0, st, x, q, scale, z.batch, z.dim, z.L,
+                           z.pitch, tiles);
+        return true;
+    };
+    typedef std::integral_constant<int, 1> one;
+    typedef std::integral_constant<int, 2> two;
+    typedef std::integral_constant<int, 4> four;
+    constexpr std::integral_constant<int, 1024> most{};
+    if constexpr (!NARROW)
+        if (z.pitch > 1024 && z.pitch <= 2048 && tokens >= 6000) return go(most, four{}, two{});
+    if (z.pitch <= 2048) return go(std::integral_constant<int, 256>{}, two{}, one{}) || go(std::integral_constant<int, 512>{}, two{}, one{}) || go(most, two{}, one{});
+    if constexpr (NARROW) {
+        if (z.pitch > 4096) return z.pitch <= 6144 && tokens <= 3000 && go(most, one{}, two{});
+        if (tokens >= 4000) return go(most, four{}, four{});
+    } else if (tokens >= 3000) {
+        return go(most, two{}, two{});
+    }
+    return go(std::integral_constant<int, 512>{}, one{}, two{});
+}
 template <typename T>
 void quant_launch(const QuantSizes& z, bool seq_last, const void* xv, int8_t* q, float* scale, uint32_t* tops, hipStream_t st)
 {
     const T* x = static_cast<const T*>(xv);
     if (seq_last) {
+        if (quant_held<T>(z, x, q, scale, st)) return;
         hipLaunchKernelGGL(quant_tops_kernel<T>, dim3((unsigned)((z.L + 255) / 256), (unsigned)z.chunks, (unsigned)z.batch), dim3(256), 0, st, x, tops, z.batch,
                            z.dim, z.L);
         hipLaunchKernelGGL(quant_turn_kernel<T>, dim3((unsigned)((z.L + TURN_TOKENS - 1) / TURN_TOKENS), (unsigned)(z.pitch / Q_STEP), (unsigned)z.batch), dim3(256), 0, st, x, tops,

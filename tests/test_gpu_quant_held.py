@@ -1,0 +1,63 @@
+"""The quantiser of tokens with the sequence last where registers hold all channels of a tile of tokens: both sides of every change
+of its form, ragged tiles, rows without a scale.  The quantiser's arithmetic is fixed to the bit."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import block_oracle as bo
+from paper_2312_00752_amd import binding as B
+from tests import op_util as u
+
+pytestmark = pytest.mark.gpu
+
+
+def check(batch, dim, seqlen, io, change=None, bad=()):
+    """``bad``: tokens whose scale must be NaN"""
+    rng = np.random.default_rng(dim * 31 + seqlen)
+    x = u.rounded(rng.standard_normal((batch, dim, seqlen)) * np.where(rng.random((batch, 1, seqlen)) < 0.1, 50.0, 1.0), io)
+    if change:
+        change(x)
+    q, s = B.ss_quant_rows(u.upload(x, io), seq_last=True)
+    rq, rs = bo.quant_rows(np.swapaxes(x, 1, 2).reshape(-1, dim))
+    q, s = q.cpu().numpy(), s.cpu().numpy()
+    assert not q[:, dim:].any()
+    assert np.array_equal(s, rs, equal_nan=True) and set(np.flatnonzero(np.isnan(s))) == set(bad)
+    assert np.array_equal(q[:, :dim], rq)
+
+
+@pytest.mark.parametrize("io", ["f32", "bf16"])
+@pytest.mark.parametrize("dim", [1, 3, 127, 511, 512, 513, 1000, 1024, 1025, 2048, 2049, 4095, 4096, 4097, 6144, 6145])
+def test_widths(dim, io):
+    check(2, dim, 37, io)
+
+
+@pytest.mark.parametrize("io", ["f32", "bf16"])
+@pytest.mark.parametrize("dim,tokens", [(300, 9000), (1500, 5999), (1500, 6000), (2047, 6003), (2500, 2999), (2500, 3000), (4096, 3999), (4096, 4001), (4500, 3000), (4500, 3001)])
+def test_many_tokens(dim, tokens, io):
+    check(1, dim, tokens, io)
+
+
+@pytest.mark.parametrize("io", ["f32", "bf16"])
+@pytest.mark.parametrize("seqlen", [1, 5, 7, 8, 9, 15, 16, 17, 31, 32, 33, 65])
+def test_tiles(seqlen, io):
+    check(5, 130, seqlen, io)
+    check(2, 2100, seqlen, io)
+    check(130, 2100, 33 if seqlen == 33 else seqlen % 30 + 31, io)
+
+
+@pytest.mark.parametrize("io", ["f32", "bf16"])
+@pytest.mark.parametrize("dim", [40, 1100, 2100])
+def test_rows_without_a_scale(dim, io):
+    """Their bytes are 0 as well, also those of a NaN whose bits are not the usual ones."""
+    def change(x):
+        x[0, :, 3] = 0
+        x[0, :, 4] = 1e-37
+        x[0, dim // 2, 5] = np.inf
+        x[1, 0, 0] = np.nan
+        x[1, dim - 1, 18] = -np.inf
+    check(2, dim, 19, io, change, bad=(5, 19, 37))
+    bits = torch.full((1, dim, 3), 0x7fe500a5, dtype=torch.int32, device="cuda").view(torch.float32)
+    x = torch.ones(1, dim, 3, device="cuda")
+    x[:, 7::9] = bits[:, 7::9]
+    q, s = B.ss_quant_rows(x if io == "f32" else (x.view(torch.int32) >> 16).to(torch.int16).view(torch.bfloat16), seq_last=True)
+    assert torch.isnan(s).all() and not q.any()
