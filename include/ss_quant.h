@@ -5,7 +5,7 @@
  * serving time, with weights held in 8 bits and tokens brought to 8 bits as they come.  Rows (tokens, or
  * a weight's output channels) are quantised symmetrically:
  *
- *     scale = max_k |x_k| / 127,     q_k = round(x_k * (127 / max_k |x_k|))     ties to even; float32 arithmetic
+ *     scale = max_k |x_k| / 127,     q_k = round(x_k * (127 * (1 / max_k |x_k|)))    ties to even; float32 arithmetic
  *
  * and a product is summed exactly in 32-bit integers:
  *

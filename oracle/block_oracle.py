@@ -100,7 +100,7 @@ def quant_rows(x):
     top = np.abs(x).max(1, initial=0.0)
     some = top >= np.float32(2.0 ** -120)
     with np.errstate(divide="ignore", over="ignore", invalid="ignore"):
-        inv = np.where(some, np.float32(127.0) / top, np.float32(0.0)).astype(np.float32)
+        inv = np.where(some, np.float32(127.0) * (np.float32(1.0) / top), np.float32(0.0)).astype(np.float32)
         scale = np.where(np.isfinite(top), np.where(some, top / np.float32(127.0), np.float32(0.0)), np.float32(np.nan)).astype(np.float32)
         p = x * inv[:, None]
     q = np.where(np.isnan(p), np.float32(0.0), np.rint(p)).astype(np.int64)

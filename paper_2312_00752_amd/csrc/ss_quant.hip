@@ -38,7 +38,7 @@ __device__ __forceinline__ RowScale row_scale(uint32_t top)
         r.inv = 0.0f;
     } else {
         r.scale = m / 127.0f;
-        r.inv = 127.0f / m;
+        r.inv = 127.0f * (1.0f / m);
     }
     return r;
 }

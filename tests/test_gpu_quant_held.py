@@ -61,3 +61,12 @@ def test_rows_without_a_scale(dim, io):
     x[:, 7::9] = bits[:, 7::9]
     q, s = B.ss_quant_rows(x if io == "f32" else (x.view(torch.int32) >> 16).to(torch.int16).view(torch.bfloat16), seq_last=True)
     assert torch.isnan(s).all() and not q.any()
+
+
+@pytest.mark.parametrize("dim", [700, 4096, 5000])
+def test_bytes_of_elementary_operations(dim):
+    """The quantiser rounds as round(x * (127.0 / max |x|)) in torch does, so that products agree to the integer."""
+    x = torch.randn(1, 1500, dim, device="cuda") * torch.rand(1, 1500, 1, device="cuda").mul(20).exp()
+    want = torch.round(x * (127.0 / x.abs().amax(-1, keepdim=True)))[0].to(torch.int8)
+    for t, last in ((x, False), (x.transpose(1, 2).contiguous(), True)):
+        assert torch.equal(B.ss_quant_rows(t, seq_last=last)[0][:, :dim], want)
