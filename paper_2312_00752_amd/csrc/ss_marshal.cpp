@@ -14,6 +14,7 @@
 #include <ATen/ATen.h>
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/custom_function.h>
+#include <torch/csrc/autograd/functions/basic_ops.h>
 #include <torch/csrc/autograd/python_variable.h>
 
 #include "ss_gate.h"
@@ -618,6 +619,15 @@ PyObject* py_norm_bwd(PyObject*, PyObject* const* argv, Py_ssize_t n)
 
 // Layer norm as a node of torch's graph (what autograd._LayerNorm is in Python): the backward pass runs on the stream of the forward pass,
 // which is also the one that torch makes current for it.
+// A backward pass's gradients have no graph of their own: where one is being built, going through them again is an error.
+torch::autograd::variable_list differentiable_once(torch::autograd::variable_list grads)
+{
+    if (!at::GradMode::is_enabled()) return grads;
+    for (at::Tensor& g : grads)
+        if (g.defined()) g = g.detach().set_requires_grad(true);
+    torch::autograd::DelayedError error("the gradients of layer_norm and gated_recurrence cannot be differentiated again", (int64_t)grads.size());
+    return error(std::move(grads));
+}
 struct NormFunction : torch::autograd::Function<NormFunction> {
     static torch::autograd::variable_list forward(torch::autograd::AutogradContext* ctx, const at::Tensor& x, const Optional& weight_, const Optional& bias_,
                                                   const Optional& residual_, double eps, int64_t stream)
@@ -642,13 +652,13 @@ struct NormFunction : torch::autograd::Function<NormFunction> {
         const at::Tensor more = res && grads[1].defined() ? grads[1].contiguous() : at::Tensor();
         if (!grads[0].defined()) {   // only the sum was used
             const auto io = (at::ScalarType)ctx->saved_data["io"].toInt();
-            return {more.defined() ? more.to(io) : at::Tensor(), at::Tensor(), at::Tensor(), more, at::Tensor(), at::Tensor()};
+            return differentiable_once({more.defined() ? more.to(io) : at::Tensor(), at::Tensor(), at::Tensor(), more, at::Tensor(), at::Tensor()});
         }
         const auto saved = ctx->get_saved_variables();
         NormGrads g;
         backward_check(g.bwd(grads[0].contiguous(), saved[0], saved[2], saved[1], ctx->saved_data["bias"].toBool(), res, more,
                              ctx->saved_data["eps"].toDouble(), reinterpret_cast<void*>(ctx->saved_data["stream"].toInt())));
-        return {g.dx, g.dweight, g.dbias, g.dresidual, at::Tensor(), at::Tensor()};
+        return differentiable_once({g.dx, g.dweight, g.dbias, g.dresidual, at::Tensor(), at::Tensor()});
     }
 };
 // layer_norm(x, weight, bias, residual, eps, stream) -> (out,) or (out, summed), with gradients
@@ -879,7 +889,7 @@ struct GateFunction : torch::autograd::Function<GateFunction> {
         GateGrads g;
         backward_check(g.bwd(x, p, t[9], grads[0].contiguous(), grads.size() > 1 ? grads[1].contiguous() : at::Tensor(), t[8].defined(),
                              reinterpret_cast<void*>(ctx->saved_data["stream"].toInt())));
-        return {g.dx, g.df, g.di, g.dz, g.drate, g.df_bias, g.di_bias, at::Tensor(), g.dh0, at::Tensor(), at::Tensor(), at::Tensor()};
+        return differentiable_once({g.dx, g.df, g.di, g.dz, g.drate, g.df_bias, g.di_bias, at::Tensor(), g.dh0, at::Tensor(), at::Tensor(), at::Tensor()});
     }
 };
 // gated_recurrence(x, f, i, z, rate, f_bias, i_bias, reset, h0, want_last, stream) -> (out,) or (out, h_last), with gradients

@@ -137,3 +137,19 @@ def test_axes():
                  lambda: B.ss_qlinear(one, *B.ss_quant_rows(torch.ones(2, 3, device="cuda")))):
         with pytest.raises(ValueError):
             call()
+
+
+@pytest.mark.parametrize("compiled", [True, False])
+def test_gradients_cannot_be_differentiated_again(compiled, monkeypatch):
+    """They are computed outside of the graph: a second pass through them is refused, not silently without their part."""
+    if not compiled:
+        monkeypatch.setattr(B, "_native", B._NoMarshal)
+    x, res, f = (torch.randn(2, 8, 40, device="cuda", requires_grad=True) for _ in range(3))
+    w, rate = torch.ones(40, device="cuda", requires_grad=True), torch.ones(8, device="cuda", requires_grad=True)
+    out, summed = ag.layer_norm(x, w, residual=res)
+    for y, inputs in ((out, (x, w, res)), (summed, (x, res)), (ag.gated_recurrence(x, f, rate), (x, f, rate))):
+        once = torch.autograd.grad(y.square().sum(), inputs, create_graph=True)
+        plain = torch.autograd.grad(y.square().sum(), inputs, retain_graph=True)
+        assert all(torch.allclose(a, b) for a, b in zip(once, plain))
+        with pytest.raises(RuntimeError):
+            sum(g.square().sum() for g in once).backward()
