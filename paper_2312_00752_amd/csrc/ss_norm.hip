@@ -452,7 +452,6 @@ __global__ __launch_bounds__(256) void norm_columns_kernel(NormArgs a)
 
 // ---- forms ----------------------------------------------------------------------------------------
 constexpr int NORM_WIDEST = 16384;   // widest row that is held in registers
-constexpr int NORM_PARTS = 512;      // most workgroups of a backward call = rows of partial sums
 
 struct NormForm {
     int lanes, slices;   // lanes of a row (0: the kernels for wider rows) and slices of a lane
@@ -489,13 +488,19 @@ void with_form(NormForm f, F go)
     else if (f.lanes == 1024) lanes(std::integral_constant<int, 1024>{});
     else if constexpr (BWD) lanes(std::integral_constant<int, 512>{});
 }
+// Workgroups of a backward call, each with a row of partial sums: one or two for a unit, as each costs 8 bytes a column twice, and
+// counts between leave units idle at the end.  us of a call with 128 / 256 / 384 / 512 / 768 (rows x columns, no residual): bf16 16384 x 1024 27.4 22.9
+// 27.8 27.3 31.4, 2048 x 16384 67.5 55.3 67.4 71.2 86.0, 500 x 8192 16.6 19.6 21.0 24.2 23.9, 2048 x 2048 20.8 15.1 15.5 15.0 16.9; workgroups of 256 lanes are too
+// few to keep memory busy then: 16384 x 2048 113 62.6 52.0 43.2 39.4, 8192 x 4096 81.1 48.5 45.4 44.2 45.1 (float32 134 80.3 84.3 78.5
+// 81.8 and 111 78.8 87.3 82.5 85.3).
 int norm_parts(int rows, int width)
 {
     const NormForm f = norm_form(rows, width, true);
     if (f.lanes == 0) return rows < 64 ? rows : 64;
     const int side = f.lanes > WAVE ? 1 : 512 / f.lanes;
     const int n = (rows + side - 1) / side;
-    return n < NORM_PARTS ? n : NORM_PARTS;
+    const int most = f.lanes == 256 && rows >= 4096 ? 512 : (width > 4096 && rows < 1024 ? 128 : 256);
+    return n < most ? n : most;
 }
 
 template <typename T, typename S, bool RES>
