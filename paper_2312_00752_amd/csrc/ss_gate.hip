@@ -12,7 +12,7 @@
 // a, b and h live in registers only.  The backward pass recomputes the states of a piece from the state
 // before it, which the forward pass left (one float per piece), and runs the adjoint through the same scan backwards in time:
 //
-//     lam_t = dy_t + G_{t+1},   G_t = a_t lam_t,   dL/d(log a_t) = lam_t (a_t h_{t-1} - m_t' ...)   (see gate_bwd_kernel)
+//     lam_t = dy_t + G_{t+1},   G_t = a_t lam_t,   dL/d(log a_t) = lam_t a_t (h_{t-1} - g_t x_t a_t / m_t)
 //
 // G_t is again an affine map of G_{t+1}, with a_t and b = a_t dy_t.
 #include <hip/hip_runtime.h>
@@ -321,6 +321,9 @@ __device__ __forceinline__ void slice_map(const float (&av)[8], const float (&bv
 
 template <int TEAM> constexpr int gate_threads() { return (TEAM > 1 ? TEAM : GATE_WAVES) * WAVE; }
 
+// Bound by HBM on full grids: 32768 rows of 2048 bf16 with input gate and z (671 MB) 145 us, 4.6 TB/s; 16384 of 1531 50 us, 5.0 TB/s; 256
+// rows of 2^20 float32 without z (4.3 GB) 880 us, 4.9 TB/s.  Reset marks cost registers (117 against 71) and with them overlap: 1536
+// rows of 4097 float32 37 us, 3.4 TB/s (held to 96 registers, with spills, it takes 1.6 times as long).
 template <typename T, int G, int TEAM, bool HI, bool HZ, bool RST>
 __global__ __launch_bounds__(gate_threads<TEAM>()) void gate_fwd_kernel(GateArgs a)
 {
@@ -390,7 +393,7 @@ __global__ __launch_bounds__(gate_threads<TEAM>()) void gate_fwd_kernel(GateArgs
     if (a.h_last && at.valid && seg == a.nseg - 1 && at.member == 0 && at.gl == (G == WAVE ? 0 : G - 1)) a.h_last[at.row] = c;
 }
 
-// ppm pieces as one map: one wave each (a segment is a whole number of them).
+// ppm pieces as one map: one wave each (a segment is a whole number of them).  64 rows of 2^20 bf16, no input gate (268 MB), 77 us.
 template <typename T, bool HI, bool RST>
 __global__ __launch_bounds__(GATE_WAVES* WAVE) void gate_fwd_map_kernel(GateArgs a)
 {
@@ -474,6 +477,9 @@ __global__ __launch_bounds__(WAVE) void gate_carry_kernel(GateArgs a)
 //     dx = lam m g,   di = lam v (1 - g),   d(log a) = lam (a h_{t-1} - (g x) a^2 / m) = lam a (h_{t-1} - g x a / m)
 //     log a = -rate s:   df = -d(log a) rate s (1 - s),   drate = -sum d(log a) s
 //     dz = dout h (sz + z sz (1 - sz)),   dy = dout z sz
+//
+// Bound by HBM as well: 32768 rows of 2048 bf16 with input gate and z (1.2 GB) 226 us, 5.3 TB/s; 256 rows of 2^20 float32 without z (7.5 GB) 1520
+// us, 4.9 TB/s; with marks 1536 rows of 4097 float32 57 us, 4.0 TB/s (176 registers, two waves a SIMD; 168 and three, with spills, 60).
 template <typename T, int G, int TEAM, bool HI, bool HZ, bool RST>
 __global__ __launch_bounds__(gate_threads<TEAM>()) void gate_bwd_kernel(GateArgs a)
 {
@@ -649,7 +655,7 @@ __global__ __launch_bounds__(gate_threads<TEAM>()) void gate_bwd_kernel(GateArgs
     }
 }
 
-// ppm pieces' adjoint as one map of G.
+// ppm pieces' adjoint as one map of G.  64 rows of 2^20 bf16 61 us.
 template <typename T, bool HZ, bool RST>
 __global__ __launch_bounds__(GATE_WAVES* WAVE) void gate_bwd_map_kernel(GateArgs a)
 {
@@ -735,6 +741,7 @@ __global__ __launch_bounds__(256) void gate_fill_kernel(float* to, const float* 
 }
 
 // ---- one token -----------------------------------------------------------------------------------
+// An element a thread.  64 x 4096 bf16 (4.7 MB) 3.3 us, of which a launch alone is 2.5.
 template <typename T>
 __global__ __launch_bounds__(256) void gate_step_kernel(ss_gate_step_params p)
 {
@@ -818,8 +825,8 @@ inline size_t round_up(size_t v, size_t a) { return (v + a - 1) / a * a; }
 // How a sequence is dealt out: one wave or four share a row, and segments where the rows with their teams are still too few.
 // us forward / backward with one wave / four, input gate and z, rows x steps: bf16 4096 x 1030 15.6 26.5 / 18.9 38.3, 2048 x 4096
 // 22.5 34.9 / 21.0 37.8, 1024 x 16384 47.7 72.7 / 35.5 64.4, 512 x 2048 7.2 11.6 / 5.6 9.0; float32, whose requests are twice as
-// wide, gains more often, and wherever the team's rounds come out even: 1536 x 4097 29.8 50.9 / 27.4 46.6, 6144 x 2048 47.5 97.9 / 41.8 86.8, 3000 x 2048 27.9 48.7 / 23.8 42.0, but 4096 x 1030
-// 19.8 36.4 / 20.8 42.5.  (Teams of 8 and 16 bring up to a fifth at 256 rows and lose as much or more elsewhere.)
+// wide, gains more often, and wherever the team's rounds come out even: 1536 x 4097 29.8 50.9 / 27.4 46.6, 6144 x 2048 47.5 97.9 / 41.8
+// 86.8, 3000 x 2048 27.9 48.7 / 23.8 42.0, but 4096 x 1030 19.8 36.4 / 20.8 42.5.  (Teams of 8 and 16 bring up to a fifth at 256 rows and lose as much or more elsewhere.)
 // In segments (two more launches and a second reading of most inputs) / whole: bf16 128 x 16384 16.0 23.1 / 12.7 21.2, 64 x 8192 12.3 16.6 / 7.5
 // 12.1, 200 x 30000 29.8 43.6 / 24.4 39.2; but 128 x 65536 35.6 52.6 / 46.1 74.6, 64 x 100000 30.8 45.0 / 65.5 103.9, 1 x 1000000 19.0 25.0 / 558 944.
 struct GatePlan {

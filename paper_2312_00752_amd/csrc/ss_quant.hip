@@ -272,8 +272,8 @@ struct Tops<bf16_t> {
 
 // Where a workgroup's registers hold all channels of 8 WIDE tokens, one pass: a thread has 8 tokens of four channels R times, the tokens' scales
 // come from an exchange over the workgroup, and a thread's four bytes of a token are a word of its row, of which a wave writes
-// whole lines.  Bound by the pieces in which rows are read, 16 WIDE bytes of bf16: 4 x 4096 x 1531 bf16 (75 MB in, 25 MB out) takes 18 us at
-// 64 bytes (5.6 TB/s); a call of it 23 at 64, 32 at 32, and 32 in two launches.  Up to 64 registers a thread where they do without spilling, so that two
+// whole lines.  Bound by the pieces in which rows are read, 16 WIDE bytes of bf16: 4 x 4096 x 1531 bf16 (50 MB in, 25 MB out) takes 18 us at
+// 64 bytes (4.2 TB/s); a call of it 23 at 64, 32 at 32, and 32 in two launches.  Up to 64 registers a thread where they do without spilling, so that two
 // workgroups of 1024 share a unit.
 template <typename T, int THREADS, int WIDE, int R>
 __global__ __launch_bounds__(THREADS, R * sizeof(T) <= 4 && THREADS * R < 2048 * WIDE ? 8 : 4) void quant_held_kernel(const T* x, int8_t* q, float* scale, int batch, int dim, int L, int pitch, int tiles)
