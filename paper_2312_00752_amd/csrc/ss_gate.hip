@@ -204,17 +204,6 @@ __device__ __forceinline__ uint2 marks_settle(uint2 m, int t0, int L)
     const uint64_t w = s < 64 ? ((uint64_t(m.y) << 32) | m.x) >> s : 0;
     return make_uint2((uint32_t)w, (uint32_t)(w >> 32));
 }
-// f with true where a lane of the wave has a mark, else with false: most pieces have none, and do without the selects
-template <bool RST, typename F>
-__device__ __forceinline__ void with_marks(bool any, F f)
-{
-    if constexpr (RST) {
-        if (any) f(std::true_type{});
-        else f(std::false_type{});
-    } else {
-        f(std::false_type{});
-    }
-}
 __device__ __forceinline__ bool marked(uint2 m, int j) { return ((j < 4 ? m.x : m.y) & (0xffu << (8 * (j & 3)))) != 0; }
 
 // ---- the gates of one step ------------------------------------------------------------------
@@ -322,8 +311,9 @@ __device__ __forceinline__ void slice_map(const float (&av)[8], const float (&bv
 template <int TEAM> constexpr int gate_threads() { return (TEAM > 1 ? TEAM : GATE_WAVES) * WAVE; }
 
 // Bound by HBM on full grids: 32768 rows of 2048 bf16 with input gate and z (671 MB) 145 us, 4.6 TB/s; 16384 of 1531 50 us, 5.0 TB/s; 256
-// rows of 2^20 float32 without z (4.3 GB) 880 us, 4.9 TB/s.  Reset marks cost registers (117 against 71) and with them overlap: 1536
-// rows of 4097 float32 37 us, 3.4 TB/s (held to 96 registers, with spills, it takes 1.6 times as long).
+// rows of 2^20 float32 without z (4.3 GB) 880 us, 4.9 TB/s.  With reset marks 1536
+// rows of 4097 float32 35 us, 3.6 TB/s: 4097 steps are nine pieces, three rounds of a team of four.  (Marks are selects in every step; a second path
+// without them for waves that have no mark took 117 registers instead of 77, and 37 us.)
 template <typename T, int G, int TEAM, bool HI, bool HZ, bool RST>
 __global__ __launch_bounds__(gate_threads<TEAM>()) void gate_fwd_kernel(GateArgs a)
 {
@@ -363,30 +353,23 @@ __global__ __launch_bounds__(gate_threads<TEAM>()) void gate_fwd_kernel(GateArgs
             if constexpr (HZ) at.template settle<T>(rz, t0, a.L);
         }
         if constexpr (RST) r.m = marks_settle(r.m, t0, a.L);
-        const bool any = RST && __any((r.m.x | r.m.y) != 0u);
         LaneScan<G, false> lanes;
         float A, B;
-        with_marks<RST>(any, [&](auto marks) {
-            constexpr bool S = decltype(marks)::value;
-            steps_of<T, HI, S>(r, ch, n, av, bv);
-            if constexpr (HZ) io8<T>::unpack(rz, zv);
-            if (q + TEAM < p1) load(min(p + TEAM, a.pieces - 1));
-            slice_map<S>(av, bv, A, B);
-            lanes.template scan<S>(A, B, at.lane);
-            if constexpr (TEAM > 1) lanes.template whole<S>(A, B);
-        });
+        steps_of<T, HI, RST>(r, ch, n, av, bv);
+        if constexpr (HZ) io8<T>::unpack(rz, zv);
+        if (q + TEAM < p1) load(min(p + TEAM, a.pieces - 1));
+        slice_map<RST>(av, bv, A, B);
+        lanes.template scan<RST>(A, B, at.lane);
+        if constexpr (TEAM > 1) lanes.template whole<RST>(A, B);
         float own = c;
         if constexpr (TEAM > 1) own = team(A, B, c, at.member, at.lane);
         if (a.ckpt && at.valid && at.gl == 0 && p < p1) a.ckpt[(int64_t)p * a.R + at.row] = own;
-        with_marks<RST>(any, [&](auto marks) {
-            constexpr bool S = decltype(marks)::value;
-            float h = lanes.template apply<S>(own, at.lane);
+        float h = lanes.template apply<RST>(own, at.lane);
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                h = affine_of<S>(av[j], bv[j], h);
-                y[j] = HZ ? h * zv[j] * gate_sigmoid(zv[j]) : h;
-            }
-        });
+        for (int j = 0; j < 8; ++j) {
+            h = affine_of<RST>(av[j], bv[j], h);
+            y[j] = HZ ? h * zv[j] * gate_sigmoid(zv[j]) : h;
+        }
         if constexpr (TEAM == 1) c = own;
         if (at.valid) slice_store<T>(out, t0, n, y);
     }
@@ -479,7 +462,7 @@ __global__ __launch_bounds__(WAVE) void gate_carry_kernel(GateArgs a)
 //     dz = dout h (sz + z sz (1 - sz)),   dy = dout z sz
 //
 // Bound by HBM as well: 32768 rows of 2048 bf16 with input gate and z (1.2 GB) 226 us, 5.3 TB/s; 256 rows of 2^20 float32 without z (7.5 GB) 1520
-// us, 4.9 TB/s; with marks 1536 rows of 4097 float32 57 us, 4.0 TB/s (176 registers, two waves a SIMD; 168 and three, with spills, 60).
+// us, 4.9 TB/s; with marks 1536 rows of 4097 float32 51 us, 4.4 TB/s (two paths: 176 registers, two waves a SIMD instead of three, 57).
 template <typename T, int G, int TEAM, bool HI, bool HZ, bool RST>
 __global__ __launch_bounds__(gate_threads<TEAM>()) void gate_bwd_kernel(GateArgs a)
 {
@@ -521,7 +504,6 @@ __global__ __launch_bounds__(gate_threads<TEAM>()) void gate_bwd_kernel(GateArgs
         float start = a.ckpt[(int64_t)min(p, a.pieces - 1) * a.R + at.row];
         float av[8], bv[8], sv[8], gx[8], gv[8], iq[8], hp[8], dy[8], o[8], zv[8];   // iq: 1 / m
         const uint2 marks = RST ? marks_settle(r.m, t0, a.L) : r.m;
-        const bool any = RST && __any((marks.x | marks.y) != 0u);
         if (!at.whole) {
             at.template settle<T>(r.x, t0, a.L);
             at.template settle<T>(r.f, t0, a.L);
@@ -531,89 +513,83 @@ __global__ __launch_bounds__(gate_threads<TEAM>()) void gate_bwd_kernel(GateArgs
         }
         LaneScan<G, true> back;
         float A, B;
-        with_marks<RST>(any, [&](auto have) {
-            constexpr bool S = decltype(have)::value;
-            {
-                float xv[8], fv[8], ivv[8];
-                io8<T>::unpack(r.x, xv);
-                io8<T>::unpack(r.f, fv);
-                io8<T>::unpack(rd, dy);
-                if constexpr (HI) io8<T>::unpack(r.i, ivv);
-                if constexpr (HZ) io8<T>::unpack(rz, zv);
-                if (q > p0) load(p - TEAM);
-#pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    const bool in = j < n, mk = S && marked(marks, j);
-                    const float s = gate_sigmoid(fv[j] + ch.f_bias);
-                    const float aa = exp2_fast(k * s);
-                    const float m2 = one_minus_square(rate2 * s, aa);
-                    float rm = __builtin_amdgcn_rsqf(m2);
-                    rm = m2 == 0.0f ? 0.0f : rm;
-                    const float g = HI ? gate_sigmoid(ivv[j] + ch.i_bias) : 1.0f;
-                    const float m = mk ? 1.0f : m2 * rm;
-                    sv[j] = s;
-                    gv[j] = g;
-                    iq[j] = rm;
-                    gx[j] = in ? g * xv[j] : 0.0f;
-                    av[j] = in ? (mk ? -1.0f : aa) : 1.0f;
-                    bv[j] = in ? m * gx[j] : 0.0f;
-                    dy[j] = in ? dy[j] : 0.0f;
-                }
-            }
-            slice_map<S>(av, bv, A, B);
-            LaneScan<G, false> lanes;
-            lanes.template scan<S>(A, B, at.lane);
-            float h = lanes.template apply<S>(start, at.lane);
+        {
+            float xv[8], fv[8], ivv[8];
+            io8<T>::unpack(r.x, xv);
+            io8<T>::unpack(r.f, fv);
+            io8<T>::unpack(rd, dy);
+            if constexpr (HI) io8<T>::unpack(r.i, ivv);
+            if constexpr (HZ) io8<T>::unpack(rz, zv);
+            if (q > p0) load(p - TEAM);
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-                hp[j] = h;
-                h = affine_of<S>(av[j], bv[j], h);
-                if constexpr (HZ) {
-                    const float sz = gate_sigmoid(zv[j]);
-                    o[j] = dy[j] * h * fmaf(zv[j] * sz, 1.0f - sz, sz);
-                    dy[j] = j < n ? dy[j] * zv[j] * sz : 0.0f;
-                }
+                const bool in = j < n, mk = RST && marked(marks, j);
+                const float s = gate_sigmoid(fv[j] + ch.f_bias);
+                const float aa = exp2_fast(k * s);
+                const float m2 = one_minus_square(rate2 * s, aa);
+                float rm = __builtin_amdgcn_rsqf(m2);
+                rm = m2 == 0.0f ? 0.0f : rm;
+                const float g = HI ? gate_sigmoid(ivv[j] + ch.i_bias) : 1.0f;
+                const float m = mk ? 1.0f : m2 * rm;
+                sv[j] = s;
+                gv[j] = g;
+                iq[j] = rm;
+                gx[j] = in ? g * xv[j] : 0.0f;
+                av[j] = in ? (mk ? -1.0f : aa) : 1.0f;
+                bv[j] = in ? m * gx[j] : 0.0f;
+                dy[j] = in ? dy[j] : 0.0f;
             }
-            // G of the slice as one map, from its last step to its first: G_t = a (dy + G_{t+1}), 0 at a reset
-            A = 1.0f;
-            B = 0.0f;
+        }
+        slice_map<RST>(av, bv, A, B);
+        LaneScan<G, false> lanes;
+        lanes.template scan<RST>(A, B, at.lane);
+        float h = lanes.template apply<RST>(start, at.lane);
 #pragma unroll
-            for (int j = 7; j >= 0; --j) {
-                float A1 = av[j], B1 = av[j] * dy[j];
-                if (S && A1 < 0.0f) B1 = 0.0f;
-                affine_after<S>(A1, B1, A, B);
-                A = A1;
-                B = B1;
+        for (int j = 0; j < 8; ++j) {
+            hp[j] = h;
+            h = affine_of<RST>(av[j], bv[j], h);
+            if constexpr (HZ) {
+                const float sz = gate_sigmoid(zv[j]);
+                o[j] = dy[j] * h * fmaf(zv[j] * sz, 1.0f - sz, sz);
+                dy[j] = j < n ? dy[j] * zv[j] * sz : 0.0f;
             }
-            back.template scan<S>(A, B, at.lane);
-            if constexpr (TEAM > 1) back.template whole<S>(A, B);
-        });
+        }
+        // G of the slice as one map, from its last step to its first: G_t = a (dy + G_{t+1}), 0 at a reset
+        A = 1.0f;
+        B = 0.0f;
+#pragma unroll
+        for (int j = 7; j >= 0; --j) {
+            float A1 = av[j], B1 = av[j] * dy[j];
+            if (RST && A1 < 0.0f) B1 = 0.0f;
+            affine_after<RST>(A1, B1, A, B);
+            A = A1;
+            B = B1;
+        }
+        back.template scan<RST>(A, B, at.lane);
+        if constexpr (TEAM > 1) back.template whole<RST>(A, B);
         if constexpr (HZ)
             if (at.valid) slice_store<T>(dz, t0, n, o);
         float own = c;
         if constexpr (TEAM > 1) own = team(A, B, c, at.member, at.lane);
         float sq = 0.0f, sf = 0.0f, si = 0.0f;
         float gz[8], o2[8];
-        with_marks<RST>(any, [&](auto have) {
-            constexpr bool S = decltype(have)::value;
-            float gn = back.template apply<S>(own, at.lane);
+        float gn = back.template apply<RST>(own, at.lane);
 #pragma unroll
-            for (int j = 7; j >= 0; --j) {
-                const bool in = j < n, mk = S && av[j] < 0.0f;
-                const float lam = dy[j] + gn;
-                const float m = mk ? 1.0f : (iq[j] == 0.0f ? 0.0f : rcp_fast(iq[j]));
-                gz[j] = lam * m * gv[j];                      // dx
-                if constexpr (HI) {
-                    o[j] = in ? lam * bv[j] * (1.0f - gv[j]) : 0.0f;
-                    si += o[j];
-                }
-                const float dr = mk || !in ? 0.0f : lam * av[j] * (hp[j] - gx[j] * av[j] * iq[j]) * sv[j];
-                sq -= dr;
-                o2[j] = -ch.rate * dr * (1.0f - sv[j]);
-                sf += o2[j];
-                gn = mk ? 0.0f : (in ? av[j] * lam : gn);
+        for (int j = 7; j >= 0; --j) {
+            const bool in = j < n, mk = RST && av[j] < 0.0f;
+            const float lam = dy[j] + gn;
+            const float m = mk ? 1.0f : (iq[j] == 0.0f ? 0.0f : rcp_fast(iq[j]));
+            gz[j] = lam * m * gv[j];                      // dx
+            if constexpr (HI) {
+                o[j] = in ? lam * bv[j] * (1.0f - gv[j]) : 0.0f;
+                si += o[j];
             }
-        });
+            const float dr = mk || !in ? 0.0f : lam * av[j] * (hp[j] - gx[j] * av[j] * iq[j]) * sv[j];
+            sq -= dr;
+            o2[j] = -ch.rate * dr * (1.0f - sv[j]);
+            sf += o2[j];
+            gn = mk ? 0.0f : (in ? av[j] * lam : gn);
+        }
         if constexpr (TEAM == 1) c = own;
         sum_q += sq;
         sum_f += sf;
