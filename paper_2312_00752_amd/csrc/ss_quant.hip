@@ -743,6 +743,8 @@ struct QuantSizes {
     int batch, L, dim, pitch;
     int chunks;   // of channels, sequence last
 };
+constexpr int64_t MOST_THREADS = 0x7fffffff;   // of a launch (its limit is 2^32)
+
 // One pass over tokens with the sequence last, where that is faster.  us, not in a cache, one pass / two: bf16, 70, 1000, 4100 and 16384 tokens of
 // 2048 channels 4.7 7.0 9.8 34.2 / 9.7 13.7 17.3 33.3, of 4096 9.5 9.8 21.1 58.4 / 10.2 15.1 27.5 71.3; 1000 of 5120 11.8 / 16.6; float32 of
 // 2048 8.7 8.8 15.4 38.4 / 9.2 13.8 23.7 55.2, of 4096 11.6 11.4 27.7 89.7 / 9.5 15.9 35.2 114; but 4100 of 5120 31.4 / 31.7 (float32 45.4 / 41.3) and
@@ -757,6 +759,7 @@ bool quant_held(const QuantSizes& z, const T* x, int8_t* q, float* scale, hipStr
         constexpr int THREADS = decltype(threads)::value, WIDE = decltype(wide)::value, R = decltype(r)::value;
         if (z.pitch > 4 * (THREADS / WIDE) * R) return false;
         const int tiles = (z.L + 8 * WIDE - 1) / (8 * WIDE);
+        if ((int64_t)tiles * z.batch * THREADS > MOST_THREADS) return false;
         hipLaunchKernelGGL((quant_held_kernel<T, THREADS, WIDE, R>), dim3((unsigned)(tiles * z.batch)), dim3(THREADS), 0, st, x, q, scale, z.batch, z.dim, z.L,
                            z.pitch, tiles);
         return true;
@@ -789,10 +792,17 @@ void quant_launch(const QuantSizes& z, bool seq_last, const void* xv, int8_t* q,
         return;
     }
     const int rows = z.batch * z.L;
+    // f(first row, rows) for as many rows at a time as a launch has threads for
+    auto in_parts = [&](int lanes, auto f) {
+        const int most = (int)(MOST_THREADS / lanes / 4 * 4);
+        for (int r = 0; r < rows; r += min(most, rows - r)) f(r, min(most, rows - r));
+    };
     auto go = [&](auto g, auto v) {
         constexpr int G = decltype(g)::value, V = decltype(v)::value, SIDE = (G > 256 ? G : 256) / G;
-        hipLaunchKernelGGL((quant_rows_kernel<T, G, V>), dim3((unsigned)((rows + SIDE - 1) / SIDE)), dim3(G > 256 ? G : 256), 0, st, x, q, scale, rows, z.dim,
-                           z.pitch);
+        in_parts(G, [&](int r, int n) {
+            hipLaunchKernelGGL((quant_rows_kernel<T, G, V>), dim3((unsigned)((n + SIDE - 1) / SIDE)), dim3(G > 256 ? G : 256), 0, st, x + (int64_t)r * z.dim,
+                               q + (int64_t)r * z.pitch, scale + r, n, z.dim, z.pitch);
+        });
     };
     typedef std::integral_constant<int, 1> one;
     typedef std::integral_constant<int, 2> two;
@@ -805,7 +815,9 @@ void quant_launch(const QuantSizes& z, bool seq_last, const void* xv, int8_t* q,
     else if (z.pitch <= 4096) go(std::integral_constant<int, 256>{}, two{});
     else if (z.pitch <= 8192) go(std::integral_constant<int, 256>{}, four{});
     else if (z.pitch <= 16384) go(std::integral_constant<int, 1024>{}, two{});
-    else hipLaunchKernelGGL(quant_rows_wide_kernel<T>, dim3((unsigned)rows), dim3(1024), 0, st, x, q, scale, z.dim, z.pitch);
+    else in_parts(1024, [&](int r, int n) {
+        hipLaunchKernelGGL(quant_rows_wide_kernel<T>, dim3((unsigned)n), dim3(1024), 0, st, x + (int64_t)r * z.dim, q + (int64_t)r * z.pitch, scale + r, z.dim, z.pitch);
+    });
 }
 
 }  // namespace ss

@@ -70,3 +70,29 @@ def test_bytes_of_elementary_operations(dim):
     want = torch.round(x * (127.0 / x.abs().amax(-1, keepdim=True)))[0].to(torch.int8)
     for t, last in ((x, False), (x.transpose(1, 2).contiguous(), True)):
         assert torch.equal(B.ss_quant_rows(t, seq_last=last)[0][:, :dim], want)
+
+
+def test_more_rows_than_threads():
+    """70 million tokens: offsets past 32 bits, and more threads than one launch may have, in either order."""
+    n = 70_000_000
+    few = torch.randn(8, 1000, device="cuda").bfloat16()
+    last = torch.zeros(1, 8, n, dtype=torch.bfloat16, device="cuda")
+    places = torch.cat((torch.arange(500), torch.arange(n - 500, n))).cuda()
+    last[0][:, places] = few
+    want = B.ss_quant_rows(few[None].contiguous(), seq_last=True)
+    assert torch.equal(want[0][:, :8], B.ss_quant_rows(few.t().contiguous())[0][:, :8])
+    for x, seq_last in ((last, True), (last[0].t().contiguous(), False)):
+        q, s = B.ss_quant_rows(x, seq_last=seq_last)
+        assert torch.equal(q[places], want[0]) and torch.equal(s[places], want[1])
+        assert not s[500:n - 500].any() and not q[34_000_000:36_000_000].any()
+        del q, s
+
+
+@pytest.mark.parametrize("io", ["f32", "bf16"])
+def test_rows_off_a_word(io):
+    """Tokens' tensors that start one element into their memory."""
+    for dim, tokens in ((40, 33), (2100, 100), (4000, 4100)):
+        x = torch.randn(1, dim, tokens, device="cuda").to(u.TYPES[io])
+        off = torch.empty(x.numel() + 1, dtype=x.dtype, device="cuda")[1:].view(x.shape).copy_(x)
+        for a, b in zip(B.ss_quant_rows(x, seq_last=True), B.ss_quant_rows(off, seq_last=True)):
+            assert torch.equal(a, b)
