@@ -858,6 +858,7 @@ int check_gate(const ss_gate_params* p, bool for_bwd)
     const bool hi = p->flags & SS_GATE_HAS_I, hz = p->flags & SS_GATE_HAS_Z;
     if ((p->flags & SS_GATE_HAS_I_BIAS) && !hi) return SS_ERR_UNSUPPORTED;
     if ((long)p->batch * p->dim >= 0x7fffffffL || p->seqlen > 0x7fffffff - 2 * ss::GATE_PIECE) return SS_ERR_UNSUPPORTED;
+    if ((int64_t)p->batch * p->dim * ss::lanes_for(p->seqlen) > 0xffffffffL - 65536) return SS_ERR_UNSUPPORTED;   // a launch has fewer than 2^32 threads
     const bool empty = p->seqlen == 0;
     if (!empty && (!p->x || !p->f || (hi && !p->i) || (hz && !p->z) || (!for_bwd && !p->out))) return SS_ERR_NULL;
     if (!p->rate || ((p->flags & SS_GATE_HAS_F_BIAS) && !p->f_bias) || ((p->flags & SS_GATE_HAS_I_BIAS) && !p->i_bias)) return SS_ERR_NULL;

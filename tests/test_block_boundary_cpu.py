@@ -192,3 +192,9 @@ def test_headers_stand_alone(name, tmp_path):
     src = tmp_path / "h.c"
     src.write_text("#include \"%s\"\n%s p;\n" % (header, name))
     subprocess.run(["gcc", "-std=c99", "-Wall", "-Werror", "-fsyntax-only", "-I", os.path.join(ROOT, "include"), str(src)], check=True)
+
+
+def test_gate_rows_of_one_launch():
+    big = lambda dim, seqlen: dict(batch=1 << 13, dim=dim, seqlen=seqlen, x_batch=dim * seqlen, f_batch=dim * seqlen, i_batch=dim * seqlen, z_batch=dim * seqlen)
+    expect(B.lib().ss_gate_fwd, gate, [big(1 << 13, 200), big(1 << 15, 128), big(1 << 17, 9)], B.SS_ERR_UNSUPPORTED)
+    expect(B.lib().ss_gate_fwd, gate, [dict(workspace=None, **big((1 << 13) - 64, 200))], B.SS_ERR_WORKSPACE)
