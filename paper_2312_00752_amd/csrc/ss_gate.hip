@@ -311,10 +311,13 @@ __device__ __forceinline__ void slice_map(const float (&av)[8], const float (&bv
 template <int TEAM> constexpr int gate_threads() { return (TEAM > 1 ? TEAM : GATE_WAVES) * WAVE; }
 
 // Bound by HBM on full grids: 32768 rows of 2048 bf16 with input gate and z (671 MB) 145 us, 4.6 TB/s; 16384 of 1531 50 us, 5.0 TB/s; 256
-// rows of 2^20 float32 without z (4.3 GB) 880 us, 4.9 TB/s.  With reset marks 1536
+// rows of 2^20 float32 without z (4.3 GB) 860 us, 5.0 TB/s.  With reset marks 1536
 // rows of 4097 float32 35 us, 3.6 TB/s: 4097 steps are nine pieces, three rounds of a team of four.  (Marks are selects in every step; a second path
 // without them for waves that have no mark took 117 registers instead of 77, and 37 us.)
-template <typename T, int G, int TEAM, bool HI, bool HZ, bool RST>
+//
+// AHEAD: rounds whose inputs have been requested while one is worked on.  Two where a SIMD has but one or two waves: 256 rows of 243260 float32
+// 357 us with one, 268 with two, bf16 199 / 182, 384 of 100182 197 / 178 and 113 / 109; but 700 of 9000 bf16 18.3 / 20.1, 1024 of 16384 32.7 / 35.4.
+template <typename T, int G, int TEAM, int AHEAD, bool HI, bool HZ, bool RST>
 __global__ __launch_bounds__(gate_threads<TEAM>()) void gate_fwd_kernel(GateArgs a)
 {
     const Place<G, TEAM> at(a);
@@ -331,9 +334,14 @@ __global__ __launch_bounds__(gate_threads<TEAM>()) void gate_fwd_kernel(GateArgs
     __shared__ float2 maps[2][TEAM];
     TeamScan<TEAM, false, RST> team{maps};
 
-    fwd_raw<T, HI> r;
-    typename io8<T>::raw rz;
-    auto load = [&](int p) {
+    struct Request {
+        fwd_raw<T, HI> r;
+        typename io8<T>::raw rz;
+    };
+    Request req[AHEAD];
+    auto load = [&](int p, Request& to) {
+        auto& r = to.r;
+        auto& rz = to.rz;
         const int t0 = p * GATE_PIECE + at.gl * LANE_STEPS;
         r.x = at.template request<T>(x, t0, a.L);
         r.f = at.template request<T>(f, t0, a.L);
@@ -342,8 +350,9 @@ __global__ __launch_bounds__(gate_threads<TEAM>()) void gate_fwd_kernel(GateArgs
         if constexpr (RST) r.m = marks_request<G == 4>(reset, t0, a.L);
     };
     // a team's members that have no piece left take part with maps that change nothing
-    load(min(p0 + at.member, a.pieces - 1));
-    for (int q = p0; q < p1; q += TEAM) {
+    auto round = [&](int q, Request& now) {
+        auto& r = now.r;
+        auto& rz = now.rz;
         const int p = q + at.member, t0 = p * GATE_PIECE + at.gl * LANE_STEPS, n = p < p1 ? a.L - t0 : 0;
         float av[8], bv[8], zv[8], y[8];
         if (!at.whole) {
@@ -357,7 +366,7 @@ __global__ __launch_bounds__(gate_threads<TEAM>()) void gate_fwd_kernel(GateArgs
         float A, B;
         steps_of<T, HI, RST>(r, ch, n, av, bv);
         if constexpr (HZ) io8<T>::unpack(rz, zv);
-        if (q + TEAM < p1) load(min(p + TEAM, a.pieces - 1));
+        if (q + AHEAD * TEAM < p1) load(min(p + AHEAD * TEAM, a.pieces - 1), now);
         slice_map<RST>(av, bv, A, B);
         lanes.template scan<RST>(A, B, at.lane);
         if constexpr (TEAM > 1) lanes.template whole<RST>(A, B);
@@ -372,6 +381,16 @@ __global__ __launch_bounds__(gate_threads<TEAM>()) void gate_fwd_kernel(GateArgs
         }
         if constexpr (TEAM == 1) c = own;
         if (at.valid) slice_store<T>(out, t0, n, y);
+    };
+#pragma unroll
+    for (int k = 0; k < AHEAD; ++k)
+        if (k == 0 || p0 + k * TEAM < p1) load(min(p0 + k * TEAM + at.member, a.pieces - 1), req[k]);
+    for (int q = p0; q < p1; q += AHEAD * TEAM) {
+        round(q, req[0]);
+        if constexpr (AHEAD == 2) {
+            if (q + TEAM >= p1) break;
+            round(q + TEAM, req[1]);
+        }
     }
     if (a.h_last && at.valid && seg == a.nseg - 1 && at.member == 0 && at.gl == (G == WAVE ? 0 : G - 1)) a.h_last[at.row] = c;
 }
@@ -754,14 +773,14 @@ void with_flags(unsigned flags, F f)
 // Lanes of a row: all 64 from 128 steps on; below, as many as a power of four (one piece then holds the row)
 int lanes_for(int L) { return L > 16 * LANE_STEPS ? WAVE : (L > 4 * LANE_STEPS ? 16 : 4); }
 
-template <typename T, int G, int TEAM>
+template <typename T, int G, int TEAM, int AHEAD>
 void launch_main(const GateArgs& a, bool bwd, hipStream_t st)
 {
     const int rows = TEAM > 1 ? 1 : GATE_WAVES * (WAVE / G);
     const dim3 grid((unsigned)((a.R + rows - 1) / rows), (unsigned)a.nseg), block(gate_threads<TEAM>());
     with_flags(a.flags, [&](auto i, auto z, auto rst) {
         if (bwd) hipLaunchKernelGGL((gate_bwd_kernel<T, G, TEAM, decltype(i)::value, decltype(z)::value, decltype(rst)::value>), grid, block, 0, st, a);
-        else hipLaunchKernelGGL((gate_fwd_kernel<T, G, TEAM, decltype(i)::value, decltype(z)::value, decltype(rst)::value>), grid, block, 0, st, a);
+        else hipLaunchKernelGGL((gate_fwd_kernel<T, G, TEAM, AHEAD, decltype(i)::value, decltype(z)::value, decltype(rst)::value>), grid, block, 0, st, a);
     });
 }
 template <typename T>
@@ -781,10 +800,11 @@ void launch_all(const GateArgs& a, int team, bool bwd, hipStream_t st)
         });
     }
     const int g = lanes_for(a.L);
-    if (g == 4) launch_main<T, 4, 1>(a, bwd, st);
-    else if (g == 16) launch_main<T, 16, 1>(a, bwd, st);
-    else if (team == 1) launch_main<T, WAVE, 1>(a, bwd, st);
-    else launch_main<T, WAVE, 4>(a, bwd, st);
+    if (g == 4) launch_main<T, 4, 1, 1>(a, bwd, st);
+    else if (g == 16) launch_main<T, 16, 1, 1>(a, bwd, st);
+    else if (team == 1) launch_main<T, WAVE, 1, 1>(a, bwd, st);
+    else if (!bwd && (int64_t)a.R * a.nseg < 512) launch_main<T, WAVE, 4, 2>(a, bwd, st);
+    else launch_main<T, WAVE, 4, 1>(a, bwd, st);
 }
 
 }  // namespace ss

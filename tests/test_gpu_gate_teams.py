@@ -23,3 +23,11 @@ def test_one_long_row():
 def test_many_resets(reset):
     check(1, 6, 20000, "f32", reset=reset, h0=True)
     check(1, 1030, 2000, "bf16", reset=reset, h0=True)
+
+
+@pytest.mark.parametrize("io", ["f32", "bf16"])
+@pytest.mark.parametrize("rows", [3, 511, 512])
+def test_rounds(rows, io):
+    """One round of a team's pieces and more, even and odd numbers of them, whole and not: two are requested ahead below 512 rows."""
+    for nl in (1025, 2048, 2049, 4095, 4096, 4097, 6144, 8193):
+        check(1, rows, nl, io, seed=nl, h0=True, reset=0.001 if nl % 2 else 0.0)
