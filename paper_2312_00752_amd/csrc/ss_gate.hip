@@ -605,7 +605,8 @@ __global__ __launch_bounds__(gate_threads<TEAM>()) void gate_bwd_kernel(GateArgs
             }
             const float dr = mk || !in ? 0.0f : lam * av[j] * (hp[j] - gx[j] * av[j] * iq[j]) * sv[j];
             sq -= dr;
-            o2[j] = -ch.rate * dr * (1.0f - sv[j]);
+            // not by way of dr = 0: sv is NaN where f is, behind the row or at a mark
+            o2[j] = mk || !in ? 0.0f : -ch.rate * dr * (1.0f - sv[j]);
             sf += o2[j];
             gn = mk ? 0.0f : (in ? av[j] * lam : gn);
         }
