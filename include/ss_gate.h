@@ -87,7 +87,8 @@ typedef struct {
 } ss_gate_bwd_params;
 
 /* Gradient of <out, dout> + <h_last, dh_last>.  The states are recomputed from the checkpoints.
- * Where m_t is 0 (rate or s_t is 0) its derivative, which has no finite value, counts as 0.
+ * Where m_t is 0 (rate or s_t is 0) its derivative, which has no finite value, counts as 0.  m_t counts as 0,
+ * forward and backward, where 1 - a_t^2 is below the least normal number, 2^-126.
  * Deterministic. */
 int ss_gate_bwd(const ss_gate_bwd_params *p, void *stream);
 

@@ -27,6 +27,9 @@ constexpr int LANE_STEPS = 8;                       // steps of one lane
 constexpr int GATE_PIECE = WAVE * LANE_STEPS;       // steps of a whole wave: the distance of the checkpoints
 constexpr int GATE_WAVES = 4;                  // waves of a workgroup where each has rows of its own
 constexpr float GATE_LOG2E = 1.44269504088896340736f;
+// 2^-126, the least normal number: of anything smaller the hardware's square root is 0 and its reciprocal square root infinite, so a step
+// whose 1 - a^2 lies below it has m = 0 in every pass, and no derivative of m
+constexpr float GATE_LEAST_M2 = 0x1p-126f;
 
 struct GateArgs {
     int B, D, L, R;                            // R = B D rows
@@ -547,7 +550,7 @@ __global__ __launch_bounds__(gate_threads<TEAM>()) void gate_bwd_kernel(GateArgs
                 const float aa = exp2_fast(k * s);
                 const float m2 = one_minus_square(rate2 * s, aa);
                 float rm = __builtin_amdgcn_rsqf(m2);
-                rm = m2 == 0.0f ? 0.0f : rm;
+                rm = m2 < GATE_LEAST_M2 ? 0.0f : rm;
                 const float g = HI ? gate_sigmoid(ivv[j] + ch.i_bias) : 1.0f;
                 const float m = mk ? 1.0f : m2 * rm;
                 sv[j] = s;
