@@ -5,6 +5,8 @@ workspace the library filled, ``backward`` enqueues ``ss_scan_bwd`` / ``ss_layer
 arithmetic happens in the HIP kernels.  Tensors use the library's layouts (sequence axis
 last): u, delta, z (B,D,L); B, C (B,N,L) or a time-invariant (D,N) float32; A (D,N) float32.
 """
+import functools
+
 import torch
 from torch.autograd.function import once_differentiable
 
@@ -13,6 +15,37 @@ from . import binding as B
 
 def _code(t):
     return B.SS_BF16 if t.dtype == torch.bfloat16 else B.SS_F32
+
+
+class _NoGradient(torch.autograd.Function):
+    """Gradients as results of what they were computed from; differentiating them is an error."""
+
+    @staticmethod
+    def forward(ctx, grads, *sources):
+        return tuple(g.detach() for g in grads)
+
+    @staticmethod
+    def backward(ctx, *_):
+        raise RuntimeError("the gradients of this operator cannot be differentiated again")
+
+
+def last_derivative(backward):
+    """Of a backward function that computes its gradients outside of torch's graph: where a graph of them is being built, they are
+    connected to everything that they depend on through an error, so that a second derivative is refused whichever way it
+    is asked for (an error without connections is passed over where torch looks for the way to given inputs)."""
+    @functools.wraps(backward)
+    def call(ctx, *douts):
+        with torch.no_grad():
+            grads = backward(ctx, *douts)
+        sources = [t for t in (*ctx.saved_tensors, *douts) if t is not None and t.requires_grad] if torch.is_grad_enabled() else []
+        if not sources:
+            return grads
+        some = [k for k, g in enumerate(grads) if g is not None]
+        grads = list(grads)
+        for k, g in zip(some, _NoGradient.apply([grads[k] for k in some], *sources)):
+            grads[k] = g
+        return tuple(grads)
+    return call
 
 
 class _SelectiveScan(torch.autograd.Function):

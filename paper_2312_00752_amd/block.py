@@ -25,6 +25,7 @@ class _Projection(torch.autograd.Function):
         return B.ss_proj_gemm(W, h, out, trans_b=True)
 
     @staticmethod
+    @autograd.last_derivative
     def backward(ctx, dout):
         W, h = ctx.saved_tensors
         dout = dout.contiguous()
@@ -45,6 +46,7 @@ class _ProjectionBack(torch.autograd.Function):
         return B.ss_proj_gemm(y, W, out, trans_a=True, trans_b=True)
 
     @staticmethod
+    @autograd.last_derivative
     def backward(ctx, dout):
         W, y = ctx.saved_tensors
         dout = dout.contiguous()
