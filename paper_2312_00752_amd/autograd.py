@@ -8,7 +8,6 @@ last): u, delta, z (B,D,L); B, C (B,N,L) or a time-invariant (D,N) float32; A (D
 import functools
 
 import torch
-from torch.autograd.function import once_differentiable
 
 from . import binding as B
 
@@ -130,7 +129,7 @@ class _LayerNorm(torch.autograd.Function):
         return out if summed is None else (out, summed)
 
     @staticmethod
-    @once_differentiable
+    @last_derivative
     def backward(ctx, dout, dsummed=None):
         s, weight, stats = ctx.saved_tensors
         has_bias, held, eps, io = ctx.opts
@@ -161,7 +160,7 @@ class _GatedRecurrence(torch.autograd.Function):
         return (out, h_last) if return_last_state else out
 
     @staticmethod
-    @once_differentiable
+    @last_derivative
     def backward(ctx, dout, dh_last=None):
         x, f, rate, i, z, f_bias, i_bias, reset, h0, ws = ctx.saved_tensors
         g = B.ss_gate_bwd(dout.contiguous(), x, f, rate, ws, i=i, z=z, f_bias=f_bias, i_bias=i_bias, reset=reset, h0=h0,

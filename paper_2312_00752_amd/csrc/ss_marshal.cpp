@@ -619,14 +619,25 @@ PyObject* py_norm_bwd(PyObject*, PyObject* const* argv, Py_ssize_t n)
 
 // Layer norm as a node of torch's graph (what autograd._LayerNorm is in Python): the backward pass runs on the stream of the forward pass,
 // which is also the one that torch makes current for it.
-// A backward pass's gradients have no graph of their own: where one is being built, going through them again is an error.
-torch::autograd::variable_list differentiable_once(torch::autograd::variable_list grads)
+// A backward pass's gradients have no graph of their own: where one is being built, they are connected to what they depend on through
+// an error, so that going through them again is refused whichever way it is asked for.
+torch::autograd::variable_list differentiable_once(torch::autograd::variable_list grads, std::initializer_list<const torch::autograd::variable_list*> from)
 {
     if (!at::GradMode::is_enabled()) return grads;
+    torch::autograd::variable_list sources;
+    for (const auto* list : from)
+        for (const at::Tensor& t : *list)
+            if (t.defined() && t.requires_grad()) sources.push_back(t);
+    if (sources.empty()) return grads;
+    const std::shared_ptr<torch::autograd::Node> error(
+        new torch::autograd::Error("the gradients of layer_norm and gated_recurrence cannot be differentiated again", torch::autograd::collect_next_edges(sources)),
+        torch::autograd::deleteNode);
     for (at::Tensor& g : grads)
-        if (g.defined()) g = g.detach().set_requires_grad(true);
-    torch::autograd::DelayedError error("the gradients of layer_norm and gated_recurrence cannot be differentiated again", (int64_t)grads.size());
-    return error(std::move(grads));
+        if (g.defined()) {
+            g = g.detach();
+            torch::autograd::create_gradient_edge(g, error);
+        }
+    return grads;
 }
 struct NormFunction : torch::autograd::Function<NormFunction> {
     static torch::autograd::variable_list forward(torch::autograd::AutogradContext* ctx, const at::Tensor& x, const Optional& weight_, const Optional& bias_,
@@ -652,13 +663,13 @@ struct NormFunction : torch::autograd::Function<NormFunction> {
         const at::Tensor more = res && grads[1].defined() ? grads[1].contiguous() : at::Tensor();
         if (!grads[0].defined()) {   // only the sum was used
             const auto io = (at::ScalarType)ctx->saved_data["io"].toInt();
-            return differentiable_once({more.defined() ? more.to(io) : at::Tensor(), at::Tensor(), at::Tensor(), more, at::Tensor(), at::Tensor()});
+            return differentiable_once({more.defined() ? more.to(io) : at::Tensor(), at::Tensor(), at::Tensor(), more, at::Tensor(), at::Tensor()}, {&grads});
         }
         const auto saved = ctx->get_saved_variables();
         NormGrads g;
         backward_check(g.bwd(grads[0].contiguous(), saved[0], saved[2], saved[1], ctx->saved_data["bias"].toBool(), res, more,
                              ctx->saved_data["eps"].toDouble(), reinterpret_cast<void*>(ctx->saved_data["stream"].toInt())));
-        return differentiable_once({g.dx, g.dweight, g.dbias, g.dresidual, at::Tensor(), at::Tensor()});
+        return differentiable_once({g.dx, g.dweight, g.dbias, g.dresidual, at::Tensor(), at::Tensor()}, {&saved, &grads});
     }
 };
 // layer_norm(x, weight, bias, residual, eps, stream) -> (out,) or (out, summed), with gradients
@@ -889,7 +900,7 @@ struct GateFunction : torch::autograd::Function<GateFunction> {
         GateGrads g;
         backward_check(g.bwd(x, p, t[9], grads[0].contiguous(), grads.size() > 1 ? grads[1].contiguous() : at::Tensor(), t[8].defined(),
                              reinterpret_cast<void*>(ctx->saved_data["stream"].toInt())));
-        return differentiable_once({g.dx, g.df, g.di, g.dz, g.drate, g.df_bias, g.di_bias, at::Tensor(), g.dh0, at::Tensor(), at::Tensor(), at::Tensor()});
+        return differentiable_once({g.dx, g.df, g.di, g.dz, g.drate, g.df_bias, g.di_bias, at::Tensor(), g.dh0, at::Tensor(), at::Tensor(), at::Tensor()}, {&t, &grads});
     }
 };
 // gated_recurrence(x, f, i, z, rate, f_bias, i_bias, reset, h0, want_last, stream) -> (out,) or (out, h_last), with gradients

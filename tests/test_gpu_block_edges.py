@@ -2,6 +2,8 @@
 import pytest
 import torch
 
+from paper_2312_00752_amd import autograd as ag
+from paper_2312_00752_amd import binding as B
 from paper_2312_00752_amd import block as bk
 
 pytestmark = pytest.mark.gpu
@@ -43,3 +45,29 @@ def test_training_after_a_graph_of_gradients():
     want = torch.autograd.grad(block(x)[0].sum(), list(block.parameters()))
     got = torch.autograd.grad(block(x)[0].sum(), list(block.parameters()), create_graph=True)
     assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+@pytest.mark.parametrize("constant", [False, True])
+@pytest.mark.parametrize("compiled", [True, False])
+def test_norm_and_recurrence_refuse_for_given_inputs(compiled, constant, monkeypatch):
+    """As above; where nothing that a gradient depends on is a variable, it is a constant and nothing is refused."""
+    if not compiled:
+        monkeypatch.setattr(B, "_native", B._NoMarshal)
+    x, res, f = (torch.randn(2, 8, 40, device="cuda", requires_grad=True) for _ in range(3))
+    w, rate = torch.ones(40, device="cuda", requires_grad=True), torch.ones(8, device="cuda", requires_grad=True)
+    h0 = torch.randn(2, 8, device="cuda", requires_grad=True)
+    for y, inputs in ((ag.layer_norm(x, w), (x, w)), (ag.layer_norm(x, w, residual=res)[0], (x, w, res)),
+                      (ag.gated_recurrence(x, f, rate, h0=h0), (x, f, rate, h0))):
+        loss = y.sum() if constant else y.square().sum()
+        once = torch.autograd.grad(loss, inputs, create_graph=True)
+        plain = torch.autograd.grad(loss, inputs, retain_graph=True)
+        assert all(torch.equal(a, b) for a, b in zip(once, plain))
+        for g in once:
+            for t in inputs:
+                with pytest.raises(RuntimeError):
+                    torch.autograd.grad(loss + g.square().sum(), t, retain_graph=True)
+            with pytest.raises(RuntimeError):
+                (loss + g.square().sum()).backward(retain_graph=True)
+    b = torch.zeros(40, device="cuda", requires_grad=True)
+    g, = torch.autograd.grad(ag.layer_norm(x.detach(), None, b).sum(), b, create_graph=True)
+    assert not g.requires_grad and torch.equal(g, torch.full_like(g, 16.0))
