@@ -15,6 +15,11 @@ import torch
 from . import autograd, binding as B
 
 
+def _sum_like(W, terms):
+    """Float32 memory for a sum of products, the first of which overwrites it; 0 where there is none."""
+    return (torch.empty if terms else torch.zeros)(W.shape, dtype=torch.float32, device=W.device)
+
+
 class _Projection(torch.autograd.Function):
     """W (M,K) times tokens h (B,L,K): (B,M,L), on the library's projection kernels (include/ss_layer.h)."""
 
@@ -30,7 +35,7 @@ class _Projection(torch.autograd.Function):
         W, h = ctx.saved_tensors
         dout = dout.contiguous()
         dh = B.ss_proj_gemm(dout, W, torch.empty_like(h), trans_a=True)
-        dW = torch.empty(W.shape, dtype=torch.float32, device=W.device)
+        dW = _sum_like(W, len(h))
         for b in range(h.shape[0]):
             B.ss_proj_gemm(dout[b], h[b], dW, accumulate=b > 0)
         return dW.to(W.dtype), dh
@@ -51,7 +56,7 @@ class _ProjectionBack(torch.autograd.Function):
         W, y = ctx.saved_tensors
         dout = dout.contiguous()
         dy = B.ss_proj_gemm(W, dout, torch.empty_like(y), trans_a=True, trans_b=True)
-        dW = torch.empty(W.shape, dtype=torch.float32, device=W.device)
+        dW = _sum_like(W, len(y))
         for b in range(y.shape[0]):
             B.ss_proj_gemm(dout[b], y[b], dW, trans_a=True, trans_b=True, accumulate=b > 0)
         return dW.to(W.dtype), dy

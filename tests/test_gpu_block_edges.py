@@ -71,3 +71,16 @@ def test_norm_and_recurrence_refuse_for_given_inputs(compiled, constant, monkeyp
     b = torch.zeros(40, device="cuda", requires_grad=True)
     g, = torch.autograd.grad(ag.layer_norm(x.detach(), None, b).sum(), b, create_graph=True)
     assert not g.requires_grad and torch.equal(g, torch.full_like(g, 16.0))
+
+
+@pytest.mark.parametrize("io", [torch.float32, torch.bfloat16])
+def test_no_batch_entries(io):
+    """A projection of no tokens: the weight's gradient is 0."""
+    W = torch.randn(12, 16, device="cuda").to(io).requires_grad_(True)
+    for f, shape in ((bk._Projection, (0, 24, 16)), (bk._ProjectionBack, (0, 16, 24))):
+        t = torch.randn(shape, device="cuda").to(io).requires_grad_(True)
+        out = f.apply(W, t)
+        junk = [torch.full((12, 16), float("nan"), device="cuda") for _ in range(4)]   # what fresh tensors may hold
+        del junk
+        dW, dt = torch.autograd.grad(out, (W, t), torch.zeros_like(out))
+        assert dt.shape == t.shape and dW.dtype == io and not dW.any()
