@@ -95,13 +95,14 @@ class GatedBlock(torch.nn.Module):
 
 
 class ServedBlock:
-    """A block with its projections in 8-bit integers: ``prompt`` gives (out, residual, state), ``step`` continues from the state,
-    which it updates in place."""
+    """A block as it stands, with its projections in 8-bit integers: ``prompt`` gives (out, residual, state), ``step`` continues from
+    the state, which it updates in place."""
 
     @torch.no_grad()
     def __init__(self, block):
-        self.norm_weight, self.norm_bias, self.eps = block.norm_weight.detach(), block.norm_bias.detach(), block.eps
-        self.rate, self.f_bias, self.i_bias = block.rate().detach(), block.f_bias.detach(), block.i_bias.detach()
+        own = lambda v: v.detach().clone()   # as the 8-bit weights and the rate are: training goes on without this block
+        self.norm_weight, self.norm_bias, self.eps = own(block.norm_weight), own(block.norm_bias), block.eps
+        self.rate, self.f_bias, self.i_bias = block.rate(), own(block.f_bias), own(block.i_bias)
         self.W_in, self.in_scale = B.ss_quant_rows(block.W_in.detach())
         self.W_out, self.out_scale = B.ss_quant_rows(block.W_out.detach())
 

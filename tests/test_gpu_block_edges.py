@@ -1,4 +1,5 @@
-"""The block of norm, projections and gated recurrence where its gradients end."""
+"""The block of norm, projections and gated recurrence at its edges: gradients that have no gradients, an empty batch, a served block
+that is trained on."""
 import pytest
 import torch
 
@@ -84,3 +85,24 @@ def test_no_batch_entries(io):
         del junk
         dW, dt = torch.autograd.grad(out, (W, t), torch.zeros_like(out))
         assert dt.shape == t.shape and dW.dtype == io and not dW.any()
+
+
+@pytest.mark.parametrize("io", [torch.float32, torch.bfloat16])
+def test_a_served_block_is_a_snapshot(io):
+    """Training goes on behind the served block's back."""
+    torch.manual_seed(1)
+    block = bk.GatedBlock(24, 40, dtype=io)
+    served = block.serving()
+    x = torch.randn(2, 9, 24, device="cuda").to(io)
+    state = torch.randn(2, 40, device="cuda")
+
+    def answers():
+        st = state.clone()
+        out = served.prompt(x, state=st)
+        return [*out, *served.step(x[:, 0].contiguous(), st), st]
+    want = answers()
+    with torch.no_grad():
+        for p in block.parameters():
+            p.add_(torch.randn_like(p))
+    for a, b in zip(want, answers()):
+        assert torch.equal(a, b)
