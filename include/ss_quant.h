@@ -18,6 +18,8 @@
  * being 0.  Rules as in ss_scan.h (device pointers owned by the caller, outputs overwritten, host-side
  * validation before any device call, SS_OK or a negative SS_ERR_* code, nothing allocated), but io
  * pointers need be aligned to their element only.  1 <= dim <= SS_QUANT_MAX_DIM; batch or seqlen 0 is valid.
+ * SS_ERR_UNSUPPORTED: batch seqlen or features of 2^31 - 65536 and more; more than 65535 batch entries where a
+ * sequence axis comes last; results of 2^31 and more tiles of 64 x 64.
  *      x                : (batch, seqlen, dim)  io_dtype;  (batch, dim, seqlen) with SS_Q_X_SEQ_LAST;
  *                         with SS_Q_X_QUANTISED (batch seqlen, pitch) int8, 16-byte aligned
  *      q, x_scale       : (batch seqlen, pitch) int8, 16-byte aligned; (batch seqlen) float32

@@ -14,6 +14,7 @@
 namespace ss {
 
 constexpr int Q_STEP = 128;                      // bytes of the contraction index that a step takes
+constexpr int64_t MOST_THREADS = 0x7fffffff;      // of a launch (its limit is 2^32)
 constexpr float Q_LEAST = 7.52316384526264e-37f;  // 2^-120
 
 typedef int i32x4 __attribute__((ext_vector_type(4)));
@@ -730,7 +731,10 @@ void qgemm_launch(const QGemmArgs& a, hipStream_t st)
         const double rounds = alone * (double)((n + at_once - 1) / at_once), all = each * (double)n;
         return ends + a.K / Q_STEP * (rounds > all ? rounds : all);
     };
-    const double t256 = us(tiles(256), 256, 10.0, 1.13, 0.0082), t128 = us(tiles(128), 512, 6.0, 0.56, 0.0023), t64 = us(tiles(64), 512, 4.2, 0.27, 0.00095);
+    // tiles of 256 stay, so they take no more workgroups than units; of the others a launch may have no threads for as many
+    const double never = 1e300, t256 = us(tiles(256), 256, 10.0, 1.13, 0.0082);
+    const double t128 = tiles(128) * 256 > MOST_THREADS ? never : us(tiles(128), 512, 6.0, 0.56, 0.0023);
+    const double t64 = tiles(64) * 256 > MOST_THREADS ? never : us(tiles(64), 512, 4.2, 0.27, 0.00095);
     if (t256 <= t128 && t256 <= t64)
         hipLaunchKernelGGL((qgemm_kernel<T, 4, 2, 2, 4, 2, true>), dim3((unsigned)(tiles(256) < 256 ? tiles(256) : 256)), dim3(512), 0, st, a);
     else if (t128 <= t64 && tiles(128) > 256) hipLaunchKernelGGL((qgemm_kernel<T, 2, 2, 2, 2, 2, false>), dim3((unsigned)tiles(128)), dim3(256), 0, st, a);
@@ -743,7 +747,6 @@ struct QuantSizes {
     int batch, L, dim, pitch;
     int chunks;   // of channels, sequence last
 };
-constexpr int64_t MOST_THREADS = 0x7fffffff;   // of a launch (its limit is 2^32)
 
 // One pass over tokens with the sequence last, where that is faster.  us, not in a cache, one pass / two: bf16, 70, 1000, 4100 and 16384 tokens of
 // 2048 channels 4.7 7.0 9.8 34.2 / 9.7 13.7 17.3 33.3, of 4096 9.5 9.8 21.1 58.4 / 10.2 15.1 27.5 71.3; 1000 of 5120 11.8 / 16.6; float32 of
@@ -910,7 +913,7 @@ int ss_qlinear(const ss_qlinear_params* p, void* stream)
     if (p->batch == 0 || p->seqlen == 0) return SS_OK;
     if ((x_last || out_last) && p->batch > 65535) return SS_ERR_UNSUPPORTED;
     const int64_t rows = (int64_t)p->batch * p->seqlen;
-    // the grid of the product is one-dimensional, of tiles of at least 64 x 64
+    // what the product's tiles, of at least 64 x 64, are numbered with
     const int64_t tm = ((out_last ? p->features : rows) + 63) / 64, tn = ((out_last ? p->seqlen : p->features) + 63) / 64;
     if (tm * tn > 0x7fffffff / (out_last ? p->batch : 1)) return SS_ERR_UNSUPPORTED;
     if (!p->x || !p->weight || !p->scale || !p->out || (done && !p->x_scale) || (hb && !p->bias)) return SS_ERR_NULL;
@@ -927,7 +930,8 @@ int ss_qlinear(const ss_qlinear_params* p, void* stream)
     const int pitch = (int)ss_quant_pitch(p->dim);
     const int8_t* q = static_cast<const int8_t*>(p->x);
     const float* q_scale = p->x_scale;
-    const bool few = rows <= ss::FEW_TOKENS && !out_last;
+    // (16 features and 256 threads a workgroup where there are as many features as that)
+    const bool few = rows <= ss::FEW_TOKENS && !out_last && p->features <= ss::MOST_THREADS / 16;
     const bool fused = few && !done && !x_last && ss::few_fused((int)rows, p->dim, pitch, ss::few_waves(p->features, pitch));
     if (!done && !fused) {
         const ss::QuantSizes z = {p->batch, p->seqlen, p->dim, pitch, chunks_of(p->dim)};
