@@ -16,6 +16,7 @@
 //
 // G_t is again an affine map of G_{t+1}, with a_t and b = a_t dy_t.
 #include <hip/hip_runtime.h>
+#include <algorithm>
 #include <type_traits>
 
 #include "ss_gate.h"
@@ -712,23 +713,27 @@ __global__ __launch_bounds__(GATE_WAVES* WAVE) void gate_bwd_map_kernel(GateArgs
 }
 
 // Sums of the rows' partial sums over batch entries and segments, in a fixed order: 16 channels of one of the three
-// gradients per workgroup, 16 threads a channel.
+// gradients per workgroup and round, 16 threads a channel.
 __global__ __launch_bounds__(256) void gate_sums_kernel(const float* part, float* drate, float* df, float* di, int64_t plane, int D, int n)
 {
     const int which = blockIdx.y;
     float* const to = which == 0 ? drate : (which == 1 ? df : di);
     if (!to) return;
     __shared__ float s[16][17];
-    const int d = blockIdx.x * 16 + (threadIdx.x & 15), k0 = threadIdx.x >> 4;
-    float v = 0.0f;
-    if (d < D)
-        for (int k = k0; k < n; k += 16) v += part[which * plane + (int64_t)k * D + d];
-    s[k0][threadIdx.x & 15] = v;
-    __syncthreads();
-    if (threadIdx.x < 16 && d < D) {
-        float t = 0.0f;
-        for (int k = 0; k < 16; ++k) t += s[k][threadIdx.x];
-        to[d] = t;
+    const int k0 = threadIdx.x >> 4;
+    for (int64_t d0 = (int64_t)blockIdx.x * 16; d0 < D; d0 += (int64_t)gridDim.x * 16) {
+        const int64_t d = d0 + (threadIdx.x & 15);
+        float v = 0.0f;
+        if (d < D)
+            for (int k = k0; k < n; k += 16) v += part[which * plane + (int64_t)k * D + d];
+        s[k0][threadIdx.x & 15] = v;
+        __syncthreads();
+        if (threadIdx.x < 16 && d < D) {
+            float t = 0.0f;
+            for (int k = 0; k < 16; ++k) t += s[k][threadIdx.x];
+            to[d] = t;
+        }
+        __syncthreads();
     }
 }
 
@@ -819,6 +824,7 @@ using ss::GateArgs;
 constexpr uint32_t kGateFlags = SS_GATE_HAS_I | SS_GATE_HAS_Z | SS_GATE_HAS_F_BIAS | SS_GATE_HAS_I_BIAS | SS_GATE_HAS_RESET | SS_GATE_HAS_H0 |
                                 SS_GATE_WRITE_H_LAST | SS_GATE_SAVE_FOR_BWD;
 constexpr uint32_t kGateStepFlags = SS_GATE_HAS_I | SS_GATE_HAS_Z | SS_GATE_HAS_F_BIAS | SS_GATE_HAS_I_BIAS | SS_GATE_HAS_RESET;
+constexpr int64_t MOST_THREADS = 0xffffffffL - 65536;   // of a launch, which has fewer than 2^32
 inline bool aligned_to(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) % a) == 0; }
 inline size_t round_up(size_t v, size_t a) { return (v + a - 1) / a * a; }
 
@@ -837,7 +843,7 @@ GatePlan gate_plan(long rows, int L, int io)
     GatePlan g;
     g.pieces = (L + ss::GATE_PIECE - 1) / ss::GATE_PIECE;
     const bool fill = 10 * g.pieces >= 9 * ((g.pieces + 3) / 4 * 4);
-    g.team = g.pieces >= 3 && (rows < (io == SS_F32 ? 2048 : 1536) || (io == SS_F32 && fill)) ? 4 : 1;
+    g.team = g.pieces >= 3 && (rows < (io == SS_F32 ? 2048 : 1536) || (io == SS_F32 && fill && rows <= MOST_THREADS / (4 * ss::WAVE))) ? 4 : 1;   // a team's waves are threads too
     long n = rows > 160 || g.pieces < 48 ? 1 : (768 + rows - 1) / rows;
     const long most = (g.pieces + 7) / 8;   // a segment has two rounds of its team's at least
     if (n > most) n = most;
@@ -882,7 +888,7 @@ int check_gate(const ss_gate_params* p, bool for_bwd)
     const bool hi = p->flags & SS_GATE_HAS_I, hz = p->flags & SS_GATE_HAS_Z;
     if ((p->flags & SS_GATE_HAS_I_BIAS) && !hi) return SS_ERR_UNSUPPORTED;
     if ((long)p->batch * p->dim >= 0x7fffffffL || p->seqlen > 0x7fffffff - 2 * ss::GATE_PIECE) return SS_ERR_UNSUPPORTED;
-    if ((int64_t)p->batch * p->dim * ss::lanes_for(p->seqlen) > 0xffffffffL - 65536) return SS_ERR_UNSUPPORTED;   // a launch has fewer than 2^32 threads
+    if ((int64_t)p->batch * p->dim * ss::lanes_for(p->seqlen) > MOST_THREADS) return SS_ERR_UNSUPPORTED;
     const bool empty = p->seqlen == 0;
     if (!empty && (!p->x || !p->f || (hi && !p->i) || (hz && !p->z) || (!for_bwd && !p->out))) return SS_ERR_NULL;
     if (!p->rate || ((p->flags & SS_GATE_HAS_F_BIAS) && !p->f_bias) || ((p->flags & SS_GATE_HAS_I_BIAS) && !p->i_bias)) return SS_ERR_NULL;
@@ -1013,7 +1019,7 @@ int ss_gate_bwd(const ss_gate_bwd_params* p, void* stream)
     if (q->io_dtype == SS_BF16) ss::launch_all<ss::bf16_t>(a, g.team, true, st);
     else ss::launch_all<float>(a, g.team, true, st);
     if (!direct)
-        hipLaunchKernelGGL(ss::gate_sums_kernel, dim3((unsigned)((q->dim + 15) / 16), ib ? 3u : (fb ? 2u : 1u)), dim3(256), 0, st, part, p->drate,
+        hipLaunchKernelGGL(ss::gate_sums_kernel, dim3((unsigned)std::min<int64_t>(((int64_t)q->dim + 15) / 16, MOST_THREADS / 256), ib ? 3u : (fb ? 2u : 1u)), dim3(256), 0, st, part, p->drate,
                            fb ? p->df_bias : nullptr, ib ? p->di_bias : nullptr, plane, q->dim, g.nseg * q->batch);
     return hipGetLastError() == hipSuccess ? SS_OK : SS_ERR_LAUNCH;
 }

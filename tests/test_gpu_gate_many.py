@@ -1,0 +1,28 @@
+"""The gated recurrence with more channels than the sums of its parameters' gradients have threads for at a time."""
+import pytest
+import torch
+
+from paper_2312_00752_amd import binding as B
+
+pytestmark = pytest.mark.gpu
+
+
+def test_many_channels():
+    """Two entries of one step of 2^28 channels and some: the same bits as the ends by themselves."""
+    if torch.cuda.mem_get_info()[0] < 40 << 30:
+        pytest.skip("needs 40 GiB")
+    nb, nd = 2, (1 << 28) + 21
+
+    def gradients(x, f, dout, rate, f_bias):
+        ws = torch.empty(max(256, B.ss_gate_workspace_bytes(*x.shape)), dtype=torch.uint8, device="cuda")
+        out, _ = B.ss_gate_fwd(x, f, rate, f_bias=f_bias, workspace=ws, save_for_bwd=True)
+        return {"out": out, **B.ss_gate_bwd(dout, x, f, rate, ws, f_bias=f_bias)}
+    x, f, dout = (torch.randn(nb, nd, 1, device="cuda", dtype=torch.bfloat16) for _ in range(3))
+    rate = torch.rand(nd, device="cuda")
+    whole = gradients(x, f, dout, rate, rate)
+    for cut in (slice(0, 100), slice(nd // 2, nd // 2 + 40), slice(nd - 100, nd)):
+        part = gradients(*(t[:, cut].contiguous() for t in (x, f, dout)), rate[cut].contiguous(), rate[cut].contiguous())
+        for name, t in part.items():
+            if t is not None:
+                w = whole[name][cut] if t.dim() == 1 else whole[name][:, cut]
+                assert torch.equal(t, w), (name, cut)

@@ -118,3 +118,48 @@ static void one()
     look(ss_quant_rows(&p, nullptr), "ss_quant_rows", p.batch, p.seqlen, p.dim, 0, p.io_dtype, p.flags);
 }
 """)
+
+
+GATE = r"""
+static void one()
+{
+    ss_gate_bwd_params q{};
+    ss_gate_params& p = q.fwd;
+    p.io_dtype = coin(2);
+    p.flags = (uint32_t)coin(256);
+    p.batch = coin(2) ? 1 : any(1 << 24);
+    p.dim = any(2147483646);
+    p.seqlen = coin(8) ? any(1 << 22) : any(2147482623);
+    if (uniform() < 0.05) {   // rows about the most threads that teams of four waves have, lengths whose pieces fill them
+        p.batch = 1 + coin(2);
+        p.dim = ((1 << 24) - 300 + coin(600)) / p.batch;
+        p.seqlen = 1500 + coin(600);
+    }
+    const double one_tensor = (double)p.batch * p.dim * p.seqlen * (p.io_dtype == SS_BF16 ? 2 : 4);
+    if (2 * one_tensor > CARD) return;   // one tensor may serve as several inputs
+    p.x = p.f = p.i = p.z = p.out = p.workspace = fake;
+    p.x_batch = p.f_batch = p.i_batch = p.z_batch = (int64_t)p.dim * p.seqlen;
+    p.rate = p.f_bias = p.i_bias = p.h0 = p.h_last = static_cast<float*>(fake);
+    p.reset = static_cast<uint8_t*>(fake);
+    p.workspace_bytes = ss_gate_workspace_bytes(&p, 1);
+    const bool forward = ss_gate_fwd(&p, nullptr) == SS_OK;
+    look(forward ? SS_OK : SS_ERR_UNSUPPORTED, "ss_gate_fwd", p.batch, p.dim, p.seqlen, 0, p.io_dtype, p.flags);
+    if (5 * one_tensor > CARD) return;
+    q.dout = q.dx = q.df = q.di = q.dz = fake;
+    q.dh_last = q.drate = q.df_bias = q.di_bias = q.dh0 = static_cast<float*>(fake);
+    q.dx_batch = q.df_batch = q.di_batch = q.dz_batch = (int64_t)p.dim * p.seqlen;
+    const bool backward = ss_gate_bwd(&q, nullptr) == SS_OK;
+    look(backward == forward ? (backward ? SS_OK : SS_ERR_UNSUPPORTED) : 1, "ss_gate_bwd", p.batch, p.dim, p.seqlen, 0, p.io_dtype, p.flags);
+    ss_gate_step_params t{};
+    t.batch = p.batch; t.dim = p.dim; t.io_dtype = p.io_dtype;
+    t.flags = p.flags & (SS_GATE_HAS_I | SS_GATE_HAS_Z);
+    t.x_t = t.f_t = t.i_t = t.z_t = t.out_t = fake;
+    t.x_batch = t.f_batch = t.i_batch = t.z_batch = p.dim;
+    t.h = static_cast<float*>(fake); t.rate = p.rate;
+    look(ss_gate_step(&t, nullptr), "ss_gate_step", p.batch, p.dim, 1, 0, p.io_dtype, t.flags);
+}
+"""
+
+
+def test_recurrence(tmp_path):
+    run(tmp_path, "ss_gate.hip", GATE)
