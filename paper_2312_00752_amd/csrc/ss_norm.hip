@@ -350,30 +350,34 @@ __global__ __launch_bounds__(norm_threads<G>(true)) void norm_bwd_kernel(NormArg
     }
 }
 
-// dweight and dbias from the parts: 32 columns of one of the two per workgroup, 32 threads a column.  512 parts of 2048 columns 4.0 us.
+// dweight and dbias from the parts: 32 columns of one of the two per workgroup and round, 32 threads a column.  512 parts of 2048 columns 4.0 us.
 __global__ __launch_bounds__(1024) void norm_parts_kernel(const float* part, float* dweight, float* dbias, int W, int parts)
 {
     float* const to = blockIdx.y == 0 ? dweight : dbias;
     if (!to) return;
     __shared__ float s[32][33];
-    const int c = blockIdx.x * 32 + threadIdx.x % 32, k0 = threadIdx.x / 32;
-    float v = 0.0f;
-    if (c < W) {
+    const int k0 = threadIdx.x / 32;
+    for (int64_t c0 = (int64_t)blockIdx.x * 32; c0 < W; c0 += (int64_t)gridDim.x * 32) {
+        const int64_t c = c0 + threadIdx.x % 32;
+        float v = 0.0f;
+        if (c < W) {
 #pragma unroll 8
-        for (int k = k0; k < parts; k += 32) v += part[((int64_t)k * 2 + blockIdx.y) * W + c];
-    }
-    s[threadIdx.x % 32][k0] = v;
-    __syncthreads();
-    // a column's 32 sums in the lanes of half a wave
-    float t = s[threadIdx.x / 32][threadIdx.x % 32];
+            for (int k = k0; k < parts; k += 32) v += part[((int64_t)k * 2 + blockIdx.y) * W + c];
+        }
+        s[threadIdx.x % 32][k0] = v;
+        __syncthreads();
+        // a column's 32 sums in the lanes of half a wave
+        float t = s[threadIdx.x / 32][threadIdx.x % 32];
 #pragma unroll
-    for (int k = 1; k < 32; k *= 2) t += __shfl_xor(t, k);
-    const int col = blockIdx.x * 32 + threadIdx.x / 32;
-    if (threadIdx.x % 32 == 0 && col < W) to[col] = t;
+        for (int k = 1; k < 32; k *= 2) t += __shfl_xor(t, k);
+        const int64_t col = c0 + threadIdx.x / 32;
+        if (threadIdx.x % 32 == 0 && col < W) to[col] = t;
+        __syncthreads();
+    }
 }
 
 // ---- rows that do not fit the registers of a workgroup ------------------------------------------
-// A workgroup a row, which is read once for each sweep, after the first from the caches.  2048 x 20000 bf16: 80 us forward (164 MB),
+// A workgroup a row at a time, which is read once for each sweep, after the first from the caches.  2048 x 20000 bf16: 80 us forward (164 MB),
 // 75 + 40 backward.
 template <typename T, typename S, bool RES>
 __global__ __launch_bounds__(1024) void norm_fwd_wide_kernel(NormArgs a)
@@ -381,34 +385,36 @@ __global__ __launch_bounds__(1024) void norm_fwd_wide_kernel(NormArgs a)
     __shared__ float lds[2][1][16];
     RowSum<1024, 1> sum{lds};
     const int W = a.width;
-    const int64_t off = (int64_t)blockIdx.x * W;
-    const T* x = static_cast<const T*>(a.x) + off;
-    const S* r = static_cast<const S*>(a.residual) + off;
-    S* held = static_cast<S*>(a.summed) + off;
-    T* out = static_cast<T*>(a.out) + off;
-    auto value = [&](int c) {
-        if constexpr (RES) return io_to_f32<S>(held[c]);   // as this thread wrote it
-        else return io_to_f32<T>(x[c]);
-    };
-    float t[1] = {0.0f};
-    for (int c = threadIdx.x; c < W; c += 1024) {
-        if constexpr (RES) held[c] = f32_to_io<S>(io_to_f32<T>(x[c]) + io_to_f32<S>(r[c]));
-        t[0] += value(c);
-    }
-    sum(t);
-    const float mean = t[0] / (float)W;
-    t[0] = 0.0f;
-    for (int c = threadIdx.x; c < W; c += 1024) {
-        const float v = value(c) - mean;
-        t[0] = fmaf(v, v, t[0]);
-    }
-    sum(t);
-    const float rstd = 1.0f / sqrtf(t[0] / (float)W + a.eps);
-    for (int c = threadIdx.x; c < W; c += 1024)
-        out[c] = f32_to_io<T>(fmaf((value(c) - mean) * rstd, a.weight ? a.weight[c] : 1.0f, a.bias ? a.bias[c] : 0.0f));
-    if (a.mean && threadIdx.x == 0) {
-        a.mean[blockIdx.x] = mean;
-        a.rstd[blockIdx.x] = rstd;
+    for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
+        const int64_t off = row * W;
+        const T* x = static_cast<const T*>(a.x) + off;
+        const S* r = static_cast<const S*>(a.residual) + off;
+        S* held = static_cast<S*>(a.summed) + off;
+        T* out = static_cast<T*>(a.out) + off;
+        auto value = [&](int c) {
+            if constexpr (RES) return io_to_f32<S>(held[c]);   // as this thread wrote it
+            else return io_to_f32<T>(x[c]);
+        };
+        float t[1] = {0.0f};
+        for (int c = threadIdx.x; c < W; c += 1024) {
+            if constexpr (RES) held[c] = f32_to_io<S>(io_to_f32<T>(x[c]) + io_to_f32<S>(r[c]));
+            t[0] += value(c);
+        }
+        sum(t);
+        const float mean = t[0] / (float)W;
+        t[0] = 0.0f;
+        for (int c = threadIdx.x; c < W; c += 1024) {
+            const float v = value(c) - mean;
+            t[0] = fmaf(v, v, t[0]);
+        }
+        sum(t);
+        const float rstd = 1.0f / sqrtf(t[0] / (float)W + a.eps);
+        for (int c = threadIdx.x; c < W; c += 1024)
+            out[c] = f32_to_io<T>(fmaf((value(c) - mean) * rstd, a.weight ? a.weight[c] : 1.0f, a.bias ? a.bias[c] : 0.0f));
+        if (a.mean && threadIdx.x == 0) {
+            a.mean[row] = mean;
+            a.rstd[row] = rstd;
+        }
     }
 }
 template <typename T, typename S, bool RES>
@@ -417,24 +423,26 @@ __global__ __launch_bounds__(1024) void norm_bwd_wide_kernel(NormArgs a)
     __shared__ float lds[2][2][16];
     RowSum<1024, 2> sum{lds};
     const int W = a.width;
-    const int64_t off = (int64_t)blockIdx.x * W;
-    const S *s = static_cast<const S*>(a.s) + off, *more = static_cast<const S*>(a.dsummed) + off;
-    const T* dout = static_cast<const T*>(a.dout) + off;
-    const float mean = a.mean[blockIdx.x], rstd = a.rstd[blockIdx.x];
-    float t[2] = {0.0f, 0.0f};
-    for (int c = threadIdx.x; c < W; c += 1024) {
-        const float g = io_to_f32<T>(dout[c]) * (a.weight ? a.weight[c] : 1.0f);
-        t[0] += g;
-        t[1] = fmaf(g, (io_to_f32<S>(s[c]) - mean) * rstd, t[1]);
-    }
-    sum(t);
-    const float c1 = t[0] / (float)W, c2 = t[1] / (float)W;
-    for (int c = threadIdx.x; c < W; c += 1024) {
-        const float g = io_to_f32<T>(dout[c]) * (a.weight ? a.weight[c] : 1.0f);
-        float o = rstd * (g - c1 - (io_to_f32<S>(s[c]) - mean) * rstd * c2);
-        if (RES && a.dsummed) o += io_to_f32<S>(more[c]);
-        static_cast<T*>(a.dx)[off + c] = f32_to_io<T>(o);
-        if constexpr (RES && sizeof(S) != sizeof(T)) static_cast<S*>(a.dresidual)[off + c] = o;
+    for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
+        const int64_t off = row * W;
+        const S *s = static_cast<const S*>(a.s) + off, *more = static_cast<const S*>(a.dsummed) + off;
+        const T* dout = static_cast<const T*>(a.dout) + off;
+        const float mean = a.mean[row], rstd = a.rstd[row];
+        float t[2] = {0.0f, 0.0f};
+        for (int c = threadIdx.x; c < W; c += 1024) {
+            const float g = io_to_f32<T>(dout[c]) * (a.weight ? a.weight[c] : 1.0f);
+            t[0] += g;
+            t[1] = fmaf(g, (io_to_f32<S>(s[c]) - mean) * rstd, t[1]);
+        }
+        sum(t);
+        const float c1 = t[0] / (float)W, c2 = t[1] / (float)W;
+        for (int c = threadIdx.x; c < W; c += 1024) {
+            const float g = io_to_f32<T>(dout[c]) * (a.weight ? a.weight[c] : 1.0f);
+            float o = rstd * (g - c1 - (io_to_f32<S>(s[c]) - mean) * rstd * c2);
+            if (RES && a.dsummed) o += io_to_f32<S>(more[c]);
+            static_cast<T*>(a.dx)[off + c] = f32_to_io<T>(o);
+            if constexpr (RES && sizeof(S) != sizeof(T)) static_cast<S*>(a.dresidual)[off + c] = o;
+        }
     }
 }
 // columns' sums over blockIdx.y's share of the rows
@@ -457,6 +465,7 @@ __global__ __launch_bounds__(256) void norm_columns_kernel(NormArgs a)
 
 // ---- forms ----------------------------------------------------------------------------------------
 constexpr int NORM_WIDEST = 16384;   // widest row that is held in registers
+constexpr int NORM_MOST_WORKGROUPS = (1 << 22) - 1;   // of 1024 threads: a launch has fewer than 2^32
 
 struct NormForm {
     int lanes, slices;   // lanes of a row (0: the kernels for wider rows) and slices of a lane
@@ -513,10 +522,11 @@ void norm_launch(const NormArgs& a, bool bwd, hipStream_t st)
 {
     const NormForm f = norm_form(a.rows, a.width, bwd);
     if (f.lanes == 0) {
+        const dim3 grid((unsigned)(a.rows < NORM_MOST_WORKGROUPS ? a.rows : NORM_MOST_WORKGROUPS));
         if (!bwd) {
-            hipLaunchKernelGGL((norm_fwd_wide_kernel<T, S, RES>), dim3((unsigned)a.rows), dim3(1024), 0, st, a);
+            hipLaunchKernelGGL((norm_fwd_wide_kernel<T, S, RES>), grid, dim3(1024), 0, st, a);
         } else {
-            hipLaunchKernelGGL((norm_bwd_wide_kernel<T, S, RES>), dim3((unsigned)a.rows), dim3(1024), 0, st, a);
+            hipLaunchKernelGGL((norm_bwd_wide_kernel<T, S, RES>), grid, dim3(1024), 0, st, a);
             if (a.part)
                 hipLaunchKernelGGL((norm_columns_kernel<T, S>), dim3((unsigned)((a.width + 255) / 256), (unsigned)norm_parts(a.rows, a.width)),
                                    dim3(256), 0, st, a);
@@ -643,9 +653,12 @@ int ss_norm_bwd(const ss_norm_bwd_params* p, void* stream)
         a.part = static_cast<float*>(p->workspace);
         ss::norm_dispatch(a, q->io_dtype, q->flags, true, st);
     }
-    if (hw || hb)
-        hipLaunchKernelGGL(ss::norm_parts_kernel, dim3((unsigned)((q->width + 31) / 32), hb ? 2u : 1u), dim3(1024), 0, st, a.part, hw ? p->dweight : nullptr,
+    if (hw || hb) {
+        const int columns = (q->width + 31) / 32;
+        const dim3 grid((unsigned)(columns < ss::NORM_MOST_WORKGROUPS ? columns : ss::NORM_MOST_WORKGROUPS), hb ? 2u : 1u);
+        hipLaunchKernelGGL(ss::norm_parts_kernel, grid, dim3(1024), 0, st, a.part, hw ? p->dweight : nullptr,
                            hb ? p->dbias : nullptr, q->width, q->rows > 0 ? ss::norm_parts(q->rows, q->width) : 0);
+    }
     return hipGetLastError() == hipSuccess ? SS_OK : SS_ERR_LAUNCH;
 }
 

@@ -163,3 +163,32 @@ static void one()
 
 def test_recurrence(tmp_path):
     run(tmp_path, "ss_gate.hip", GATE)
+
+
+NORM = r"""
+static void one()
+{
+    ss_norm_bwd_params q{};
+    ss_norm_params& p = q.fwd;
+    p.io_dtype = coin(2);
+    p.flags = (uint32_t)coin(16) | SS_NORM_SAVE_STATS;
+    p.rows = any(2147418111);
+    p.width = any(2147418111);
+    p.eps = 1e-5f;
+    const double io = (double)p.rows * p.width * (p.io_dtype == SS_BF16 ? 2 : 4);
+    const bool res = p.flags & SS_NORM_HAS_RESIDUAL;
+    if ((res ? 3 : 1) * io > CARD) return;   // out may be x, summed the residual
+    p.x = p.residual = p.out = p.summed = fake;
+    p.weight = p.bias = p.stats = static_cast<float*>(fake);
+    look(ss_norm_fwd(&p, nullptr), "ss_norm_fwd", p.rows, p.width, 0, 0, p.io_dtype, p.flags);
+    if (3 * io > CARD) return;
+    q.dout = q.dsummed = q.dx = q.dresidual = q.workspace = fake;
+    q.dweight = q.dbias = static_cast<float*>(fake);
+    q.workspace_bytes = ss_norm_workspace_bytes(&p);
+    look(ss_norm_bwd(&q, nullptr), "ss_norm_bwd", p.rows, p.width, 0, 0, p.io_dtype, p.flags);
+}
+"""
+
+
+def test_norm(tmp_path):
+    run(tmp_path, "ss_norm.hip", NORM)
