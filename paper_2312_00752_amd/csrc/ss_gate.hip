@@ -201,11 +201,11 @@ __device__ __forceinline__ uint2 marks_request(const uint8_t* row, int t0, int L
     const u2 v = load_any<u2>(row + min(t0, L - 8), 0u);
     return make_uint2(v[0], v[1]);
 }
-__device__ __forceinline__ uint2 marks_settle(uint2 m, int t0, int L)
+__host__ __device__ __forceinline__ uint2 marks_settle(uint2 m, int t0, int L)
 {
-    const int s = 8 * (t0 - (L - 8));   // L < 8: the marks are in place
-    if (s <= 0 || L < 8) return m;
-    const uint64_t w = s < 64 ? ((uint64_t(m.y) << 32) | m.x) >> s : 0;
+    const int past = t0 - (L - 8);   // L < 8: the marks are in place
+    if (past <= 0 || L < 8) return m;
+    const uint64_t w = past < 8 ? ((uint64_t(m.y) << 32) | m.x) >> (8 * past) : 0;
     return make_uint2((uint32_t)w, (uint32_t)(w >> 32));
 }
 __device__ __forceinline__ bool marked(uint2 m, int j) { return ((j < 4 ? m.x : m.y) & (0xffu << (8 * (j & 3)))) != 0; }

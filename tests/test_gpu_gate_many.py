@@ -1,8 +1,11 @@
-"""The gated recurrence with more channels than the sums of its parameters' gradients have threads for at a time."""
+"""The gated recurrence with more channels than the sums of its parameters' gradients have threads for at a time, and with rows of more
+than 2^28 steps.  Tolerance as in test_gpu_gate.py."""
 import pytest
 import torch
 
 from paper_2312_00752_amd import binding as B
+from tests import op_util as u
+from tests.test_gpu_gate import FWD
 
 pytestmark = pytest.mark.gpu
 
@@ -26,3 +29,22 @@ def test_many_channels():
             if t is not None:
                 w = whole[name][cut] if t.dim() == 1 else whole[name][:, cut]
                 assert torch.equal(t, w), (name, cut)
+
+
+def test_marks_of_very_long_rows():
+    """A row of 2^28 steps and some: marks at its start, within and at its end, against the pieces that begin there."""
+    if torch.cuda.mem_get_info()[0] < 20 << 30:
+        pytest.skip("needs 20 GiB")
+    nl = (1 << 28) + 13
+    x, f = (torch.randn(1, 1, nl, device="cuda") for _ in range(2))
+    rate = torch.ones(1, device="cuda")
+    reset = torch.zeros(1, nl, dtype=torch.bool, device="cuda")
+    starts = [0, 3, nl // 2 + 1, nl - 700, nl - 5]
+    reset[0, starts] = True
+    h0 = torch.full((1, 1), 1e30, device="cuda")
+    out, last = B.ss_gate_fwd(x, f, rate, reset=reset, h0=h0, return_last_state=True)
+    for a, b in zip(starts, starts[1:] + [nl]):
+        b = min(b, a + 600)
+        part = B.ss_gate_fwd(x[..., a:b].contiguous(), f[..., a:b].contiguous(), rate, reset=reset[:, a:b].contiguous())[0]
+        u.close(out[..., a:b], u.host(part), FWD, "from %d" % a)
+    assert torch.equal(last, out[..., -1])
