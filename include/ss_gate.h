@@ -29,7 +29,7 @@
  *      reset                      : (B, L)     uint8
  *      h0, h_last, dh_last, dh0   : (B, D)     float32
  * Rows (B D) are limited by the threads of a launch: fewer than 2^26 of more than 128 steps, 2^28 of more
- * than 32, 2^30 else; more are SS_ERR_UNSUPPORTED.
+ * than 32, 2^30 else; more, and rows of 2^31 - 2048 steps and more, are SS_ERR_UNSUPPORTED.
  * seqlen == 0 is valid: h_last receives h0 or 0, and the backward call returns zero parameter
  * gradients and dh0 = dh_last.
  */

@@ -887,7 +887,7 @@ int check_gate(const ss_gate_params* p, bool for_bwd)
     if (p->flags & ~kGateFlags) return SS_ERR_UNSUPPORTED;
     const bool hi = p->flags & SS_GATE_HAS_I, hz = p->flags & SS_GATE_HAS_Z;
     if ((p->flags & SS_GATE_HAS_I_BIAS) && !hi) return SS_ERR_UNSUPPORTED;
-    if ((long)p->batch * p->dim >= 0x7fffffffL || p->seqlen > 0x7fffffff - 2 * ss::GATE_PIECE) return SS_ERR_UNSUPPORTED;
+    if ((long)p->batch * p->dim >= 0x7fffffffL || p->seqlen > 0x7fffffff - 4 * ss::GATE_PIECE) return SS_ERR_UNSUPPORTED;   // room for a team's last round
     if ((int64_t)p->batch * p->dim * ss::lanes_for(p->seqlen) > MOST_THREADS) return SS_ERR_UNSUPPORTED;
     const bool empty = p->seqlen == 0;
     if (!empty && (!p->x || !p->f || (hi && !p->i) || (hz && !p->z) || (!for_bwd && !p->out))) return SS_ERR_NULL;

@@ -1,8 +1,10 @@
 """Reset marks of a lane's eight steps shifted into place at the end of a row, for rows up to the longest that is accepted: csrc/ss_gate.hip
 compiled for the host, with signed overflow trapped."""
+import ctypes
 import os
 import subprocess
 
+from paper_2312_00752_amd import binding as B
 from paper_2312_00752_amd import build
 
 PROGRAM = r"""
@@ -44,3 +46,20 @@ def test_marks_of_long_rows(tmp_path):
     subprocess.run(["g++", obj, "-o", program], check=True, capture_output=True)
     out = subprocess.run([program], capture_output=True, text=True)
     assert out.returncode == 0 and out.stdout == "done\n", (out.returncode, out.stdout)
+
+
+def test_steps_past_the_longest_row():
+    """The last round of a team of four may lie up to three pieces of 512 steps behind the row; its steps are numbered in 32 bits too, so a row
+    that leaves no room for them is refused."""
+    p = B.GateParams()
+    p.batch = p.dim = 1
+    p.io_dtype = B.SS_BF16
+    p.flags = B.SS_GATE_SAVE_FOR_BWD
+    for f in ("x", "f", "rate", "out"):
+        setattr(p, f, 1 << 20)
+    for seqlen, code in ((2 ** 31 - 1 - 2 * 512, B.SS_ERR_UNSUPPORTED), (2 ** 31 - 1 - 2039, B.SS_ERR_UNSUPPORTED), (2 ** 31 - 1 - 2048, B.SS_ERR_WORKSPACE)):
+        p.seqlen = seqlen
+        last = -(-seqlen // 512) - 1 + 3   # piece
+        if code != B.SS_ERR_UNSUPPORTED:
+            assert last * 512 + 64 * 8 < 2 ** 31
+        assert B.lib().ss_gate_fwd(ctypes.byref(p), None) == code, seqlen

@@ -129,7 +129,7 @@ static void one()
     p.flags = (uint32_t)coin(256);
     p.batch = coin(2) ? 1 : any(1 << 24);
     p.dim = any(2147483646);
-    p.seqlen = coin(8) ? any(1 << 22) : any(2147482623);
+    p.seqlen = coin(8) ? any(1 << 22) : any(2147481599);
     if (uniform() < 0.05) {   // rows about the most threads that teams of four waves have, lengths whose pieces fill them
         p.batch = 1 + coin(2);
         p.dim = ((1 << 24) - 300 + coin(600)) / p.batch;
