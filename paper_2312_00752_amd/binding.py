@@ -840,6 +840,14 @@ def _check(rc):
         raise SsError(rc)
 
 
+def _counts(*ns):
+    """Sizes as the library counts them, in 32 bits; ctypes would cut larger ones to their low bits."""
+    for n in ns:
+        if n > 0x7fffffff:
+            raise SsError(SS_ERR_UNSUPPORTED)
+    return ns
+
+
 def _bytes(n, device):
     return torch.empty(max(256, n), dtype=torch.uint8, device=device)
 
@@ -865,7 +873,7 @@ def _norm_params(x, weight, bias, residual, eps):
         raise ValueError("a tensor without axes cannot be normalised")
     p = NormParams()
     width = x.shape[-1]
-    p.rows, p.width = (x.numel() // width if width else 0), width
+    p.rows, p.width = _counts(x.numel() // width if width else 0, width)
     p.eps = eps
     if weight is not None:
         p.weight = _ptr(weight, f32, (width,), "weight")
@@ -915,7 +923,7 @@ def ss_norm_fwd(x, weight=None, bias=None, residual=None, eps=1e-5, out=None, su
 
 def ss_norm_workspace_bytes(rows, width):
     p = NormParams()
-    p.rows, p.width = rows, width
+    p.rows, p.width = _counts(rows, width)
     return int(lib().ss_norm_workspace_bytes(ctypes.byref(p)))
 
 
@@ -989,7 +997,7 @@ def _gate_inputs(p, x, f, i, z, rate, f_bias, i_bias, names=("x", "f", "i", "z")
     f32, shape, io = torch.float32, x.shape, x.dtype
     if len(shape) != (3 if names[0] == "x" else 2):
         raise ValueError("%s must have %s axes" % (names[0], "three" if names[0] == "x" else "two"))
-    p.batch, p.dim = shape[0], shape[1]
+    p.batch, p.dim = _counts(*shape)[:2]
     p.io_dtype = _io_code(x)
     for name, t in zip(names, (x, f, i, z)):
         ptr, batch = _rows_of(t, io, shape, name)
@@ -1030,7 +1038,7 @@ def _gate_params(x, f, rate, i, z, f_bias, i_bias, reset, h0):
 
 def ss_gate_workspace_bytes(batch, dim, seqlen, for_backward=True):
     p = GateParams()
-    p.batch, p.dim, p.seqlen = batch, dim, seqlen
+    p.batch, p.dim, p.seqlen = _counts(batch, dim, seqlen)
     return int(lib().ss_gate_workspace_bytes(ctypes.byref(p), int(bool(for_backward))))
 
 
@@ -1138,7 +1146,7 @@ def ss_gate_step(h, x_t, f_t, rate, i_t=None, z_t=None, f_bias=None, i_bias=None
 # ---------------------------------------------------------------- products in 8-bit integers
 def ss_quant_pitch(dim):
     """Bytes from one quantised row of ``dim`` values to the next."""
-    return int(lib().ss_quant_pitch(dim))
+    return int(lib().ss_quant_pitch(*_counts(dim)))
 
 
 def ss_quant_rows(x, seq_last=False, scratch=None, stream=None):
@@ -1151,11 +1159,11 @@ def ss_quant_rows(x, seq_last=False, scratch=None, stream=None):
         raise ValueError("x must have %s" % ("three axes" if seq_last else "an axis to quantise"))
     p = QuantParams()
     if seq_last:
-        p.batch, p.dim, p.seqlen = x.shape
+        p.batch, p.dim, p.seqlen = _counts(*x.shape)
         p.flags = SS_Q_X_SEQ_LAST
     else:
-        p.dim = x.shape[-1]
-        p.batch, p.seqlen = 1, x.numel() // max(1, p.dim)
+        p.dim, p.seqlen = _counts(x.shape[-1], x.numel() // max(1, x.shape[-1]))
+        p.batch = 1
     p.io_dtype = _io_code(x)
     p.x = _ptr(x, None, None, "x")
     rows = p.batch * p.seqlen
@@ -1171,7 +1179,7 @@ def ss_quant_rows(x, seq_last=False, scratch=None, stream=None):
 
 def _qlinear_sizes(batch, seqlen, dim, features, x_seq_last, out_seq_last, quantised):
     p = QLinearParams()
-    p.batch, p.seqlen, p.dim, p.features = batch, seqlen, dim, features
+    p.batch, p.seqlen, p.dim, p.features = _counts(batch, seqlen, dim, features)
     p.flags = ((SS_Q_X_SEQ_LAST if x_seq_last else 0) | (SS_Q_OUT_SEQ_LAST if out_seq_last else 0)
                | (SS_Q_X_QUANTISED if quantised else 0))
     return p
