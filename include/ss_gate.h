@@ -13,7 +13,8 @@
  *     h_t   = a_t h_{t-1} + m_t g_t x[b,d,t]
  *     out_t = h_t * z_t * sigmoid(z_t) if SS_GATE_HAS_Z, else h_t      (Section 3.4 gate)
  *
- * with h_{-1} = h0[b,d] (SS_GATE_HAS_H0) or 0, and h_last = h_{L-1}.  With SS_GATE_HAS_RESET, where
+ * with h_{-1} = h0[b,d] (SS_GATE_HAS_H0) or 0, and h_last = h_{L-1} (whose memory may be that of h0, and dh0's that of
+ * dh_last: a state that is carried on in place).  With SS_GATE_HAS_RESET, where
  * reset[b,t] is not 0, a_t = 0 and m_t = 1: a sequence begins at t (documents packed into one
  * row; the boundary resetting of Section 3.5.2), and nothing of what stands before t, an infinity
  * or NaN included, reaches t or anything behind it, forward or backward.

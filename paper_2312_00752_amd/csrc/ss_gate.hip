@@ -333,7 +333,7 @@ __global__ __launch_bounds__(gate_threads<TEAM>()) void gate_fwd_kernel(GateArgs
     const uint8_t* reset = RST ? a.reset + (int64_t)at.b * a.L : nullptr;
     const int seg = blockIdx.y, p0 = seg * a.spp, p1 = min(p0 + a.spp, a.pieces);
     float c = 0.0f;   // the state before what the team has at hand
-    if (seg > 0) c = a.carry[(int64_t)seg * a.R + at.row];
+    if (a.nseg > 1) c = a.carry[(int64_t)seg * a.R + at.row];   // the first segment's too: h_last, which the last one writes, may be h0
     else if (a.flags & SS_GATE_HAS_H0) c = a.h0[at.row];
     __shared__ float2 maps[2][TEAM];
     TeamScan<TEAM, false, RST> team{maps};
@@ -501,7 +501,7 @@ __global__ __launch_bounds__(gate_threads<TEAM>()) void gate_bwd_kernel(GateArgs
     const uint8_t* reset = RST ? a.reset + (int64_t)at.b * a.L : nullptr;
     const int seg = blockIdx.y, p0 = seg * a.spp, p1 = min(p0 + a.spp, a.pieces);
     float c = 0.0f;   // G behind the piece
-    if (seg < a.nseg - 1) c = a.carry[(int64_t)seg * a.R + at.row];
+    if (a.nseg > 1) c = a.carry[(int64_t)seg * a.R + at.row];   // the last segment's too: dh0, which the first one writes, may be dh_last
     else if (a.dh_last) c = a.dh_last[at.row];
     const float k = -GATE_LOG2E * ch.rate, rate2 = 2.0f * ch.rate;
     float sum_q = 0.0f, sum_f = 0.0f, sum_i = 0.0f;
