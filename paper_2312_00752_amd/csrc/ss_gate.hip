@@ -211,7 +211,8 @@ __host__ __device__ __forceinline__ uint2 marks_settle(uint2 m, int t0, int L)
 __device__ __forceinline__ bool marked(uint2 m, int j) { return ((j < 4 ? m.x : m.y) & (0xffu << (8 * (j & 3)))) != 0; }
 
 // ---- the gates of one step ------------------------------------------------------------------
-// sigmoid by the hardware's exponential and reciprocal (1 ulp each): relative error below 3e-7 everywhere
+// sigmoid by the hardware's exponential and reciprocal (1 ulp each).  The exponential's argument is rounded, so the relative error grows
+// with |v|: at most (1.25 |v| + 6) 2^-24, 1e-6 at -8 and 7e-6 at -87; below -87.33, where it is less than 2^-126, it becomes 0.
 __device__ __forceinline__ float gate_sigmoid(float v) { return rcp_fast(1.0f + exp2_fast(-GATE_LOG2E * v)); }
 // 1 - a^2 with a = exp(-y / 2): the difference loses 2^-24 / y, so below y = 1/8 the series y (1 - y/2 + y^2/6 - ...), whose
 // first term left out is y^5 / 720 (4e-8); the difference is off by 1e-6 there and less above.
