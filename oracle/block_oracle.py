@@ -86,9 +86,9 @@ def gate_bwd(dout, x, f, rate, i=None, z=None, f_bias=None, i_bias=None, reset=N
     with np.errstate(divide="ignore", invalid="ignore"):
         slope = np.where(m > 0.0, a * a / m, 0.0)   # -dm / d(log a)
         dla = np.where(mark, 0.0, lam * (before * a - g * x * slope))
-    df = dla * la * (1.0 - s)
+    with np.errstate(invalid="ignore"):   # at a mark the logit, whatever it is, has no part
+        df, dr = np.where(mark, 0.0, dla * la * (1.0 - s)), np.where(mark, 0.0, -dla * s)
     r["df"], r["df_bias"], r["df_bias_size"] = df, df.sum((0, 2)), np.abs(df).sum((0, 2))
-    dr = -dla * s
     r["drate"], r["drate_size"] = dr.sum((0, 2)), np.abs(dr).sum((0, 2))
     return r
 
