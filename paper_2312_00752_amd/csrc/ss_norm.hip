@@ -60,7 +60,8 @@ struct RowSum {
 
 // Threads of a workgroup and the rows it works on side by side.
 template <int G> constexpr int norm_threads(bool bwd) { return G > WAVE ? G : (bwd ? 512 : 256); }
-// The next row is requested before this one is worked on, but with 1024 lanes, which have 128 registers each.
+// The next row is requested before this one is worked on, but with 1024 lanes, which have 128 registers each (the backward kernels spill
+// of them: 3 to 5 in float32, 14 to 22 in bf16 and with a float32 residual).
 template <int G> constexpr bool norm_ahead() { return G < 1024; }
 
 __device__ __forceinline__ void load_columns(const float* p, int at, int width, float none, float (&v)[8])
@@ -377,8 +378,9 @@ __global__ __launch_bounds__(1024) void norm_parts_kernel(const float* part, flo
 }
 
 // ---- rows that do not fit the registers of a workgroup ------------------------------------------
-// A workgroup a row at a time, which is read once for each sweep, after the first from the caches.  2048 x 20000 bf16: 80 us forward (164 MB),
-// 75 + 40 backward.
+// A workgroup a row at a time, which is read once for each sweep, after the first from the caches.  An element a thread and access, which
+// is what bounds them: 2048 x 20000 bf16 (164 MB), not in a cache, 101 us forward and 143 a backward call (float32 127 and 211); in a cache 80 and
+// 115.  Kept simple, as rows this wide are few.
 template <typename T, typename S, bool RES>
 __global__ __launch_bounds__(1024) void norm_fwd_wide_kernel(NormArgs a)
 {
@@ -506,7 +508,8 @@ void with_form(NormForm f, F go)
 // counts between leave units idle at the end.  us of a call with 128 / 256 / 384 / 512 / 768 (rows x columns, no residual): bf16 16384 x 1024 27.4 22.9
 // 27.8 27.3 31.4, 2048 x 16384 67.5 55.3 67.4 71.2 86.0, 500 x 8192 16.6 19.6 21.0 24.2 23.9, 2048 x 2048 20.8 15.1 15.5 15.0 16.9; workgroups of 256 lanes are too
 // few to keep memory busy then: 16384 x 2048 113 62.6 52.0 43.2 39.4, 8192 x 4096 81.1 48.5 45.4 44.2 45.1 (float32 134 80.3 84.3 78.5
-// 81.8 and 111 78.8 87.3 82.5 85.3).
+// 81.8 and 111 78.8 87.3 82.5 85.3).  512 for both types and all rows from 4096 on:
+// the least over these four together, though 768 (251.6 us against 248.4) is ahead in the first.
 int norm_parts(int rows, int width)
 {
     const NormForm f = norm_form(rows, width, true);

@@ -110,7 +110,8 @@ __global__ __launch_bounds__(G > 256 ? G : 256) void quant_rows_kernel(const T* 
     }
     if (gl == 0) scale[row] = s.scale;
 }
-// Rows that do not fit: a workgroup a row, read twice, the second time from the caches.  2048 x 20000 bf16 57 us.
+// Rows that do not fit: a workgroup a row, read twice, the second time from the caches.  An element a thread and access, which
+// is what bounds it: 2048 x 20000 bf16 (123 MB) 57 us, 2.2 TB/s; kept simple, as rows this wide are few.
 template <typename T>
 __global__ __launch_bounds__(1024) void quant_rows_wide_kernel(const T* x, int8_t* q, float* scale, int dim, int pitch)
 {
@@ -684,7 +685,11 @@ __global__ __launch_bounds__(WAVES* WAVE) void qfew_kernel(QFewArgs a)
 // Where the tiles begin to pay: 33 tokens, weights and tokens not in a cache, the quantiser's launch included, would take here (four groups
 // of 16) / take in tiles of 64 (us) 13.4 / 11.9 at 2048 x 8192, 14.3 / 16.1 at 4096 x 2048, 8.1 / 7.4 at 768 x 3008, 9.5 / 9.4 at 1500 x 700.
 constexpr int FEW_TOKENS = 32;
-// Waves of a workgroup: enough to fill the chip with (8 to a compute unit), while each has a unit.
+// Waves of a workgroup: enough to fill the chip with (8 to a compute unit), while each has a unit.  us with 4 / 8 / 16 of them, weights
+// and tokens not in a cache, one token and 16: 2048 x 8192 (dim x features) 6.2 7.8 13.1 and 10.3 11.6 15.9, 768 x 16384 7.5 12.6 23.2 and 11.5
+// 15.5 26.4, 768 x 3008 4.0 4.9 6.8 and 7.0 7.5 8.0, 2560 x 5120 7.6 7.5 12.9 and 12.3 12.3 16.5, 5120 x 2560 8.5 8.5 7.7 and 12.9 12.3 12.5.  The
+// lines between them are rough: fewer are ahead at 4096 x 2048 (6.5 5.7 7.4 and 10.7 9.6 11.5, 16 are taken), 2048 x 4096 (4.9 5.8 7.6 and 8.4 8.8
+// 10.4, 8 are taken) and 1500 x 700 (4.0 4.8 6.7 and 7.3 7.8 9.6, 8 are taken), more at 8192 x 8192 (16.9 15.5 16.7 and 24.7 22.7 23.8, 4 are taken).
 int few_waves(int features, int pitch)
 {
     const int blocks = (features + 15) / 16;
