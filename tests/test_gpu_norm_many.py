@@ -39,3 +39,5 @@ def test_many_wide_rows():
     B.ss_norm_fwd(x, out=x)
     assert torch.equal(x[:3], want[:3]) and torch.equal(x[-7:], want[3:])
     assert not x[3:100].any() and not x[-107:-7].any()
+    del x
+    torch.cuda.empty_cache()
