@@ -121,10 +121,10 @@ def selective_ssm_layer(x, z, conv_w, conv_b, W_x, W_dt, dt_bias, A, Dskip):
 
 class _LayerNorm(torch.autograd.Function):
     @staticmethod
-    def forward(ctx, x, weight, bias, residual, eps):
-        out, summed, stats = B.ss_norm_fwd(x, weight, bias, residual=residual, eps=eps, save_stats=True)
+    def forward(ctx, x, weight, bias, residual, eps, rms=False):
+        out, summed, stats = B.ss_norm_fwd(x, weight, bias, residual=residual, eps=eps, save_stats=True, rms=rms)
         ctx.save_for_backward(x if summed is None else summed, weight, stats)
-        ctx.opts = (bias is not None, None if residual is None else residual.dtype, eps, x.dtype)
+        ctx.opts = (bias is not None, None if residual is None else residual.dtype, eps, x.dtype, rms)
         ctx.set_materialize_grads(False)
         return out if summed is None else (out, summed)
 
@@ -132,22 +132,31 @@ class _LayerNorm(torch.autograd.Function):
     @last_derivative
     def backward(ctx, dout, dsummed=None):
         s, weight, stats = ctx.saved_tensors
-        has_bias, held, eps, io = ctx.opts
+        has_bias, held, eps, io, rms = ctx.opts
         if dout is None:   # only the sum was used
-            return (None if dsummed is None else dsummed.to(io)), None, None, dsummed, None
+            return (None if dsummed is None else dsummed.to(io)), None, None, dsummed, None, None
         g = B.ss_norm_bwd(dout.contiguous(), s, stats, weight, has_bias=has_bias, residual_dtype=held, eps=eps,
-                          dsummed=None if dsummed is None else dsummed.contiguous())
-        return g["dx"], g["dweight"], g["dbias"], g["dresidual"], None
+                          dsummed=None if dsummed is None else dsummed.contiguous(), rms=rms)
+        return g["dx"], g["dweight"], g["dbias"], g["dresidual"], None, None
+
+
+def _norm(x, weight, bias, residual, eps, rms):
+    if x.is_cuda:
+        r = B.layer_norm_node(x, weight, bias, residual, eps, rms)
+        if r is not None:
+            return r if residual is not None else r[0]
+    return _LayerNorm.apply(x, weight, bias, residual, eps, rms)
 
 
 def layer_norm(x, weight=None, bias=None, residual=None, eps=1e-5):
     """Differentiable layer norm over the last axis.  With ``residual`` (float32 or x's dtype) the sum of the two is normalised
     and returned as well, in residual's dtype: (out, summed), the residual stream that the next block continues."""
-    if x.is_cuda:
-        r = B.layer_norm_node(x, weight, bias, residual, eps)
-        if r is not None:
-            return r if residual is not None else r[0]
-    return _LayerNorm.apply(x, weight, bias, residual, eps)
+    return _norm(x, weight, bias, residual, eps, False)
+
+
+def rms_norm(x, weight=None, bias=None, residual=None, eps=1e-5):
+    """Differentiable root-mean-square norm over the last axis: ``layer_norm`` without taking the mean off."""
+    return _norm(x, weight, bias, residual, eps, True)
 
 
 class _GatedRecurrence(torch.autograd.Function):

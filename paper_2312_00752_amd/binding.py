@@ -119,6 +119,10 @@ class NormParams(ctypes.Structure):
                 ("summed", _vp), ("stats", _vp)]
 
 
+class NormQuantParams(ctypes.Structure):
+    _fields_ = [("fwd", NormParams), ("q", _vp), ("scale", _vp)]
+
+
 class NormBwdParams(ctypes.Structure):
     _fields_ = [("fwd", NormParams), ("dout", _vp), ("dsummed", _vp), ("dx", _vp), ("dresidual", _vp),
                 ("dweight", _vp), ("dbias", _vp), ("workspace", _vp), ("workspace_bytes", ctypes.c_size_t)]
@@ -161,6 +165,7 @@ SS_ERR_BACKEND = -7
 SS_CONV_SILU, SS_CONV_HAS_BIAS, SS_CONV_HAS_STATE, SS_CONV_WRITE_STATE = 1, 2, 4, 8
 SS_CONV_MAX_WIDTH = 4
 SS_NORM_HAS_WEIGHT, SS_NORM_HAS_BIAS, SS_NORM_HAS_RESIDUAL, SS_NORM_RESIDUAL_F32, SS_NORM_SAVE_STATS = 1, 2, 4, 8, 16
+SS_NORM_RMS = 64
 SS_GATE_HAS_I, SS_GATE_HAS_Z, SS_GATE_HAS_F_BIAS, SS_GATE_HAS_I_BIAS = 1, 2, 4, 8
 SS_GATE_HAS_RESET, SS_GATE_HAS_H0, SS_GATE_WRITE_H_LAST, SS_GATE_SAVE_FOR_BWD = 16, 32, 64, 128
 SS_Q_X_SEQ_LAST, SS_Q_OUT_SEQ_LAST, SS_Q_HAS_BIAS, SS_Q_X_QUANTISED = 1, 2, 4, 8
@@ -211,7 +216,8 @@ def lib():
         l.ss_proj_gemm_workspace_bytes.argtypes = [ctypes.POINTER(GemmParams)]
         l.ss_proj_gemm_workspace_bytes.restype = ctypes.c_size_t
         l.ss_strerror.argtypes = [ctypes.c_int]
-        for name, params in (("ss_norm_fwd", NormParams), ("ss_norm_bwd", NormBwdParams), ("ss_gate_fwd", GateParams),
+        for name, params in (("ss_norm_fwd", NormParams), ("ss_norm_quant", NormQuantParams), ("ss_norm_bwd", NormBwdParams),
+                             ("ss_gate_fwd", GateParams),
                              ("ss_gate_bwd", GateBwdParams), ("ss_gate_step", GateStepParams), ("ss_quant_rows", QuantParams),
                              ("ss_qlinear", QLinearParams)):
             getattr(l, name).restype = ctypes.c_int
@@ -237,7 +243,7 @@ class _NoMarshal:
         return None
 
     step = layer_step = scan_fwd = scan_bwd = layer_fwd = layer_bwd = staticmethod(_none)
-    norm_fwd = norm_bwd = gate_fwd = gate_bwd = gate_step = qlinear = layer_norm = gated_recurrence = staticmethod(_none)
+    norm_fwd = norm_quant = norm_bwd = gate_fwd = gate_bwd = gate_step = qlinear = layer_norm = gated_recurrence = staticmethod(_none)
 
 
 def _marshal():
@@ -834,7 +840,7 @@ def ss_proj_gemm_workspace_bytes(C):
     return int(lib().ss_proj_gemm_workspace_bytes(ctypes.byref(p)))
 
 
-# ---------------------------------------------------------------- layer norm
+# ---------------------------------------------------------------- layer norm and RMS norm
 def _check(rc):
     if rc != SS_OK:
         raise SsError(rc)
@@ -867,7 +873,7 @@ def _lend(given, need, device, name):
     return _ptr(given, torch.uint8, None, name), given.numel()
 
 
-def _norm_params(x, weight, bias, residual, eps):
+def _norm_params(x, weight, bias, residual, eps, rms):
     f32 = torch.float32
     if x.dim() < 1:
         raise ValueError("a tensor without axes cannot be normalised")
@@ -875,6 +881,7 @@ def _norm_params(x, weight, bias, residual, eps):
     width = x.shape[-1]
     p.rows, p.width = _counts(x.numel() // width if width else 0, width)
     p.eps = eps
+    p.flags = SS_NORM_RMS if rms else 0
     if weight is not None:
         p.weight = _ptr(weight, f32, (width,), "weight")
         p.flags |= SS_NORM_HAS_WEIGHT
@@ -888,23 +895,9 @@ def _norm_params(x, weight, bias, residual, eps):
     return p
 
 
-def ss_norm_fwd(x, weight=None, bias=None, residual=None, eps=1e-5, out=None, summed=None, save_stats=False, stream=None):
-    """Enqueue layer norm over the last axis, of ``x`` or of ``x + residual`` (float32 or of x's dtype; the sum is held in its
-    dtype and normalised as held).  Returns (out, summed or None, stats or None); ``summed`` may be given as ``residual`` itself,
-    ``stats`` (2, rows) is what ``ss_norm_bwd`` needs."""
-    if stream is not None:
-        with _current(stream):
-            return ss_norm_fwd(x, weight, bias, residual, eps, out, summed, save_stats)
-    if out is None and summed is None and x.is_cuda:
-        r = (_native or _marshal()).norm_fwd(x, weight, bias, residual, eps, bool(save_stats), _stream(stream))
-        if r is not None:
-            return _result(r)
-    p = _norm_params(x, weight, bias, residual, eps)
+def _norm_inputs(p, x, residual, summed):
     p.io_dtype = _io_code(x)
     p.x = _ptr(x, None, None, "x")
-    if out is None:
-        out = torch.empty_like(x)
-    p.out = _ptr(out, x.dtype, x.shape, "out")
     if residual is not None:
         p.residual = _ptr(residual, None, x.shape, "residual")
         if summed is None:
@@ -912,13 +905,52 @@ def ss_norm_fwd(x, weight=None, bias=None, residual=None, eps=1e-5, out=None, su
         p.summed = _ptr(summed, residual.dtype, x.shape, "summed")
     elif summed is not None:
         raise ValueError("summed is given, residual is not")
+    return summed
+
+
+def ss_norm_fwd(x, weight=None, bias=None, residual=None, eps=1e-5, out=None, summed=None, save_stats=False, stream=None, rms=False):
+    """Enqueue layer norm over the last axis, with ``rms`` root-mean-square norm, of ``x`` or of ``x + residual`` (float32 or of x's
+    dtype; the sum is held in its dtype and normalised as held).  Returns (out, summed or None, stats or None); ``summed`` may be given as
+    ``residual`` itself, ``stats`` (2, rows), with ``rms`` (rows), is what ``ss_norm_bwd`` needs."""
+    if stream is not None:
+        with _current(stream):
+            return ss_norm_fwd(x, weight, bias, residual, eps, out, summed, save_stats, None, rms)
+    if out is None and summed is None and x.is_cuda:
+        r = (_native or _marshal()).norm_fwd(x, weight, bias, residual, eps, bool(rms), bool(save_stats), _stream(stream))
+        if r is not None:
+            return _result(r)
+    p = _norm_params(x, weight, bias, residual, eps, rms)
+    summed = _norm_inputs(p, x, residual, summed)
+    if out is None:
+        out = torch.empty_like(x)
+    p.out = _ptr(out, x.dtype, x.shape, "out")
     stats = None
     if save_stats:
-        stats = torch.empty((2, p.rows), dtype=torch.float32, device=x.device)
+        stats = torch.empty((p.rows,) if rms else (2, p.rows), dtype=torch.float32, device=x.device)
         p.stats = stats.data_ptr()
         p.flags |= SS_NORM_SAVE_STATS
     _check(lib().ss_norm_fwd(ctypes.byref(p), _stream(stream)))
     return out, summed, stats
+
+
+def ss_norm_quant(x, weight=None, bias=None, residual=None, eps=1e-5, rms=False, summed=None, stream=None):
+    """Enqueue the norm of ``ss_norm_fwd`` with its result in 8 bits, as ``ss_qlinear`` takes it with ``x_scale``: the bits that
+    ``ss_quant_rows`` makes of that call's result.  Returns (q, scale, summed or None): q (rows, ss_quant_pitch(width)) int8, scale (rows)."""
+    if stream is not None:
+        with _current(stream):
+            return ss_norm_quant(x, weight, bias, residual, eps, rms, summed)
+    if summed is None and x.is_cuda:
+        r = (_native or _marshal()).norm_quant(x, weight, bias, residual, eps, bool(rms), _stream(stream))
+        if r is not None:
+            return _result(r)
+    p = NormQuantParams()
+    p.fwd = _norm_params(x, weight, bias, residual, eps, rms)
+    summed = _norm_inputs(p.fwd, x, residual, summed)
+    q = torch.empty((p.fwd.rows, ss_quant_pitch(p.fwd.width)), dtype=torch.int8, device=x.device)
+    scale = torch.empty(p.fwd.rows, dtype=torch.float32, device=x.device)
+    p.q, p.scale = q.data_ptr(), scale.data_ptr()
+    _check(lib().ss_norm_quant(ctypes.byref(p), _stream(stream)))
+    return q, scale, summed
 
 
 def ss_norm_workspace_bytes(rows, width):
@@ -927,19 +959,21 @@ def ss_norm_workspace_bytes(rows, width):
     return int(lib().ss_norm_workspace_bytes(ctypes.byref(p)))
 
 
-def ss_norm_bwd(dout, s, stats, weight=None, has_bias=False, residual_dtype=None, dsummed=None, eps=1e-5, workspace=None, stream=None):
+def ss_norm_bwd(dout, s, stats, weight=None, has_bias=False, residual_dtype=None, dsummed=None, eps=1e-5, workspace=None, stream=None,
+                rms=False):
     """Enqueue the backward pass.  ``s`` is what was normalised (``summed``, or ``x`` of a call without a residual, with
     ``residual_dtype`` None) and ``dsummed`` the gradient that reaches the sum from behind, or None.  Returns a dict with dx,
     dresidual (dx itself where the dtypes agree), dweight and dbias."""
     if stream is not None:
         with _current(stream):
-            return ss_norm_bwd(dout, s, stats, weight, has_bias, residual_dtype, dsummed, eps, workspace)
+            return ss_norm_bwd(dout, s, stats, weight, has_bias, residual_dtype, dsummed, eps, workspace, None, rms)
     if workspace is None and dout.is_cuda and (residual_dtype is None or s.dtype == residual_dtype):
-        r = (_native or _marshal()).norm_bwd(dout, s, stats, weight, bool(has_bias), residual_dtype is not None, dsummed, eps, _stream(stream))
+        r = (_native or _marshal()).norm_bwd(dout, s, stats, weight, bool(has_bias), residual_dtype is not None, dsummed, eps, bool(rms),
+                                             _stream(stream))
         if r is not None:
             return _result(r)
     p = NormBwdParams()
-    p.fwd = _norm_params(dout, weight, None, None, eps)
+    p.fwd = _norm_params(dout, weight, None, None, eps, rms)
     p.fwd.io_dtype = _io_code(dout)
     held = dout.dtype if residual_dtype is None else residual_dtype
     if has_bias:
@@ -954,7 +988,7 @@ def ss_norm_bwd(dout, s, stats, weight=None, has_bias=False, residual_dtype=None
         if dsummed is not None:
             raise ValueError("dsummed without a residual")
         p.fwd.x = _ptr(s, held, dout.shape, "s")
-    p.fwd.stats = _ptr(stats, torch.float32, (2, p.fwd.rows), "stats")
+    p.fwd.stats = _ptr(stats, torch.float32, (p.fwd.rows,) if rms else (2, p.fwd.rows), "stats")
     p.dout = _ptr(dout, None, None, "dout")
     dev, width = dout.device, p.fwd.width
     g = {"dx": torch.empty_like(dout), "dresidual": None,
@@ -1248,9 +1282,9 @@ def ss_qlinear(x, weight, scale, bias=None, x_seq_last=False, out_seq_last=False
 
 
 # ---------------------------------------------------------------- gradient functions of the compiled module
-def layer_norm_node(x, weight, bias, residual, eps):
-    """(out,) or (out, summed) of autograd.layer_norm from the compiled module, or None where it does not serve the call."""
-    r = (_native or _marshal()).layer_norm(x, weight, bias, residual, eps, _stream(None))
+def layer_norm_node(x, weight, bias, residual, eps, rms=False):
+    """(out,) or (out, summed) of autograd.layer_norm or rms_norm from the compiled module, or None where it does not serve the call."""
+    r = (_native or _marshal()).layer_norm(x, weight, bias, residual, eps, rms, _stream(None))
     return r if r is None else _result(r)
 
 

@@ -1,4 +1,4 @@
-"""A block made of the library's operators: layer norm with the residual stream, a projection, the gated linear recurrence, a
+"""A block made of the library's operators: layer or RMS norm with the residual stream, a projection, the gated linear recurrence, a
 projection back (the homogeneous block of arXiv 2312.00752, Section 3.4, with the recurrence of its Theorem 1 in the scan's place).
 
     h, residual = norm(x + residual)
@@ -63,14 +63,17 @@ class _ProjectionBack(torch.autograd.Function):
 
 
 class GatedBlock(torch.nn.Module):
-    """x (B,L,width) of ``dtype``; the residual stream is float32 or of that type.  Calls give (out, residual)."""
+    """x (B,L,width) of ``dtype``; the residual stream is float32 or of that type.  ``norm`` is "layer" or "rms" (which has no bias).
+    Calls give (out, residual)."""
 
-    def __init__(self, width, inner, dtype=torch.float32, device="cuda", eps=1e-5):
+    def __init__(self, width, inner, dtype=torch.float32, device="cuda", eps=1e-5, norm="layer"):
         super().__init__()
-        self.inner, self.eps = inner, eps
+        if norm not in ("layer", "rms"):
+            raise ValueError("norm must be \"layer\" or \"rms\", got %r" % (norm,))
+        self.inner, self.eps, self.rms = inner, eps, norm == "rms"
         f32 = {"dtype": torch.float32, "device": device}
         self.norm_weight = torch.nn.Parameter(torch.ones(width, **f32))
-        self.norm_bias = torch.nn.Parameter(torch.zeros(width, **f32))
+        self.norm_bias = None if self.rms else torch.nn.Parameter(torch.zeros(width, **f32))
         self.W_in = torch.nn.Parameter((torch.randn(4 * inner, width, **f32) * width ** -0.5).to(dtype))
         self.W_out = torch.nn.Parameter((torch.randn(width, inner, **f32) * inner ** -0.5).to(dtype))
         # decays at a logit of 0 between 0.9 and 0.999, as rate sigmoid(f_bias) = -log a
@@ -85,7 +88,8 @@ class GatedBlock(torch.nn.Module):
     def forward(self, x, residual=None, reset=None):
         if residual is None:
             residual = torch.zeros_like(x)
-        h, residual = autograd.layer_norm(x, self.norm_weight, self.norm_bias, residual=residual, eps=self.eps)
+        norm = autograd.rms_norm if self.rms else autograd.layer_norm
+        h, residual = norm(x, self.norm_weight, self.norm_bias, residual=residual, eps=self.eps)
         xs, f, i, z = _Projection.apply(self.W_in, h).chunk(4, 1)
         y = autograd.gated_recurrence(xs, f, self.rate(), i=i, z=z, f_bias=self.f_bias, i_bias=self.i_bias, reset=reset)
         return _ProjectionBack.apply(self.W_out, y), residual
@@ -100,8 +104,8 @@ class ServedBlock:
 
     @torch.no_grad()
     def __init__(self, block):
-        own = lambda v: v.detach().clone()   # as the 8-bit weights and the rate are: training goes on without this block
-        self.norm_weight, self.norm_bias, self.eps = own(block.norm_weight), own(block.norm_bias), block.eps
+        own = lambda v: v if v is None else v.detach().clone()   # as the 8-bit weights and the rate are: training goes on without this block
+        self.norm_weight, self.norm_bias, self.eps, self.rms = own(block.norm_weight), own(block.norm_bias), block.eps, block.rms
         self.rate, self.f_bias, self.i_bias = block.rate(), own(block.f_bias), own(block.i_bias)
         self.W_in, self.in_scale = B.ss_quant_rows(block.W_in.detach())
         self.W_out, self.out_scale = B.ss_quant_rows(block.W_out.detach())
@@ -109,8 +113,9 @@ class ServedBlock:
     def prompt(self, x, residual=None, reset=None, state=None):
         if residual is None:
             residual = torch.zeros_like(x)
-        h, residual, _ = B.ss_norm_fwd(x, self.norm_weight, self.norm_bias, residual=residual, eps=self.eps)
-        xs, f, i, z = B.ss_qlinear(h, self.W_in, self.in_scale, out_seq_last=True).chunk(4, 1)
+        q, scale, residual = B.ss_norm_quant(x, self.norm_weight, self.norm_bias, residual=residual, eps=self.eps, rms=self.rms)
+        xs, f, i, z = B.ss_qlinear(q.view(*x.shape[:2], -1), self.W_in, self.in_scale, x_scale=scale, dim=x.shape[2], out_dtype=x.dtype,
+                                   out_seq_last=True).chunk(4, 1)
         y, state = B.ss_gate_fwd(xs, f, self.rate, i=i, z=z, f_bias=self.f_bias, i_bias=self.i_bias, reset=reset, h0=state,
                                  return_last_state=True)
         return B.ss_qlinear(y, self.W_out, self.out_scale, x_seq_last=True), residual, state
@@ -119,7 +124,8 @@ class ServedBlock:
         """One token: x_t (B,width).  Returns (out_t, residual_t)."""
         if residual_t is None:
             residual_t = torch.zeros_like(x_t)
-        h, residual_t, _ = B.ss_norm_fwd(x_t, self.norm_weight, self.norm_bias, residual=residual_t, eps=self.eps)
+        # the product of a few tokens brings them to 8 bits in its own launch
+        h, residual_t, _ = B.ss_norm_fwd(x_t, self.norm_weight, self.norm_bias, residual=residual_t, eps=self.eps, rms=self.rms)
         xs, f, i, z = B.ss_qlinear(h, self.W_in, self.in_scale).chunk(4, 1)
         y = B.ss_gate_step(state, xs, f, self.rate, i_t=i, z_t=z, f_bias=self.f_bias, i_bias=self.i_bias, reset_t=reset_t)
         return B.ss_qlinear(y, self.W_out, self.out_scale), residual_t

@@ -467,7 +467,7 @@ const at::Tensor* held(Args& a, int i, const at::Tensor& x)
 // The calls themselves, on tensors that have been looked at.  They hold no lock and are also what the gradient functions call.
 struct Norm {
     at::Tensor out, summed, stats;
-    int fwd(const at::Tensor& x, const at::Tensor& weight, const at::Tensor& bias, const at::Tensor& residual, double eps, bool save, void* stream)
+    int fwd(const at::Tensor& x, const at::Tensor& weight, const at::Tensor& bias, const at::Tensor& residual, double eps, bool rms, bool save, void* stream)
     {
         ss_norm_params p{};
         if (!norm_sizes(x, p)) return SS_ERR_SHAPE;
@@ -475,7 +475,7 @@ struct Norm {
         p.x = x.data_ptr();
         p.weight = data<const float>(weight);
         p.bias = data<const float>(bias);
-        p.flags = (weight.defined() ? SS_NORM_HAS_WEIGHT : 0u) | (bias.defined() ? SS_NORM_HAS_BIAS : 0u);
+        p.flags = (weight.defined() ? SS_NORM_HAS_WEIGHT : 0u) | (bias.defined() ? SS_NORM_HAS_BIAS : 0u) | (rms ? SS_NORM_RMS : 0u);
         out = empty_io(x);
         p.out = out.data_ptr();
         if (residual.defined()) {
@@ -486,7 +486,7 @@ struct Norm {
         }
         if (save) {
             p.flags |= SS_NORM_SAVE_STATS;
-            stats = empty_f32({2, p.rows}, x);
+            stats = rms ? empty_f32({p.rows}, x) : empty_f32({2, p.rows}, x);
             p.stats = data<float>(stats);
         }
         return ss_norm_fwd(&p, stream);
@@ -495,12 +495,13 @@ struct Norm {
 struct NormGrads {
     at::Tensor dx, dresidual, dweight, dbias;
     int bwd(const at::Tensor& dout, const at::Tensor& s, const at::Tensor& stats, const at::Tensor& weight, bool has_bias, bool res, const at::Tensor& more,
-            double eps, void* stream)
+            double eps, bool rms, void* stream)
     {
         ss_norm_bwd_params q{};
         ss_norm_params& p = q.fwd;
         if (!norm_sizes(dout, p)) return SS_ERR_SHAPE;
         p.eps = (float)eps;
+        p.flags = rms ? SS_NORM_RMS : 0u;
         p.stats = data<float>(stats);
         p.weight = data<const float>(weight);
         dx = empty_io(dout);
@@ -564,8 +565,30 @@ at::Tensor given(const Optional& t) { return t.has_value() ? *t : at::Tensor(); 
 Optional optional(const at::Tensor& t) { return t.defined() ? Optional(t) : Optional(); }
 void backward_check(int rc) { TORCH_CHECK(rc == SS_OK, "ss_scan error ", rc, ": ", ss_strerror(rc)); }
 
-// norm_fwd(x, weight, bias, residual, eps, save, stream) -> (out, summed or None, stats or None)
+// norm_fwd(x, weight, bias, residual, eps, rms, save, stream) -> (out, summed or None, stats or None)
 PyObject* py_norm_fwd(PyObject*, PyObject* const* argv, Py_ssize_t n)
+{
+    HANDLE_TH_ERRORS
+    if (n != 8) Py_RETURN_NONE;
+    Args a{argv};
+    at::Tensor t[4];
+    double eps;
+    if (!norm_tensors(a, 0, t) || !real_number(argv[4], eps)) Py_RETURN_NONE;
+    void* stream = a.stream(7);
+    if (!a.ok) Py_RETURN_NONE;
+    Norm c;
+    int rc;
+    {
+        Unlocked u;
+        rc = c.fwd(t[0], t[1], t[2], t[3], eps, argv[5] == Py_True, argv[6] == Py_True, stream);
+    }
+    if (rc != SS_OK) return PyLong_FromLong(rc);
+    return tuple_of({c.out, c.summed, c.stats});
+    END_HANDLE_TH_ERRORS
+}
+
+// norm_quant(x, weight, bias, residual, eps, rms, stream) -> (q, scale, summed or None)
+PyObject* py_norm_quant(PyObject*, PyObject* const* argv, Py_ssize_t n)
 {
     HANDLE_TH_ERRORS
     if (n != 7) Py_RETURN_NONE;
@@ -574,23 +597,37 @@ PyObject* py_norm_fwd(PyObject*, PyObject* const* argv, Py_ssize_t n)
     double eps;
     if (!norm_tensors(a, 0, t) || !real_number(argv[4], eps)) Py_RETURN_NONE;
     void* stream = a.stream(6);
-    if (!a.ok) Py_RETURN_NONE;
-    Norm c;
-    int rc;
-    {
-        Unlocked u;
-        rc = c.fwd(t[0], t[1], t[2], t[3], eps, argv[5] == Py_True, stream);
+    ss_norm_quant_params p{};
+    if (!a.ok || !norm_sizes(t[0], p.fwd) || !p.fwd.width) Py_RETURN_NONE;
+    p.fwd.eps = (float)eps;
+    p.fwd.flags = argv[5] == Py_True ? SS_NORM_RMS : 0u;
+    p.fwd.x = t[0].data_ptr();
+    p.fwd.weight = data<const float>(t[1]);
+    p.fwd.bias = data<const float>(t[2]);
+    if (t[1].defined()) p.fwd.flags |= SS_NORM_HAS_WEIGHT;
+    if (t[2].defined()) p.fwd.flags |= SS_NORM_HAS_BIAS;
+    at::Tensor summed;
+    if (t[3].defined()) {
+        p.fwd.flags |= SS_NORM_HAS_RESIDUAL | (t[3].scalar_type() == at::kFloat ? SS_NORM_RESIDUAL_F32 : 0u);
+        p.fwd.residual = t[3].data_ptr();
+        summed = empty_io(t[3]);
+        p.fwd.summed = summed.data_ptr();
     }
+    const at::Tensor q = at::empty({p.fwd.rows, (int64_t)ss_quant_pitch(p.fwd.width)}, t[0].options().dtype(at::kChar).requires_grad(false));
+    const at::Tensor scale = empty_f32({p.fwd.rows}, t[0]);
+    p.q = static_cast<int8_t*>(q.data_ptr());
+    p.scale = data<float>(scale);
+    const int rc = call(ss_norm_quant, p, stream);
     if (rc != SS_OK) return PyLong_FromLong(rc);
-    return tuple_of({c.out, c.summed, c.stats});
+    return tuple_of({q, scale, summed});
     END_HANDLE_TH_ERRORS
 }
 
-// norm_bwd(dout, s, stats, weight, has_bias, has_residual, dsummed, eps, stream) -> dict of gradients
+// norm_bwd(dout, s, stats, weight, has_bias, has_residual, dsummed, eps, rms, stream) -> dict of gradients
 PyObject* py_norm_bwd(PyObject*, PyObject* const* argv, Py_ssize_t n)
 {
     HANDLE_TH_ERRORS
-    if (n != 9) Py_RETURN_NONE;
+    if (n != 10) Py_RETURN_NONE;
     Args a{argv};
     ss_norm_params p{};
     const at::Tensor* dout = a.tensor(0);
@@ -599,10 +636,12 @@ PyObject* py_norm_bwd(PyObject*, PyObject* const* argv, Py_ssize_t n)
     const bool res = argv[5] == Py_True;
     const at::Tensor* s = held(a, 1, *dout);
     if (!s || (!res && (s->scalar_type() != dout->scalar_type() || !a.none(6)))) Py_RETURN_NONE;
-    a.ptr(2, at::kFloat, {2, p.rows});
+    const bool rms = argv[8] == Py_True;
+    if (rms) a.ptr(2, at::kFloat, {p.rows});
+    else a.ptr(2, at::kFloat, {2, p.rows});
     a.ptr(3, at::kFloat, {p.width}, true);
     const at::Tensor* more = a.ok && !a.none(6) ? held(a, 6, *dout) : nullptr;
-    void* stream = a.stream(8);
+    void* stream = a.stream(9);
     if (!a.ok || (more && more->scalar_type() != s->scalar_type())) Py_RETURN_NONE;
     const at::Tensor& stats = THPVariable_Unpack(argv[2]);
     const at::Tensor weight = a.none(3) ? at::Tensor() : THPVariable_Unpack(argv[3]), dsummed = more ? *more : at::Tensor();
@@ -610,14 +649,14 @@ PyObject* py_norm_bwd(PyObject*, PyObject* const* argv, Py_ssize_t n)
     int rc;
     {
         Unlocked u;
-        rc = g.bwd(*dout, *s, stats, weight, argv[4] == Py_True, res, dsummed, eps, stream);
+        rc = g.bwd(*dout, *s, stats, weight, argv[4] == Py_True, res, dsummed, eps, rms, stream);
     }
     if (rc != SS_OK) return PyLong_FromLong(rc);
     return dict_of({{"dx", g.dx}, {"dresidual", g.dresidual}, {"dweight", g.dweight}, {"dbias", g.dbias}});
     END_HANDLE_TH_ERRORS
 }
 
-// Layer norm as a node of torch's graph (what autograd._LayerNorm is in Python): the backward pass runs on the stream of the forward pass,
+// Layer norm and RMS norm as a node of torch's graph (what autograd._LayerNorm is in Python): the backward pass runs on the stream of the forward pass,
 // which is also the one that torch makes current for it.
 // A backward pass's gradients have no graph of their own: where one is being built, they are connected to what they depend on through
 // an error, so that going through them again is refused whichever way it is asked for.
@@ -630,7 +669,7 @@ torch::autograd::variable_list differentiable_once(torch::autograd::variable_lis
             if (t.defined() && t.requires_grad()) sources.push_back(t);
     if (sources.empty()) return grads;
     const std::shared_ptr<torch::autograd::Node> error(
-        new torch::autograd::Error("the gradients of layer_norm and gated_recurrence cannot be differentiated again", torch::autograd::collect_next_edges(sources)),
+        new torch::autograd::Error("the gradients of this operator cannot be differentiated again", torch::autograd::collect_next_edges(sources)),
         torch::autograd::deleteNode);
     for (at::Tensor& g : grads)
         if (g.defined()) {
@@ -641,17 +680,18 @@ torch::autograd::variable_list differentiable_once(torch::autograd::variable_lis
 }
 struct NormFunction : torch::autograd::Function<NormFunction> {
     static torch::autograd::variable_list forward(torch::autograd::AutogradContext* ctx, const at::Tensor& x, const Optional& weight_, const Optional& bias_,
-                                                  const Optional& residual_, double eps, int64_t stream)
+                                                  const Optional& residual_, double eps, bool rms, int64_t stream)
     {
         const at::Tensor weight = given(weight_), bias = given(bias_), residual = given(residual_);
         Norm c;
-        const int rc = c.fwd(x, weight, bias, residual, eps, true, reinterpret_cast<void*>(stream));
+        const int rc = c.fwd(x, weight, bias, residual, eps, rms, true, reinterpret_cast<void*>(stream));
         if (rc != SS_OK) throw Refused{rc};
         ctx->set_materialize_grads(false);
         ctx->save_for_backward({residual.defined() ? c.summed : x, weight, c.stats});
         ctx->saved_data["bias"] = bias.defined();
         ctx->saved_data["residual"] = residual.defined();
         ctx->saved_data["eps"] = eps;
+        ctx->saved_data["rms"] = rms;
         ctx->saved_data["stream"] = stream;
         ctx->saved_data["io"] = (int64_t)x.scalar_type();
         if (residual.defined()) return {c.out, c.summed};
@@ -663,30 +703,31 @@ struct NormFunction : torch::autograd::Function<NormFunction> {
         const at::Tensor more = res && grads[1].defined() ? grads[1].contiguous() : at::Tensor();
         if (!grads[0].defined()) {   // only the sum was used
             const auto io = (at::ScalarType)ctx->saved_data["io"].toInt();
-            return differentiable_once({more.defined() ? more.to(io) : at::Tensor(), at::Tensor(), at::Tensor(), more, at::Tensor(), at::Tensor()}, {&grads});
+            return differentiable_once({more.defined() ? more.to(io) : at::Tensor(), at::Tensor(), at::Tensor(), more, at::Tensor(), at::Tensor(), at::Tensor()}, {&grads});
         }
         const auto saved = ctx->get_saved_variables();
         NormGrads g;
         backward_check(g.bwd(grads[0].contiguous(), saved[0], saved[2], saved[1], ctx->saved_data["bias"].toBool(), res, more,
-                             ctx->saved_data["eps"].toDouble(), reinterpret_cast<void*>(ctx->saved_data["stream"].toInt())));
-        return differentiable_once({g.dx, g.dweight, g.dbias, g.dresidual, at::Tensor(), at::Tensor()}, {&saved, &grads});
+                             ctx->saved_data["eps"].toDouble(), ctx->saved_data["rms"].toBool(), reinterpret_cast<void*>(ctx->saved_data["stream"].toInt())));
+        return differentiable_once({g.dx, g.dweight, g.dbias, g.dresidual, at::Tensor(), at::Tensor(), at::Tensor()}, {&saved, &grads});
     }
 };
-// layer_norm(x, weight, bias, residual, eps, stream) -> (out,) or (out, summed), with gradients
+// layer_norm(x, weight, bias, residual, eps, rms, stream) -> (out,) or (out, summed), with gradients
 PyObject* py_layer_norm(PyObject*, PyObject* const* argv, Py_ssize_t n)
 {
     HANDLE_TH_ERRORS
-    if (n != 6) Py_RETURN_NONE;
+    if (n != 7) Py_RETURN_NONE;
     Args a{argv};
     at::Tensor t[4];
     double eps;
     if (!norm_tensors(a, 0, t) || !real_number(argv[4], eps)) Py_RETURN_NONE;
-    void* stream = a.stream(5);
+    const bool rms = argv[5] == Py_True;
+    void* stream = a.stream(6);
     if (!a.ok) Py_RETURN_NONE;
     torch::autograd::variable_list r;
     try {
         Unlocked u;
-        r = NormFunction::apply(t[0], optional(t[1]), optional(t[2]), optional(t[3]), eps, reinterpret_cast<int64_t>(stream));
+        r = NormFunction::apply(t[0], optional(t[1]), optional(t[2]), optional(t[3]), eps, rms, reinterpret_cast<int64_t>(stream));
     } catch (const Refused& e) {
         return PyLong_FromLong(e.rc);
     }
@@ -1001,7 +1042,7 @@ PyObject* py_qlinear(PyObject*, PyObject* const* argv, Py_ssize_t n)
 
 #define SS_METHOD(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)(void)>(py_##name)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {SS_METHOD(step), SS_METHOD(layer_step), SS_METHOD(scan_fwd), SS_METHOD(scan_bwd),
-                         SS_METHOD(layer_fwd), SS_METHOD(layer_bwd), SS_METHOD(norm_fwd), SS_METHOD(norm_bwd), SS_METHOD(gate_fwd),
+                         SS_METHOD(layer_fwd), SS_METHOD(layer_bwd), SS_METHOD(norm_fwd), SS_METHOD(norm_quant), SS_METHOD(norm_bwd), SS_METHOD(gate_fwd),
                          SS_METHOD(gate_bwd), SS_METHOD(gate_step), SS_METHOD(qlinear), SS_METHOD(layer_norm), SS_METHOD(gated_recurrence), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_marshal", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

@@ -1,16 +1,18 @@
-// Layer norm with the residual sum before it, forward and backward, for gfx950, with the C-ABI entry
-// points (see include/ss_norm.h).
+// Layer norm and root-mean-square norm with the residual sum before them, forward and backward, the forward pass also with a result in
+// 8 bits, for gfx950, with the C-ABI entry points (see include/ss_norm.h).
 //
 // Both passes move a few values per element and compute about ten operations on each, so they are bound by HBM and
 // every tensor is touched once: a row is held in the registers of the G lanes that share it, the mean is taken, then the variance
 // about that mean (two sweeps over registers, exact to float32 where a sum of squares would cancel), then the result is
-// formed.  A group of lanes walks rows with the weights of its columns in registers.  The backward pass keeps its columns' sums
+// formed.  RMS: no mean is taken off, so one sum is enough (with a mean of 0 the rest is the same).  A group of lanes walks rows with the weights of its columns in registers.  The backward pass keeps its columns' sums
 // for dweight and dbias in registers as well; a workgroup's go to the workspace and a second kernel adds them up in a fixed order.
 #include <hip/hip_runtime.h>
 #include <cmath>
 #include <type_traits>
 
 #include "ss_norm.h"
+#include "ss_quant.h"
+#include "ss_round8.h"
 #include "ss_slices.h"
 
 namespace ss {
@@ -26,6 +28,9 @@ struct NormArgs {
     void *dx, *dresidual;
     float *dweight, *dbias;
     float* part;   // (parts, 2, width)
+    int8_t* q;     // 8-bit result: rows `pitch` bytes apart
+    float* scale;
+    int pitch;
 };
 
 // ---- sums over the G lanes of a row -----------------------------------------------------------
@@ -58,6 +63,27 @@ struct RowSum {
     }
 };
 
+// The largest of the lanes' values, the same way.
+template <int G>
+struct RowMax {
+    static constexpr int WAVES = G > WAVE ? G / WAVE : 1;
+    uint32_t (*lds)[WAVES];
+    int turn = 0;
+    __device__ __forceinline__ uint32_t operator()(uint32_t v)
+    {
+#pragma unroll
+        for (int s = 1; s < (G < WAVE ? G : WAVE); s *= 2) v = max(v, (uint32_t)__shfl_xor((int)v, s));
+        if constexpr (G > WAVE) {
+            if (threadIdx.x % WAVE == 0) lds[turn][threadIdx.x / WAVE] = v;
+            __syncthreads();
+#pragma unroll
+            for (int w = 0; w < WAVES; ++w) v = max(v, lds[turn][w]);
+            turn ^= 1;
+        }
+        return v;
+    }
+};
+
 // Threads of a workgroup and the rows it works on side by side.
 template <int G> constexpr int norm_threads(bool bwd) { return G > WAVE ? G : (bwd ? 512 : 256); }
 // The next row is requested before this one is worked on, but with 1024 lanes, which have 128 registers each (the backward kernels spill
@@ -80,12 +106,15 @@ __device__ __forceinline__ void load_columns(const float* p, int at, int width, 
 
 // Lane l of the G of a row has slices l, l + G, ... (V of them).  At the rate of a large copy (5.15 TB/s): 16384 x 2048 bf16 with a
 // residual of float32 (403 MB) 79 us, of bf16 (268 MB) 47; 2048 x 16384 (134 MB) 27.  One row of 2048 is a launch, 2.6 us.
-template <typename T, typename S, int G, int V, bool RES>
+// Q8: the result, rounded to T as it would be stored, goes to 8 bits from the registers (bit for bit what ss_quant_rows makes of the stored one).
+template <typename T, typename S, int G, int V, bool RES, bool RMS, bool Q8>
 __global__ __launch_bounds__(norm_threads<G>(false)) void norm_fwd_kernel(NormArgs a)
 {
     constexpr int THREADS = norm_threads<G>(false), SIDE = THREADS / G;
     __shared__ float lds[2][1][RowSum<G, 1>::WAVES];
+    __shared__ uint32_t lds_top[2][RowMax<G>::WAVES];
     RowSum<G, 1> sum{lds};
+    RowMax<G> most{lds_top};
     const int gl = threadIdx.x % G, W = a.width;
     float w[V][8], b[V][8];
 #pragma unroll
@@ -151,11 +180,13 @@ __global__ __launch_bounds__(norm_threads<G>(false)) void norm_fwd_kernel(NormAr
 #pragma unroll
                 for (int j = 0; j < 8; ++j) s[v][j] = j < n ? s[v][j] : 0.0f;
             }
+            if constexpr (!RMS) {
 #pragma unroll
-            for (int j = 0; j < 8; ++j) t[0] += s[v][j];
+                for (int j = 0; j < 8; ++j) t[0] += s[v][j];
+            }
         }
-        sum(t);
-        const float mean = t[0] * inv_w;
+        if constexpr (!RMS) sum(t);
+        const float mean = RMS ? 0.0f : t[0] * inv_w;
         t[0] = 0.0f;
 #pragma unroll
         for (int v = 0; v < V; ++v) {
@@ -170,7 +201,33 @@ __global__ __launch_bounds__(norm_threads<G>(false)) void norm_fwd_kernel(NormAr
         }
         sum(t);
         const float rstd = 1.0f / sqrtf(t[0] * inv_w + a.eps);
-        if (valid) {
+        if constexpr (Q8) {
+            S* held = static_cast<S*>(a.summed) + (int64_t)row * W;
+            uint32_t top = 0u;
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                const int at = (v * G + gl) * 8, n = W - at;
+                if constexpr (RES)
+                    if (valid) slice_store<S>(held, at, n, s[v]);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    float o = fmaf((s[v][j] - mean) * rstd, w[v][j], b[v][j]);
+                    if constexpr (sizeof(T) == 2) o = bf16_to_f32(f32_to_io<bf16_t>(o));
+                    s[v][j] = j < n ? o : 0.0f;
+                    top = max(top, magnitude(s[v][j]));
+                }
+            }
+            const RowScale rs = row_scale(most(top));
+            if (valid) {
+                int8_t* q = a.q + (int64_t)row * a.pitch;
+#pragma unroll
+                for (int v = 0; v < V; ++v) {
+                    const int at = (v * G + gl) * 8;
+                    if (at < a.pitch) *reinterpret_cast<uint2*>(q + at) = quantised8(s[v], rs.inv);
+                }
+                if (gl == 0) a.scale[row] = rs.scale;
+            }
+        } else if (valid) {
             T* out = static_cast<T*>(a.out) + (int64_t)row * W;
             S* held = static_cast<S*>(a.summed) + (int64_t)row * W;
 #pragma unroll
@@ -182,23 +239,23 @@ __global__ __launch_bounds__(norm_threads<G>(false)) void norm_fwd_kernel(NormAr
                 for (int j = 0; j < 8; ++j) o[j] = fmaf((s[v][j] - mean) * rstd, w[v][j], b[v][j]);
                 slice_store<T>(out, at, n, o);
             }
-            if (a.mean && gl == 0) {
-                a.mean[row] = mean;
+            if (a.rstd && gl == 0) {
+                if constexpr (!RMS) a.mean[row] = mean;
                 a.rstd[row] = rstd;
             }
         }
     }
 }
 
-// With g = dout w and xh the normalised row: ds = rstd (g - mean g - xh mean(g xh)) + dsummed, two sums a row in one exchange; dweight
-// and dbias are sums over rows of dout xh and dout.  Bound by HBM: 16384 x 2048 bf16 with residual (268 MB) 47 us, 5.7 TB/s; 5199 x 1021
+// With g = dout w and xh the normalised row: ds = rstd (g - mean g - xh mean(g xh)) + dsummed, two sums a row in one exchange (RMS: without the
+// mean of g, one); dweight and dbias are sums over rows of dout xh and dout.  Bound by HBM: 16384 x 2048 bf16 with residual (268 MB) 47 us, 5.7 TB/s; 5199 x 1021
 // float32 (64 MB) 16 us, 4.0 TB/s (a wave has three rows, the first and last of which overlap with nothing); 2048 x 16384 (201 MB) 44.
-template <typename T, typename S, int G, int V, bool RES>
+template <typename T, typename S, int G, int V, bool RES, bool RMS>
 __global__ __launch_bounds__(norm_threads<G>(true)) void norm_bwd_kernel(NormArgs a)
 {
-    constexpr int THREADS = norm_threads<G>(true), SIDE = THREADS / G;
-    __shared__ float lds[2][2][RowSum<G, 2>::WAVES];
-    RowSum<G, 2> sum{lds};
+    constexpr int THREADS = norm_threads<G>(true), SIDE = THREADS / G, SUMS = RMS ? 1 : 2;
+    __shared__ float lds[2][SUMS][RowSum<G, SUMS>::WAVES];
+    RowSum<G, SUMS> sum{lds};
     const int gl = threadIdx.x % G, W = a.width;
     float w[V][8], dw[V][8], db[V][8];
 #pragma unroll
@@ -225,7 +282,7 @@ __global__ __launch_bounds__(norm_threads<G>(true)) void norm_bwd_kernel(NormArg
             if constexpr (RES && norm_ahead<G>())
                 if (more) rm[v] = slice_request<S, G == 16>(static_cast<const S*>(a.dsummed) + off, at, W, limit);
         }
-        mean_next = a.mean[row];
+        mean_next = RMS ? 0.0f : a.mean[row];
         rstd_next = a.rstd[row];
     };
     const int first = blockIdx.x * SIDE + threadIdx.x / G;
@@ -235,7 +292,7 @@ __global__ __launch_bounds__(norm_threads<G>(true)) void norm_bwd_kernel(NormArg
         const bool valid = row < a.rows;
         const float mean = mean_next, rstd = rstd_next;
         float x[V][8], g[V][8], m[V][8];
-        float t[2] = {0.0f, 0.0f};
+        float t[SUMS] = {};
         if (!slice_whole(W, row >= a.rows - 1)) {
             const int limit = slice_limit(W, false);
 #pragma unroll
@@ -276,11 +333,11 @@ __global__ __launch_bounds__(norm_threads<G>(true)) void norm_bwd_kernel(NormArg
                 dw[v][j] = fmaf(g[v][j], x[v][j], dw[v][j]);
                 db[v][j] += g[v][j];
                 g[v][j] *= w[v][j];
-                t[0] += g[v][j];
-                t[1] = fmaf(g[v][j], x[v][j], t[1]);
+                if constexpr (!RMS) t[1] += g[v][j];
+                t[0] = fmaf(g[v][j], x[v][j], t[0]);
             }
         sum(t);
-        const float c1 = t[0] * inv_w, c2 = t[1] * inv_w;
+        const float c1 = RMS ? 0.0f : t[SUMS - 1] * inv_w, c2 = t[0] * inv_w;
         if (valid) {
             const int64_t off = (int64_t)row * W;
 #pragma unroll
@@ -381,11 +438,13 @@ __global__ __launch_bounds__(1024) void norm_parts_kernel(const float* part, flo
 // A workgroup a row at a time, which is read once for each sweep, after the first from the caches.  An element a thread and access, which
 // is what bounds them: 2048 x 20000 bf16 (164 MB), not in a cache, 101 us forward and 143 a backward call (float32 127 and 211); in a cache 80 and
 // 115.  Kept simple, as rows this wide are few.
-template <typename T, typename S, bool RES>
+template <typename T, typename S, bool RES, bool RMS, bool Q8>
 __global__ __launch_bounds__(1024) void norm_fwd_wide_kernel(NormArgs a)
 {
     __shared__ float lds[2][1][16];
+    __shared__ uint32_t lds_top[2][16];
     RowSum<1024, 1> sum{lds};
+    RowMax<1024> most{lds_top};
     const int W = a.width;
     for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
         const int64_t off = row * W;
@@ -400,26 +459,40 @@ __global__ __launch_bounds__(1024) void norm_fwd_wide_kernel(NormArgs a)
         float t[1] = {0.0f};
         for (int c = threadIdx.x; c < W; c += 1024) {
             if constexpr (RES) held[c] = f32_to_io<S>(io_to_f32<T>(x[c]) + io_to_f32<S>(r[c]));
-            t[0] += value(c);
+            if constexpr (!RMS) t[0] += value(c);
+            else t[0] = fmaf(value(c), value(c), t[0]);
         }
         sum(t);
-        const float mean = t[0] / (float)W;
-        t[0] = 0.0f;
-        for (int c = threadIdx.x; c < W; c += 1024) {
-            const float v = value(c) - mean;
-            t[0] = fmaf(v, v, t[0]);
+        const float mean = RMS ? 0.0f : t[0] / (float)W;
+        if constexpr (!RMS) {
+            t[0] = 0.0f;
+            for (int c = threadIdx.x; c < W; c += 1024) {
+                const float v = value(c) - mean;
+                t[0] = fmaf(v, v, t[0]);
+            }
+            sum(t);
         }
-        sum(t);
         const float rstd = 1.0f / sqrtf(t[0] / (float)W + a.eps);
-        for (int c = threadIdx.x; c < W; c += 1024)
-            out[c] = f32_to_io<T>(fmaf((value(c) - mean) * rstd, a.weight ? a.weight[c] : 1.0f, a.bias ? a.bias[c] : 0.0f));
-        if (a.mean && threadIdx.x == 0) {
-            a.mean[row] = mean;
-            a.rstd[row] = rstd;
+        auto result = [&](int c) {
+            return f32_to_io<T>(fmaf((value(c) - mean) * rstd, a.weight ? a.weight[c] : 1.0f, a.bias ? a.bias[c] : 0.0f));
+        };
+        if constexpr (Q8) {
+            uint32_t top = 0u;
+            for (int c = threadIdx.x; c < W; c += 1024) top = max(top, magnitude(io_to_f32<T>(result(c))));
+            const RowScale rs = row_scale(most(top));
+            for (int c = threadIdx.x; c < a.pitch; c += 1024)
+                a.q[row * a.pitch + c] = c < W ? (int8_t)quantised4(io_to_f32<T>(result(c)), 0.0f, 0.0f, 0.0f, rs.inv) : (int8_t)0;
+            if (threadIdx.x == 0) a.scale[row] = rs.scale;
+        } else {
+            for (int c = threadIdx.x; c < W; c += 1024) out[c] = result(c);
+            if (a.rstd && threadIdx.x == 0) {
+                if constexpr (!RMS) a.mean[row] = mean;
+                a.rstd[row] = rstd;
+            }
         }
     }
 }
-template <typename T, typename S, bool RES>
+template <typename T, typename S, bool RES, bool RMS>
 __global__ __launch_bounds__(1024) void norm_bwd_wide_kernel(NormArgs a)
 {
     __shared__ float lds[2][2][16];
@@ -429,7 +502,7 @@ __global__ __launch_bounds__(1024) void norm_bwd_wide_kernel(NormArgs a)
         const int64_t off = row * W;
         const S *s = static_cast<const S*>(a.s) + off, *more = static_cast<const S*>(a.dsummed) + off;
         const T* dout = static_cast<const T*>(a.dout) + off;
-        const float mean = a.mean[row], rstd = a.rstd[row];
+        const float mean = RMS ? 0.0f : a.mean[row], rstd = a.rstd[row];
         float t[2] = {0.0f, 0.0f};
         for (int c = threadIdx.x; c < W; c += 1024) {
             const float g = io_to_f32<T>(dout[c]) * (a.weight ? a.weight[c] : 1.0f);
@@ -437,7 +510,7 @@ __global__ __launch_bounds__(1024) void norm_bwd_wide_kernel(NormArgs a)
             t[1] = fmaf(g, (io_to_f32<S>(s[c]) - mean) * rstd, t[1]);
         }
         sum(t);
-        const float c1 = t[0] / (float)W, c2 = t[1] / (float)W;
+        const float c1 = RMS ? 0.0f : t[0] / (float)W, c2 = t[1] / (float)W;
         for (int c = threadIdx.x; c < W; c += 1024) {
             const float g = io_to_f32<T>(dout[c]) * (a.weight ? a.weight[c] : 1.0f);
             float o = rstd * (g - c1 - (io_to_f32<S>(s[c]) - mean) * rstd * c2);
@@ -448,7 +521,7 @@ __global__ __launch_bounds__(1024) void norm_bwd_wide_kernel(NormArgs a)
     }
 }
 // columns' sums over blockIdx.y's share of the rows
-template <typename T, typename S>
+template <typename T, typename S, bool RMS>
 __global__ __launch_bounds__(256) void norm_columns_kernel(NormArgs a)
 {
     const int c = blockIdx.x * 256 + threadIdx.x;
@@ -457,7 +530,7 @@ __global__ __launch_bounds__(256) void norm_columns_kernel(NormArgs a)
     for (int row = blockIdx.y; row < a.rows; row += gridDim.y) {
         const int64_t e = (int64_t)row * a.width + c;
         const float g = io_to_f32<T>(static_cast<const T*>(a.dout)[e]);
-        dw = fmaf(g, (io_to_f32<S>(static_cast<const S*>(a.s)[e]) - a.mean[row]) * a.rstd[row], dw);
+        dw = fmaf(g, (io_to_f32<S>(static_cast<const S*>(a.s)[e]) - (RMS ? 0.0f : a.mean[row])) * a.rstd[row], dw);
         db += g;
     }
     float* const part = a.part + (int64_t)blockIdx.y * 2 * a.width;
@@ -520,52 +593,70 @@ int norm_parts(int rows, int width)
     return n < most ? n : most;
 }
 
-template <typename T, typename S, bool RES>
-void norm_launch(const NormArgs& a, bool bwd, hipStream_t st)
+enum NormPass { NORM_FWD, NORM_Q8, NORM_BWD };
+
+template <typename T, typename S, bool RES, bool RMS, bool Q8>
+void norm_launch_fwd(const NormArgs& a, hipStream_t st)
 {
-    const NormForm f = norm_form(a.rows, a.width, bwd);
+    const NormForm f = norm_form(a.rows, a.width, false);
     if (f.lanes == 0) {
-        const dim3 grid((unsigned)(a.rows < NORM_MOST_WORKGROUPS ? a.rows : NORM_MOST_WORKGROUPS));
-        if (!bwd) {
-            hipLaunchKernelGGL((norm_fwd_wide_kernel<T, S, RES>), grid, dim3(1024), 0, st, a);
-        } else {
-            hipLaunchKernelGGL((norm_bwd_wide_kernel<T, S, RES>), grid, dim3(1024), 0, st, a);
-            if (a.part)
-                hipLaunchKernelGGL((norm_columns_kernel<T, S>), dim3((unsigned)((a.width + 255) / 256), (unsigned)norm_parts(a.rows, a.width)),
-                                   dim3(256), 0, st, a);
-        }
+        hipLaunchKernelGGL((norm_fwd_wide_kernel<T, S, RES, RMS, Q8>), dim3((unsigned)(a.rows < NORM_MOST_WORKGROUPS ? a.rows : NORM_MOST_WORKGROUPS)),
+                           dim3(1024), 0, st, a);
         return;
     }
-    if (bwd) {
-        with_form<true>(f, [&](auto g, auto v) {
-            constexpr int G = decltype(g)::value, V = decltype(v)::value;
-            hipLaunchKernelGGL((norm_bwd_kernel<T, S, G, V, RES>), dim3((unsigned)norm_parts(a.rows, a.width)), dim3(norm_threads<G>(true)), 0, st, a);
-        });
-    } else {
-        with_form<false>(f, [&](auto g, auto v) {
-            constexpr int G = decltype(g)::value, V = decltype(v)::value;
-            // workgroups of 1024 lanes, which request no row ahead, have two rounds of the units' at most (2048 x 16384 float32 53 us, four 62)
-            const int side = norm_threads<G>(false) / G, n = (a.rows + side - 1) / side, most = G < 1024 ? 1024 : 512;
-            hipLaunchKernelGGL((norm_fwd_kernel<T, S, G, V, RES>), dim3((unsigned)(n < most ? n : most)), dim3(norm_threads<G>(false)), 0, st, a);
-        });
-    }
+    with_form<false>(f, [&](auto g, auto v) {
+        constexpr int G = decltype(g)::value, V = decltype(v)::value;
+        // workgroups of 1024 lanes, which request no row ahead, have two rounds of the units' at most (2048 x 16384 float32 53 us, four 62)
+        const int side = norm_threads<G>(false) / G, n = (a.rows + side - 1) / side, most = G < 1024 ? 1024 : 512;
+        hipLaunchKernelGGL((norm_fwd_kernel<T, S, G, V, RES, RMS, Q8>), dim3((unsigned)(n < most ? n : most)), dim3(norm_threads<G>(false)), 0, st, a);
+    });
 }
-void norm_dispatch(const NormArgs& a, int io, uint32_t flags, bool bwd, hipStream_t st)
+template <typename T, typename S, bool RES, bool RMS>
+void norm_launch_bwd(const NormArgs& a, hipStream_t st)
+{
+    const NormForm f = norm_form(a.rows, a.width, true);
+    if (f.lanes == 0) {
+        hipLaunchKernelGGL((norm_bwd_wide_kernel<T, S, RES, RMS>), dim3((unsigned)(a.rows < NORM_MOST_WORKGROUPS ? a.rows : NORM_MOST_WORKGROUPS)),
+                           dim3(1024), 0, st, a);
+        if (a.part)
+            hipLaunchKernelGGL((norm_columns_kernel<T, S, RMS>), dim3((unsigned)((a.width + 255) / 256), (unsigned)norm_parts(a.rows, a.width)),
+                               dim3(256), 0, st, a);
+        return;
+    }
+    with_form<true>(f, [&](auto g, auto v) {
+        constexpr int G = decltype(g)::value, V = decltype(v)::value;
+        hipLaunchKernelGGL((norm_bwd_kernel<T, S, G, V, RES, RMS>), dim3((unsigned)norm_parts(a.rows, a.width)), dim3(norm_threads<G>(true)), 0, st, a);
+    });
+}
+template <typename T, typename S, bool RES, bool RMS>
+void norm_launch(const NormArgs& a, NormPass pass, hipStream_t st)
+{
+    if (pass == NORM_FWD) norm_launch_fwd<T, S, RES, RMS, false>(a, st);
+    else if (pass == NORM_Q8) norm_launch_fwd<T, S, RES, RMS, true>(a, st);
+    else norm_launch_bwd<T, S, RES, RMS>(a, st);
+}
+template <bool RMS>
+void norm_of(const NormArgs& a, int io, uint32_t flags, NormPass pass, hipStream_t st)
 {
     const bool res = flags & SS_NORM_HAS_RESIDUAL;
     if (io == SS_F32) {
-        if (res) norm_launch<float, float, true>(a, bwd, st);
-        else norm_launch<float, float, false>(a, bwd, st);
-    } else if (!res) norm_launch<bf16_t, bf16_t, false>(a, bwd, st);
-    else if (flags & SS_NORM_RESIDUAL_F32) norm_launch<bf16_t, float, true>(a, bwd, st);
-    else norm_launch<bf16_t, bf16_t, true>(a, bwd, st);
+        if (res) norm_launch<float, float, true, RMS>(a, pass, st);
+        else norm_launch<float, float, false, RMS>(a, pass, st);
+    } else if (!res) norm_launch<bf16_t, bf16_t, false, RMS>(a, pass, st);
+    else if (flags & SS_NORM_RESIDUAL_F32) norm_launch<bf16_t, float, true, RMS>(a, pass, st);
+    else norm_launch<bf16_t, bf16_t, true, RMS>(a, pass, st);
+}
+void norm_dispatch(const NormArgs& a, int io, uint32_t flags, NormPass pass, hipStream_t st)
+{
+    if (flags & SS_NORM_RMS) norm_of<true>(a, io, flags, pass, st);
+    else norm_of<false>(a, io, flags, pass, st);
 }
 
 }  // namespace ss
 
 namespace {
 
-constexpr uint32_t kNormFlags = SS_NORM_HAS_WEIGHT | SS_NORM_HAS_BIAS | SS_NORM_HAS_RESIDUAL | SS_NORM_RESIDUAL_F32 | SS_NORM_SAVE_STATS;
+constexpr uint32_t kNormFlags = SS_NORM_HAS_WEIGHT | SS_NORM_HAS_BIAS | SS_NORM_HAS_RESIDUAL | SS_NORM_RESIDUAL_F32 | SS_NORM_SAVE_STATS | SS_NORM_RMS;
 inline bool aligned_to(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) % a) == 0; }
 
 struct NormSizes {
@@ -614,9 +705,31 @@ int ss_norm_fwd(const ss_norm_params* p, void* stream)
     a.x = p->x; a.residual = p->residual; a.out = p->out; a.summed = p->summed;
     if (save) {
         a.mean = p->stats;
-        a.rstd = p->stats + p->rows;
+        a.rstd = p->stats + (p->flags & SS_NORM_RMS ? 0 : p->rows);
     }
-    ss::norm_dispatch(a, p->io_dtype, p->flags, false, static_cast<hipStream_t>(stream));
+    ss::norm_dispatch(a, p->io_dtype, p->flags, ss::NORM_FWD, static_cast<hipStream_t>(stream));
+    return hipGetLastError() == hipSuccess ? SS_OK : SS_ERR_LAUNCH;
+}
+
+int ss_norm_quant(const ss_norm_quant_params* p, void* stream)
+{
+    if (!p) return SS_ERR_NULL;
+    const ss_norm_params* f = &p->fwd;
+    NormSizes e;
+    const int rc = check_norm(f, e, false);
+    if (rc != SS_OK) return rc;
+    if (f->width > SS_QUANT_MAX_DIM || (f->flags & SS_NORM_SAVE_STATS)) return SS_ERR_UNSUPPORTED;
+    const bool res = f->flags & SS_NORM_HAS_RESIDUAL;
+    if (f->rows == 0) return SS_OK;
+    if (!f->x || !p->q || !p->scale || (res && (!f->residual || !f->summed))) return SS_ERR_NULL;
+    if (!aligned_to(f->x, e.io) || !aligned_to(p->q, 16) || !aligned_to(p->scale, 4) ||
+        (res && (!aligned_to(f->residual, e.held) || !aligned_to(f->summed, e.held))))
+        return SS_ERR_ALIGN;
+    ss::NormArgs a = norm_args(f);
+    a.x = f->x; a.residual = f->residual; a.summed = f->summed;
+    a.q = p->q; a.scale = p->scale;
+    a.pitch = (int)ss::quant_pitch(f->width);
+    ss::norm_dispatch(a, f->io_dtype, f->flags, ss::NORM_Q8, static_cast<hipStream_t>(stream));
     return hipGetLastError() == hipSuccess ? SS_OK : SS_ERR_LAUNCH;
 }
 
@@ -652,9 +765,9 @@ int ss_norm_bwd(const ss_norm_bwd_params* p, void* stream)
         a.s = s; a.dout = p->dout; a.dsummed = res ? p->dsummed : nullptr;
         a.dx = p->dx; a.dresidual = p->dresidual;
         a.mean = q->stats;
-        a.rstd = q->stats + q->rows;
+        a.rstd = q->stats + (q->flags & SS_NORM_RMS ? 0 : q->rows);
         a.part = static_cast<float*>(p->workspace);
-        ss::norm_dispatch(a, q->io_dtype, q->flags, true, st);
+        ss::norm_dispatch(a, q->io_dtype, q->flags, ss::NORM_BWD, st);
     }
     if (hw || hb) {
         const int columns = (q->width + 31) / 32;

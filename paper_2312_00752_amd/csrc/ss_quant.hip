@@ -9,56 +9,17 @@
 #include <type_traits>
 
 #include "ss_quant.h"
+#include "ss_round8.h"
 #include "ss_slices.h"
 
 namespace ss {
 
-constexpr int Q_STEP = 128;                      // bytes of the contraction index that a step takes
 constexpr int64_t MOST_THREADS = 0x7fffffff;      // of a launch (its limit is 2^32)
-constexpr float Q_LEAST = 7.52316384526264e-37f;  // 2^-120
 
 typedef int i32x4 __attribute__((ext_vector_type(4)));
 typedef int i32x16 __attribute__((ext_vector_type(16)));
 
 // ---- the quantiser --------------------------------------------------------------------------------
-// max |x| of a row, as the bits of a float: for magnitudes the order of the bits is that of the numbers, and infinities and NaN
-// are above all of them.
-__device__ __forceinline__ uint32_t magnitude(float v) { return __float_as_uint(v) & 0x7fffffffu; }
-struct RowScale {
-    float scale, inv;
-};
-__device__ __forceinline__ RowScale row_scale(uint32_t top)
-{
-    RowScale r;
-    const float m = __uint_as_float(top);
-    if (top >= 0x7f800000u) {          // an infinity or NaN
-        r.scale = __uint_as_float(0x7fc00000u);
-        r.inv = 0.0f;
-    } else if (m < Q_LEAST) {
-        r.scale = 0.0f;
-        r.inv = 0.0f;
-    } else {
-        r.scale = m / 127.0f;
-        r.inv = 127.0f * (1.0f / m);
-    }
-    return r;
-}
-// round(v inv) of four values, ties to even, as the bytes of a word: 1.5 2^23 added to the rounded product leaves the whole number in the
-// low byte.  inv is 0 in rows that come out as zeros or NaN; their bytes are 0 whatever stands in them.
-__device__ __forceinline__ uint32_t quantised4(float v0, float v1, float v2, float v3, float inv)
-{
-#pragma clang fp contract(off)
-    constexpr float up = 12582912.0f;
-    const float p0 = v0 * inv, p1 = v1 * inv, p2 = v2 * inv, p3 = v3 * inv;
-    const uint32_t low = __builtin_amdgcn_perm(__float_as_uint(p1 + up), __float_as_uint(p0 + up), 0x0c0c0400u);
-    const uint32_t high = __builtin_amdgcn_perm(__float_as_uint(p3 + up), __float_as_uint(p2 + up), 0x04000c0cu);
-    return inv == 0.0f ? 0u : low | high;
-}
-__device__ __forceinline__ uint2 quantised8(const float (&v)[8], float inv)
-{
-    return make_uint2(quantised4(v[0], v[1], v[2], v[3], inv), quantised4(v[4], v[5], v[6], v[7], inv));
-}
-
 // Rows contiguous along dim: G lanes hold a row in registers, V slices of 8 each, so it is read once.  Bound by HBM: 16384 x 2048 bf16
 // (67 MB in, 34 MB out) 24 us when not in a cache, 4.2 TB/s.
 template <typename T, int G, int V>
@@ -871,7 +832,7 @@ QSpace q_space(const ss_qlinear_params* p)
 
 extern "C" {
 
-size_t ss_quant_pitch(int32_t dim) { return dim < 1 ? 0 : round_up((size_t)dim, ss::Q_STEP); }
+size_t ss_quant_pitch(int32_t dim) { return ss::quant_pitch(dim); }
 
 size_t ss_quant_rows_scratch_bytes(const ss_quant_params* p)
 {

@@ -1,0 +1,28 @@
+"""What the entry points around the block launch, over sizes up to what a card's memory holds: every launch within what a launch can be, and nothing
+launched by a call that is refused.  The entry points of a source file run on the host with the launches recorded instead of made."""
+from tests.test_launch_sizes_cpu import run
+
+NORM = r"""
+static void one()
+{
+    ss_norm_quant_params q{};
+    ss_norm_params& p = q.fwd;
+    p.io_dtype = coin(2);
+    p.flags = (uint32_t)coin(16) | (coin(2) ? SS_NORM_RMS : 0u);
+    p.rows = any(2147418111);
+    p.width = any(2 * SS_QUANT_MAX_DIM);
+    p.eps = 1e-5f;
+    if (2.0 * p.rows * p.width * (p.io_dtype == SS_BF16 ? 2 : 4) > CARD) return;
+    p.x = p.residual = p.summed = fake;
+    p.weight = p.bias = static_cast<float*>(fake);
+    q.q = static_cast<int8_t*>(fake);
+    q.scale = static_cast<float*>(fake);
+    const int rc = ss_norm_quant(&q, nullptr);
+    if ((rc == SS_OK) != (p.width <= SS_QUANT_MAX_DIM)) std::exit(1);
+    look(rc, "ss_norm_quant", p.rows, p.width, 0, 0, p.io_dtype, p.flags);
+}
+"""
+
+
+def test_norm_quant(tmp_path):
+    run(tmp_path, "ss_norm.hip", NORM)

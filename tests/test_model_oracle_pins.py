@@ -1,0 +1,39 @@
+"""The float64 oracles of RMS norm, embedding, log probabilities and AdamW against closed forms, torch in float64 and finite differences."""
+import numpy as np
+import torch
+
+from oracle import model_oracle as mo
+
+
+def differences(f, x, dout, h=1e-6):
+    """Gradient of <f(x), dout> by central differences, coordinate by coordinate."""
+    g = np.zeros_like(x)
+    for k in np.ndindex(*x.shape):
+        at = [x.copy(), x.copy()]
+        at[0][k] += h
+        at[1][k] -= h
+        g[k] = sum(s * (f(a) * dout).sum() for s, a in zip((1, -1), at)) / (2 * h)
+    return g
+
+
+# ---- RMS norm -----------------------------------------------------------------------------------------
+def test_rms_norm_closed_forms():
+    out, xhat, rstd = mo.rms_fwd([[3.0, 4.0]], eps=0.0)   # mean square 12.5
+    assert np.allclose(out, [[3 / 12.5 ** 0.5, 4 / 12.5 ** 0.5]]) and np.allclose(rstd, 12.5 ** -0.5)
+    s = np.random.default_rng(0).standard_normal((5, 9))
+    assert np.allclose((mo.rms_fwd(s, eps=0.0)[1] ** 2).mean(1), 1.0)
+    assert np.allclose(mo.rms_fwd(7.0 * s, eps=0.0)[0], mo.rms_fwd(s, eps=0.0)[0])   # scale does not matter
+    assert np.allclose(mo.rms_fwd(np.zeros((1, 4)))[0], 0.0)
+    w, b = np.arange(9.0), np.ones(9)
+    assert np.allclose(mo.rms_fwd(s, w, b)[0], mo.rms_fwd(s)[0] * w + b)
+
+
+def test_rms_norm_gradients():
+    rng = np.random.default_rng(1)
+    s, w, dout, more = rng.standard_normal((3, 7)), rng.standard_normal(7), rng.standard_normal((3, 7)), rng.standard_normal((3, 7))
+    g = mo.rms_bwd(dout, s, w, more)
+    assert np.allclose(g["ds"] - more, differences(lambda v: mo.rms_fwd(v, w)[0], s, dout), atol=1e-7)
+    assert np.allclose(g["dweight"], differences(lambda v: mo.rms_fwd(s, v)[0], w, dout), atol=1e-7)
+    assert np.allclose(g["dbias"], dout.sum(0))
+    # a gradient along s itself changes nothing when eps is 0
+    assert np.allclose((mo.rms_bwd(dout, s, w, eps=0.0)["ds"] * s).sum(1), 0.0, atol=1e-12)
