@@ -28,3 +28,23 @@ def rms_bwd(dout, s, weight=None, dsummed=None, eps=1e-5):
         ds = ds + np.asarray(dsummed, f64)
     return {"ds": ds, "dweight": (dout * xhat).sum(0), "dweight_size": np.abs(dout * xhat).sum(0),
             "dbias": dout.sum(0), "dbias_size": np.abs(dout).sum(0)}
+
+
+# ---- embedding ------------------------------------------------------------------------------------
+def embed_fwd(ids, table, scale=1.0):
+    """ids of any shape, table (vocab, dim)."""
+    table = np.asarray(table, f64)
+    out = np.zeros(np.shape(ids) + table.shape[1:])
+    for k in np.ndindex(*np.shape(ids)):
+        if 0 <= ids[k] < len(table):
+            out[k] = scale * table[ids[k]]
+    return out
+
+
+def embed_bwd(dout, ids, vocab, scale=1.0):
+    grad, size = np.zeros((vocab, dout.shape[-1])), np.zeros((vocab, dout.shape[-1]))
+    for k in np.ndindex(*np.shape(ids)):
+        if 0 <= ids[k] < vocab:
+            grad[ids[k]] += scale * np.asarray(dout[k], f64)
+            size[ids[k]] += np.abs(scale * np.asarray(dout[k], f64))
+    return {"dtable": grad, "dtable_size": size}

@@ -1,4 +1,5 @@
-"""``torch.autograd`` front-ends of the library: the selective scan, the layer around it, layer norm and the gated recurrence.
+"""``torch.autograd`` front-ends of the library: the selective scan, the layer around it, layer and RMS norm, the gated recurrence, and
+the embedding.
 
 Still marshalling only: ``forward`` enqueues ``ss_scan_fwd`` / ``ss_layer_fwd`` and keeps the
 workspace the library filled, ``backward`` enqueues ``ss_scan_bwd`` / ``ss_layer_bwd``; all
@@ -185,3 +186,25 @@ def gated_recurrence(x, f, rate, i=None, z=None, f_bias=None, i_bias=None, reset
         if r is not None:
             return r if return_last_state else r[0]
     return _GatedRecurrence.apply(x, f, rate, i, z, f_bias, i_bias, reset, h0, return_last_state)
+
+
+class _Embedding(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, ids, table, scale, out_dtype):
+        ctx.save_for_backward(ids)
+        ctx.opts = (table.shape[0], scale, table.dtype)
+        return B.ss_embed_fwd(ids, table, scale=scale, out_dtype=out_dtype)
+
+    @staticmethod
+    @last_derivative
+    def backward(ctx, dout):
+        ids, = ctx.saved_tensors
+        vocab, scale, dtype = ctx.opts
+        return None, B.ss_embed_bwd(dout.contiguous(), ids, vocab, scale=scale, dtype=dtype), None, None
+
+
+def embedding(ids, table, scale=1.0, out_dtype=None):
+    """Differentiable lookup: rows of ``table`` (vocab, dim), times ``scale``, for token ids of any shape, in ``out_dtype`` (the table's unless
+    given).  Ids outside the table (-1 for padding) give zeros and no gradient.  The table's gradient is a sum in token order:
+    the same bits every time."""
+    return _Embedding.apply(ids, table, scale, out_dtype)

@@ -1,5 +1,5 @@
 """Thin binding (ctypes, and a compiled module for the hot calls) of the C-ABI library declared in the headers of ``include/`` (``ss_scan.h``, ``ss_conv.h``, ``ss_layer.h``,
-``ss_norm.h``, ``ss_gate.h``, ``ss_quant.h``).
+``ss_norm.h``, ``ss_gate.h``, ``ss_quant.h``, ``ss_embed.h``).
 
 Argument marshalling only: every step of the path runs in the library's HIP kernels.
 PyTorch appears here solely as the owner of device memory and streams.  The library must
@@ -160,6 +160,15 @@ class QLinearParams(ctypes.Structure):
                 ("scale", _vp), ("bias", _vp), ("out", _vp), ("scratch", _vp), ("scratch_bytes", ctypes.c_size_t)]
 
 
+class EmbedParams(ctypes.Structure):
+    _fields_ = [("tokens", ctypes.c_int32), ("vocab", ctypes.c_int32), ("dim", ctypes.c_int32), ("table_dtype", ctypes.c_int32),
+                ("io_dtype", ctypes.c_int32), ("flags", ctypes.c_uint32), ("scale", ctypes.c_float), ("ids", _vp), ("table", _vp), ("out", _vp)]
+
+
+class EmbedBwdParams(ctypes.Structure):
+    _fields_ = [("fwd", EmbedParams), ("dout", _vp), ("dtable", _vp), ("workspace", _vp), ("workspace_bytes", ctypes.c_size_t)]
+
+
 SS_GEMM_C_FLOAT, SS_GEMM_ACCUMULATE, SS_GEMM_GENERAL = 1, 2, 4
 SS_ERR_BACKEND = -7
 SS_CONV_SILU, SS_CONV_HAS_BIAS, SS_CONV_HAS_STATE, SS_CONV_WRITE_STATE = 1, 2, 4, 8
@@ -170,6 +179,7 @@ SS_GATE_HAS_I, SS_GATE_HAS_Z, SS_GATE_HAS_F_BIAS, SS_GATE_HAS_I_BIAS = 1, 2, 4, 
 SS_GATE_HAS_RESET, SS_GATE_HAS_H0, SS_GATE_WRITE_H_LAST, SS_GATE_SAVE_FOR_BWD = 16, 32, 64, 128
 SS_Q_X_SEQ_LAST, SS_Q_OUT_SEQ_LAST, SS_Q_HAS_BIAS, SS_Q_X_QUANTISED = 1, 2, 4, 8
 SS_QUANT_MAX_DIM = 131072
+SS_EMBED_IDS_32 = 1
 
 _lib = None
 
@@ -219,13 +229,14 @@ def lib():
         for name, params in (("ss_norm_fwd", NormParams), ("ss_norm_quant", NormQuantParams), ("ss_norm_bwd", NormBwdParams),
                              ("ss_gate_fwd", GateParams),
                              ("ss_gate_bwd", GateBwdParams), ("ss_gate_step", GateStepParams), ("ss_quant_rows", QuantParams),
-                             ("ss_qlinear", QLinearParams)):
+                             ("ss_qlinear", QLinearParams), ("ss_embed_fwd", EmbedParams), ("ss_embed_bwd", EmbedBwdParams)):
             getattr(l, name).restype = ctypes.c_int
             getattr(l, name).argtypes = [ctypes.POINTER(params), _vp]
         for name, args in (("ss_norm_workspace_bytes", [ctypes.POINTER(NormParams)]),
                            ("ss_gate_workspace_bytes", [ctypes.POINTER(GateParams), ctypes.c_int]),
                            ("ss_quant_rows_scratch_bytes", [ctypes.POINTER(QuantParams)]),
-                           ("ss_qlinear_scratch_bytes", [ctypes.POINTER(QLinearParams)]), ("ss_quant_pitch", [ctypes.c_int32])):
+                           ("ss_qlinear_scratch_bytes", [ctypes.POINTER(QLinearParams)]), ("ss_quant_pitch", [ctypes.c_int32]),
+                           ("ss_embed_workspace_bytes", [ctypes.POINTER(EmbedParams)])):
             getattr(l, name).restype = ctypes.c_size_t
             getattr(l, name).argtypes = args
         l.ss_version.restype = ctypes.c_int
@@ -1278,6 +1289,79 @@ def ss_qlinear(x, weight, scale, bias=None, x_seq_last=False, out_seq_last=False
     if need:
         p.scratch, p.scratch_bytes = _lend(scratch, need, x.device, "scratch")
     _check(lib().ss_qlinear(ctypes.byref(p), _stream(stream)))
+    return out
+
+
+# ---------------------------------------------------------------- embedding
+def _on_current(*tensors):
+    """The tensors of a call lie on the device whose stream it takes."""
+    if _raw_stream is None:
+        _find_raw_stream()
+    for t in tensors:
+        if t is not None and t.is_cuda and t.get_device() != _device_index():
+            raise ValueError("a tensor lies on %s, the current device is cuda:%d" % (t.device, _device_index()))
+
+
+def _embed_params(ids, vocab, dim, scale):
+    p = EmbedParams()
+    if ids.dtype is not torch.int64 and ids.dtype is not torch.int32:
+        raise TypeError("ids must be int64 or int32, got %s" % ids.dtype)
+    p.tokens, p.vocab, p.dim = _counts(ids.numel(), vocab, dim)
+    p.flags = SS_EMBED_IDS_32 if ids.dtype is torch.int32 else 0
+    p.scale = scale
+    p.ids = _ptr(ids, None, None, "ids")
+    return p
+
+
+def ss_embed_fwd(ids, table, scale=1.0, out_dtype=None, out=None, stream=None):
+    """Enqueue the rows of ``table`` (vocab, dim), times ``scale``, for token ids (int64 or int32, any shape), as (*ids.shape, dim) of
+    ``out_dtype`` (the table's unless given).  Ids outside the table give zeros."""
+    if stream is not None:
+        with _current(stream):
+            return ss_embed_fwd(ids, table, scale, out_dtype, out)
+    _on_current(ids, table, out)
+    if table.dim() != 2:
+        raise ValueError("table must have two axes")
+    p = _embed_params(ids, table.shape[0], table.shape[1], scale)
+    p.table_dtype = _io_code(table)
+    p.table = _ptr(table, None, None, "table")
+    shape = tuple(ids.shape) + (table.shape[1],)
+    if out is None:
+        out = torch.empty(shape, dtype=table.dtype if out_dtype is None else out_dtype, device=table.device)
+    p.out = _ptr(out, out_dtype, shape, "out")
+    p.io_dtype = _io_code(out)
+    _check(lib().ss_embed_fwd(ctypes.byref(p), _stream(stream)))
+    return out
+
+
+def ss_embed_workspace_bytes(tokens, vocab, dim):
+    p = EmbedParams()
+    p.tokens, p.vocab, p.dim = _counts(tokens, vocab, dim)
+    return int(lib().ss_embed_workspace_bytes(ctypes.byref(p)))
+
+
+def ss_embed_bwd(dout, ids, vocab, scale=1.0, dtype=None, out=None, workspace=None, stream=None):
+    """Enqueue the gradient of the table (vocab, dim), of ``dtype`` (dout's unless given), from ``dout`` (*ids.shape, dim): the rows of the
+    tokens of every id added up in their order, without atomics."""
+    if stream is not None:
+        with _current(stream):
+            return ss_embed_bwd(dout, ids, vocab, scale, dtype, out, workspace)
+    _on_current(dout, ids, out, workspace)
+    if dout.dim() < 1:
+        raise ValueError("dout must have an axis")
+    dim = dout.shape[-1]
+    q = EmbedBwdParams()
+    q.fwd = _embed_params(ids, vocab, dim, scale)
+    q.fwd.io_dtype = _io_code(dout)
+    q.dout = _ptr(dout, None, tuple(ids.shape) + (dim,), "dout")
+    if out is None:
+        out = torch.empty((vocab, dim), dtype=dout.dtype if dtype is None else dtype, device=dout.device)
+    q.dtable = _ptr(out, dtype, (vocab, dim), "out")
+    q.fwd.table_dtype = _io_code(out)
+    need = int(lib().ss_embed_workspace_bytes(ctypes.byref(q.fwd)))
+    if need:
+        q.workspace, q.workspace_bytes = _lend(workspace, need, dout.device, "workspace")
+    _check(lib().ss_embed_bwd(ctypes.byref(q), _stream(stream)))
     return out
 
 

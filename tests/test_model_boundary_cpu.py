@@ -1,4 +1,4 @@
-"""What the entry points of RMS norm with its 8-bit result refuse, on the host, before any device call; and their structs as the C compiler lays them out."""
+"""What the entry points of the norms' 8-bit results and of the embedding refuse, on the host, before any device call; and their structs as the C compiler lays them out."""
 import ctypes
 import os
 import subprocess
@@ -12,8 +12,8 @@ ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 FAKE = 0x7F0000001000   # non-null, 4096-byte aligned, never dereferenced
 MANY = 2 ** 32 + 5
 
-STRUCTS = {"ss_norm_quant_params": B.NormQuantParams}
-HEADERS = ["ss_norm.h"]
+STRUCTS = {"ss_norm_quant_params": B.NormQuantParams, "ss_embed_params": B.EmbedParams, "ss_embed_bwd_params": B.EmbedBwdParams}
+HEADERS = ["ss_norm.h", "ss_embed.h"]
 
 
 def t(*shape, dtype=torch.bfloat16):
@@ -92,3 +92,46 @@ def test_norm_sizes_beyond_32_bits(call):
 def test_norm_tensors_on_the_host_are_refused():
     with pytest.raises(ValueError, match="GPU"):
         B.ss_norm_quant(torch.zeros(3, 4), rms=True)
+
+
+# ---- embedding ----------------------------------------------------------------------------------------
+def embed():
+    p = B.EmbedParams()
+    p.tokens, p.vocab, p.dim, p.table_dtype, p.io_dtype, p.scale = 4, 10, 32, B.SS_F32, B.SS_BF16, 1.0
+    p.ids = p.table = p.out = FAKE
+    return p
+
+
+def embed_bwd():
+    p = B.EmbedBwdParams()
+    p.fwd = embed()
+    p.dout = p.dtable = p.workspace = FAKE
+    p.workspace_bytes = B.ss_embed_workspace_bytes(4, 10, 32)
+    return p
+
+
+def test_embed():
+    call = B.lib().ss_embed_fwd
+    assert call(None, None) == B.SS_ERR_NULL
+    expect(call, embed, [dict(ids=None), dict(table=None), dict(out=None)], B.SS_ERR_NULL)
+    expect(call, embed, [dict(tokens=-1), dict(vocab=0), dict(dim=0)], B.SS_ERR_SHAPE)
+    inf = float("inf")
+    expect(call, embed, [dict(table_dtype=2), dict(io_dtype=-1), dict(flags=2), dict(scale=inf), dict(scale=float("nan")), dict(tokens=2 ** 31 - 1),
+                         dict(vocab=2 ** 31 - 1), dict(dim=2 ** 31 - 1)], B.SS_ERR_UNSUPPORTED)
+    expect(call, embed, [dict(ids=FAKE + 4), dict(ids=FAKE + 2, flags=1), dict(table=FAKE + 2), dict(out=FAKE + 1)], B.SS_ERR_ALIGN)
+    expect(call, embed, [dict(tokens=0, ids=None, table=None, out=None)], B.SS_OK)
+    call = B.lib().ss_embed_bwd
+    assert call(None, None) == B.SS_ERR_NULL
+    expect(call, embed_bwd, [{"fwd.ids": None}, dict(dout=None), dict(dtable=None), {"fwd.tokens": 0, "dtable": None}], B.SS_ERR_NULL)
+    expect(call, embed_bwd, [dict(dout=FAKE + 1), dict(dtable=FAKE + 2), dict(workspace=FAKE + 128)], B.SS_ERR_ALIGN)
+    expect(call, embed_bwd, [dict(workspace=None), dict(workspace_bytes=embed_bwd().workspace_bytes - 1)], B.SS_ERR_WORKSPACE)
+    assert B.ss_embed_workspace_bytes(0, 10, 32) == 0
+
+
+@pytest.mark.parametrize("call", [lambda: B.ss_embed_fwd(t(MANY, dtype=torch.int64), t(3, 4)), lambda: B.ss_embed_fwd(t(3, dtype=torch.int64), t(MANY, 1)),
+                                  lambda: B.ss_embed_fwd(t(3, dtype=torch.int64), t(1, MANY)), lambda: B.ss_embed_bwd(t(MANY, 1), t(MANY, dtype=torch.int32), 5),
+                                  lambda: B.ss_embed_bwd(t(3, 4), t(3, dtype=torch.int32), MANY), lambda: B.ss_embed_workspace_bytes(4, 4, MANY)])
+def test_embed_sizes_beyond_32_bits(call):
+    with pytest.raises(B.SsError) as e:
+        call()
+    assert e.value.code == B.SS_ERR_UNSUPPORTED

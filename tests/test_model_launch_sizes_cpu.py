@@ -26,3 +26,34 @@ static void one()
 
 def test_norm_quant(tmp_path):
     run(tmp_path, "ss_norm.hip", NORM)
+
+
+EMBED = r"""
+static void one()
+{
+    ss_embed_bwd_params q{};
+    ss_embed_params& p = q.fwd;
+    p.table_dtype = coin(2);
+    p.io_dtype = coin(2);
+    p.flags = (uint32_t)coin(2);
+    p.scale = 1.0f;
+    p.tokens = any(2147418111);
+    p.vocab = 1 + any(2147418110);
+    p.dim = 1 + any(65535.0 * 2048 - 1);
+    const double io = (double)p.tokens * p.dim * (p.io_dtype == SS_BF16 ? 2 : 4), table = (double)p.vocab * p.dim * (p.table_dtype == SS_BF16 ? 2 : 4);
+    if (io + table > CARD) return;
+    p.ids = p.table = q.dout = fake;
+    p.out = q.dtable = q.workspace = fake;
+    const int rc = ss_embed_fwd(&p, nullptr);
+    if (rc != SS_OK) std::exit(1);
+    look(rc, "ss_embed_fwd", p.tokens, p.vocab, p.dim, p.table_dtype, p.io_dtype, p.flags);
+    q.workspace_bytes = ss_embed_workspace_bytes(&p);
+    const int rb = ss_embed_bwd(&q, nullptr);
+    if (rb != SS_OK) std::exit(1);
+    look(rb, "ss_embed_bwd", p.tokens, p.vocab, p.dim, p.table_dtype, p.io_dtype, p.flags);
+}
+"""
+
+
+def test_embed(tmp_path):
+    run(tmp_path, "ss_embed.hip", EMBED)

@@ -37,3 +37,17 @@ def test_rms_norm_gradients():
     assert np.allclose(g["dbias"], dout.sum(0))
     # a gradient along s itself changes nothing when eps is 0
     assert np.allclose((mo.rms_bwd(dout, s, w, eps=0.0)["ds"] * s).sum(1), 0.0, atol=1e-12)
+
+
+# ---- embedding ----------------------------------------------------------------------------------------
+def test_embedding():
+    rng = np.random.default_rng(2)
+    ids, table, dout = rng.integers(0, 5, (3, 4)), rng.standard_normal((5, 6)), rng.standard_normal((3, 4, 6))
+    w = torch.from_numpy(table).requires_grad_(True)
+    out = 0.5 * torch.nn.functional.embedding(torch.from_numpy(ids), w)
+    out.backward(torch.from_numpy(dout))
+    assert np.allclose(mo.embed_fwd(ids, table, 0.5), out.detach()) and np.allclose(mo.embed_bwd(dout, ids, 5, 0.5)["dtable"], w.grad)
+    ids[0, 0], ids[1, 1] = -1, 5   # outside: zeros, and no gradient
+    assert (mo.embed_fwd(ids, table)[0, 0] == 0).all() and (mo.embed_fwd(ids, table)[1, 1] == 0).all()
+    total = mo.embed_bwd(dout, ids, 5)["dtable"].sum(0)
+    assert np.allclose(total, dout.sum((0, 1)) - dout[0, 0] - dout[1, 1])
