@@ -48,3 +48,68 @@ def embed_bwd(dout, ids, vocab, scale=1.0):
             grad[ids[k]] += scale * np.asarray(dout[k], f64)
             size[ids[k]] += np.abs(scale * np.asarray(dout[k], f64))
     return {"dtable": grad, "dtable_size": size}
+
+
+# ---- log probabilities of tokens --------------------------------------------------------------------
+def logprob_fwd(logits, targets=None, top=0):
+    """logits (rows, vocab), targets (rows) or None.  Returns a dict with logp, entropy, max, total (sum of exp(x - max)), p, top_logp, top_ids, and
+    sizes that float32 errors are relative to: logp_size, entropy_size, top_size."""
+    x = np.asarray(logits, f64)
+    rows, vocab = x.shape
+    r = {k: np.zeros(rows) for k in ("logp", "entropy", "max", "total", "logp_size", "entropy_size")}
+    r["p"], r["d"] = np.zeros((rows, vocab)), np.zeros((rows, vocab))
+    r["top_logp"], r["top_size"], r["top_ids"] = np.zeros((rows, top)), np.zeros((rows, top)), np.zeros((rows, top), np.int64)
+    for k in range(rows):
+        t = -1 if targets is None else int(targets[k])
+        asked = 0 <= t < vocab
+        v = x[k]
+        real = np.where(np.isnan(v), -np.inf, v)
+        order = np.lexsort((np.arange(vocab), -real, np.isnan(v)))[:top]   # numbers first, then by value, then by column
+        r["top_ids"][k] = np.where(np.isnan(v[order]), -1, order)
+        if np.isnan(v).any() or (v == np.inf).any():
+            for name in ("entropy", "max", "total"):
+                r[name][k] = np.nan
+            r["logp"][k] = np.nan if asked else 0.0
+            r["top_logp"][k] = r["p"][k] = np.nan
+            continue
+        if (v == -np.inf).all():
+            r["logp"][k] = -np.inf if asked else 0.0
+            r["top_logp"][k] = -np.inf
+            continue
+        m = v.max()
+        d = v - m
+        e = np.exp(d)
+        total = e.sum()
+        d = np.where(e == 0, 0.0, d)
+        p = e / total
+        ls = np.log(total)
+        r["max"][k], r["total"][k], r["p"][k], r["d"][k] = m, total, p, d
+        r["entropy"][k] = ls - (p * d).sum()
+        r["entropy_size"][k] = 1 + ls + (p * (d * d - d)).sum()
+        if asked:
+            r["logp"][k] = v[t] - m - ls
+            r["logp_size"][k] = 1 + ls + (0.0 if np.isinf(v[t]) else m - v[t])
+        r["top_logp"][k] = v[order] - m - ls
+        r["top_size"][k] = 1 + ls + np.where(np.isinf(v[order]), 0.0, m - v[order])
+    return r
+
+
+def logprob_bwd(f, targets=None, dlogp=None, dentropy=None):
+    """Gradient of the logits from ``f``, the forward pass's dict; and the sizes of its terms."""
+    rows, vocab = f["p"].shape
+    grad, size = np.zeros((rows, vocab)), np.zeros((rows, vocab))
+    for k in range(rows):
+        t = -1 if targets is None else int(targets[k])
+        asked = 0 <= t < vocab
+        dl = 0.0 if dlogp is None or not asked else float(dlogp[k])
+        dh = 0.0 if dentropy is None else float(dentropy[k])
+        if f["total"][k] == 0.0 or (dl == 0.0 and dh == 0.0):
+            continue
+        p, d = f["p"][k], f["d"][k]
+        logp = d - np.log(f["total"][k])
+        grad[k] = -p * (dl + dh * (logp + f["entropy"][k]))
+        size[k] = p * (1 - d) * (abs(dl) + abs(dh) * (f["entropy_size"][k] + np.abs(logp)))
+        if asked:
+            grad[k, t] += dl
+            size[k, t] += abs(dl)
+    return {"dlogits": grad, "dlogits_size": size}

@@ -1,5 +1,5 @@
-"""``torch.autograd`` front-ends of the library: the selective scan, the layer around it, layer and RMS norm, the gated recurrence, and
-the embedding.
+"""``torch.autograd`` front-ends of the library: the selective scan, the layer around it, layer and RMS norm, the gated recurrence, the
+embedding and the log probabilities of tokens.
 
 Still marshalling only: ``forward`` enqueues ``ss_scan_fwd`` / ``ss_layer_fwd`` and keeps the
 workspace the library filled, ``backward`` enqueues ``ss_scan_bwd`` / ``ss_layer_bwd``; all
@@ -208,3 +208,31 @@ def embedding(ids, table, scale=1.0, out_dtype=None):
     given).  Ids outside the table (-1 for padding) give zeros and no gradient.  The table's gradient is a sum in token order:
     the same bits every time."""
     return _Embedding.apply(ids, table, scale, out_dtype)
+
+
+class _TokenLogprobs(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, logits, targets, top):
+        logp, entropy, stats, top_logp, top_ids = B.ss_logprob_fwd(logits, targets, top=top)
+        ctx.save_for_backward(logits, targets, entropy, stats)
+        ctx.set_materialize_grads(False)
+        if not top:
+            return logp, entropy
+        ctx.mark_non_differentiable(top_logp, top_ids)
+        return logp, entropy, top_logp, top_ids
+
+    @staticmethod
+    @last_derivative
+    def backward(ctx, dlogp, dentropy, *_):
+        logits, targets, entropy, stats = ctx.saved_tensors
+        if dlogp is None and dentropy is None:
+            return None, None, None
+        return B.ss_logprob_bwd(logits, stats, targets, dlogp=None if dlogp is None else dlogp.contiguous(), entropy=entropy,
+                                dentropy=None if dentropy is None else dentropy.contiguous()), None, None
+
+
+def token_logprobs(logits, targets, top=0):
+    """Differentiable log probabilities of ``targets`` (...) under ``logits`` (..., vocab) and the entropies, float32 (...): (logp, entropy).  A target
+    outside the vocabulary (-1 for padding) has the log probability 0 and no gradient from it; logits of -infinity have probability 0.  With
+    ``top`` also (top_logp, top_ids), (..., top): the most probable columns in order, without a gradient."""
+    return _TokenLogprobs.apply(logits, targets, top)

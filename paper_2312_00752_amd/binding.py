@@ -1,5 +1,5 @@
 """Thin binding (ctypes, and a compiled module for the hot calls) of the C-ABI library declared in the headers of ``include/`` (``ss_scan.h``, ``ss_conv.h``, ``ss_layer.h``,
-``ss_norm.h``, ``ss_gate.h``, ``ss_quant.h``, ``ss_embed.h``).
+``ss_norm.h``, ``ss_gate.h``, ``ss_quant.h``, ``ss_embed.h``, ``ss_logprob.h``).
 
 Argument marshalling only: every step of the path runs in the library's HIP kernels.
 PyTorch appears here solely as the owner of device memory and streams.  The library must
@@ -169,6 +169,16 @@ class EmbedBwdParams(ctypes.Structure):
     _fields_ = [("fwd", EmbedParams), ("dout", _vp), ("dtable", _vp), ("workspace", _vp), ("workspace_bytes", ctypes.c_size_t)]
 
 
+class LogprobParams(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int32), ("vocab", ctypes.c_int32), ("top", ctypes.c_int32), ("io_dtype", ctypes.c_int32), ("flags", ctypes.c_uint32),
+                ("row_stride", ctypes.c_int64), ("logits", _vp), ("targets", _vp), ("logp", _vp), ("entropy", _vp), ("stats", _vp),
+                ("top_logp", _vp), ("top_ids", _vp), ("workspace", _vp), ("workspace_bytes", ctypes.c_size_t)]
+
+
+class LogprobBwdParams(ctypes.Structure):
+    _fields_ = [("fwd", LogprobParams), ("dlogp", _vp), ("dentropy", _vp), ("dlogits", _vp)]
+
+
 SS_GEMM_C_FLOAT, SS_GEMM_ACCUMULATE, SS_GEMM_GENERAL = 1, 2, 4
 SS_ERR_BACKEND = -7
 SS_CONV_SILU, SS_CONV_HAS_BIAS, SS_CONV_HAS_STATE, SS_CONV_WRITE_STATE = 1, 2, 4, 8
@@ -180,6 +190,8 @@ SS_GATE_HAS_RESET, SS_GATE_HAS_H0, SS_GATE_WRITE_H_LAST, SS_GATE_SAVE_FOR_BWD = 
 SS_Q_X_SEQ_LAST, SS_Q_OUT_SEQ_LAST, SS_Q_HAS_BIAS, SS_Q_X_QUANTISED = 1, 2, 4, 8
 SS_QUANT_MAX_DIM = 131072
 SS_EMBED_IDS_32 = 1
+SS_LOGPROB_TARGETS_32 = 1
+SS_LOGPROB_MAX_TOP = 64
 
 _lib = None
 
@@ -229,14 +241,16 @@ def lib():
         for name, params in (("ss_norm_fwd", NormParams), ("ss_norm_quant", NormQuantParams), ("ss_norm_bwd", NormBwdParams),
                              ("ss_gate_fwd", GateParams),
                              ("ss_gate_bwd", GateBwdParams), ("ss_gate_step", GateStepParams), ("ss_quant_rows", QuantParams),
-                             ("ss_qlinear", QLinearParams), ("ss_embed_fwd", EmbedParams), ("ss_embed_bwd", EmbedBwdParams)):
+                             ("ss_qlinear", QLinearParams), ("ss_embed_fwd", EmbedParams), ("ss_embed_bwd", EmbedBwdParams),
+                             ("ss_logprob_fwd", LogprobParams), ("ss_logprob_bwd", LogprobBwdParams)):
             getattr(l, name).restype = ctypes.c_int
             getattr(l, name).argtypes = [ctypes.POINTER(params), _vp]
         for name, args in (("ss_norm_workspace_bytes", [ctypes.POINTER(NormParams)]),
                            ("ss_gate_workspace_bytes", [ctypes.POINTER(GateParams), ctypes.c_int]),
                            ("ss_quant_rows_scratch_bytes", [ctypes.POINTER(QuantParams)]),
                            ("ss_qlinear_scratch_bytes", [ctypes.POINTER(QLinearParams)]), ("ss_quant_pitch", [ctypes.c_int32]),
-                           ("ss_embed_workspace_bytes", [ctypes.POINTER(EmbedParams)])):
+                           ("ss_embed_workspace_bytes", [ctypes.POINTER(EmbedParams)]),
+                           ("ss_logprob_workspace_bytes", [ctypes.POINTER(LogprobParams)])):
             getattr(l, name).restype = ctypes.c_size_t
             getattr(l, name).argtypes = args
         l.ss_version.restype = ctypes.c_int
@@ -1362,6 +1376,107 @@ def ss_embed_bwd(dout, ids, vocab, scale=1.0, dtype=None, out=None, workspace=No
     if need:
         q.workspace, q.workspace_bytes = _lend(workspace, need, dout.device, "workspace")
     _check(lib().ss_embed_bwd(ctypes.byref(q), _stream(stream)))
+    return out
+
+
+# ---------------------------------------------------------------- log probabilities of tokens
+def _row_stride(t, name):
+    """Elements between the rows of a tensor (..., columns) whose rows are dense and equally far from each other."""
+    if t.dim() < 1 or t.shape[-1] < 1:
+        raise ValueError("%s must have an axis of logits" % name)
+    if t.is_contiguous():
+        return t.shape[-1]
+    if t.stride(-1) != 1 and t.shape[-1] != 1:
+        raise ValueError("the last axis of %s must be contiguous" % name)
+    stride, at = None, None
+    for n, s in zip(reversed(t.shape[:-1]), reversed(t.stride()[:-1])):
+        if n == 1:
+            continue
+        if stride is None:
+            stride = s
+        elif s != at:
+            raise ValueError("the rows of %s must be equally far from each other" % name)
+        at = s * n
+    stride = t.shape[-1] if stride is None else stride
+    if stride < t.shape[-1]:
+        raise ValueError("the rows of %s must not overlap" % name)
+    return stride
+
+
+def _logprob_params(logits, targets, top):
+    p = LogprobParams()
+    p.row_stride = _row_stride(logits, "logits")
+    p.vocab = _counts(logits.shape[-1])[0]
+    p.rows, p.top = _counts(logits.numel() // logits.shape[-1], top)
+    p.io_dtype = _io_code(logits)
+    if not logits.is_cuda:
+        raise ValueError("logits must live on the GPU")
+    p.logits = logits.data_ptr()
+    if targets is not None:
+        if targets.dtype is not torch.int64 and targets.dtype is not torch.int32:
+            raise TypeError("targets must be int64 or int32, got %s" % targets.dtype)
+        p.flags = SS_LOGPROB_TARGETS_32 if targets.dtype is torch.int32 else 0
+        p.targets = _ptr(targets, None, logits.shape[:-1], "targets")
+    return p
+
+
+def ss_logprob_workspace_bytes(rows, vocab, top=0):
+    p = LogprobParams()
+    p.rows, p.vocab, p.top = _counts(rows, vocab, top)
+    return int(lib().ss_logprob_workspace_bytes(ctypes.byref(p)))
+
+
+def ss_logprob_fwd(logits, targets=None, top=0, workspace=None, stream=None):
+    """Enqueue the log probabilities of ``targets`` (...) (int64 or int32; outside the vocabulary: none, 0) under ``logits`` (..., vocab), whose rows may
+    lie in wider ones (a slice of a padded vocabulary).  Returns (logp or None, entropy, stats, top_logp, top_ids): float32 of the rows' shape, stats
+    (2, rows) for ``ss_logprob_bwd``, and with ``top`` the most probable columns (..., top) in order, int64, of equal ones the lowest first (else None)."""
+    if stream is not None:
+        with _current(stream):
+            return ss_logprob_fwd(logits, targets, top, workspace)
+    _on_current(logits, targets, workspace)
+    p = _logprob_params(logits, targets, top)
+    shape, dev, f32 = tuple(logits.shape[:-1]), logits.device, torch.float32
+    logp = None if targets is None else torch.empty(shape, dtype=f32, device=dev)
+    entropy, stats = torch.empty(shape, dtype=f32, device=dev), torch.empty((2, p.rows), dtype=f32, device=dev)
+    top_logp = top_ids = None
+    if top:
+        if top < 0 or top > min(p.vocab, SS_LOGPROB_MAX_TOP):
+            raise ValueError("top must be between 0 and %d, got %d" % (min(p.vocab, SS_LOGPROB_MAX_TOP), top))
+        top_logp, top_ids = torch.empty(shape + (top,), dtype=f32, device=dev), torch.empty(shape + (top,), dtype=torch.int64, device=dev)
+        p.top_logp, p.top_ids = top_logp.data_ptr(), top_ids.data_ptr()
+    p.logp = None if logp is None else logp.data_ptr()
+    p.entropy, p.stats = entropy.data_ptr(), stats.data_ptr()
+    need = int(lib().ss_logprob_workspace_bytes(ctypes.byref(p)))
+    if need:
+        p.workspace, p.workspace_bytes = _lend(workspace, need, dev, "workspace")
+    _check(lib().ss_logprob_fwd(ctypes.byref(p), _stream(stream)))
+    return logp, entropy, stats, top_logp, top_ids
+
+
+def ss_logprob_bwd(logits, stats, targets=None, dlogp=None, entropy=None, dentropy=None, out=None, stream=None):
+    """Enqueue the gradient of the logits, dense, of their dtype, from ``dlogp`` (...) and ``dentropy`` (...) (either may be None), the forward call's
+    ``stats``, and with ``dentropy`` its ``entropy``."""
+    if stream is not None:
+        with _current(stream):
+            return ss_logprob_bwd(logits, stats, targets, dlogp, entropy, dentropy, out)
+    _on_current(logits, stats, targets, dlogp, entropy, dentropy, out)
+    q = LogprobBwdParams()
+    q.fwd = _logprob_params(logits, targets, 0)
+    f32, shape = torch.float32, logits.shape[:-1]
+    q.fwd.stats = _ptr(stats, f32, (2, q.fwd.rows), "stats")
+    q.dlogp = _ptr(dlogp, f32, shape, "dlogp")
+    if dentropy is not None:
+        if entropy is None:
+            raise ValueError("dentropy is given, entropy is not")
+        q.fwd.entropy = _ptr(entropy, f32, shape, "entropy")
+        q.dentropy = _ptr(dentropy, f32, shape, "dentropy")
+    if out is None:
+        out = torch.empty(logits.shape, dtype=logits.dtype, device=logits.device)
+    q.dlogits = _ptr(out, logits.dtype, logits.shape, "out")
+    size = logits.element_size()
+    if q.fwd.rows and q.dlogits < q.fwd.logits + ((q.fwd.rows - 1) * q.fwd.row_stride + q.fwd.vocab) * size and q.fwd.logits < q.dlogits + out.numel() * size:
+        raise ValueError("out must not share memory with the logits")
+    _check(lib().ss_logprob_bwd(ctypes.byref(q), _stream(stream)))
     return out
 
 

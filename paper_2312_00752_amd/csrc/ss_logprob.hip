@@ -1,0 +1,492 @@
+// Log probabilities of given tokens with the entropy and the most probable alternatives, and their gradient, for gfx950, with the C-ABI
+// entry points (see include/ss_logprob.h).
+//
+// The logits are read once by each pass, and the gradient is written: both are bound by HBM.  Forward: every lane keeps the
+// largest logit m that it has seen, S = sum exp(x - m) and U = sum exp(x - m) (x - m), which are brought to a new m by
+// S <- c S, U <- c (U + S (m_old - m)) with c = exp(m_old - m); lanes, waves and workgroups are joined by the same rule.  Then
+// lse = m + log S and the entropy log S - U / S.  Few rows are cut into pieces for several workgroups.
+// Alternatives: a wave holds its best, in order, one a lane.  Of 64 groups of logits, one a lane, the top-th largest maximum is a bound below
+// which nothing can be among the top, so of thousands of logits only about `top` are looked at one by one; each is put in its
+// place by a ballot and a shift.
+#include <hip/hip_runtime.h>
+#include <algorithm>
+#include <cmath>
+#include <type_traits>
+
+#include "ss_logprob.h"
+#include "ss_slices.h"
+
+namespace ss {
+
+struct LogprobArgs {
+    int rows, vocab, top;
+    int64_t row_stride;
+    const void *logits, *targets;
+    float *logp, *entropy, *max, *inv, *top_logp;
+    int64_t* top_ids;
+    int pieces, piece;        // workgroups of a row, columns of each
+    float* part;              // (rows, pieces): m, S, U and the best
+    const float *dlogp, *dentropy;
+    void* dlogits;
+};
+
+constexpr float FAR = -200.0f;   // exp of it is 0 in float32; a logarithm of a probability that is 0 is cut off here, so that 0 times it is 0
+
+struct Stat {
+    float m, s, u;
+};
+__device__ __forceinline__ float exp_of(float v) { return __builtin_amdgcn_exp2f(v * 1.44269504f); }
+// what m is taken as where nothing but -infinity has been seen
+__device__ __forceinline__ float reference(float m) { return m == -INFINITY ? 0.0f : m; }
+__device__ __forceinline__ void shift(Stat& a, float ref)
+{
+    const float d = fmaxf(a.m - ref, FAR), c = exp_of(d);
+    a.u = (a.u + a.s * d) * c;
+    a.s *= c;
+}
+__device__ __forceinline__ Stat join(Stat a, Stat b)
+{
+    const float m = fmaxf(a.m, b.m), ref = reference(m);
+    shift(a, ref);
+    shift(b, ref);
+    return {m, a.s + b.s, a.u + b.u};
+}
+__device__ __forceinline__ Stat join_wave(Stat a)
+{
+#pragma unroll
+    for (int s = 1; s < WAVE; s *= 2) a = join(a, {__shfl_xor(a.m, s), __shfl_xor(a.s, s), __shfl_xor(a.u, s)});
+    return a;
+}
+
+// ---- the best of a wave ---------------------------------------------------------------------------
+// Lane l holds the l-th best (value, column); a column of -1 is an empty place.  All lanes call; `top` lanes are kept exact.
+struct Best {
+    float v = -INFINITY;
+    int i = -1;
+    __device__ __forceinline__ bool ahead(float x, int k) const { return i >= 0 && (v > x || (v == x && i < k)); }
+    __device__ __forceinline__ void insert(float x, int k)   // the same in all lanes
+    {
+        const int place = __popcll(__ballot(ahead(x, k))), lane = threadIdx.x % WAVE;
+        const float pv = __shfl_up(v, 1);
+        const int pi = __shfl_up(i, 1);
+        if (lane > place) {
+            v = pv;
+            i = pi;
+        } else if (lane == place) {
+            v = x;
+            i = k;
+        }
+    }
+    // N values a lane; column(j) is -1 for those that are left out
+    template <int N, typename F>
+    __device__ __forceinline__ void absorb(const float (&x)[N], F column, int top)
+    {
+        static_assert(N <= 32, "a bit each");
+        const int lane = threadIdx.x % WAVE;
+        float lv = __shfl(v, top - 1);
+        int li = __shfl(i, top - 1);
+        uint32_t open = 0;   // what the last of the top is not ahead of
+        float most = -INFINITY;
+#pragma unroll
+        for (int j = 0; j < N; ++j) {
+            const int k = column(j);
+            if (k >= 0 && !(li >= 0 && (lv > x[j] || (lv == x[j] && li < k)))) {
+                open |= 1u << j;
+                most = fmaxf(most, x[j]);
+            }
+        }
+        if (!__ballot(open != 0)) return;
+        if (li < 0) {   // the top is not full yet: the top-th largest of the lanes' maxima is a bound, as that many values are no less
+            int above = 0;
+            for (int l = 0; l < WAVE; ++l) {
+                const float o = __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(most), l));
+                above += o > most || (o == most && l < lane) ? 1 : 0;
+            }
+            const float bound = __shfl(most, __ffsll((long long)__ballot(above == top - 1)) - 1);
+#pragma unroll
+            for (int j = 0; j < N; ++j)
+                if (!(x[j] >= bound)) open &= ~(1u << j);
+        }
+        while (__ballot(open != 0)) {
+            // every lane's first candidate
+            float cv = 0.0f;
+            int ck = -1;
+#pragma unroll
+            for (int j = N - 1; j >= 0; --j)
+                if (open >> j & 1) {
+                    cv = x[j];
+                    ck = column(j);
+                }
+            open &= open - 1;
+            bool late = behind(cv, ck, top);
+            uint64_t ask = __ballot(ck >= 0 && !late);
+            while (ask) {
+                const int l = __ffsll((long long)ask) - 1;
+                insert(__shfl(cv, l), __shfl(ck, l));
+                ask &= ask - 1;
+                late = behind(cv, ck, top);
+                ask &= __ballot(!late);
+            }
+        }
+    }
+    // whether the last of the top is ahead of (x, k); all lanes call
+    __device__ __forceinline__ bool behind(float x, int k, int top) const
+    {
+        const float lv = __shfl(v, top - 1);
+        const int li = __shfl(i, top - 1);
+        return li >= 0 && (lv > x || (lv == x && li < k));
+    }
+};
+
+// ---- results of a row -----------------------------------------------------------------------------
+template <typename I>
+__device__ __forceinline__ int target_of(const LogprobArgs& a, int row)   // -1: none
+{
+    if (!a.targets) return -1;
+    const I t = static_cast<const I*>(a.targets)[row];
+    return t >= 0 && t < a.vocab ? (int)t : -1;
+}
+template <typename T, typename I, bool TOP>
+__device__ __forceinline__ void results(const LogprobArgs& a, int row, Stat t, const Best& best)
+{
+    const int lane = threadIdx.x % WAVE;
+    const bool none = t.s == 0.0f;   // the largest logit alone makes S one
+    const float ls = logf(t.s);
+    auto logp = [&](float x) { return none ? -INFINITY : (x - t.m) - ls; };
+    if (lane == 0) {
+        if (a.logp) {
+            const int k = target_of<I>(a, row);
+            a.logp[row] = k < 0 ? 0.0f : logp(io_to_f32<T>(static_cast<const T*>(a.logits)[row * a.row_stride + k]));
+        }
+        a.entropy[row] = none ? 0.0f : ls - t.u / t.s;
+        a.max[row] = none ? 0.0f : t.m;
+        a.inv[row] = none ? 0.0f : 1.0f / t.s;
+    }
+    if constexpr (TOP) {
+        if (lane < a.top) {
+            a.top_logp[(int64_t)row * a.top + lane] = best.i < 0 ? __uint_as_float(0x7fc00000u) : logp(best.v);
+            a.top_ids[(int64_t)row * a.top + lane] = best.i;
+        }
+    }
+}
+// floats of a workgroup's share of a row: m, S, U, then `top` values and as many columns
+__host__ __device__ __forceinline__ int part_floats(int top) { return 4 + 2 * top; }
+
+// G lanes a row (a wave: rows side by side) or piece of one; V slices of eight a lane and step, the next step's requested ahead.
+template <typename T, typename I, int G, bool TOP>
+__global__ __launch_bounds__(256) void logprob_fwd_kernel(LogprobArgs a)
+{
+    constexpr int V = 4, SIDE = 256 / G, WAVES = G / WAVE;
+    const int gl = threadIdx.x % G;
+    const unsigned group = blockIdx.x * SIDE + threadIdx.x / G;
+    const int row = (int)(group / (unsigned)a.pieces), piece = (int)(group % (unsigned)a.pieces);
+    if (row >= a.rows) return;   // a whole wave
+    const T* x = static_cast<const T*>(a.logits) + row * a.row_stride;
+    const int W = a.vocab, from = piece * a.piece, to = min(from + a.piece, W);
+    const bool whole = W % 8 == 0;
+    const int limit = slice_limit(W, whole);
+    typename io8<T>::raw raw[V];
+    auto load = [&](int base) {
+#pragma unroll
+        for (int v = 0; v < V; ++v) raw[v] = slice_request<T, true>(x, base + (v * G + gl) * 8, W, limit);
+    };
+    Stat t = {-INFINITY, 0.0f, 0.0f};
+    Best best;
+    load(from);
+    for (int base = from; base < to; base += V * G * 8) {
+        float f[V][8];
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            const int at = base + (v * G + gl) * 8, n = to - at;
+            slice_settle<T>(raw[v], at, W, limit, whole);
+            io8<T>::unpack(raw[v], f[v]);
+            if (n < 8) {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) f[v][j] = j < n ? f[v][j] : -INFINITY;
+            }
+        }
+        if (base + V * G * 8 < to) load(base + V * G * 8);
+        float m = t.m;
+#pragma unroll
+        for (int v = 0; v < V; ++v)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) m = fmaxf(m, f[v][j]);
+        const float ref = reference(m);
+        shift(t, ref);
+        t.m = m;
+#pragma unroll
+        for (int v = 0; v < V; ++v)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const float d = f[v][j] - ref, e = exp_of(d);   // NaN stays NaN in e
+                t.s += e;
+                t.u = fmaf(e, fmaxf(d, FAR), t.u);
+            }
+        if constexpr (TOP) {
+            const float(&all)[V * 8] = reinterpret_cast<const float(&)[V * 8]>(f);
+            best.absorb(all, [&](int j) {
+                const int k = base + (j / 8 * G + gl) * 8 + j % 8;
+                return k < to && all[j] == all[j] ? k : -1;
+            }, a.top);
+        }
+    }
+    t = join_wave(t);
+    if constexpr (WAVES > 1) {
+        __shared__ Stat stats[WAVES];
+        __shared__ float values[WAVES][TOP ? WAVE : 1];
+        __shared__ int columns[WAVES][TOP ? WAVE : 1];
+        const int wave = threadIdx.x / WAVE, lane = threadIdx.x % WAVE;
+        if (lane == 0) stats[wave] = t;
+        if constexpr (TOP) {
+            values[wave][lane] = best.v;
+            columns[wave][lane] = lane < a.top ? best.i : -1;
+        }
+        __syncthreads();
+        if (wave != 0) return;
+        for (int w = 1; w < WAVES; ++w) t = join(t, stats[w]);
+        if constexpr (TOP) {
+            float f[WAVES - 1];
+#pragma unroll
+            for (int w = 1; w < WAVES; ++w) f[w - 1] = values[w][lane];
+            best.absorb(f, [&](int j) { return columns[j + 1][lane]; }, a.top);
+        }
+        if (a.pieces > 1) {
+            float* p = a.part + (int64_t)group * part_floats(a.top);
+            if (lane == 0) {
+                p[0] = t.m;
+                p[1] = t.s;
+                p[2] = t.u;
+            }
+            if constexpr (TOP) {
+                if (lane < a.top) {
+                    p[4 + lane] = best.v;
+                    p[4 + a.top + lane] = __int_as_float(best.i);
+                }
+            }
+            return;
+        }
+    }
+    results<T, I, TOP>(a, row, t, best);
+}
+// The pieces of a row, a wave a row.
+template <typename T, typename I, bool TOP>
+__global__ __launch_bounds__(64) void logprob_join_kernel(LogprobArgs a)
+{
+    const int row = blockIdx.x, lane = threadIdx.x;
+    const float* p = a.part + (int64_t)row * a.pieces * part_floats(a.top);
+    Stat t = {-INFINITY, 0.0f, 0.0f};
+    for (int k = lane; k < a.pieces; k += WAVE) {
+        const float* q = p + (int64_t)k * part_floats(a.top);
+        t = join(t, {q[0], q[1], q[2]});
+    }
+    t = join_wave(t);
+    Best best;
+    if constexpr (TOP) {
+        constexpr int N = 8;
+        const int all = a.pieces * a.top;
+        for (int c0 = 0; c0 < all; c0 += N * WAVE) {
+            float f[N];
+            int k[N];
+#pragma unroll
+            for (int j = 0; j < N; ++j) {
+                const int c = c0 + j * WAVE + lane;
+                const float* q = p + (int64_t)(min(c, all - 1) / a.top) * part_floats(a.top) + 4 + min(c, all - 1) % a.top;
+                f[j] = q[0];
+                k[j] = c < all ? __float_as_int(q[a.top]) : -1;
+            }
+            best.absorb(f, [&](int j) { return k[j]; }, a.top);
+        }
+    }
+    results<T, I, TOP>(a, row, t, best);
+}
+
+// ---- backward -------------------------------------------------------------------------------------
+// G lanes a row or piece of one, all of its slices requested at once.
+template <typename T, typename I, int G>
+__global__ __launch_bounds__(256) void logprob_bwd_kernel(LogprobArgs a)
+{
+    constexpr int V = 4, SIDE = 256 / G;
+    const int gl = threadIdx.x % G;
+    const unsigned group = blockIdx.x * SIDE + threadIdx.x / G;
+    const int row = (int)(group / (unsigned)a.pieces), from = (int)(group % (unsigned)a.pieces) * a.piece;
+    if (row >= a.rows) return;
+    const int W = a.vocab, k = target_of<I>(a, row);
+    const float inv = a.inv[row];
+    const bool some = inv != 0.0f;   // also where it is NaN
+    const float dl = a.dlogp && k >= 0 && some ? a.dlogp[row] : 0.0f, dh = a.dentropy && some ? a.dentropy[row] : 0.0f;
+    T* out = static_cast<T*>(a.dlogits) + (int64_t)row * W;
+    if (dl == 0.0f && dh == 0.0f) {
+        const float z[8] = {};
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            const int at = from + (v * G + gl) * 8;
+            slice_store<T>(out, at, W - at, z);
+        }
+        return;
+    }
+    const T* x = static_cast<const T*>(a.logits) + row * a.row_stride;
+    const bool whole = W % 8 == 0;
+    const int limit = slice_limit(W, whole);
+    typename io8<T>::raw raw[V];
+#pragma unroll
+    for (int v = 0; v < V; ++v) raw[v] = slice_request<T, true>(x, from + (v * G + gl) * 8, W, limit);
+    const float m = a.max[row], ls = logf(inv);
+    // dx = -p (dl + dh (log p + H)) = -p (c0 + dh d), d = x - m
+    const float c0 = dh == 0.0f ? dl : fmaf(dh, ls + a.entropy[row], dl);
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+        const int at = from + (v * G + gl) * 8;
+        float f[8];
+        slice_settle<T>(raw[v], at, W, limit, whole);
+        io8<T>::unpack(raw[v], f);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const float d = f[j] - m, p = exp_of(d) * inv;
+            f[j] = -p * fmaf(dh, fmaxf(d, FAR), c0);
+            if (at + j == k) f[j] += dl;
+        }
+        slice_store<T>(out, at, W - at, f);
+    }
+}
+
+// ---- sizes ----------------------------------------------------------------------------------------
+constexpr int LOGPROB_STEP = 4 * 256 * 8;    // columns that a workgroup has in registers at once
+constexpr int LOGPROB_WAVE = 4 * 64 * 8;     // and a wave: up to here a row is one wave's
+
+struct LogprobPlan {
+    int pieces, piece;
+    size_t bytes;
+};
+// Rows are cut where there are fewer than 2048 workgroups of them, into pieces of 2048 columns at least.
+LogprobPlan logprob_plan(int rows, int vocab, int top)
+{
+    LogprobPlan p = {1, vocab, 0};
+    if (vocab <= LOGPROB_WAVE || rows >= 2048) return p;
+    const int units = (vocab + 2047) / 2048, want = std::min({(2048 + rows - 1) / rows, units, 1024});
+    const int each = (units + want - 1) / want;
+    p.piece = each * 2048;
+    p.pieces = (units + each - 1) / each;
+    if (p.pieces > 1) p.bytes = (size_t)rows * p.pieces * part_floats(top) * sizeof(float);
+    return p;
+}
+
+template <typename T, typename I, bool TOP>
+void logprob_forward(const LogprobArgs& a, hipStream_t st)
+{
+    if (a.vocab <= LOGPROB_WAVE) {
+        hipLaunchKernelGGL((logprob_fwd_kernel<T, I, 64, TOP>), dim3((unsigned)(((int64_t)a.rows + 3) / 4)), dim3(256), 0, st, a);
+        return;
+    }
+    hipLaunchKernelGGL((logprob_fwd_kernel<T, I, 256, TOP>), dim3((unsigned)((int64_t)a.rows * a.pieces)), dim3(256), 0, st, a);
+    if (a.pieces > 1) hipLaunchKernelGGL((logprob_join_kernel<T, I, TOP>), dim3((unsigned)a.rows), dim3(64), 0, st, a);
+}
+template <typename T, typename I>
+void logprob_backward(LogprobArgs a, hipStream_t st)
+{
+    if (a.vocab <= LOGPROB_WAVE) {
+        a.pieces = 1;
+        a.piece = LOGPROB_WAVE;
+        hipLaunchKernelGGL((logprob_bwd_kernel<T, I, 64>), dim3((unsigned)(((int64_t)a.rows + 3) / 4)), dim3(256), 0, st, a);
+        return;
+    }
+    a.piece = LOGPROB_STEP;
+    a.pieces = (a.vocab + LOGPROB_STEP - 1) / LOGPROB_STEP;
+    hipLaunchKernelGGL((logprob_bwd_kernel<T, I, 256>), dim3((unsigned)((int64_t)a.rows * a.pieces)), dim3(256), 0, st, a);
+}
+template <typename F>
+void with_types(const ss_logprob_params* p, F go)
+{
+    auto targets = [&](auto t) {
+        if (p->flags & SS_LOGPROB_TARGETS_32) go(t, (int32_t)0);
+        else go(t, (int64_t)0);
+    };
+    if (p->io_dtype == SS_F32) targets(float());
+    else targets(bf16_t());
+}
+
+}  // namespace ss
+
+namespace {
+
+inline bool aligned_to(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) % a) == 0; }
+constexpr int64_t LOGPROB_MOST = ((int64_t)1 << 24) - 1;   // workgroups of 256 threads: a launch has fewer than 2^32
+
+int check_logprob(const ss_logprob_params* p)
+{
+    if (!p) return SS_ERR_NULL;
+    if (p->rows < 0 || p->vocab < 1 || p->top < 0 || p->row_stride < p->vocab) return SS_ERR_SHAPE;
+    if (p->io_dtype != SS_F32 && p->io_dtype != SS_BF16) return SS_ERR_UNSUPPORTED;
+    if (p->flags & ~(uint32_t)SS_LOGPROB_TARGETS_32) return SS_ERR_UNSUPPORTED;
+    if (p->top > p->vocab || p->top > SS_LOGPROB_MAX_TOP) return SS_ERR_UNSUPPORTED;
+    if (p->vocab > 0x7fffffff - 65536) return SS_ERR_UNSUPPORTED;   // room for the last steps of the kernels' loops
+    const int64_t pieces = p->vocab <= ss::LOGPROB_WAVE ? 1 : (p->vocab + ss::LOGPROB_STEP - 1) / ss::LOGPROB_STEP;
+    if (p->rows * pieces > (p->vocab <= ss::LOGPROB_WAVE ? 4 * LOGPROB_MOST : LOGPROB_MOST)) return SS_ERR_UNSUPPORTED;
+    if (p->rows > 0 && (!p->logits || !p->stats)) return SS_ERR_NULL;
+    if (!aligned_to(p->logits, p->io_dtype == SS_BF16 ? 2 : 4) || !aligned_to(p->stats, 4)) return SS_ERR_ALIGN;
+    if (!aligned_to(p->targets, p->flags & SS_LOGPROB_TARGETS_32 ? 4 : 8)) return SS_ERR_ALIGN;
+    return SS_OK;
+}
+ss::LogprobArgs logprob_args(const ss_logprob_params* p)
+{
+    ss::LogprobArgs a{};
+    a.rows = p->rows; a.vocab = p->vocab; a.top = p->top; a.row_stride = p->row_stride;
+    a.logits = p->logits; a.targets = p->targets;
+    a.entropy = p->entropy;
+    a.max = p->stats;
+    a.inv = p->stats + p->rows;
+    return a;
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t ss_logprob_workspace_bytes(const ss_logprob_params* p)
+{
+    if (!p || p->rows < 1 || p->vocab < 1 || p->top < 0 || p->top > SS_LOGPROB_MAX_TOP) return 0;
+    return ss::logprob_plan(p->rows, p->vocab, p->top).bytes;
+}
+
+int ss_logprob_fwd(const ss_logprob_params* p, void* stream)
+{
+    const int rc = check_logprob(p);
+    if (rc != SS_OK) return rc;
+    if (p->rows == 0) return SS_OK;
+    if (!p->entropy || (p->targets && !p->logp) || (p->top && (!p->top_logp || !p->top_ids))) return SS_ERR_NULL;
+    if (!aligned_to(p->logp, 4) || !aligned_to(p->entropy, 4) || (p->top && (!aligned_to(p->top_logp, 4) || !aligned_to(p->top_ids, 8)))) return SS_ERR_ALIGN;
+    const ss::LogprobPlan plan = ss::logprob_plan(p->rows, p->vocab, p->top);
+    if (plan.bytes) {
+        if (!p->workspace || p->workspace_bytes < plan.bytes) return SS_ERR_WORKSPACE;
+        if (!aligned_to(p->workspace, 256)) return SS_ERR_ALIGN;
+    }
+    ss::LogprobArgs a = logprob_args(p);
+    a.logp = p->logp;
+    a.top_logp = p->top_logp; a.top_ids = p->top_ids;
+    a.pieces = plan.pieces; a.piece = plan.piece;
+    a.part = static_cast<float*>(p->workspace);
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    ss::with_types(p, [&](auto t, auto i) {
+        if (p->top) ss::logprob_forward<decltype(t), decltype(i), true>(a, st);
+        else ss::logprob_forward<decltype(t), decltype(i), false>(a, st);
+    });
+    return hipGetLastError() == hipSuccess ? SS_OK : SS_ERR_LAUNCH;
+}
+
+int ss_logprob_bwd(const ss_logprob_bwd_params* p, void* stream)
+{
+    if (!p) return SS_ERR_NULL;
+    const ss_logprob_params* f = &p->fwd;
+    const int rc = check_logprob(f);
+    if (rc != SS_OK) return rc;
+    if (f->rows == 0) return SS_OK;
+    if (!p->dlogits || (p->dentropy && !f->entropy)) return SS_ERR_NULL;
+    if (!aligned_to(p->dlogits, f->io_dtype == SS_BF16 ? 2 : 4) || !aligned_to(p->dlogp, 4) || !aligned_to(p->dentropy, 4) || !aligned_to(f->entropy, 4))
+        return SS_ERR_ALIGN;
+    ss::LogprobArgs a = logprob_args(f);
+    a.dlogp = p->dlogp; a.dentropy = p->dentropy;
+    a.dlogits = p->dlogits;
+    ss::with_types(f, [&](auto t, auto i) { ss::logprob_backward<decltype(t), decltype(i)>(a, static_cast<hipStream_t>(stream)); });
+    return hipGetLastError() == hipSuccess ? SS_OK : SS_ERR_LAUNCH;
+}
+
+}  // extern "C"

@@ -1,4 +1,4 @@
-"""What the entry points of the norms' 8-bit results and of the embedding refuse, on the host, before any device call; and their structs as the C compiler lays them out."""
+"""What the entry points of the norms' 8-bit results, the embedding and the log probabilities refuse, on the host, before any device call; and their structs as the C compiler lays them out."""
 import ctypes
 import os
 import subprocess
@@ -12,8 +12,9 @@ ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 FAKE = 0x7F0000001000   # non-null, 4096-byte aligned, never dereferenced
 MANY = 2 ** 32 + 5
 
-STRUCTS = {"ss_norm_quant_params": B.NormQuantParams, "ss_embed_params": B.EmbedParams, "ss_embed_bwd_params": B.EmbedBwdParams}
-HEADERS = ["ss_norm.h", "ss_embed.h"]
+STRUCTS = {"ss_norm_quant_params": B.NormQuantParams, "ss_embed_params": B.EmbedParams, "ss_embed_bwd_params": B.EmbedBwdParams,
+           "ss_logprob_params": B.LogprobParams, "ss_logprob_bwd_params": B.LogprobBwdParams}
+HEADERS = ["ss_norm.h", "ss_embed.h", "ss_logprob.h"]
 
 
 def t(*shape, dtype=torch.bfloat16):
@@ -132,6 +133,50 @@ def test_embed():
                                   lambda: B.ss_embed_fwd(t(3, dtype=torch.int64), t(1, MANY)), lambda: B.ss_embed_bwd(t(MANY, 1), t(MANY, dtype=torch.int32), 5),
                                   lambda: B.ss_embed_bwd(t(3, 4), t(3, dtype=torch.int32), MANY), lambda: B.ss_embed_workspace_bytes(4, 4, MANY)])
 def test_embed_sizes_beyond_32_bits(call):
+    with pytest.raises(B.SsError) as e:
+        call()
+    assert e.value.code == B.SS_ERR_UNSUPPORTED
+
+
+# ---- log probabilities --------------------------------------------------------------------------------
+def logprob():
+    p = B.LogprobParams()
+    p.rows, p.vocab, p.top, p.io_dtype, p.row_stride = 4, 20000, 5, B.SS_BF16, 20000
+    for f in ("logits", "targets", "logp", "entropy", "stats", "top_logp", "top_ids", "workspace"):
+        setattr(p, f, FAKE)
+    p.workspace_bytes = B.ss_logprob_workspace_bytes(4, 20000, 5)
+    return p
+
+
+def logprob_bwd():
+    p = B.LogprobBwdParams()
+    p.fwd = logprob()
+    p.dlogp = p.dentropy = p.dlogits = FAKE
+    return p
+
+
+def test_logprob():
+    call = B.lib().ss_logprob_fwd
+    assert call(None, None) == B.SS_ERR_NULL
+    expect(call, logprob, [{f: None} for f in ("logits", "logp", "entropy", "stats", "top_logp", "top_ids")], B.SS_ERR_NULL)
+    expect(call, logprob, [dict(rows=-1), dict(vocab=0), dict(top=-1), dict(row_stride=19999)], B.SS_ERR_SHAPE)
+    big = 2 ** 31 - 1
+    expect(call, logprob, [dict(io_dtype=2), dict(flags=2), dict(top=65), dict(vocab=4, top=5), dict(vocab=big, row_stride=big), dict(rows=big),
+                           dict(rows=2 ** 24 // 3 + 1), dict(rows=2 ** 26, vocab=2048)], B.SS_ERR_UNSUPPORTED)
+    expect(call, logprob, [dict(logits=FAKE + 1), dict(targets=FAKE + 4), dict(logp=FAKE + 2), dict(entropy=FAKE + 2), dict(stats=FAKE + 1),
+                           dict(top_logp=FAKE + 2), dict(top_ids=FAKE + 4), dict(workspace=FAKE + 128), dict(flags=1, targets=FAKE + 2)], B.SS_ERR_ALIGN)
+    expect(call, logprob, [dict(workspace=None), dict(workspace_bytes=logprob().workspace_bytes - 1)], B.SS_ERR_WORKSPACE)
+    expect(call, logprob, [dict(rows=0, logits=None, stats=None)], B.SS_OK)
+    call = B.lib().ss_logprob_bwd
+    assert call(None, None) == B.SS_ERR_NULL
+    expect(call, logprob_bwd, [{"fwd.logits": None}, {"fwd.stats": None}, {"fwd.entropy": None}, dict(dlogits=None)], B.SS_ERR_NULL)
+    expect(call, logprob_bwd, [dict(dlogp=FAKE + 2), dict(dentropy=FAKE + 1), dict(dlogits=FAKE + 1), {"fwd.entropy": FAKE + 2}], B.SS_ERR_ALIGN)
+    assert B.ss_logprob_workspace_bytes(4, 2048, 5) == 0 and B.ss_logprob_workspace_bytes(0, 20000) == 0 and B.ss_logprob_workspace_bytes(5000, 20000) == 0
+
+
+@pytest.mark.parametrize("call", [lambda: B.ss_logprob_fwd(t(MANY, 4)), lambda: B.ss_logprob_fwd(t(1, MANY)), lambda: B.ss_logprob_workspace_bytes(1, MANY),
+                                  lambda: B.ss_logprob_bwd(t(MANY, 4), t(2, MANY, dtype=torch.float32))])
+def test_logprob_sizes_beyond_32_bits(call):
     with pytest.raises(B.SsError) as e:
         call()
     assert e.value.code == B.SS_ERR_UNSUPPORTED

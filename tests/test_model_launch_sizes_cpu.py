@@ -57,3 +57,35 @@ static void one()
 
 def test_embed(tmp_path):
     run(tmp_path, "ss_embed.hip", EMBED)
+
+
+LOGPROB = r"""
+static void one()
+{
+    ss_logprob_bwd_params q{};
+    ss_logprob_params& p = q.fwd;
+    p.io_dtype = coin(2);
+    p.flags = (uint32_t)coin(2);
+    p.rows = any(2147418111);
+    p.vocab = 1 + any(2147418110);
+    p.top = coin(2) ? coin(65) : 0;
+    p.row_stride = p.vocab + coin(100);
+    if ((double)p.rows * p.row_stride * (p.io_dtype == SS_BF16 ? 2 : 4) > CARD) return;
+    p.logits = p.targets = fake;
+    p.logp = p.entropy = p.stats = p.top_logp = static_cast<float*>(fake);
+    p.top_ids = static_cast<int64_t*>(fake);
+    p.workspace = q.dlogits = fake;
+    q.dlogp = q.dentropy = static_cast<float*>(fake);
+    p.workspace_bytes = ss_logprob_workspace_bytes(&p);
+    const int rc = ss_logprob_fwd(&p, nullptr);
+    const int64_t workgroups = p.vocab <= 2048 ? ((int64_t)p.rows + 3) / 4 : (int64_t)p.rows * ((p.vocab + 8191) / 8192);
+    if ((rc == SS_OK) != (p.top <= p.vocab && workgroups < (1 << 24))) std::exit(1);
+    look(rc, "ss_logprob_fwd", p.rows, p.vocab, p.top, p.row_stride, p.io_dtype, p.flags);
+    if (ss_logprob_bwd(&q, nullptr) != rc) std::exit(1);
+    look(rc, "ss_logprob_bwd", p.rows, p.vocab, p.top, p.row_stride, p.io_dtype, p.flags);
+}
+"""
+
+
+def test_logprob(tmp_path):
+    run(tmp_path, "ss_logprob.hip", LOGPROB)

@@ -51,3 +51,31 @@ def test_embedding():
     assert (mo.embed_fwd(ids, table)[0, 0] == 0).all() and (mo.embed_fwd(ids, table)[1, 1] == 0).all()
     total = mo.embed_bwd(dout, ids, 5)["dtable"].sum(0)
     assert np.allclose(total, dout.sum((0, 1)) - dout[0, 0] - dout[1, 1])
+
+
+# ---- log probabilities --------------------------------------------------------------------------------
+def test_log_probabilities():
+    rng = np.random.default_rng(3)
+    x, t, dl, dh = 3 * rng.standard_normal((6, 11)), rng.integers(0, 11, 6), rng.standard_normal(6), rng.standard_normal(6)
+    t[4] = -1
+    v = torch.from_numpy(x).requires_grad_(True)
+    logs = torch.log_softmax(v, -1)
+    logp = torch.where(torch.from_numpy(t) < 0, 0.0, logs[torch.arange(6), torch.from_numpy(t).clamp(min=0)])
+    entropy = -(logs.exp() * logs).sum(-1)
+    grad, = torch.autograd.grad((logp * torch.from_numpy(dl)).sum() + (entropy * torch.from_numpy(dh)).sum(), v)
+    f = mo.logprob_fwd(x, t, 4)
+    assert np.allclose(f["logp"], logp.detach()) and np.allclose(f["entropy"], entropy.detach()) and np.allclose(f["p"].sum(1), 1.0)
+    assert np.allclose(mo.logprob_bwd(f, t, dl, dh)["dlogits"], grad)
+    assert np.array_equal(f["top_ids"], torch.topk(v, 4).indices) and np.allclose(f["top_logp"], torch.topk(logs, 4).values.detach())
+    assert np.allclose(mo.logprob_bwd(f, t, dl)["dlogits"].sum(1), 0.0)   # a shift of all logits changes nothing
+
+
+def test_log_probabilities_of_masked_rows():
+    inf = np.inf
+    x = np.array([[0.0, -inf, 0.0, 0.0], [-inf] * 4, [-inf, 2.0, -inf, -inf], [0.0, np.nan, 1.0, inf]])
+    f = mo.logprob_fwd(x, [1, 2, 1, 0], 3)
+    assert np.array_equal(f["logp"][:3], [-inf, -inf, 0.0]) and np.allclose(f["entropy"][:3], [np.log(3), 0.0, 0.0]) and np.isnan(f["logp"][3])
+    assert f["top_ids"].tolist() == [[0, 2, 3], [0, 1, 2], [1, 0, 2], [3, 2, 0]]
+    g = mo.logprob_bwd(f, [1, 2, 1, 0], np.ones(4), np.ones(4))["dlogits"]
+    assert np.allclose(g[0], [-1 / 3, 1.0, -1 / 3, -1 / 3]) and (g[1] == 0).all() and (g[2] == 0).all() and np.isnan(g[3]).any()
+    assert mo.logprob_fwd(np.array([[np.nan, 1.0]]), None, 2)["top_ids"].tolist() == [[1, -1]]
