@@ -113,3 +113,47 @@ def logprob_bwd(f, targets=None, dlogp=None, dentropy=None):
             grad[k, t] += dl
             size[k, t] += abs(dl)
     return {"dlogits": grad, "dlogits_size": size}
+
+
+# ---- AdamW ------------------------------------------------------------------------------------------
+def adamw(param, grad, m, v, step, lr, beta1, beta2, eps, weight_decay):
+    """One step on float64 arrays, the moments' factors as float32 holds them.  Returns param, m, v, and what the error of the parameter's step is relative to:
+    the step that the magnitudes of m's two terms, which may cancel, would make."""
+    f32 = lambda b: f64(np.float32(b))
+    size = f32(beta1) * np.abs(m) + f32(1 - beta1) * np.abs(grad)
+    m = f32(beta1) * m + f32(1 - beta1) * grad
+    v = f32(beta2) * v + f32(1 - beta2) * grad * grad
+    rate = lr / (1 - beta1 ** step) / (np.sqrt(v / (1 - beta2 ** step)) + eps)
+    return param * (1 - lr * weight_decay) - rate * m, m, v, rate * size
+
+
+ADAMW_BLOCK = 256
+
+
+def adamw_codes(x, step, signed):
+    """x (n), m or sqrt(v): (codes, scale) as the moments are held in 8 bits, in exact arithmetic."""
+    x = np.asarray(x, f64)
+    n, top = len(x), 127 if signed else 255
+    c0, c1 = (0x6A09E667, 0xBB67AE85) if signed else (0x3C6EF372, 0xA54FF53A)
+    codes, scale = np.zeros(n, np.int64), np.zeros(-(-n // ADAMW_BLOCK))
+    for b in range(len(scale)):
+        at = slice(b * ADAMW_BLOCK, min(n, (b + 1) * ADAMW_BLOCK))
+        a = np.abs(x[at]).max()
+        if not np.isfinite(a):
+            scale[b] = np.nan
+            continue
+        if a < 2.0 ** -100:
+            continue
+        scale[b] = a
+        y = top * top * np.abs(x[at]) / a
+        q = np.floor(np.sqrt(y))
+        u = np.array([((i * c0 + step * c1) % 2 ** 32 >> 8) / 2.0 ** 24 for i in range(at.start, at.stop)])
+        q = np.minimum(q + ((y - q * q) / (2 * q + 1) > u), top)
+        codes[at] = np.where(x[at] < 0, -q, q) if signed else np.where(x[at] > 0, np.maximum(q, 1), 0)
+    return codes, scale
+
+
+def adamw_values(codes, scale, signed):
+    codes = np.asarray(codes, f64)
+    top = 127 if signed else 255
+    return np.sign(codes) * (codes / top) ** 2 * np.repeat(np.asarray(scale, f64), ADAMW_BLOCK)[: len(codes)]

@@ -1,5 +1,5 @@
 """Thin binding (ctypes, and a compiled module for the hot calls) of the C-ABI library declared in the headers of ``include/`` (``ss_scan.h``, ``ss_conv.h``, ``ss_layer.h``,
-``ss_norm.h``, ``ss_gate.h``, ``ss_quant.h``, ``ss_embed.h``, ``ss_logprob.h``).
+``ss_norm.h``, ``ss_gate.h``, ``ss_quant.h``, ``ss_embed.h``, ``ss_logprob.h``, ``ss_adamw.h``).
 
 Argument marshalling only: every step of the path runs in the library's HIP kernels.
 PyTorch appears here solely as the owner of device memory and streams.  The library must
@@ -179,6 +179,21 @@ class LogprobBwdParams(ctypes.Structure):
     _fields_ = [("fwd", LogprobParams), ("dlogp", _vp), ("dentropy", _vp), ("dlogits", _vp)]
 
 
+class AdamwTensor(ctypes.Structure):
+    _fields_ = [("n", ctypes.c_int64), ("param_dtype", ctypes.c_int32), ("grad_dtype", ctypes.c_int32), ("param", _vp), ("grad", _vp), ("master", _vp),
+                ("m", _vp), ("v", _vp), ("m_scale", _vp), ("v_scale", _vp)]
+
+
+class AdamwParams(ctypes.Structure):
+    _fields_ = [("tensors", ctypes.c_int32), ("state_bits", ctypes.c_int32), ("list", ctypes.POINTER(AdamwTensor)), ("count", _vp),
+                ("lr", ctypes.c_double), ("beta1", ctypes.c_double), ("beta2", ctypes.c_double), ("eps", ctypes.c_double),
+                ("weight_decay", ctypes.c_double), ("lr_device", _vp), ("grad_scale", _vp)]
+
+
+class AdamwValuesParams(ctypes.Structure):
+    _fields_ = [("n", ctypes.c_int64), ("with_sign", ctypes.c_int32), ("out_dtype", ctypes.c_int32), ("codes", _vp), ("scale", _vp), ("out", _vp)]
+
+
 SS_GEMM_C_FLOAT, SS_GEMM_ACCUMULATE, SS_GEMM_GENERAL = 1, 2, 4
 SS_ERR_BACKEND = -7
 SS_CONV_SILU, SS_CONV_HAS_BIAS, SS_CONV_HAS_STATE, SS_CONV_WRITE_STATE = 1, 2, 4, 8
@@ -192,6 +207,7 @@ SS_QUANT_MAX_DIM = 131072
 SS_EMBED_IDS_32 = 1
 SS_LOGPROB_TARGETS_32 = 1
 SS_LOGPROB_MAX_TOP = 64
+SS_ADAMW_BLOCK = 256
 
 _lib = None
 
@@ -242,7 +258,8 @@ def lib():
                              ("ss_gate_fwd", GateParams),
                              ("ss_gate_bwd", GateBwdParams), ("ss_gate_step", GateStepParams), ("ss_quant_rows", QuantParams),
                              ("ss_qlinear", QLinearParams), ("ss_embed_fwd", EmbedParams), ("ss_embed_bwd", EmbedBwdParams),
-                             ("ss_logprob_fwd", LogprobParams), ("ss_logprob_bwd", LogprobBwdParams)):
+                             ("ss_logprob_fwd", LogprobParams), ("ss_logprob_bwd", LogprobBwdParams),
+                             ("ss_adamw_step", AdamwParams), ("ss_adamw_values", AdamwValuesParams)):
             getattr(l, name).restype = ctypes.c_int
             getattr(l, name).argtypes = [ctypes.POINTER(params), _vp]
         for name, args in (("ss_norm_workspace_bytes", [ctypes.POINTER(NormParams)]),
@@ -268,7 +285,7 @@ class _NoMarshal:
         return None
 
     step = layer_step = scan_fwd = scan_bwd = layer_fwd = layer_bwd = staticmethod(_none)
-    norm_fwd = norm_quant = norm_bwd = gate_fwd = gate_bwd = gate_step = qlinear = layer_norm = gated_recurrence = staticmethod(_none)
+    norm_fwd = norm_quant = norm_bwd = gate_fwd = gate_bwd = gate_step = qlinear = layer_norm = gated_recurrence = adamw_step = staticmethod(_none)
 
 
 def _marshal():
@@ -1477,6 +1494,90 @@ def ss_logprob_bwd(logits, stats, targets=None, dlogp=None, entropy=None, dentro
     if q.fwd.rows and q.dlogits < q.fwd.logits + ((q.fwd.rows - 1) * q.fwd.row_stride + q.fwd.vocab) * size and q.fwd.logits < q.dlogits + out.numel() * size:
         raise ValueError("out must not share memory with the logits")
     _check(lib().ss_logprob_bwd(ctypes.byref(q), _stream(stream)))
+    return out
+
+
+# ---------------------------------------------------------------- AdamW
+def _scalar(t, dtype, name, n=1):
+    if t is not None and t.numel() != n:
+        raise ValueError("%s must have %d element%s" % (name, n, "" if n == 1 else "s"))
+    return _ptr(t, dtype, None, name)
+
+
+def ss_adamw_step(params, grads, m, v, count, lr, betas=(0.9, 0.999), eps=1e-8, weight_decay=0.0, master=None, m_scale=None, v_scale=None,
+                  grad_scale=None, stream=None):
+    """Enqueue a step of AdamW over lists of tensors, in place: params and grads (float32 or bfloat16 each), moments m and v of the same shapes in float32,
+    or with ``m_scale`` and ``v_scale`` (lists of float32 tensors of a scale for every ``SS_ADAMW_BLOCK`` elements) in int8 and uint8.
+    ``master``: a list of float32 copies of the bfloat16 params that are updated in their place, None where there is none.  ``count``
+    is an int32 tensor (2), at first zeros: the steps taken, which the call counts, so that a captured one may be replayed.  ``lr`` is a number
+    or a float32 tensor of one element, ``grad_scale`` such a tensor, or None, that the gradients are multiplied with."""
+    if stream is not None:
+        with _current(stream):
+            return ss_adamw_step(params, grads, m, v, count, lr, betas, eps, weight_decay, master, m_scale, v_scale, grad_scale)
+    tensor_lr = isinstance(lr, torch.Tensor)
+    beta1, beta2 = betas
+    if (m_scale is None) != (v_scale is None):
+        raise ValueError("m_scale and v_scale come together")
+    _on_current(count)
+    if isinstance(params, list) and isinstance(grads, list) and isinstance(m, list) and isinstance(v, list):
+        r = (_native or _marshal()).adamw_step(params, grads, m, v, master, m_scale, v_scale, count, 0.0 if tensor_lr else float(lr),
+                                               lr if tensor_lr else None, float(beta1), float(beta2), float(eps), float(weight_decay),
+                                               grad_scale, _stream(stream))
+        if r is not None:
+            _result(r)
+            return
+    f32, n = torch.float32, len(params)
+    lists = {"grads": grads, "m": m, "v": v, "master": master, "m_scale": m_scale, "v_scale": v_scale}
+    for name, list_ in lists.items():
+        if list_ is not None and len(list_) != n:
+            raise ValueError("%s has %d tensors, params %d" % (name, len(list_), n))
+    if len({t.data_ptr() for t in params if t.numel()}) != sum(1 for t in params if t.numel()):
+        raise ValueError("a tensor is among params twice")
+    eight = m_scale is not None
+    p = AdamwParams()
+    p.tensors, p.state_bits = _counts(n)[0], 8 if eight else 32
+    p.list = (AdamwTensor * max(1, n))()
+    for k, t in enumerate(params):
+        e = p.list[k]
+        e.n, blocks = t.numel(), -(-t.numel() // SS_ADAMW_BLOCK)
+        e.param_dtype, e.grad_dtype = _io_code(t), _io_code(grads[k])
+        e.param, e.grad = _ptr(t, None, None, "a param"), _ptr(grads[k], None, t.shape, "its grad")
+        e.m = _ptr(m[k], torch.int8 if eight else f32, t.shape, "its m")
+        e.v = _ptr(v[k], torch.uint8 if eight else f32, t.shape, "its v")
+        tensors = [t, grads[k], m[k], v[k]]
+        if master is not None and master[k] is not None:
+            if e.param_dtype != SS_BF16:
+                raise TypeError("a master belongs to a bfloat16 param")
+            e.master = _ptr(master[k], f32, t.shape, "its master")
+            tensors.append(master[k])
+        if eight:
+            e.m_scale, e.v_scale = _ptr(m_scale[k], f32, (blocks,), "its m_scale"), _ptr(v_scale[k], f32, (blocks,), "its v_scale")
+            tensors += [m_scale[k], v_scale[k]]
+        _on_current(*tensors)
+    _on_current(grad_scale, lr if tensor_lr else None)
+    p.count = _scalar(count, torch.int32, "count", 2)
+    p.lr, p.lr_device = (0.0, _scalar(lr, f32, "lr")) if tensor_lr else (float(lr), None)
+    p.beta1, p.beta2, p.eps, p.weight_decay = beta1, beta2, eps, weight_decay
+    p.grad_scale = _scalar(grad_scale, f32, "grad_scale")
+    _check(lib().ss_adamw_step(ctypes.byref(p), _stream(stream)))
+
+
+def ss_adamw_values(codes, scale, dtype=None, stream=None):
+    """Enqueue what 8-bit moments stand for, in ``dtype`` (float32 unless given): m of int8 codes, the square root of v of uint8 ones."""
+    if stream is not None:
+        with _current(stream):
+            return ss_adamw_values(codes, scale, dtype)
+    if codes.dtype is not torch.int8 and codes.dtype is not torch.uint8:
+        raise TypeError("codes must be int8 or uint8, got %s" % codes.dtype)
+    _on_current(codes, scale)
+    p = AdamwValuesParams()
+    p.n, p.with_sign = codes.numel(), int(codes.dtype is torch.int8)
+    p.codes = _ptr(codes, None, None, "codes")
+    p.scale = _ptr(scale, torch.float32, (-(-p.n // SS_ADAMW_BLOCK),), "scale")
+    out = torch.empty(codes.shape, dtype=torch.float32 if dtype is None else dtype, device=codes.device)
+    p.out_dtype = _io_code(out)
+    p.out = out.data_ptr()
+    _check(lib().ss_adamw_values(ctypes.byref(p), _stream(stream)))
     return out
 
 

@@ -17,6 +17,10 @@
 #include <torch/csrc/autograd/functions/basic_ops.h>
 #include <torch/csrc/autograd/python_variable.h>
 
+#include <algorithm>
+#include <vector>
+
+#include "ss_adamw.h"
 #include "ss_gate.h"
 #include "ss_layer.h"
 #include "ss_norm.h"
@@ -1040,10 +1044,105 @@ PyObject* py_qlinear(PyObject*, PyObject* const* argv, Py_ssize_t n)
     END_HANDLE_TH_ERRORS
 }
 
+// Plain tensors of a list, all on one device; `ok` falls when one of them is not.
+struct Listed {
+    PyObject* list;
+    Py_ssize_t n = 0;
+    bool ok = true;
+    Listed(PyObject* o, bool optional) : list(o)
+    {
+        if (optional && o == Py_None) list = nullptr;
+        else if (!PyList_CheckExact(o)) ok = false;
+        else n = PyList_GET_SIZE(o);
+    }
+    const at::Tensor* at(Py_ssize_t k, const at::Tensor* like, bool optional = false)
+    {
+        PyObject* o = PyList_GET_ITEM(list, k);
+        if (optional && o == Py_None) return nullptr;
+        if (!THPVariable_CheckExact(o)) { ok = false; return nullptr; }
+        const at::Tensor& t = THPVariable_Unpack(o);
+        if (!t.is_cuda() || !t.has_storage() || !t.is_contiguous() || (like && t.device() != like->device())) { ok = false; return nullptr; }
+        return &t;
+    }
+};
+const float* one_float(PyObject* o, const at::Tensor& like, bool& ok)
+{
+    if (o == Py_None) return nullptr;
+    if (!THPVariable_CheckExact(o)) { ok = false; return nullptr; }
+    const at::Tensor& t = THPVariable_Unpack(o);
+    if (!t.is_cuda() || !t.has_storage() || t.device() != like.device() || t.scalar_type() != at::kFloat || t.numel() != 1) { ok = false; return nullptr; }
+    return static_cast<const float*>(t.data_ptr());
+}
+// adamw_step(params, grads, m, v, masters or None, m_scales or None, v_scales or None, count, lr, lr tensor or None, beta1, beta2, eps, weight_decay,
+//            grad_scale or None, stream) -> True
+PyObject* py_adamw_step(PyObject*, PyObject* const* argv, Py_ssize_t n)
+{
+    HANDLE_TH_ERRORS
+    if (n != 16) Py_RETURN_NONE;
+    Args a{argv};
+    const at::Tensor* count = a.tensor(7);
+    if (!a.ok || count->scalar_type() != at::kInt || count->numel() != 2) Py_RETURN_NONE;
+    Listed params(argv[0], false), grads(argv[1], false), m(argv[2], false), v(argv[3], false), masters(argv[4], true), ms(argv[5], true), vs(argv[6], true);
+    if (!params.ok || !grads.ok || !m.ok || !v.ok || !masters.ok || !ms.ok || !vs.ok) Py_RETURN_NONE;
+    const bool eight = ms.list && vs.list;
+    const Py_ssize_t all = params.n;
+    if (grads.n != all || m.n != all || v.n != all || (masters.list && masters.n != all) || (eight && (ms.n != all || vs.n != all)) ||
+        (!ms.list != !vs.list) || !fits(all))
+        Py_RETURN_NONE;
+    ss_adamw_params p{};
+    if (!real_number(argv[8], p.lr) || !real_number(argv[10], p.beta1) || !real_number(argv[11], p.beta2) || !real_number(argv[12], p.eps) ||
+        !real_number(argv[13], p.weight_decay))
+        Py_RETURN_NONE;
+    bool ok = true;
+    p.lr_device = one_float(argv[9], *count, ok);
+    p.grad_scale = one_float(argv[14], *count, ok);
+    void* stream = a.stream(15);
+    if (!ok || !a.ok) Py_RETURN_NONE;
+    std::vector<ss_adamw_tensor> list((size_t)all);
+    std::vector<void*> seen;
+    seen.reserve((size_t)all);
+    const at::ScalarType m_type = eight ? at::kChar : at::kFloat, v_type = eight ? at::kByte : at::kFloat;
+    for (Py_ssize_t k = 0; k < all; ++k) {
+        ss_adamw_tensor& e = list[(size_t)k];
+        const at::Tensor *t = params.at(k, count), *g = grads.at(k, count), *tm = m.at(k, count), *tv = v.at(k, count);
+        const at::Tensor* master = masters.list ? masters.at(k, count, true) : nullptr;
+        if (!params.ok || !grads.ok || !m.ok || !v.ok || !masters.ok) Py_RETURN_NONE;
+        e.n = t->numel();
+        if (!io_type(*t, e.param_dtype) || !io_type(*g, e.grad_dtype) || tm->scalar_type() != m_type || tv->scalar_type() != v_type) Py_RETURN_NONE;
+        if (!g->sizes().equals(t->sizes()) || !tm->sizes().equals(t->sizes()) || !tv->sizes().equals(t->sizes())) Py_RETURN_NONE;
+        if (master && (master->scalar_type() != at::kFloat || e.param_dtype != SS_BF16 || !master->sizes().equals(t->sizes()))) Py_RETURN_NONE;
+        if (eight) {
+            const at::Tensor *a1 = ms.at(k, count), *a2 = vs.at(k, count);
+            const int64_t blocks = (e.n + SS_ADAMW_BLOCK - 1) / SS_ADAMW_BLOCK;
+            if (!ms.ok || !vs.ok || a1->scalar_type() != at::kFloat || a2->scalar_type() != at::kFloat || a1->dim() != 1 || a2->dim() != 1 ||
+                a1->numel() != blocks || a2->numel() != blocks)
+                Py_RETURN_NONE;
+            e.m_scale = data<float>(*a1);
+            e.v_scale = data<float>(*a2);
+        }
+        e.param = t->data_ptr();
+        e.grad = g->data_ptr();
+        e.master = master ? data<float>(*master) : nullptr;
+        e.m = tm->data_ptr();
+        e.v = tv->data_ptr();
+        if (e.n) seen.push_back(e.param);
+    }
+    std::sort(seen.begin(), seen.end());
+    if (std::adjacent_find(seen.begin(), seen.end()) != seen.end()) Py_RETURN_NONE;
+    p.tensors = (int32_t)all;
+    p.state_bits = eight ? 8 : 32;
+    p.list = list.data();
+    p.count = static_cast<int32_t*>(count->data_ptr());
+    const int rc = call(ss_adamw_step, p, stream);
+    if (rc != SS_OK) return PyLong_FromLong(rc);
+    Py_RETURN_TRUE;
+    END_HANDLE_TH_ERRORS
+}
+
 #define SS_METHOD(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)(void)>(py_##name)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {SS_METHOD(step), SS_METHOD(layer_step), SS_METHOD(scan_fwd), SS_METHOD(scan_bwd),
                          SS_METHOD(layer_fwd), SS_METHOD(layer_bwd), SS_METHOD(norm_fwd), SS_METHOD(norm_quant), SS_METHOD(norm_bwd), SS_METHOD(gate_fwd),
-                         SS_METHOD(gate_bwd), SS_METHOD(gate_step), SS_METHOD(qlinear), SS_METHOD(layer_norm), SS_METHOD(gated_recurrence), {nullptr, nullptr, 0, nullptr}};
+                         SS_METHOD(gate_bwd), SS_METHOD(gate_step), SS_METHOD(qlinear), SS_METHOD(layer_norm), SS_METHOD(gated_recurrence), SS_METHOD(adamw_step), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_marshal", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

@@ -1,0 +1,79 @@
+"""AdamW on the library's kernel (include/ss_adamw.h): all tensors of a group in a launch, moments in float32 or in 8 bits."""
+import torch
+
+from . import binding as B
+
+
+class AdamW(torch.optim.Optimizer):
+    """AdamW with decoupled weight decay over GPU tensors in float32 or bfloat16.
+
+    ``state_bits`` 8 holds the moments in a byte each and a scale for every 256 elements.  Tensors in bfloat16 get a float32 copy that is
+    updated in their place (``master=False``: none, the sum is rounded to bfloat16).  All state is allocated here, and steps are counted on the device, once for
+    a group, so a step can be captured in a graph and replayed.  A tensor without a gradient is left out of a step, though its group's count goes on.
+    A group's ``lr`` may be a float32 tensor of one element on the GPU, which a graph reads as it is at its replay."""
+
+    def __init__(self, params, lr=1e-3, betas=(0.9, 0.999), eps=1e-8, weight_decay=1e-2, state_bits=32, master=True):
+        if state_bits not in (8, 32):
+            raise ValueError("state_bits must be 8 or 32, got %r" % (state_bits,))
+        super().__init__(params, {"lr": lr, "betas": betas, "eps": eps, "weight_decay": weight_decay, "state_bits": state_bits, "master": master})
+
+    def add_param_group(self, group):
+        super().add_param_group(group)
+        group = self.param_groups[-1]
+        for p in group["params"]:
+            if p.dtype not in (torch.float32, torch.bfloat16) or not p.is_cuda or not p.is_contiguous():
+                raise ValueError("parameters must be contiguous float32 or bfloat16 tensors on the GPU")
+            s = self.state[p]
+            eight = group["state_bits"] == 8
+            s["m"] = torch.zeros(p.shape, dtype=torch.int8 if eight else torch.float32, device=p.device)
+            s["v"] = torch.zeros(p.shape, dtype=torch.uint8 if eight else torch.float32, device=p.device)
+            if eight:
+                blocks = -(-p.numel() // B.SS_ADAMW_BLOCK)
+                s["m_scale"], s["v_scale"] = (torch.zeros(blocks, dtype=torch.float32, device=p.device) for _ in range(2))
+            if p.dtype == torch.bfloat16 and group["master"]:
+                s["master"] = p.detach().float()
+        device = group["params"][0].device if group["params"] else "cuda"
+        group["count"] = torch.zeros(2, dtype=torch.int32, device=device)
+
+    @torch.no_grad()
+    def step(self, closure=None, grad_scale=None):
+        """``grad_scale``: a float32 tensor of one element that the gradients are multiplied with (of clipping, or of a scaled loss)."""
+        loss = None
+        if closure is not None:
+            with torch.enable_grad():
+                loss = closure()
+        for group in self.param_groups:
+            params = [p for p in group["params"] if p.grad is not None]
+            states = [self.state[p] for p in params]
+            each = lambda name: [s.get(name) for s in states]
+            eight = group["state_bits"] == 8
+            B.ss_adamw_step(params, [p.grad.contiguous() for p in params], each("m"), each("v"), group["count"], group["lr"],
+                            betas=group["betas"], eps=group["eps"], weight_decay=group["weight_decay"], master=each("master"),
+                            m_scale=each("m_scale") if eight else None, v_scale=each("v_scale") if eight else None, grad_scale=grad_scale)
+            torch.autograd.graph.increment_version(params)   # a graph that still needs them as they were is told
+        return loss
+
+    @torch.no_grad()
+    def load_state_dict(self, state):
+        """Of an optimiser of the same groups.  What is loaded is copied into this one's tensors, which a captured step goes on using."""
+        groups = state["param_groups"]
+        if [len(g["params"]) for g in groups] != [len(g["params"]) for g in self.param_groups]:
+            raise ValueError("the loaded state has other parameter groups")
+        for theirs, mine in zip(groups, self.param_groups):
+            if (theirs["state_bits"], theirs["master"]) != (mine["state_bits"], mine["master"]):
+                raise ValueError("the loaded state is of state_bits %r and master %r" % (theirs["state_bits"], theirs["master"]))
+            for k, p in zip(theirs["params"], mine["params"]):
+                given, own = state["state"][k], self.state[p]
+                if {n: (t.dtype, t.shape) for n, t in given.items()} != {n: (t.dtype, t.shape) for n, t in own.items()}:
+                    raise ValueError("the loaded state is of other tensors")
+        for theirs, mine in zip(groups, self.param_groups):
+            for k, p in zip(theirs["params"], mine["params"]):
+                for name, t in self.state[p].items():
+                    t.copy_(state["state"][k][name])
+            mine["count"].copy_(theirs["count"])
+            for name, value in theirs.items():
+                if name not in ("params", "count"):
+                    if name == "lr" and isinstance(mine["lr"], torch.Tensor):
+                        mine["lr"].fill_(float(value))
+                    else:
+                        mine[name] = value.clone() if isinstance(value, torch.Tensor) else value

@@ -1,4 +1,4 @@
-"""What the entry points of the norms' 8-bit results, the embedding and the log probabilities refuse, on the host, before any device call; and their structs as the C compiler lays them out."""
+"""What the entry points of the norms' 8-bit results, the embedding, the log probabilities and AdamW refuse, on the host, before any device call; and their structs as the C compiler lays them out."""
 import ctypes
 import os
 import subprocess
@@ -13,8 +13,9 @@ FAKE = 0x7F0000001000   # non-null, 4096-byte aligned, never dereferenced
 MANY = 2 ** 32 + 5
 
 STRUCTS = {"ss_norm_quant_params": B.NormQuantParams, "ss_embed_params": B.EmbedParams, "ss_embed_bwd_params": B.EmbedBwdParams,
-           "ss_logprob_params": B.LogprobParams, "ss_logprob_bwd_params": B.LogprobBwdParams}
-HEADERS = ["ss_norm.h", "ss_embed.h", "ss_logprob.h"]
+           "ss_logprob_params": B.LogprobParams, "ss_logprob_bwd_params": B.LogprobBwdParams,
+           "ss_adamw_tensor": B.AdamwTensor, "ss_adamw_params": B.AdamwParams, "ss_adamw_values_params": B.AdamwValuesParams}
+HEADERS = ["ss_norm.h", "ss_embed.h", "ss_logprob.h", "ss_adamw.h"]
 
 
 def t(*shape, dtype=torch.bfloat16):
@@ -180,3 +181,61 @@ def test_logprob_sizes_beyond_32_bits(call):
     with pytest.raises(B.SsError) as e:
         call()
     assert e.value.code == B.SS_ERR_UNSUPPORTED
+
+
+# ---- AdamW --------------------------------------------------------------------------------------------
+LISTS = []   # what the structs point to
+
+
+def adamw(bits=32, **tensor):
+    p = B.AdamwParams()
+    p.tensors, p.state_bits, p.lr, p.beta1, p.beta2, p.eps, p.weight_decay = 2, bits, 1e-3, 0.9, 0.95, 1e-8, 0.1
+    list_ = (B.AdamwTensor * 2)()
+    for e in list_:
+        e.n, e.param_dtype, e.grad_dtype = 1000, B.SS_BF16, B.SS_F32
+        for f in ("param", "grad", "master", "m", "v") + (("m_scale", "v_scale") if bits == 8 else ()):
+            setattr(e, f, FAKE)
+    for k, v in tensor.items():
+        setattr(list_[1], k, v)
+    LISTS.append(list_)
+    p.list = list_
+    p.count = FAKE
+    return p
+
+
+def test_adamw():
+    call = B.lib().ss_adamw_step
+    assert call(None, None) == B.SS_ERR_NULL
+    expect(call, adamw, [dict(count=None), dict(list=None)], B.SS_ERR_NULL)
+    expect(call, adamw, [dict(tensors=-1)], B.SS_ERR_SHAPE)
+    inf, nan = float("inf"), float("nan")
+    expect(call, adamw, [dict(state_bits=16), dict(lr=-1.0), dict(lr=inf), dict(lr=1e39), dict(beta1=1.0), dict(beta1=-0.1), dict(beta2=nan), dict(eps=-1.0), dict(eps=inf),
+                         dict(weight_decay=-1.0), dict(weight_decay=nan)], B.SS_ERR_UNSUPPORTED)
+    expect(call, adamw, [dict(count=FAKE + 2), dict(lr_device=FAKE + 1), dict(grad_scale=FAKE + 2)], B.SS_ERR_ALIGN)
+    for bits in (8, 32):   # of the second tensor: nothing is launched for the first
+        one = lambda code, **t: expect(call, lambda: adamw(bits, **t), [{}], code)
+        for f in ("param", "grad", "m", "v") + (("m_scale", "v_scale") if bits == 8 else ()):
+            one(B.SS_ERR_NULL, **{f: None})
+        one(B.SS_ERR_SHAPE, n=-1)
+        one(B.SS_ERR_UNSUPPORTED, n=2 ** 40 + 1)
+        one(B.SS_ERR_UNSUPPORTED, param_dtype=2)
+        one(B.SS_ERR_UNSUPPORTED, grad_dtype=-1)
+        one(B.SS_ERR_UNSUPPORTED, param_dtype=B.SS_F32)   # with a master
+        for f in ("param", "grad", "master") + (("m_scale", "v_scale") if bits == 8 else ("m", "v")):
+            one(B.SS_ERR_ALIGN, **{f: FAKE + 1})
+
+
+def adamw_values():
+    p = B.AdamwValuesParams()
+    p.n, p.with_sign, p.codes, p.scale, p.out = 1000, 1, FAKE, FAKE, FAKE
+    return p
+
+
+def test_adamw_values():
+    call = B.lib().ss_adamw_values
+    assert call(None, None) == B.SS_ERR_NULL
+    expect(call, adamw_values, [dict(codes=None), dict(scale=None), dict(out=None)], B.SS_ERR_NULL)
+    expect(call, adamw_values, [dict(n=-1)], B.SS_ERR_SHAPE)
+    expect(call, adamw_values, [dict(n=2 ** 40 + 1), dict(with_sign=2), dict(with_sign=-1), dict(out_dtype=2)], B.SS_ERR_UNSUPPORTED)
+    expect(call, adamw_values, [dict(scale=FAKE + 2), dict(out=FAKE + 2)], B.SS_ERR_ALIGN)
+    expect(call, adamw_values, [dict(n=0, codes=None)], B.SS_OK)

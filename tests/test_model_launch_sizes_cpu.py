@@ -89,3 +89,37 @@ static void one()
 
 def test_logprob(tmp_path):
     run(tmp_path, "ss_logprob.hip", LOGPROB)
+
+
+ADAMW = r"""
+static void one()
+{
+    static ss_adamw_tensor list[200];
+    ss_adamw_params p{};
+    p.state_bits = coin(2) ? 8 : 32;
+    p.tensors = coin(200);
+    p.beta1 = p.beta2 = 0.9;
+    p.count = static_cast<int32_t*>(fake);
+    p.list = list;
+    double n = 0;
+    for (int k = 0; k < p.tensors; ++k) {
+        ss_adamw_tensor& t = list[k];
+        t = {};
+        t.n = (int64_t)any(2147483647) * (coin(20) ? 1 : 1 + coin(60)) * (coin(10) ? 1 : 0);
+        if (n + (double)t.n > CARD / (p.state_bits == 8 ? 6 : 12)) t.n = 0;
+        n += (double)t.n;
+        t.param_dtype = coin(2);
+        t.grad_dtype = coin(2);
+        t.param = t.m = t.v = fake;
+        t.grad = fake;
+        t.m_scale = t.v_scale = static_cast<float*>(fake);
+    }
+    const int rc = ss_adamw_step(&p, nullptr);
+    if (rc != SS_OK || launches.empty() || launches.size() > (size_t)p.tensors / 24 + 1) std::exit(1);
+    look(rc, "ss_adamw_step", p.tensors, p.state_bits, 0, 0, 0, 0);
+}
+"""
+
+
+def test_adamw(tmp_path):
+    run(tmp_path, "ss_adamw.hip", ADAMW)

@@ -79,3 +79,35 @@ def test_log_probabilities_of_masked_rows():
     g = mo.logprob_bwd(f, [1, 2, 1, 0], np.ones(4), np.ones(4))["dlogits"]
     assert np.allclose(g[0], [-1 / 3, 1.0, -1 / 3, -1 / 3]) and (g[1] == 0).all() and (g[2] == 0).all() and np.isnan(g[3]).any()
     assert mo.logprob_fwd(np.array([[np.nan, 1.0]]), None, 2)["top_ids"].tolist() == [[1, -1]]
+
+
+# ---- AdamW --------------------------------------------------------------------------------------------
+def test_adamw_like_torch():
+    rng = np.random.default_rng(4)
+    p = torch.from_numpy(rng.standard_normal(50)).requires_grad_(True)
+    o = torch.optim.AdamW([p], lr=1e-2, betas=(0.75, 0.875), weight_decay=0.1)   # factors that float32 holds
+    x, m, v = p.detach().numpy().copy(), np.zeros(50), np.zeros(50)
+    for step in range(1, 6):
+        p.grad = torch.from_numpy(rng.standard_normal(50))
+        o.step()
+        x, m, v, _ = mo.adamw(x, p.grad.numpy(), m, v, step, 1e-2, 0.75, 0.875, 1e-8, 0.1)
+        assert np.allclose(x, p.detach(), rtol=1e-12, atol=1e-14)
+
+
+def test_adamw_codes():
+    rng = np.random.default_rng(5)
+    x = rng.standard_normal(700)
+    for signed in (True, False):
+        w = x if signed else np.abs(x)
+        top = 127 if signed else 255
+        codes, scale = mo.adamw_codes(w, 3, signed)
+        back = mo.adamw_values(codes, scale, signed)
+        at = np.repeat(scale, 256)[:700]
+        assert (np.abs(back - w) <= (2 * np.abs(codes) + 1) / top ** 2 * at).all() and np.array_equal(scale, [np.abs(w[k:k + 256]).max() for k in (0, 256, 512)])
+        assert np.abs(codes).max() == top and (np.sign(back) == np.sign(w))[np.abs(codes) > 0].all()
+        # the mean over many steps is the value
+        mean = np.mean([mo.adamw_values(*mo.adamw_codes(w[:64], t, signed), signed) for t in range(2000)], 0)
+        assert np.abs(mean - w[:64])[np.abs(w[:64]) > 1e-3].max() < 0.02 * (2 * np.abs(codes).max() + 1) / top ** 2 * scale[0]
+    codes, scale = mo.adamw_codes([0.0] * 256 + [1.0, np.nan] + [0.0] * 254 + [1e-40], 1, True)
+    assert (codes[:256] == 0).all() and scale[0] == 0 and np.isnan(scale[1]) and scale[2] == 0
+    assert mo.adamw_codes([1.0, 1e-9, 0.0], 1, False)[0].tolist() == [255, 1, 0]
