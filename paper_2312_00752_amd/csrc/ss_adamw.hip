@@ -37,51 +37,49 @@ struct AdamwArgs {
     const float *lr_device, *grad_scale;
 };
 
-// four consecutive elements, of which n are there
-__device__ __forceinline__ void load4(const void* p, bool low, int64_t i, int n, float (&v)[4])
+// ---- four consecutive elements of a lane, of which n are there (FULL: all) ---------------------------
+template <bool FULL, typename T>
+__device__ __forceinline__ void load4(const T* p, int n, float (&v)[4])
 {
-    if (n >= 4) {
-        if (low) {
-            const u32x2v x = load_any<u32x2v>(static_cast<const bf16_t*>(p) + i, 0u);
+    if (FULL || n >= 4) {
+        if constexpr (sizeof(T) == 2) {
+            const u32x2v x = load_any<u32x2v>(p, 0u);
             v[0] = bf16_lo(x.x); v[1] = bf16_hi(x.x); v[2] = bf16_lo(x.y); v[3] = bf16_hi(x.y);
         } else {
-            const u32x4 x = load_any<u32x4>(static_cast<const float*>(p) + i, 0u);
+            const u32x4 x = load_any<u32x4>(p, 0u);
             v[0] = __uint_as_float(x.x); v[1] = __uint_as_float(x.y); v[2] = __uint_as_float(x.z); v[3] = __uint_as_float(x.w);
         }
     } else {
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
-            v[j] = j >= n ? 0.0f : (low ? bf16_to_f32(static_cast<const bf16_t*>(p)[i + j]) : static_cast<const float*>(p)[i + j]);
+        for (int j = 0; j < 4; ++j) v[j] = j < n ? io_to_f32<T>(p[j]) : 0.0f;
     }
 }
-__device__ __forceinline__ void store4(void* p, bool low, int64_t i, int n, const float (&v)[4])
+template <bool FULL, typename T>
+__device__ __forceinline__ void store4(T* p, int n, const float (&v)[4])
 {
-    if (n >= 4) {
-        if (low) store_any(static_cast<bf16_t*>(p) + i, 0u, u32x2v{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])});
-        else store_any(static_cast<float*>(p) + i, 0u, u32x4{__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3])});
+    if (FULL || n >= 4) {
+        if constexpr (sizeof(T) == 2) store_any(p, 0u, u32x2v{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])});
+        else store_any(p, 0u, u32x4{__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3])});
     } else {
 #pragma unroll
         for (int j = 0; j < 4; ++j)
-            if (j < n) {
-                if (low) static_cast<bf16_t*>(p)[i + j] = f32_to_io<bf16_t>(v[j]);
-                else static_cast<float*>(p)[i + j] = v[j];
-            }
+            if (j < n) p[j] = f32_to_io<T>(v[j]);
     }
 }
-__device__ __forceinline__ uint32_t load_codes(const void* p, int64_t i, int n)
+template <bool FULL>
+__device__ __forceinline__ uint32_t load_codes(const uint8_t* q, int n)
 {
-    const uint8_t* q = static_cast<const uint8_t*>(p) + i;
-    if (n >= 4) return load_any<uint32_t>(q, 0u);
+    if (FULL || n >= 4) return load_any<uint32_t>(q, 0u);
     uint32_t w = 0;
 #pragma unroll
     for (int j = 0; j < 4; ++j)
         if (j < n) w |= (uint32_t)q[j] << (8 * j);
     return w;
 }
-__device__ __forceinline__ void store_codes(void* p, int64_t i, int n, uint32_t w)
+template <bool FULL>
+__device__ __forceinline__ void store_codes(uint8_t* q, int n, uint32_t w)
 {
-    uint8_t* q = static_cast<uint8_t*>(p) + i;
-    if (n >= 4) {
+    if (FULL || n >= 4) {
         store_any(q, 0u, w);
         return;
     }
@@ -89,32 +87,49 @@ __device__ __forceinline__ void store_codes(void* p, int64_t i, int n, uint32_t 
     for (int j = 0; j < 4; ++j)
         if (j < n) q[j] = (uint8_t)(w >> (8 * j));
 }
+
+// ---- moments in 8 bits ------------------------------------------------------------------------------
 template <bool SIGN>
 __device__ __forceinline__ void decode(uint32_t codes, float scale, float (&v)[4])
 {
     constexpr float top = SIGN ? 127.0f : 255.0f;
     const float c = scale * (1.0f / (top * top));
+    if (SIGN) codes ^= 0x80808080u;   // 128 more, without a sign
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-        const float q = SIGN ? (float)(int8_t)(codes >> (8 * j)) : (float)(uint8_t)(codes >> (8 * j));
+        const float q = (float)(codes >> (8 * j) & 255u) - (SIGN ? 128.0f : 0.0f);
         v[j] = q * fabsf(q) * c;
     }
 }
+// The largest of a wave's values in all of its lanes, by the vector unit's own exchanges: lanes of rows of 16, then the rows.
 __device__ __forceinline__ uint32_t wave_max(uint32_t v)
 {
-#pragma unroll
-    for (int s = 1; s < WAVE; s *= 2) v = max(v, (uint32_t)__shfl_xor((int)v, s));
-    return v;
+#define SS_MAX_FROM(control, rows) v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, control, rows, 0xf, false))
+    SS_MAX_FROM(0x111, 0xf);   // the lane one before, two, four, eight
+    SS_MAX_FROM(0x112, 0xf);
+    SS_MAX_FROM(0x114, 0xf);
+    SS_MAX_FROM(0x118, 0xf);
+    SS_MAX_FROM(0x142, 0xa);   // the last lane of the row before, into the second and fourth row
+    SS_MAX_FROM(0x143, 0xc);   // the last of the first half, into the second
+#undef SS_MAX_FROM
+    return (uint32_t)__builtin_amdgcn_readlane((int)v, WAVE - 1);
+}
+// Correctly rounded for what a moment can be: the hardware's root is off by a unit in the last place at most, and a step of Newton's method from there
+// has an exact residual.  (The compiler's own takes twice as many instructions; the step of 126 million parameters was bound by them.)
+__device__ __forceinline__ float root_of(float v)
+{
+    const float s = __builtin_amdgcn_sqrtf(v), h = 0.5f * __builtin_amdgcn_rcpf(s);
+    return s > 0.0f && s < INFINITY ? fmaf(fmaf(-s, s, v), h, s) : s;
 }
 // The codes of a wave's block, of which this lane has four values, and the block's scale.  turn: the first's place in the sequence, in 2^-32.
+// q is the floor of the hardware's root of y: where y is so near a square that it is one off, the code is the same.
 template <bool SIGN>
 __device__ __forceinline__ uint32_t encode(const float (&v)[4], uint32_t turn, uint32_t apart, float& scale)
 {
-#pragma clang fp contract(off)
     constexpr float top = SIGN ? 127.0f : 255.0f;
     uint32_t most = 0;
 #pragma unroll
-    for (int j = 0; j < 4; ++j) most = max(most, magnitude(v[j]));
+    for (int j = 0; j < 4; ++j) most = max(most, SIGN ? magnitude(v[j]) : __float_as_uint(v[j]));
     most = wave_max(most);
     scale = __uint_as_float(most);
     if (most >= 0x7f800000u) {
@@ -125,91 +140,130 @@ __device__ __forceinline__ uint32_t encode(const float (&v)[4], uint32_t turn, u
         scale = 0.0f;
         return 0u;
     }
-    const float unit = top * top * (1.0f / scale);
-    uint32_t codes = 0;
+    // 1 / scale, correctly rounded as root_of is
+    const float r0 = __builtin_amdgcn_rcpf(scale), unit = top * top * fmaf(fmaf(-scale, r0, 1.0f), r0, r0);
+    float q[4];
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-        const float y = fabsf(v[j]) * unit, q = floorf(sqrtf(y));
-        const float u = (float)((turn + j * apart) >> 8) * 0x1p-24f;
-        int k = (int)fminf(q + (y - q * q > u * (2.0f * q + 1.0f) ? 1.0f : 0.0f), top);
-        if (SIGN) k = v[j] < 0.0f ? -k : k;
-        else k = v[j] > 0.0f ? max(k, 1) : 0;
-        codes |= (uint32_t)(k & 255) << (8 * j);
+        const float y = fabsf(v[j]) * unit;
+        q[j] = floorf(__builtin_amdgcn_sqrtf(y));
+        const float u = (float)((turn + j * apart) >> 8);   // in 2^-24, and 2 q + 1 in 2^24
+        const float apart_by = u * fmaf(q[j], 0x1p-23f, 0x1p-24f);
+        q[j] = fminf(q[j] + (fmaf(-q[j], q[j], y) > apart_by ? 1.0f : 0.0f), top);
+        if (!SIGN) q[j] = fmaxf(q[j], v[j] > 0.0f ? 1.0f : 0.0f);
     }
-    return codes;
+    // whole numbers, as the low bytes of floats that have no bits below one
+    constexpr float up = 12582912.0f;
+    uint32_t b[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) b[j] = __float_as_uint((SIGN ? copysignf(q[j], v[j]) : q[j]) + up);
+    return __builtin_amdgcn_perm(b[1], b[0], 0x0c0c0400u) | __builtin_amdgcn_perm(b[3], b[2], 0x04000c0cu);
+}
+
+// ---- a step -------------------------------------------------------------------------------------------
+struct StepFactors {
+    float rate, root, decay, scale;   // of the moments' quotient, of sqrt(v), of the parameter, of the gradient
+    uint32_t step;
+};
+// A workgroup's chunk of a tensor, from element `from` on.  P: the parameter's type; MASTER: its float32 copy is updated; R: the gradient's.
+template <int BITS, typename P, bool MASTER, typename R, bool FULL>
+__device__ __forceinline__ void adamw_chunk(const AdamwArgs& a, const AdamwTensor& e, int64_t from, int n, const StepFactors& f)
+{
+#pragma clang fp contract(off)   // the moments are what the header's products and sums give, each rounded
+    P* const param = static_cast<P*>(e.param) + from;
+    const R* const grad = static_cast<const R*>(e.grad) + from;
+    float* const master = MASTER ? e.master + from : nullptr;
+    for (int i0 = 0; i0 < n; i0 += ADAMW_STEP) {
+        const int i = i0 + threadIdx.x * 4, have = FULL ? 4 : max(min(n - i, 4), 0);
+        float p[4], g[4], m[4], v[4], s[4];
+        if constexpr (MASTER) load4<FULL>(master + i, have, p);
+        else load4<FULL>(param + i, have, p);
+        load4<FULL>(grad + i, have, g);
+        const int block = (i0 + threadIdx.x / WAVE * 256) / SS_ADAMW_BLOCK;
+        const bool there = FULL || block * SS_ADAMW_BLOCK < n;   // the same for a wave
+        float *const m_scale = BITS == 8 ? e.m_scale + from / SS_ADAMW_BLOCK + block : nullptr, *const v_scale = BITS == 8 ? e.v_scale + from / SS_ADAMW_BLOCK + block : nullptr;
+        if constexpr (BITS == 32) {
+            load4<FULL>(static_cast<const float*>(e.m) + from + i, have, m);
+            load4<FULL>(static_cast<const float*>(e.v) + from + i, have, v);
+        } else {
+            const uint32_t cm = load_codes<FULL>(static_cast<const uint8_t*>(e.m) + from + i, have), cv = load_codes<FULL>(static_cast<const uint8_t*>(e.v) + from + i, have);
+            const float am = there ? *m_scale : 0.0f, av = there ? *v_scale : 0.0f;
+            decode<true>(cm, am, m);
+            decode<false>(cv, av, v);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) v[j] *= v[j];
+        }
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            g[j] *= f.scale;
+            m[j] = m[j] * a.beta1 + g[j] * a.rest1;
+            v[j] = v[j] * a.beta2 + g[j] * g[j] * a.rest2;
+            s[j] = root_of(v[j]);
+            p[j] = fmaf(-f.rate, m[j] * __builtin_amdgcn_rcpf(fmaf(s[j], f.root, a.eps)), fmaf(-f.decay, p[j], p[j]));
+        }
+        if constexpr (MASTER) store4<FULL>(master + i, have, p);
+        store4<FULL>(param + i, have, p);
+        if constexpr (BITS == 32) {
+            store4<FULL>(static_cast<float*>(e.m) + from + i, have, m);
+            store4<FULL>(static_cast<float*>(e.v) + from + i, have, v);
+        } else {
+            float am, av;
+            const uint32_t at = (uint32_t)(from + i);
+            // behind the tensor's end m and s are 0
+            store_codes<FULL>(static_cast<uint8_t*>(e.m) + from + i, have, encode<true>(m, at * 0x6a09e667u + f.step * 0xbb67ae85u, 0x6a09e667u, am));
+            store_codes<FULL>(static_cast<uint8_t*>(e.v) + from + i, have, encode<false>(s, at * 0x3c6ef372u + f.step * 0xa54ff53au, 0x3c6ef372u, av));
+            if (there && threadIdx.x % WAVE == 0) {
+                *m_scale = am;
+                *v_scale = av;
+            }
+        }
+    }
+}
+template <int BITS, typename P, bool MASTER, typename R>
+__device__ __forceinline__ void adamw_chunk_of(const AdamwArgs& a, const AdamwTensor& e, int64_t from, int n, const StepFactors& f)
+{
+    if (n % ADAMW_STEP == 0) adamw_chunk<BITS, P, MASTER, R, true>(a, e, from, n, f);
+    else adamw_chunk<BITS, P, MASTER, R, false>(a, e, from, n, f);
 }
 
 template <int BITS>
 __global__ __launch_bounds__(ADAMW_THREADS) void adamw_kernel(const AdamwArgs a)
 {
-#pragma clang fp contract(off)   // the moments are what the header's products and sums give, each rounded
+    const int taken = a.count[0];
     int k = 0, above = a.tensors;   // the tensor that has this chunk: start[k] <= blockIdx.x < start[above]
     while (above - k > 1) {
         const int mid = (k + above) / 2;
         if (a.start[mid] <= (int)blockIdx.x) k = mid;
         else above = mid;
     }
-    const int taken = a.count[0];
-    const uint32_t step = (uint32_t)taken + 1u;
-    if (a.tensors > 0) {
-        const AdamwTensor& e = a.tensor[k];
-        const bool low_param = a.low_param[k], low_grad = a.low_grad[k];
-        // 1 - beta^t = -expm1(t log beta)
-        const float c1 = -expm1f((float)(step * a.log1)), c2 = -expm1f((float)(step * a.log2));
-        const float lr = a.lr_device ? a.lr_device[0] : a.lr, gs = a.grad_scale ? a.grad_scale[0] : 1.0f;
-        const float rate = lr / c1, root = 1.0f / sqrtf(c2), decay = lr * a.decay;
-        const int64_t n = e.n, from = (int64_t)((int)blockIdx.x - a.start[k]) * a.chunk, to = min(from + a.chunk, n);
-        for (int64_t i0 = from; i0 < to; i0 += ADAMW_STEP) {
-            const int64_t i = i0 + threadIdx.x * 4;
-            const int have = (int)max(min(n - i, (int64_t)4), (int64_t)0);
-            float p[4], g[4], m[4], v[4], s[4];
-            const int64_t block = (i0 + threadIdx.x / WAVE * 256) / SS_ADAMW_BLOCK;
-            const bool there = block * SS_ADAMW_BLOCK < n;   // the same for a wave
-            load4(low_param && e.master ? static_cast<const void*>(e.master) : e.param, low_param && !e.master, i, have, p);
-            load4(e.grad, low_grad, i, have, g);
-            if constexpr (BITS == 32) {
-                load4(e.m, false, i, have, m);
-                load4(e.v, false, i, have, v);
-            } else {
-                decode<true>(load_codes(e.m, i, have), there ? e.m_scale[block] : 0.0f, m);
-                decode<false>(load_codes(e.v, i, have), there ? e.v_scale[block] : 0.0f, v);
-#pragma unroll
-                for (int j = 0; j < 4; ++j) v[j] *= v[j];
-            }
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                g[j] *= gs;
-                m[j] = m[j] * a.beta1 + g[j] * a.rest1;
-                v[j] = v[j] * a.beta2 + g[j] * g[j] * a.rest2;
-                s[j] = sqrtf(v[j]);
-                p[j] = fmaf(-decay, p[j], p[j]) - rate * (m[j] * __builtin_amdgcn_rcpf(fmaf(s[j], root, a.eps)));
-            }
-            if (low_param && e.master) store4(e.master, false, i, have, p);
-            store4(e.param, low_param, i, have, p);
-            if constexpr (BITS == 32) {
-                store4(e.m, false, i, have, m);
-                store4(e.v, false, i, have, v);
-            } else {
-                float ms, vs;
-                const uint32_t at = (uint32_t)i;
-                // behind the tensor's end m and s are 0
-                store_codes(e.m, i, have, encode<true>(m, at * 0x6a09e667u + step * 0xbb67ae85u, 0x6a09e667u, ms));
-                store_codes(e.v, i, have, encode<false>(s, at * 0x3c6ef372u + step * 0xa54ff53au, 0x3c6ef372u, vs));
-                if (there && threadIdx.x % WAVE == 0) {
-                    e.m_scale[block] = ms;
-                    e.v_scale[block] = vs;
-                }
-            }
-        }
-    }
-    if (!a.last) return;
-    __syncthreads();   // all of the workgroup have read the count
-    if (threadIdx.x == 0) {
-        __threadfence();
-        if (atomicAdd(&a.count[1], 1) == (int)gridDim.x - 1) {
+    if (a.last) {
+        __syncthreads();   // all of the workgroup have read the count; the last workgroup that says so writes it
+        if (threadIdx.x == 0 && atomicAdd(&a.count[1], 1) == (int)gridDim.x - 1) {
             a.count[1] = 0;
             a.count[0] = taken + 1;
         }
+    }
+    if (a.tensors == 0) return;
+    StepFactors f;
+    f.step = (uint32_t)taken + 1u;
+    // 1 - beta^t = -expm1(t log beta)
+    const float c1 = -expm1f((float)(f.step * a.log1)), c2 = -expm1f((float)(f.step * a.log2));
+    const float lr = a.lr_device ? a.lr_device[0] : a.lr;
+    f.rate = lr / c1;
+    f.root = 1.0f / sqrtf(c2);
+    f.decay = lr * a.decay;
+    f.scale = a.grad_scale ? a.grad_scale[0] : 1.0f;
+    const AdamwTensor& e = a.tensor[k];
+    const int64_t from = (int64_t)((int)blockIdx.x - a.start[k]) * a.chunk;
+    const int n = (int)min((int64_t)a.chunk, e.n - from);
+    if (a.low_grad[k]) {
+        if (!a.low_param[k]) adamw_chunk_of<BITS, float, false, bf16_t>(a, e, from, n, f);
+        else if (e.master) adamw_chunk_of<BITS, bf16_t, true, bf16_t>(a, e, from, n, f);
+        else adamw_chunk_of<BITS, bf16_t, false, bf16_t>(a, e, from, n, f);
+    } else {
+        if (!a.low_param[k]) adamw_chunk_of<BITS, float, false, float>(a, e, from, n, f);
+        else if (e.master) adamw_chunk_of<BITS, bf16_t, true, float>(a, e, from, n, f);
+        else adamw_chunk_of<BITS, bf16_t, false, float>(a, e, from, n, f);
     }
 }
 
@@ -219,8 +273,8 @@ __global__ __launch_bounds__(256) void adamw_values_kernel(const void* codes, co
     for (int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4; i < n; i += (int64_t)gridDim.x * 1024) {
         const int have = (int)min(n - i, (int64_t)4);
         float v[4];
-        decode<SIGN>(load_codes(codes, i, have), scale[i / SS_ADAMW_BLOCK], v);
-        store4(out, sizeof(T) == 2, i, have, v);
+        decode<SIGN>(load_codes<false>(static_cast<const uint8_t*>(codes) + i, have), scale[i / SS_ADAMW_BLOCK], v);
+        store4<false>(out + i, have, v);
     }
 }
 

@@ -51,11 +51,30 @@ __device__ __forceinline__ Stat join(Stat a, Stat b)
     shift(b, ref);
     return {m, a.s + b.s, a.u + b.u};
 }
+// The same over a wave, in all of its lanes: the largest first, then two sums of lanes that have been brought to it.  Lanes exchange by the vector
+// unit's own means: within rows of 16, then the last lane of a row into the next row, and the last of the first half into the second.
+template <int CONTROL, int ROWS>
+__device__ __forceinline__ float from_lane(float v, float none)
+{
+    return __uint_as_float((uint32_t)__builtin_amdgcn_update_dpp((int)__float_as_uint(none), (int)__float_as_uint(v), CONTROL, ROWS, 0xf, false));
+}
+template <typename F>
+__device__ __forceinline__ float over_wave(float v, float none, F op)
+{
+    v = op(v, from_lane<0x111, 0xf>(v, none));
+    v = op(v, from_lane<0x112, 0xf>(v, none));
+    v = op(v, from_lane<0x114, 0xf>(v, none));
+    v = op(v, from_lane<0x118, 0xf>(v, none));
+    v = op(v, from_lane<0x142, 0xa>(v, none));
+    v = op(v, from_lane<0x143, 0xc>(v, none));
+    return __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(v), WAVE - 1));
+}
 __device__ __forceinline__ Stat join_wave(Stat a)
 {
-#pragma unroll
-    for (int s = 1; s < WAVE; s *= 2) a = join(a, {__shfl_xor(a.m, s), __shfl_xor(a.s, s), __shfl_xor(a.u, s)});
-    return a;
+    const float m = over_wave(a.m, -INFINITY, [](float x, float y) { return fmaxf(x, y); });
+    shift(a, reference(m));
+    auto add = [](float x, float y) { return x + y; };
+    return {m, over_wave(a.s, 0.0f, add), over_wave(a.u, 0.0f, add)};
 }
 
 // ---- the best of a wave ---------------------------------------------------------------------------
@@ -64,27 +83,22 @@ struct Best {
     float v = -INFINITY;
     int i = -1;
     __device__ __forceinline__ bool ahead(float x, int k) const { return i >= 0 && (v > x || (v == x && i < k)); }
+    static __device__ __forceinline__ float value_of(float x, int lane) { return __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(x), lane)); }
     __device__ __forceinline__ void insert(float x, int k)   // the same in all lanes
     {
         const int place = __popcll(__ballot(ahead(x, k))), lane = threadIdx.x % WAVE;
-        const float pv = __shfl_up(v, 1);
-        const int pi = __shfl_up(i, 1);
-        if (lane > place) {
-            v = pv;
-            i = pi;
-        } else if (lane == place) {
-            v = x;
-            i = k;
-        }
+        const float pv = from_lane<0x138, 0xf>(v, v);   // of the lane before
+        const int pi = __builtin_amdgcn_update_dpp(i, i, 0x138, 0xf, 0xf, false);
+        v = lane > place ? pv : (lane == place ? x : v);
+        i = lane > place ? pi : (lane == place ? k : i);
     }
     // N values a lane; column(j) is -1 for those that are left out
     template <int N, typename F>
     __device__ __forceinline__ void absorb(const float (&x)[N], F column, int top)
     {
         static_assert(N <= 32, "a bit each");
-        const int lane = threadIdx.x % WAVE;
-        float lv = __shfl(v, top - 1);
-        int li = __shfl(i, top - 1);
+        float lv = value_of(v, top - 1);
+        int li = __builtin_amdgcn_readlane(i, top - 1);
         uint32_t open = 0;   // what the last of the top is not ahead of
         float most = -INFINITY;
 #pragma unroll
@@ -96,16 +110,22 @@ struct Best {
             }
         }
         if (!__ballot(open != 0)) return;
-        if (li < 0) {   // the top is not full yet: the top-th largest of the lanes' maxima is a bound, as that many values are no less
-            int above = 0;
-            for (int l = 0; l < WAVE; ++l) {
-                const float o = __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(most), l));
-                above += o > most || (o == most && l < lane) ? 1 : 0;
-            }
-            const float bound = __shfl(most, __ffsll((long long)__ballot(above == top - 1)) - 1);
+        if (li < 0) {
+            // the top is not full yet: the top-th largest of the lanes' maxima is a bound, as that many values are no less.  Its upper
+            // 16 bits are enough, found from the highest down in numbers whose order is the floats'
+            const uint32_t bits = __float_as_uint(most + 0.0f), order = open ? bits ^ ((uint32_t)((int)bits >> 31) | 0x80000000u) : 0u;
+            uint32_t bound = 0;
 #pragma unroll
-            for (int j = 0; j < N; ++j)
-                if (!(x[j] >= bound)) open &= ~(1u << j);
+            for (int b = 31; b >= 16; --b) {
+                const uint32_t higher = bound | 1u << b;
+                if (__popcll(__ballot(order >= higher)) >= top) bound = higher;
+            }
+            const float least = __uint_as_float(bound & 0x80000000u ? bound ^ 0x80000000u : ~bound);
+            if (bound > 0x007fffffu) {   // no less than -infinity
+#pragma unroll
+                for (int j = 0; j < N; ++j)
+                    if (!(x[j] >= least)) open &= ~(1u << j);
+            }
         }
         while (__ballot(open != 0)) {
             // every lane's first candidate
@@ -118,23 +138,16 @@ struct Best {
                     ck = column(j);
                 }
             open &= open - 1;
-            bool late = behind(cv, ck, top);
-            uint64_t ask = __ballot(ck >= 0 && !late);
+            uint64_t ask = __ballot(ck >= 0 && !(li >= 0 && (lv > cv || (lv == cv && li < ck))));
             while (ask) {
                 const int l = __ffsll((long long)ask) - 1;
-                insert(__shfl(cv, l), __shfl(ck, l));
+                insert(value_of(cv, l), __builtin_amdgcn_readlane(ck, l));
+                lv = value_of(v, top - 1);
+                li = __builtin_amdgcn_readlane(i, top - 1);
                 ask &= ask - 1;
-                late = behind(cv, ck, top);
-                ask &= __ballot(!late);
+                ask &= __ballot(!(li >= 0 && (lv > cv || (lv == cv && li < ck))));
             }
         }
-    }
-    // whether the last of the top is ahead of (x, k); all lanes call
-    __device__ __forceinline__ bool behind(float x, int k, int top) const
-    {
-        const float lv = __shfl(v, top - 1);
-        const int li = __shfl(i, top - 1);
-        return li >= 0 && (lv > x || (lv == x && li < k));
     }
 };
 
@@ -173,10 +186,10 @@ __device__ __forceinline__ void results(const LogprobArgs& a, int row, Stat t, c
 __host__ __device__ __forceinline__ int part_floats(int top) { return 4 + 2 * top; }
 
 // G lanes a row (a wave: rows side by side) or piece of one; V slices of eight a lane and step, the next step's requested ahead.
-template <typename T, typename I, int G, bool TOP>
+template <typename T, typename I, int G, int V, bool TOP>
 __global__ __launch_bounds__(256) void logprob_fwd_kernel(LogprobArgs a)
 {
-    constexpr int V = 4, SIDE = 256 / G, WAVES = G / WAVE;
+    constexpr int SIDE = 256 / G, WAVES = G / WAVE;
     const int gl = threadIdx.x % G;
     const unsigned group = blockIdx.x * SIDE + threadIdx.x / G;
     const int row = (int)(group / (unsigned)a.pieces), piece = (int)(group % (unsigned)a.pieces);
@@ -374,10 +387,12 @@ template <typename T, typename I, bool TOP>
 void logprob_forward(const LogprobArgs& a, hipStream_t st)
 {
     if (a.vocab <= LOGPROB_WAVE) {
-        hipLaunchKernelGGL((logprob_fwd_kernel<T, I, 64, TOP>), dim3((unsigned)(((int64_t)a.rows + 3) / 4)), dim3(256), 0, st, a);
+        hipLaunchKernelGGL((logprob_fwd_kernel<T, I, 64, 2, TOP>), dim3((unsigned)(((int64_t)a.rows + 3) / 4)), dim3(256), 0, st, a);
         return;
     }
-    hipLaunchKernelGGL((logprob_fwd_kernel<T, I, 256, TOP>), dim3((unsigned)((int64_t)a.rows * a.pieces)), dim3(256), 0, st, a);
+    const dim3 grid((unsigned)((int64_t)a.rows * a.pieces));
+    if (a.piece <= 2048) hipLaunchKernelGGL((logprob_fwd_kernel<T, I, 256, 1, TOP>), grid, dim3(256), 0, st, a);
+    else hipLaunchKernelGGL((logprob_fwd_kernel<T, I, 256, 2, TOP>), grid, dim3(256), 0, st, a);
     if (a.pieces > 1) hipLaunchKernelGGL((logprob_join_kernel<T, I, TOP>), dim3((unsigned)a.rows), dim3(64), 0, st, a);
 }
 template <typename T, typename I>
