@@ -207,6 +207,10 @@ def embedding(ids, table, scale=1.0, out_dtype=None):
     """Differentiable lookup: rows of ``table`` (vocab, dim), times ``scale``, for token ids of any shape, in ``out_dtype`` (the table's unless
     given).  Ids outside the table (-1 for padding) give zeros and no gradient.  The table's gradient is a sum in token order:
     the same bits every time."""
+    if table.is_cuda:
+        r = B.embedding_node(ids, table, scale, out_dtype)
+        if r is not None:
+            return r
     return _Embedding.apply(ids, table, scale, out_dtype)
 
 
@@ -235,4 +239,8 @@ def token_logprobs(logits, targets, top=0):
     """Differentiable log probabilities of ``targets`` (...) under ``logits`` (..., vocab) and the entropies, float32 (...): (logp, entropy).  A target
     outside the vocabulary (-1 for padding) has the log probability 0 and no gradient from it; logits of -infinity have probability 0.  With
     ``top`` also (top_logp, top_ids), (..., top): the most probable columns in order, without a gradient."""
+    if logits.is_cuda:
+        r = B.token_logprobs_node(logits, targets, top)
+        if r is not None:
+            return r
     return _TokenLogprobs.apply(logits, targets, top)

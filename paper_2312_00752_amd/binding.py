@@ -286,6 +286,7 @@ class _NoMarshal:
 
     step = layer_step = scan_fwd = scan_bwd = layer_fwd = layer_bwd = staticmethod(_none)
     norm_fwd = norm_quant = norm_bwd = gate_fwd = gate_bwd = gate_step = qlinear = layer_norm = gated_recurrence = adamw_step = staticmethod(_none)
+    embed_fwd = embedding = logprob_fwd = token_logprobs = staticmethod(_none)
 
 
 def _marshal():
@@ -1333,6 +1334,11 @@ def _on_current(*tensors):
             raise ValueError("a tensor lies on %s, the current device is cuda:%d" % (t.device, _device_index()))
 
 
+def _type_code(dtype):
+    """For the compiled module: None, or the code of an io type; what is none of them is refused behind it."""
+    return None if dtype is None else (SS_F32 if dtype is torch.float32 else (SS_BF16 if dtype is torch.bfloat16 else -1))
+
+
 def _embed_params(ids, vocab, dim, scale):
     p = EmbedParams()
     if ids.dtype is not torch.int64 and ids.dtype is not torch.int32:
@@ -1350,6 +1356,10 @@ def ss_embed_fwd(ids, table, scale=1.0, out_dtype=None, out=None, stream=None):
     if stream is not None:
         with _current(stream):
             return ss_embed_fwd(ids, table, scale, out_dtype, out)
+    if out is None and table.is_cuda:
+        r = (_native or _marshal()).embed_fwd(ids, table, float(scale), _type_code(out_dtype), _stream(stream), _device_index())
+        if r is not None:
+            return _result(r)
     _on_current(ids, table, out)
     if table.dim() != 2:
         raise ValueError("table must have two axes")
@@ -1450,6 +1460,10 @@ def ss_logprob_fwd(logits, targets=None, top=0, workspace=None, stream=None):
     if stream is not None:
         with _current(stream):
             return ss_logprob_fwd(logits, targets, top, workspace)
+    if workspace is None and logits.is_cuda:
+        r = (_native or _marshal()).logprob_fwd(logits, targets, top, _stream(stream), _device_index())
+        if r is not None:
+            return _result(r)
     _on_current(logits, targets, workspace)
     p = _logprob_params(logits, targets, top)
     shape, dev, f32 = tuple(logits.shape[:-1]), logits.device, torch.float32
@@ -1591,4 +1605,16 @@ def layer_norm_node(x, weight, bias, residual, eps, rms=False):
 def gated_recurrence_node(x, f, i, z, rate, f_bias, i_bias, reset, h0, return_last_state):
     """The same for autograd.gated_recurrence."""
     r = (_native or _marshal()).gated_recurrence(x, f, i, z, rate, f_bias, i_bias, reset, h0, bool(return_last_state), _stream(None))
+    return r if r is None else _result(r)
+
+
+def embedding_node(ids, table, scale, out_dtype):
+    """The same for autograd.embedding."""
+    r = (_native or _marshal()).embedding(ids, table, float(scale), _type_code(out_dtype), _stream(None), _device_index())
+    return r if r is None else _result(r)
+
+
+def token_logprobs_node(logits, targets, top):
+    """The same for autograd.token_logprobs."""
+    r = (_native or _marshal()).token_logprobs(logits, targets, top, _stream(None), _device_index())
     return r if r is None else _result(r)

@@ -21,8 +21,10 @@
 #include <vector>
 
 #include "ss_adamw.h"
+#include "ss_embed.h"
 #include "ss_gate.h"
 #include "ss_layer.h"
+#include "ss_logprob.h"
 #include "ss_norm.h"
 #include "ss_quant.h"
 #include "ss_scan.h"
@@ -1044,6 +1046,291 @@ PyObject* py_qlinear(PyObject*, PyObject* const* argv, Py_ssize_t n)
     END_HANDLE_TH_ERRORS
 }
 
+// ---- embedding, log probabilities, AdamW -----------------------------------------------------------
+// Whether a tensor lies on the device whose stream the call takes.
+bool on_device(const at::Tensor& t, long device) { return t.is_cuda() && t.device().index() == device; }
+// whole numbers in 64 or 32 bits
+bool whole_type(const at::Tensor& t, uint32_t flag_of_32, uint32_t& flags)
+{
+    if (t.scalar_type() == at::kInt) flags |= flag_of_32;
+    else if (t.scalar_type() != at::kLong) return false;
+    return true;
+}
+// The type of a code of io types; `ok` falls if it is none.
+at::ScalarType type_of_code(long code, bool& ok)
+{
+    if (code == SS_F32) return at::kFloat;
+    if (code != SS_BF16) ok = false;
+    return at::kBFloat16;
+}
+struct Embed {
+    at::Tensor out;
+    int fwd(const at::Tensor& ids, const at::Tensor& table, double scale, at::ScalarType type, void* stream)
+    {
+        ss_embed_params p{};
+        if (!sizes(p, ids, table.size(0), table.size(1), scale) || !io_type(table, p.table_dtype)) return SS_ERR_UNSUPPORTED;
+        c10::SmallVector<int64_t, 6> shape(ids.sizes().begin(), ids.sizes().end());
+        shape.push_back(table.size(1));
+        out = at::empty(shape, table.options().dtype(type).requires_grad(false));
+        io_type(out, p.io_dtype);
+        p.table = table.data_ptr();
+        p.out = out.data_ptr();
+        return ss_embed_fwd(&p, stream);
+    }
+    int bwd(const at::Tensor& dout, const at::Tensor& ids, int64_t vocab, double scale, at::ScalarType type, void* stream)
+    {
+        ss_embed_bwd_params q{};
+        ss_embed_params& p = q.fwd;
+        if (!sizes(p, ids, vocab, dout.size(-1), scale) || !io_type(dout, p.io_dtype)) return SS_ERR_UNSUPPORTED;
+        out = at::empty({vocab, dout.size(-1)}, dout.options().dtype(type).requires_grad(false));
+        io_type(out, p.table_dtype);
+        q.dout = dout.data_ptr();
+        q.dtable = out.data_ptr();
+        const at::Tensor ws = empty_bytes(ss_embed_workspace_bytes(&p), dout);
+        q.workspace = ws.data_ptr();
+        q.workspace_bytes = (size_t)ws.numel();
+        return ss_embed_bwd(&q, stream);
+    }
+    static bool sizes(ss_embed_params& p, const at::Tensor& ids, int64_t vocab, int64_t dim, double scale)
+    {
+        if (!fits(ids.numel()) || !fits(vocab) || !fits(dim) || !whole_type(ids, SS_EMBED_IDS_32, p.flags)) return false;
+        p.tokens = (int32_t)ids.numel(); p.vocab = (int32_t)vocab; p.dim = (int32_t)dim;
+        p.scale = (float)scale;
+        p.ids = ids.data_ptr();
+        return true;
+    }
+};
+// ids, table, scale, type of the result, stream, device
+bool embed_inputs(Args& a, double& scale, at::ScalarType& type, void*& stream)
+{
+    const at::Tensor *ids = a.tensor(0), *table = a.ok ? a.tensor(1) : nullptr;
+    if (!a.ok || table->dim() != 2 || !real_number(a.a[2], scale)) return false;
+    int32_t code;
+    uint32_t flags = 0;
+    if (!io_type(*table, code) || !whole_type(*ids, SS_EMBED_IDS_32, flags)) return false;
+    type = a.none(3) ? table->scalar_type() : type_of_code(a.number(3), a.ok);
+    stream = a.stream(4);
+    const long device = a.number(5);
+    return a.ok && on_device(*ids, device) && on_device(*table, device) && fits(ids->numel()) && fits(table->size(0)) && fits(table->size(1));
+}
+// embed_fwd(ids, table, scale, type or None, stream, device) -> out
+PyObject* py_embed_fwd(PyObject*, PyObject* const* argv, Py_ssize_t n)
+{
+    HANDLE_TH_ERRORS
+    if (n != 6) Py_RETURN_NONE;
+    Args a{argv};
+    double scale;
+    at::ScalarType type;
+    void* stream;
+    if (!embed_inputs(a, scale, type, stream)) Py_RETURN_NONE;
+    Embed e;
+    int rc;
+    {
+        Unlocked u;
+        rc = e.fwd(THPVariable_Unpack(argv[0]), THPVariable_Unpack(argv[1]), scale, type, stream);
+    }
+    if (rc != SS_OK) return PyLong_FromLong(rc);
+    return wrapped(e.out);
+    END_HANDLE_TH_ERRORS
+}
+// The embedding as a node of torch's graph (what autograd._Embedding is in Python).
+struct EmbedFunction : torch::autograd::Function<EmbedFunction> {
+    static torch::autograd::variable_list forward(torch::autograd::AutogradContext* ctx, const at::Tensor& ids, const at::Tensor& table, double scale, int64_t type, int64_t stream)
+    {
+        Embed e;
+        const int rc = e.fwd(ids, table, scale, (at::ScalarType)type, reinterpret_cast<void*>(stream));
+        if (rc != SS_OK) throw Refused{rc};
+        ctx->save_for_backward({ids});
+        ctx->saved_data["vocab"] = table.size(0);
+        ctx->saved_data["scale"] = scale;
+        ctx->saved_data["type"] = (int64_t)table.scalar_type();
+        ctx->saved_data["stream"] = stream;
+        return {e.out};
+    }
+    static torch::autograd::variable_list backward(torch::autograd::AutogradContext* ctx, torch::autograd::variable_list grads)
+    {
+        const auto saved = ctx->get_saved_variables();
+        Embed e;
+        backward_check(e.bwd(grads[0].contiguous(), saved[0], ctx->saved_data["vocab"].toInt(), ctx->saved_data["scale"].toDouble(),
+                             (at::ScalarType)ctx->saved_data["type"].toInt(), reinterpret_cast<void*>(ctx->saved_data["stream"].toInt())));
+        return differentiable_once({at::Tensor(), e.out, at::Tensor(), at::Tensor(), at::Tensor()}, {&grads});
+    }
+};
+// embedding(ids, table, scale, type or None, stream, device) -> out, with a gradient
+PyObject* py_embedding(PyObject*, PyObject* const* argv, Py_ssize_t n)
+{
+    HANDLE_TH_ERRORS
+    if (n != 6) Py_RETURN_NONE;
+    Args a{argv};
+    double scale;
+    at::ScalarType type;
+    void* stream;
+    if (!embed_inputs(a, scale, type, stream)) Py_RETURN_NONE;
+    torch::autograd::variable_list r;
+    try {
+        Unlocked u;
+        r = EmbedFunction::apply(THPVariable_Unpack(argv[0]), THPVariable_Unpack(argv[1]), scale, (int64_t)type, reinterpret_cast<int64_t>(stream));
+    } catch (const Refused& e) {
+        return PyLong_FromLong(e.rc);
+    }
+    return wrapped(r[0]);
+    END_HANDLE_TH_ERRORS
+}
+
+// Rows of logits, which may lie in wider ones: elements from one to the next; 0 where they are not equally far from each other, or overlap.
+int64_t row_stride(const at::Tensor& t)
+{
+    const int64_t width = t.size(-1);
+    if (t.is_contiguous()) return width;
+    if (t.stride(-1) != 1 && width != 1) return 0;
+    int64_t stride = 0, at = 0;
+    for (int64_t k = t.dim() - 1; k-- > 0;) {
+        if (t.size(k) == 1) continue;
+        if (stride == 0) stride = t.stride(k);
+        else if (t.stride(k) != at) return 0;
+        at = t.stride(k) * t.size(k);
+    }
+    if (stride == 0) stride = width;
+    return stride < width ? 0 : stride;
+}
+struct Logprob {
+    at::Tensor logp, entropy, stats, top_logp, top_ids;
+    static bool sizes(ss_logprob_params& p, const at::Tensor& x, const at::Tensor& targets)
+    {
+        if (x.dim() < 1 || x.size(-1) < 1 || !io_type(x, p.io_dtype)) return false;
+        const int64_t rows = x.numel() / x.size(-1);
+        p.row_stride = row_stride(x);
+        if (!p.row_stride || !fits(rows) || !fits(x.size(-1))) return false;
+        p.rows = (int32_t)rows; p.vocab = (int32_t)x.size(-1);
+        p.logits = x.data_ptr();
+        if (targets.defined()) {
+            if (!whole_type(targets, SS_LOGPROB_TARGETS_32, p.flags) || !targets.sizes().equals(x.sizes().slice(0, x.dim() - 1))) return false;
+            p.targets = targets.data_ptr();
+        }
+        return true;
+    }
+    int fwd(const at::Tensor& x, const at::Tensor& targets, int64_t top, void* stream)
+    {
+        ss_logprob_params p{};
+        if (!sizes(p, x, targets)) return SS_ERR_SHAPE;
+        p.top = (int32_t)top;
+        const at::IntArrayRef shape = x.sizes().slice(0, x.dim() - 1);
+        if (targets.defined()) logp = empty_f32(shape, x);
+        entropy = empty_f32(shape, x);
+        stats = empty_f32({2, p.rows}, x);
+        p.logp = data<float>(logp); p.entropy = data<float>(entropy); p.stats = data<float>(stats);
+        if (top) {
+            c10::SmallVector<int64_t, 6> wide(shape.begin(), shape.end());
+            wide.push_back(top);
+            top_logp = empty_f32(wide, x);
+            top_ids = at::empty(wide, x.options().dtype(at::kLong).requires_grad(false));
+            p.top_logp = data<float>(top_logp); p.top_ids = data<int64_t>(top_ids);
+        }
+        at::Tensor ws;
+        if (const size_t need = ss_logprob_workspace_bytes(&p)) {
+            ws = empty_bytes(need, x);
+            p.workspace = ws.data_ptr();
+            p.workspace_bytes = (size_t)ws.numel();
+        }
+        return ss_logprob_fwd(&p, stream);
+    }
+};
+int logprob_bwd(const at::Tensor& x, const at::Tensor& targets, const at::Tensor& entropy, const at::Tensor& stats, const at::Tensor& dlogp, const at::Tensor& dentropy,
+                at::Tensor& out, void* stream)
+{
+    ss_logprob_bwd_params q{};
+    if (!Logprob::sizes(q.fwd, x, targets)) return SS_ERR_SHAPE;
+    q.fwd.stats = data<float>(stats);
+    q.fwd.entropy = data<float>(entropy);
+    q.dlogp = data<const float>(dlogp);
+    q.dentropy = data<const float>(dentropy);
+    out = at::empty(x.sizes(), x.options().requires_grad(false));
+    q.dlogits = out.data_ptr();
+    return ss_logprob_bwd(&q, stream);
+}
+// logits, targets or None, top, stream, device
+bool logprob_inputs(Args& a, at::Tensor& x, at::Tensor& targets, int64_t& top, void*& stream)
+{
+    if (!THPVariable_CheckExact(a.a[0])) return false;
+    x = THPVariable_Unpack(a.a[0]);
+    const long device = a.number(4);
+    if (!x.has_storage() || !on_device(x, device)) return false;
+    if (!a.none(1)) {
+        const at::Tensor* t = a.tensor(1);
+        if (!t || !on_device(*t, device)) return false;
+        targets = *t;
+    }
+    top = a.number(2);
+    stream = a.stream(3);
+    ss_logprob_params p{};
+    return a.ok && Logprob::sizes(p, x, targets) && top >= 0 && top <= SS_LOGPROB_MAX_TOP && top <= p.vocab;
+}
+// logprob_fwd(logits, targets or None, top, stream, device) -> (logp or None, entropy, stats, top_logp or None, top_ids or None)
+PyObject* py_logprob_fwd(PyObject*, PyObject* const* argv, Py_ssize_t n)
+{
+    HANDLE_TH_ERRORS
+    if (n != 5) Py_RETURN_NONE;
+    Args a{argv};
+    at::Tensor x, targets;
+    int64_t top;
+    void* stream;
+    if (!logprob_inputs(a, x, targets, top, stream)) Py_RETURN_NONE;
+    Logprob l;
+    int rc;
+    {
+        Unlocked u;
+        rc = l.fwd(x, targets, top, stream);
+    }
+    if (rc != SS_OK) return PyLong_FromLong(rc);
+    return tuple_of({l.logp, l.entropy, l.stats, l.top_logp, l.top_ids});
+    END_HANDLE_TH_ERRORS
+}
+// Log probabilities as a node of torch's graph (what autograd._TokenLogprobs is in Python).
+struct LogprobFunction : torch::autograd::Function<LogprobFunction> {
+    static torch::autograd::variable_list forward(torch::autograd::AutogradContext* ctx, const at::Tensor& x, const at::Tensor& targets, int64_t top, int64_t stream)
+    {
+        Logprob l;
+        const int rc = l.fwd(x, targets, top, reinterpret_cast<void*>(stream));
+        if (rc != SS_OK) throw Refused{rc};
+        ctx->set_materialize_grads(false);
+        ctx->save_for_backward({x, targets, l.entropy, l.stats});
+        ctx->saved_data["stream"] = stream;
+        if (!top) return {l.logp, l.entropy};
+        ctx->mark_non_differentiable({l.top_logp, l.top_ids});
+        return {l.logp, l.entropy, l.top_logp, l.top_ids};
+    }
+    static torch::autograd::variable_list backward(torch::autograd::AutogradContext* ctx, torch::autograd::variable_list grads)
+    {
+        if (!grads[0].defined() && !grads[1].defined()) return {at::Tensor(), at::Tensor(), at::Tensor(), at::Tensor()};
+        const auto t = ctx->get_saved_variables();
+        at::Tensor dx;
+        auto dense = [](const at::Tensor& v) { return v.defined() ? v.contiguous() : v; };
+        const at::Tensor dlogp = dense(grads[0]), dentropy = dense(grads[1]);
+        backward_check(logprob_bwd(t[0], t[1], t[2], t[3], dlogp, dentropy, dx, reinterpret_cast<void*>(ctx->saved_data["stream"].toInt())));
+        return differentiable_once({dx, at::Tensor(), at::Tensor(), at::Tensor()}, {&t, &grads});
+    }
+};
+// token_logprobs(logits, targets, top, stream, device) -> (logp, entropy) or (logp, entropy, top_logp, top_ids), with gradients
+PyObject* py_token_logprobs(PyObject*, PyObject* const* argv, Py_ssize_t n)
+{
+    HANDLE_TH_ERRORS
+    if (n != 5) Py_RETURN_NONE;
+    Args a{argv};
+    at::Tensor x, targets;
+    int64_t top;
+    void* stream;
+    if (!logprob_inputs(a, x, targets, top, stream) || !targets.defined()) Py_RETURN_NONE;
+    torch::autograd::variable_list r;
+    try {
+        Unlocked u;
+        r = LogprobFunction::apply(x, targets, top, reinterpret_cast<int64_t>(stream));
+    } catch (const Refused& e) {
+        return PyLong_FromLong(e.rc);
+    }
+    return r.size() == 2 ? tuple_of({r[0], r[1]}) : tuple_of({r[0], r[1], r[2], r[3]});
+    END_HANDLE_TH_ERRORS
+}
+
 // Plain tensors of a list, all on one device; `ok` falls when one of them is not.
 struct Listed {
     PyObject* list;
@@ -1142,7 +1429,8 @@ PyObject* py_adamw_step(PyObject*, PyObject* const* argv, Py_ssize_t n)
 #define SS_METHOD(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)(void)>(py_##name)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {SS_METHOD(step), SS_METHOD(layer_step), SS_METHOD(scan_fwd), SS_METHOD(scan_bwd),
                          SS_METHOD(layer_fwd), SS_METHOD(layer_bwd), SS_METHOD(norm_fwd), SS_METHOD(norm_quant), SS_METHOD(norm_bwd), SS_METHOD(gate_fwd),
-                         SS_METHOD(gate_bwd), SS_METHOD(gate_step), SS_METHOD(qlinear), SS_METHOD(layer_norm), SS_METHOD(gated_recurrence), SS_METHOD(adamw_step), {nullptr, nullptr, 0, nullptr}};
+                         SS_METHOD(gate_bwd), SS_METHOD(gate_step), SS_METHOD(qlinear), SS_METHOD(layer_norm), SS_METHOD(gated_recurrence), SS_METHOD(adamw_step),
+                         SS_METHOD(embed_fwd), SS_METHOD(embedding), SS_METHOD(logprob_fwd), SS_METHOD(token_logprobs), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_marshal", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

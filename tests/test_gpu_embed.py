@@ -173,6 +173,22 @@ def test_autograd(table, io):
     assert torch.equal(w.grad, B.ss_embed_bwd(torch.ones_like(out), ids, 30, dtype=w.dtype))
 
 
+def test_the_same_in_python(monkeypatch):
+    """Where the compiled module does not serve the call."""
+    ids, w = torch.randint(-1, 30, (3, 50), device="cuda"), torch.randn(30, 65, device="cuda", requires_grad=True)
+    out = ag.embedding(ids, w, scale=3.0, out_dtype=torch.bfloat16)
+    dout = torch.randn_like(out)
+    g, = torch.autograd.grad(out, w, dout)
+    one = B.ss_embed_fwd(ids, w.detach(), scale=3.0, out_dtype=torch.bfloat16)
+    monkeypatch.setattr(B, "_native", B._NoMarshal)
+    again = ag.embedding(ids, w, scale=3.0, out_dtype=torch.bfloat16)
+    assert again.grad_fn.name() != out.grad_fn.name()
+    assert torch.equal(again, out) and torch.equal(one, out) and torch.equal(torch.autograd.grad(again, w, dout)[0], g)
+    assert torch.equal(B.ss_embed_fwd(ids, w.detach(), scale=3.0, out_dtype=torch.bfloat16), one)
+    test_second_derivative_is_refused()
+    test_refusals()
+
+
 def test_gradient_against_differences():
     torch.manual_seed(1)
     ids = torch.randint(0, 6, (40,), device="cuda")

@@ -203,6 +203,23 @@ def test_autograd(vocab, io):
     assert torch.equal(tx.grad, B.ss_logprob_bwd(tx.detach(), stats, tt, dlogp=torch.ones(3, 4, device="cuda")))
 
 
+def test_the_same_in_python(monkeypatch):
+    """Where the compiled module does not serve the call."""
+    wide = torch.randn(3, 4, 303, device="cuda")
+    x, t = wide[..., :300].requires_grad_(True), torch.randint(-1, 300, (3, 4), device="cuda")
+    douts = [torch.randn(3, 4, device="cuda") for _ in range(2)]
+    def go():
+        res = ag.token_logprobs(x, t, top=5)
+        return [v.detach() for v in res] + list(torch.autograd.grad(res[:2], x, douts)), list(B.ss_logprob_fwd(x.detach(), t, top=5)), res[0].grad_fn.name()
+    a = go()
+    monkeypatch.setattr(B, "_native", B._NoMarshal)
+    b = go()
+    assert a[2] != b[2] and all(torch.equal(v, w) for k in (0, 1) for v, w in zip(a[k], b[k]))
+    test_axes_and_strides()
+    test_second_derivative_is_refused()
+    test_refusals()
+
+
 def test_against_cross_entropy():
     x = torch.randn(40, 900, device="cuda", requires_grad=True)
     t = torch.randint(0, 900, (40,), device="cuda")
