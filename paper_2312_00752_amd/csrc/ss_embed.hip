@@ -32,6 +32,7 @@ struct EmbedArgs {
     // sums
     const int *key, *pos;
     int piece, pieces;            // sorted tokens of a piece, their number
+    int* shared;                  // their number, and the pieces that ids begin in which several share
     float* part;                  // (pieces, 2, dim): of an id that began before the piece, and of one that goes on behind it
 };
 
@@ -53,22 +54,36 @@ __device__ __forceinline__ void row_slice(const T* row, int at, int dim, float (
     io8<T>::unpack(r, v);
 }
 
-// G lanes a token, a slice of eight a lane and step.
-template <typename E, typename T, typename I, int G>
+// G lanes a token and V slices of eight a lane and step.  A row takes two trips to memory, one behind the other, so there should be many at once: a wave a token
+// where there are tokens enough, else a workgroup.
+template <typename E, typename T, typename I, int G, int V>
 __global__ __launch_bounds__(256) void embed_fwd_kernel(EmbedArgs a)
 {
     constexpr int SIDE = 256 / G;
     const int gl = threadIdx.x % G, D = a.dim;
-    for (int64_t t = (int64_t)blockIdx.x * SIDE + threadIdx.x / G; t < a.tokens; t += (int64_t)gridDim.x * SIDE) {
+    const bool whole = D % 8 == 0;
+    const int limit = slice_limit(D, whole);
+    int64_t t = (int64_t)blockIdx.x * SIDE;
+    t += G >= WAVE ? __builtin_amdgcn_readfirstlane(threadIdx.x / G) : threadIdx.x / G;
+    for (; t < a.tokens; t += (int64_t)gridDim.x * SIDE) {
         const int id = id_of<I>(a.ids, (int)t, a.vocab);
-        const E* row = static_cast<const E*>(a.table) + (int64_t)id * D;
+        const bool there = id < a.vocab;
+        const E* row = static_cast<const E*>(a.table) + (int64_t)(there ? id : 0) * D;
         T* out = static_cast<T*>(a.out) + t * D;
-        for (int at = gl * 8; at < D; at += G * 8) {
-            float v[8] = {};
-            if (id < a.vocab) row_slice<E>(row, at, D, v);
+        for (int at0 = gl * 8; at0 < D; at0 += V * G * 8) {
+            typename io8<E>::raw r[V];
 #pragma unroll
-            for (int j = 0; j < 8; ++j) v[j] *= a.scale;
-            slice_store<T>(out, at, D - at, v);
+            for (int v = 0; v < V; ++v) r[v] = slice_request<E, true>(row, at0 + v * G * 8, D, limit);
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                const int at = at0 + v * G * 8;
+                float f[8];
+                slice_settle<E>(r[v], at, D, limit, whole);
+                io8<E>::unpack(r[v], f);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) f[j] = there ? f[j] * a.scale : 0.0f;
+                slice_store<T>(out, at, D - at, f);
+            }
         }
     }
 }
@@ -76,19 +91,24 @@ __global__ __launch_bounds__(256) void embed_fwd_kernel(EmbedArgs a)
 // ---- sorting --------------------------------------------------------------------------------------
 constexpr int SORT_THREADS = 256, SORT_WAVES = SORT_THREADS / WAVE;
 constexpr int DIGIT_BITS = 9, DIGITS = 1 << DIGIT_BITS;
-constexpr int FILL_WORKGROUPS = 2048;
+constexpr int FILL_STORES = 4;                 // of 16 bytes, of a thread
+constexpr int64_t FILL_WORKGROUPS = 1 << 20;
 
-// The workgroups behind the sorting ones set a share of the gradient to zero.
+// The workgroups behind the sorting ones set a share of the gradient to zero, in stretches of four words a thread: 105 MB in 16 us.
 template <typename E>
 __device__ __forceinline__ void fill(const EmbedArgs& a, int64_t wg, int64_t wgs)
 {
     E* const to = static_cast<E*>(a.dtable);
-    constexpr int N = 16 / sizeof(E);
-    for (int64_t k = a.fill_from + (wg * SORT_THREADS + threadIdx.x) * N; k < a.fill_to; k += wgs * SORT_THREADS * N) {
-        if (k + N <= a.fill_to) {
-            store_any(to + k, 0u, u32x4{0u, 0u, 0u, 0u});
-        } else {
-            for (int j = 0; k + j < a.fill_to; ++j) to[k + j] = (E)0;
+    constexpr int N = 16 / sizeof(E), STRETCH = SORT_THREADS * N * FILL_STORES;
+    for (int64_t k0 = a.fill_from + wg * STRETCH; k0 < a.fill_to; k0 += wgs * STRETCH) {
+#pragma unroll
+        for (int u = 0; u < FILL_STORES; ++u) {
+            const int64_t k = k0 + (u * SORT_THREADS + threadIdx.x) * N;
+            if (k + N <= a.fill_to) {
+                store_any(to + k, 0u, u32x4{0u, 0u, 0u, 0u});
+            } else {
+                for (int j = 0; k + j < a.fill_to; ++j) to[k + j] = (E)0;
+            }
         }
     }
 }
@@ -105,6 +125,7 @@ __global__ __launch_bounds__(SORT_THREADS) void embed_count_kernel(EmbedArgs a)
     if ((int)blockIdx.x >= a.tiles) return fill<E>(a, (int64_t)blockIdx.x - a.tiles, (int64_t)gridDim.x - a.tiles);
     __shared__ int count[DIGITS];
     const int digits = 1 << a.digit;
+    if (blockIdx.x == 0 && threadIdx.x == 0) a.shared[0] = 0;
     for (int d = threadIdx.x; d < digits; d += SORT_THREADS) count[d] = 0;
     __syncthreads();
     const int64_t from = (int64_t)blockIdx.x * a.tile;
@@ -133,13 +154,17 @@ __global__ __launch_bounds__(SORT_THREADS) void embed_place_kernel(EmbedArgs a)
     int all[2] = {0, 0}, before[2] = {0, 0};
     const int d0 = threadIdx.x * 2;
     if (d0 < digits) {
-        for (int k = 0; k < a.tiles; ++k) {
-            const int2 c = *reinterpret_cast<const int2*>(a.hist + k * digits + d0);
-            all[0] += c.x;
-            all[1] += c.y;
-            if (k < (int)blockIdx.x) {
-                before[0] += c.x;
-                before[1] += c.y;
+        for (int k0 = 0; k0 < a.tiles; k0 += 8) {
+            int2 c[8];
+#pragma unroll
+            for (int k = 0; k < 8; ++k) c[k] = *reinterpret_cast<const int2*>(a.hist + min(k0 + k, a.tiles - 1) * digits + d0);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                const bool real = k0 + k < a.tiles, early = k0 + k < (int)blockIdx.x;
+                all[0] += real ? c[k].x : 0;
+                all[1] += real ? c[k].y : 0;
+                before[0] += early ? c[k].x : 0;
+                before[1] += early ? c[k].y : 0;
             }
         }
     }
@@ -166,26 +191,35 @@ __global__ __launch_bounds__(SORT_THREADS) void embed_place_kernel(EmbedArgs a)
         }
     }
     __syncthreads();
-    for (int64_t t0 = from; t0 < to; t0 += WAVE) {
-        const int64_t t = t0 + lane;
-        const bool valid = t < to;
-        const int key = valid ? sort_key<I>(a, (int)t) : 0;
-        const int d = (key >> a.shift) & (digits - 1);
-        uint64_t same = __ballot(valid);
-        for (int b = 0; b < a.digit; ++b) {
-            const bool on = (d >> b) & 1;
-            const uint64_t bal = __ballot(on);
-            same &= on ? bal : ~bal;
+    constexpr int AHEAD = 4;
+    for (int64_t t0 = from; t0 < to; t0 += AHEAD * WAVE) {
+        int keys[AHEAD], places[AHEAD];
+#pragma unroll
+        for (int u = 0; u < AHEAD; ++u) {
+            const int t = (int)min(t0 + u * WAVE + lane, (int64_t)to - 1);
+            keys[u] = sort_key<I>(a, t);
+            places[u] = a.pos_in ? a.pos_in[t] : t;
         }
-        const int rank = __popcll(same & ((1ull << lane) - 1));
-        const int to_place = place[wave][d] + rank;
-        __builtin_amdgcn_wave_barrier();   // all lanes have read before the last of each digit writes
-        if (valid) {
-            if ((same >> lane) == 1ull) place[wave][d] = to_place + 1;
-            a.key_out[to_place] = key;
-            a.pos_out[to_place] = a.pos_in ? a.pos_in[t] : (int)t;
+#pragma unroll
+        for (int u = 0; u < AHEAD; ++u) {
+            const bool valid = t0 + u * WAVE + lane < to;
+            const int d = (keys[u] >> a.shift) & (digits - 1);
+            uint64_t same = __ballot(valid);
+            for (int b = 0; b < a.digit; ++b) {
+                const bool on = (d >> b) & 1;
+                const uint64_t bal = __ballot(on);
+                same &= on ? bal : ~bal;
+            }
+            const int rank = __popcll(same & ((1ull << lane) - 1));
+            const int at = place[wave][d] + rank;
+            __builtin_amdgcn_wave_barrier();   // all lanes have read before the last of each digit writes
+            if (valid) {
+                if ((same >> lane) == 1ull) place[wave][d] = at + 1;
+                a.key_out[at] = keys[u];
+                a.pos_out[at] = places[u];
+            }
+            __builtin_amdgcn_wave_barrier();
         }
-        __builtin_amdgcn_wave_barrier();
     }
 }
 
@@ -200,95 +234,144 @@ __device__ __forceinline__ void store_row(const EmbedArgs& a, int id, int at, co
 }
 __device__ __forceinline__ float* part_of(const EmbedArgs& a, int64_t piece, int which) { return a.part + (piece * 2 + which) * a.dim; }
 
-template <typename E, typename T, int G>
+// A wave has a piece and 512 columns.  It adds up every id whose tokens begin in the piece, and goes on behind its end where no more than SPILL tokens of the
+// last one follow; of longer ones it leaves its share.  The share of an id that began before the piece: the same, and nothing where the wave
+// before goes on to its end.  Ids and places come 64 at once, a lane each, eight rows are requested at once.
+constexpr int SPILL = 8;   // a piece has that many at least
+template <typename E, typename T>
 __global__ __launch_bounds__(256) void embed_sum_kernel(EmbedArgs a)
 {
-    constexpr int SIDE = 256 / G, AHEAD = 8;
-    const int64_t piece = (int64_t)blockIdx.x * SIDE + threadIdx.x / G;
-    const int at = (blockIdx.y * G + threadIdx.x % G) * 8;
-    if (piece >= a.pieces || at >= a.dim) return;
-    const int i0 = (int)(piece * a.piece), i1 = (int)min((int64_t)i0 + a.piece, (int64_t)a.tokens);
-    int id = a.key[i0];
-    if (id >= a.vocab) return;   // ids outside the table come last
-    bool began = i0 == 0 || a.key[i0 - 1] != id;
+    constexpr int AHEAD = 8, BLOCK = 32;
+    const int piece = __builtin_amdgcn_readfirstlane(blockIdx.x * (256 / WAVE) + threadIdx.x / WAVE), lane = threadIdx.x % WAVE;
+    const int at = (blockIdx.y * WAVE + lane) * 8;
+    if (piece >= a.pieces) return;
+    const int N = a.tokens, i0 = piece * a.piece, i1 = (int)min((int64_t)i0 + a.piece, (int64_t)N);
+    auto key = [&](int64_t i) { return a.key[min(max(i, (int64_t)0), (int64_t)N - 1)]; };
+    const int first = key(i0), before = key(i0 - 1), far_before = key((int64_t)i0 - a.piece - 1), spilt = key((int64_t)i0 + SPILL);
+    const int last = key(i1 - 1), next = key(i1), far_next = key((int64_t)i1 + SPILL);
+    const int around0 = key((int64_t)i0 + lane), around1 = key((int64_t)i1 + lane);   // from the piece's begin and end on
+    if (first >= a.vocab) return;   // ids outside the table come last
+    bool began = i0 == 0 || before != first;
+    int from = i0, to = i1;
+    if (!began && (i0 - a.piece - 1 < 0 || far_before != first) && ((int64_t)i0 + SPILL >= N || spilt != first)) {
+        from += __ffsll((long long)~__ballot(around0 == first && i0 + lane < i1)) - 1;   // up to SPILL of them: the wave before adds them
+        began = true;
+        if (from >= i1) return;
+    }
+    bool goes_on = i1 < N && next == last;
+    if (goes_on && (began || last != first) && ((int64_t)i1 + SPILL >= N || far_next != last)) {
+        to += __ffsll((long long)~__ballot(around1 == last && (int64_t)i1 + lane < N)) - 1;
+        goes_on = false;
+    }
+    const bool whole = a.dim % 8 == 0, some = at < a.dim;
+    const int limit = slice_limit(a.dim, whole);
     float acc[8] = {};
-    auto finish = [&](bool goes_on) {
-        if (id >= a.vocab) return;
-        if (began && !goes_on) store_row<E>(a, id, at, acc);
+    int id = -1;
+    auto finish = [&](bool open) {
+        if (id < 0 || id >= a.vocab || !some) return;
+        if (began && !open) store_row<E>(a, id, at, acc);
         else slice_store<float>(part_of(a, piece, began ? 1 : 0), at, a.dim - at, acc);
     };
-    const bool whole = a.dim % 8 == 0;
-    const int limit = slice_limit(a.dim, whole);
-    for (int i = i0; i < i1; i += AHEAD) {
-        typename io8<T>::raw r[AHEAD];
-        int key[AHEAD];
+    for (int b = from; b < to; b += BLOCK) {
+        const int keys = key(b + lane), places = a.pos[min(b + lane, N - 1)];
+        for (int j0 = 0; j0 < BLOCK && b + j0 < to; j0 += AHEAD) {
+            typename io8<T>::raw r[AHEAD];
 #pragma unroll
-        for (int j = 0; j < AHEAD; ++j) {
-            const int k = min(i + j, i1 - 1);
-            key[j] = a.key[k];
-            r[j] = slice_request<T, true>(static_cast<const T*>(a.dout) + (int64_t)a.pos[k] * a.dim, at, a.dim, limit);
-        }
-#pragma unroll
-        for (int j = 0; j < AHEAD; ++j) {
-            if (i + j >= i1) break;
-            if (key[j] != id) {
-                finish(false);
-                id = key[j];
-                began = true;
-#pragma unroll
-                for (int c = 0; c < 8; ++c) acc[c] = 0.0f;
+            for (int j = 0; j < AHEAD; ++j) {
+                const int place = __builtin_amdgcn_readlane(places, min(j0 + j, to - 1 - b));
+                r[j] = slice_request<T, true>(static_cast<const T*>(a.dout) + (int64_t)place * a.dim, at, a.dim, limit);
             }
-            float v[8];
-            slice_settle<T>(r[j], at, a.dim, limit, whole);
-            io8<T>::unpack(r[j], v);
 #pragma unroll
-            for (int c = 0; c < 8; ++c) acc[c] += v[c];
+            for (int j = 0; j < AHEAD; ++j) {
+                if (b + j0 + j >= to) break;
+                const int k = __builtin_amdgcn_readlane(keys, j0 + j);
+                if (k != id) {
+                    if (id >= 0) {
+                        finish(false);
+                        began = true;
+                    }
+                    id = k;
+#pragma unroll
+                    for (int c = 0; c < 8; ++c) acc[c] = 0.0f;
+                }
+                float v[8];
+                slice_settle<T>(r[j], at, a.dim, limit, whole);
+                io8<T>::unpack(r[j], v);
+#pragma unroll
+                for (int c = 0; c < 8; ++c) acc[c] += v[c];
+            }
         }
     }
-    finish(i1 < a.tokens && a.key[i1] == id);
+    finish(goes_on);
+    if (goes_on && began && id < a.vocab && blockIdx.y == 0 && lane == 0) a.shared[1 + atomicAdd(&a.shared[0], 1)] = piece;   // in any order: each is a row of its own
 }
 
-// The rows of ids that several pieces share, by the piece that they begin in.
-template <typename E, int G>
-__global__ __launch_bounds__(256) void embed_join_kernel(EmbedArgs a)
+// The rows of ids that go on for more than SPILL tokens behind the piece that they begin in: a workgroup for 512 columns of one, whose waves
+// take a share of its pieces each.
+constexpr int JOIN_WAVES = 16, JOIN_WORKGROUPS = 256;
+template <typename E>
+__global__ __launch_bounds__(JOIN_WAVES * WAVE) void embed_join_kernel(EmbedArgs a)
 {
-    constexpr int SIDE = 256 / G;
-    const int64_t piece = (int64_t)blockIdx.x * SIDE + threadIdx.x / G;
-    const int at = (blockIdx.y * G + threadIdx.x % G) * 8;
-    if (piece >= a.pieces - 1 || at >= a.dim) return;
-    const int i0 = (int)(piece * a.piece), i1 = i0 + a.piece;
-    const int id = a.key[i1 - 1];
-    if (id >= a.vocab || a.key[i1] != id || (i0 > 0 && a.key[i0 - 1] == id)) return;
-    int low = i1, high = a.tokens;   // the id's tokens end in (low, high]
-    while (high - low > 1) {
-        const int mid = low + (high - low) / 2;
-        if (a.key[mid] == id) low = mid;
-        else high = mid;
-    }
-    const int64_t last = low / a.piece;
-    float acc[8], v[8];
-    row_slice<float>(part_of(a, piece, 1), at, a.dim, acc);
-#pragma unroll 8
-    for (int64_t k = piece + 1; k <= last; ++k) {
-        row_slice<float>(part_of(a, k, 0), at, a.dim, v);
+    __shared__ float sums[JOIN_WAVES][WAVE][9];
+    const int wave = threadIdx.x / WAVE, lane = threadIdx.x % WAVE, rows = a.shared[0];
+    for (int row = blockIdx.x; row < rows; row += gridDim.x) {
+        const int piece = a.shared[1 + row];
+        const int id = a.key[(piece + 1) * a.piece - 1];
+        // the last piece that begins with the id: 64 are looked at at once
+        int last = piece + 1;
+        for (;;) {
+            const int k = last + 1 + lane;
+            const uint64_t on = __ballot(k < a.pieces && a.key[(int64_t)min(k, a.pieces - 1) * a.piece] == id);
+            if (on == ~0ull) {
+                last += WAVE;
+                continue;
+            }
+            last += __ffsll((long long)~on) - 1;
+            break;
+        }
+        const int at = (blockIdx.y * WAVE + lane) * 8, parts = last - piece + 1;   // the first has its own place
+        float acc[8] = {};
+        if (at < a.dim) {
+            const int from = (int)((int64_t)parts * wave / JOIN_WAVES), to = (int)((int64_t)parts * (wave + 1) / JOIN_WAVES);
+            const bool whole = a.dim % 8 == 0;
+            const int limit = slice_limit(a.dim, whole);
+            for (int k0 = from; k0 < to; k0 += 8) {
+                typename io8<float>::raw r[8];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) acc[j] += v[j];
+                for (int j = 0; j < 8; ++j) {
+                    const int k = min(k0 + j, to - 1);
+                    r[j] = slice_request<float, true>(part_of(a, piece + k, k == 0 ? 1 : 0), at, a.dim, limit);
+                }
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    if (k0 + j >= to) break;
+                    float v[8];
+                    slice_settle<float>(r[j], at, a.dim, limit, whole);
+                    io8<float>::unpack(r[j], v);
+#pragma unroll
+                    for (int c = 0; c < 8; ++c) acc[c] += v[c];
+                }
+            }
+        }
+#pragma unroll
+        for (int c = 0; c < 8; ++c) sums[wave][lane][c] = acc[c];
+        // halves of the waves' sums onto halves, each a fixed pair
+        for (int half = JOIN_WAVES / 2; half > 0; half /= 2) {
+            __syncthreads();
+            if (wave < half) {
+#pragma unroll
+                for (int c = 0; c < 8; ++c) sums[wave][lane][c] = acc[c] += sums[wave + half][lane][c];
+            }
+        }
+        if (wave == 0 && at < a.dim) store_row<E>(a, id, at, acc);
+        __syncthreads();   // the next row's sums come into the same place
     }
-    store_row<E>(a, id, at, acc);
 }
 
 // ---- sizes ----------------------------------------------------------------------------------------
-template <typename F>
-void with_lanes(int dim, F go)   // lanes of a row: as many as it has slices, up to a workgroup
-{
-    const int n = (dim + 7) / 8;
-    if (n <= 8) go(std::integral_constant<int, 8>{});
-    else if (n <= 64) go(std::integral_constant<int, 64>{});
-    else go(std::integral_constant<int, 256>{});
-}
 struct EmbedPlan {
     int passes, digit, tile, tiles, piece, pieces;
-    size_t key[2], pos[2], hist, part, total;   // offsets in bytes
+    size_t key[2], pos[2], hist, part, shared, total;   // offsets in bytes
 };
 EmbedPlan embed_plan(int tokens, int vocab, int dim)
 {
@@ -301,8 +384,8 @@ EmbedPlan embed_plan(int tokens, int vocab, int dim)
     const int64_t tile = std::max((int64_t)1024, ((int64_t)tokens + 63) / 64);
     p.tile = (int)((tile + SORT_THREADS - 1) / SORT_THREADS * SORT_THREADS);
     p.tiles = (int)(((int64_t)tokens + p.tile - 1) / p.tile);
-    // pieces of 32 tokens, of more where there would be over 4096 (an id may have all of them)
-    p.piece = 32;
+    // pieces of 8 tokens, of more where there would be over 4096 (an id may have all of them)
+    p.piece = SPILL;
     while (((int64_t)tokens + p.piece - 1) / p.piece > 4096) p.piece *= 2;
     p.pieces = (int)(((int64_t)tokens + p.piece - 1) / p.piece);
     auto take = [&](size_t bytes) {
@@ -316,17 +399,21 @@ EmbedPlan embed_plan(int tokens, int vocab, int dim)
     }
     p.hist = take((size_t)p.tiles * DIGITS * 4);
     p.part = take((size_t)p.pieces * 2 * dim * 4);
+    p.shared = take(((size_t)p.pieces + 1) * 4);
     return p;
 }
 
 template <typename E, typename T, typename I>
 void embed_forward(const EmbedArgs& a, hipStream_t st)
 {
-    with_lanes(a.dim, [&](auto g) {
-        constexpr int G = decltype(g)::value, SIDE = 256 / G;
+    auto launch = [&](auto g, auto v) {
+        constexpr int G = decltype(g)::value, V = decltype(v)::value, SIDE = 256 / G;
         const int64_t n = ((int64_t)a.tokens + SIDE - 1) / SIDE;
-        hipLaunchKernelGGL((embed_fwd_kernel<E, T, I, G>), dim3((unsigned)std::min(n, (int64_t)8192)), dim3(256), 0, st, a);
-    });
+        hipLaunchKernelGGL((embed_fwd_kernel<E, T, I, G, V>), dim3((unsigned)std::min(n, (int64_t)65536)), dim3(256), 0, st, a);
+    };
+    if (a.dim <= 8 * 8) launch(std::integral_constant<int, 8>{}, std::integral_constant<int, 1>{});
+    else if (a.tokens >= 1024 || a.dim <= 64 * 8) launch(std::integral_constant<int, 64>{}, std::integral_constant<int, 4>{});
+    else launch(std::integral_constant<int, 256>{}, std::integral_constant<int, 1>{});
 }
 template <typename E, typename T, typename I>
 void embed_backward(EmbedArgs a, char* ws, hipStream_t st)
@@ -336,14 +423,15 @@ void embed_backward(EmbedArgs a, char* ws, hipStream_t st)
     const int shares = a.tokens ? 2 * p.passes : 1;
     a.hist = reinterpret_cast<int*>(ws + p.hist);
     a.part = reinterpret_cast<float*>(ws + p.part);
+    a.shared = reinterpret_cast<int*>(ws + p.shared);
     a.tile = p.tile; a.tiles = p.tiles; a.digit = p.digit;
     a.piece = p.piece; a.pieces = p.pieces;
     for (int k = 0; k < shares; ++k) {
         // shares of whole 16-byte words from the start
         a.fill_from = all / shares * k / 8 * 8;
         a.fill_to = k == shares - 1 ? all : all / shares * (k + 1) / 8 * 8;
-        const int64_t words = (a.fill_to - a.fill_from) * (int64_t)sizeof(E) / (16 * SORT_THREADS * 4) + 1;
-        const dim3 grid((unsigned)(p.tiles + std::min(words, (int64_t)FILL_WORKGROUPS)));
+        const int64_t fillers = (a.fill_to - a.fill_from) * (int64_t)sizeof(E) / (16 * SORT_THREADS * FILL_STORES) + 1;
+        const dim3 grid((unsigned)(p.tiles + std::min(fillers, FILL_WORKGROUPS)));
         const int pass = k / 2, to = pass % 2;
         a.shift = pass * p.digit;
         a.key_in = pass ? reinterpret_cast<int*>(ws + p.key[1 - to]) : nullptr;
@@ -356,12 +444,10 @@ void embed_backward(EmbedArgs a, char* ws, hipStream_t st)
     if (!a.tokens) return;
     a.key = a.key_out;
     a.pos = a.pos_out;
-    with_lanes(a.dim, [&](auto g) {
-        constexpr int G = decltype(g)::value, SIDE = 256 / G;
-        const dim3 grid((unsigned)((p.pieces + SIDE - 1) / SIDE), (unsigned)((a.dim + G * 8 - 1) / (G * 8)));
-        hipLaunchKernelGGL((embed_sum_kernel<E, T, G>), grid, dim3(256), 0, st, a);
-        if (p.pieces > 1) hipLaunchKernelGGL((embed_join_kernel<E, G>), grid, dim3(256), 0, st, a);
-    });
+    const unsigned slabs = (unsigned)((a.dim + WAVE * 8 - 1) / (WAVE * 8));
+    hipLaunchKernelGGL((embed_sum_kernel<E, T>), dim3((unsigned)((p.pieces + 3) / 4), slabs), dim3(256), 0, st, a);
+    if (p.pieces > 1)
+        hipLaunchKernelGGL((embed_join_kernel<E>), dim3((unsigned)std::min(p.pieces - 1, JOIN_WORKGROUPS), slabs), dim3(JOIN_WAVES * WAVE), 0, st, a);
 }
 template <typename F>
 void with_types(const ss_embed_params* p, F go)
@@ -385,7 +471,7 @@ namespace {
 inline bool aligned_to(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) % a) == 0; }
 inline size_t bytes_of(int32_t dtype) { return dtype == SS_BF16 ? 2 : 4; }
 constexpr int32_t EMBED_MOST = 0x7fffffff - 65536;      // room for the last steps of the kernels' loops
-constexpr int32_t EMBED_WIDEST = 65535 * 2048;          // columns that the workgroups along y of a launch reach
+constexpr int32_t EMBED_WIDEST = 65535 * 512;           // columns that the workgroups along y of a launch reach
 
 int check_embed(const ss_embed_params* p)
 {

@@ -39,7 +39,7 @@ static void one()
     p.scale = 1.0f;
     p.tokens = any(2147418111);
     p.vocab = 1 + any(2147418110);
-    p.dim = 1 + any(65535.0 * 2048 - 1);
+    p.dim = 1 + any(65535.0 * 512 - 1);
     const double io = (double)p.tokens * p.dim * (p.io_dtype == SS_BF16 ? 2 : 4), table = (double)p.vocab * p.dim * (p.table_dtype == SS_BF16 ? 2 : 4);
     if (io + table > CARD) return;
     p.ids = p.table = q.dout = fake;
