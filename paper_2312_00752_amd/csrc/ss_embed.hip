@@ -105,7 +105,7 @@ __device__ __forceinline__ void fill(const EmbedArgs& a, int64_t wg, int64_t wgs
         for (int u = 0; u < FILL_STORES; ++u) {
             const int64_t k = k0 + (u * SORT_THREADS + threadIdx.x) * N;
             if (k + N <= a.fill_to) {
-                store_any(to + k, 0u, u32x4{0u, 0u, 0u, 0u});
+                __builtin_nontemporal_store(u32x4{0u, 0u, 0u, 0u}, reinterpret_cast<typename elem_aligned<u32x4, (int)sizeof(E)>::type*>(to + k));
             } else {
                 for (int j = 0; k + j < a.fill_to; ++j) to[k + j] = (E)0;
             }
@@ -412,8 +412,10 @@ void embed_forward(const EmbedArgs& a, hipStream_t st)
         hipLaunchKernelGGL((embed_fwd_kernel<E, T, I, G, V>), dim3((unsigned)std::min(n, (int64_t)65536)), dim3(256), 0, st, a);
     };
     if (a.dim <= 8 * 8) launch(std::integral_constant<int, 8>{}, std::integral_constant<int, 1>{});
-    else if (a.tokens >= 1024 || a.dim <= 64 * 8) launch(std::integral_constant<int, 64>{}, std::integral_constant<int, 4>{});
-    else launch(std::integral_constant<int, 256>{}, std::integral_constant<int, 1>{});
+    else if (a.dim <= 64 * 8) launch(std::integral_constant<int, 64>{}, std::integral_constant<int, 1>{});
+    else if (a.dim <= 128 * 8) launch(std::integral_constant<int, 128>{}, std::integral_constant<int, 1>{});
+    else if (a.tokens < 8192) launch(std::integral_constant<int, 256>{}, std::integral_constant<int, 1>{});
+    else launch(std::integral_constant<int, 64>{}, std::integral_constant<int, 4>{});
 }
 template <typename E, typename T, typename I>
 void embed_backward(EmbedArgs a, char* ws, hipStream_t st)
