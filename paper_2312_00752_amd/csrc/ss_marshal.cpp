@@ -1183,14 +1183,15 @@ int64_t row_stride(const at::Tensor& t)
     const int64_t width = t.size(-1);
     if (t.is_contiguous()) return width;
     if (t.stride(-1) != 1 && width != 1) return 0;
-    int64_t stride = 0, at = 0;
+    int64_t stride = width, at = 0;
+    bool first = true;
     for (int64_t k = t.dim() - 1; k-- > 0;) {
         if (t.size(k) == 1) continue;
-        if (stride == 0) stride = t.stride(k);
+        if (first) stride = t.stride(k);
         else if (t.stride(k) != at) return 0;
+        first = false;
         at = t.stride(k) * t.size(k);
     }
-    if (stride == 0) stride = width;
     return stride < width ? 0 : stride;
 }
 struct Logprob {
