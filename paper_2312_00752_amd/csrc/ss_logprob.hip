@@ -195,30 +195,13 @@ __global__ __launch_bounds__(256) void logprob_fwd_kernel(LogprobArgs a)
     const int row = (int)(group / (unsigned)a.pieces), piece = (int)(group % (unsigned)a.pieces);
     if (row >= a.rows) return;   // a whole wave
     const T* x = static_cast<const T*>(a.logits) + row * a.row_stride;
+    constexpr int STEP = V * G * 8;
+    constexpr bool TINY = G == WAVE;   // rows of less than 8
     const int W = a.vocab, from = piece * a.piece, to = min(from + a.piece, W);
-    const bool whole = W % 8 == 0;
-    const int limit = slice_limit(W, whole);
-    typename io8<T>::raw raw[V];
-    auto load = [&](int base) {
-#pragma unroll
-        for (int v = 0; v < V; ++v) raw[v] = slice_request<T, true>(x, base + (v * G + gl) * 8, W, limit);
-    };
     Stat t = {-INFINITY, 0.0f, 0.0f};
     Best best;
-    load(from);
-    for (int base = from; base < to; base += V * G * 8) {
-        float f[V][8];
-#pragma unroll
-        for (int v = 0; v < V; ++v) {
-            const int at = base + (v * G + gl) * 8, n = to - at;
-            slice_settle<T>(raw[v], at, W, limit, whole);
-            io8<T>::unpack(raw[v], f[v]);
-            if (n < 8) {
-#pragma unroll
-                for (int j = 0; j < 8; ++j) f[v][j] = j < n ? f[v][j] : -INFINITY;
-            }
-        }
-        if (base + V * G * 8 < to) load(base + V * G * 8);
+    // V slices of eight columns; those behind the piece are -infinity, and no candidates
+    auto take = [&](const float (&f)[V][8], int base) {
         float m = t.m;
 #pragma unroll
         for (int v = 0; v < V; ++v)
@@ -242,6 +225,40 @@ __global__ __launch_bounds__(256) void logprob_fwd_kernel(LogprobArgs a)
                 return k < to && all[j] == all[j] ? k : -1;
             }, a.top);
         }
+    };
+    // whole steps, whose loads need no bounds and are requested a step ahead
+    int base = from;
+    if (base + STEP <= to) {
+        typename io8<T>::raw raw[V];
+        auto load = [&](int at) {
+#pragma unroll
+            for (int v = 0; v < V; ++v) raw[v] = io8<T>::load_elem(x + at + (v * G + gl) * 8, 0u);
+        };
+        load(base);
+        for (; base + STEP <= to; base += STEP) {
+            float f[V][8];
+#pragma unroll
+            for (int v = 0; v < V; ++v) io8<T>::unpack(raw[v], f[v]);
+            load(min(base + STEP, to - STEP));
+            take(f, base);
+        }
+    }
+    if (base < to) {
+        const bool whole = W % 8 == 0;
+        const int limit = slice_limit(W, whole);
+        typename io8<T>::raw raw[V];
+        float f[V][8];
+#pragma unroll
+        for (int v = 0; v < V; ++v) raw[v] = slice_request<T, TINY>(x, base + (v * G + gl) * 8, W, limit);
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            const int at = base + (v * G + gl) * 8, n = to - at;
+            slice_settle<T>(raw[v], at, W, limit, whole);
+            io8<T>::unpack(raw[v], f[v]);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) f[v][j] = j < n ? f[v][j] : -INFINITY;
+        }
+        take(f, base);
     }
     t = join_wave(t);
     if constexpr (WAVES > 1) {
@@ -321,8 +338,9 @@ __global__ __launch_bounds__(256) void logprob_bwd_kernel(LogprobArgs a)
     constexpr int V = 4, SIDE = 256 / G;
     const int gl = threadIdx.x % G;
     const unsigned group = blockIdx.x * SIDE + threadIdx.x / G;
-    const int row = (int)(group / (unsigned)a.pieces), from = (int)(group % (unsigned)a.pieces) * a.piece;
-    if (row >= a.rows) return;
+    // the last rows first: the forward pass, which has read them last, may have left them in a cache
+    const int row = a.rows - 1 - (int)(group / (unsigned)a.pieces), from = (int)(group % (unsigned)a.pieces) * a.piece;
+    if (row < 0) return;
     const int W = a.vocab, k = target_of<I>(a, row);
     const float inv = a.inv[row];
     const bool some = inv != 0.0f;   // also where it is NaN
@@ -338,26 +356,49 @@ __global__ __launch_bounds__(256) void logprob_bwd_kernel(LogprobArgs a)
         return;
     }
     const T* x = static_cast<const T*>(a.logits) + row * a.row_stride;
-    const bool whole = W % 8 == 0;
-    const int limit = slice_limit(W, whole);
-    typename io8<T>::raw raw[V];
-#pragma unroll
-    for (int v = 0; v < V; ++v) raw[v] = slice_request<T, true>(x, from + (v * G + gl) * 8, W, limit);
     const float m = a.max[row], ls = logf(inv);
     // dx = -p (dl + dh (log p + H)) = -p (c0 + dh d), d = x - m
-    const float c0 = dh == 0.0f ? dl : fmaf(dh, ls + a.entropy[row], dl);
+    const float c0 = dh == 0.0f ? dl : fmaf(dh, ls + a.entropy[row], dl), c1 = -c0 * inv;
+    auto gradient = [&](float (&f)[8], int at) {
+        if (dh == 0.0f) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) f[j] = exp_of(f[j] - m) * c1;
+        } else {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const float d = f[j] - m;
+                f[j] = -(exp_of(d) * inv) * fmaf(dh, fmaxf(d, FAR), c0);
+            }
+        }
+        if ((unsigned)(k - at) < 8u) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) f[j] += at + j == k ? dl : 0.0f;
+        }
+    };
+    typename io8<T>::raw raw[V];
+    float f[8];
+    if (from + V * G * 8 <= W) {   // loads and stores need no bounds
+#pragma unroll
+        for (int v = 0; v < V; ++v) raw[v] = io8<T>::load_elem(x + from + (v * G + gl) * 8, 0u);
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            const int at = from + (v * G + gl) * 8;
+            io8<T>::unpack(raw[v], f);
+            gradient(f, at);
+            io8<T>::store_elem(out + at, 0u, io8<T>::pack(f), 8);
+        }
+        return;
+    }
+    const bool whole = W % 8 == 0;
+    const int limit = slice_limit(W, whole);
+#pragma unroll
+    for (int v = 0; v < V; ++v) raw[v] = slice_request<T, G == WAVE>(x, from + (v * G + gl) * 8, W, limit);
 #pragma unroll
     for (int v = 0; v < V; ++v) {
         const int at = from + (v * G + gl) * 8;
-        float f[8];
         slice_settle<T>(raw[v], at, W, limit, whole);
         io8<T>::unpack(raw[v], f);
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            const float d = f[j] - m, p = exp_of(d) * inv;
-            f[j] = -p * fmaf(dh, fmaxf(d, FAR), c0);
-            if (at + j == k) f[j] += dl;
-        }
+        gradient(f, at);
         slice_store<T>(out, at, W - at, f);
     }
 }
