@@ -16,6 +16,8 @@
  * same order, -1 where there are no more).  Without a target (t outside) dlogp is not read into the row's gradient; a row whose dlogp is 0 or not
  * asked for, and whose dentropy is 0 or not given, has the gradient 0 whatever it holds.
  *
+ * What is asked for beside them does not change the bits of logp, entropy and stats.
+ *
  * Rules as in ss_scan.h (device pointers owned by the caller, outputs overwritten, host-side validation before any device
  * call, SS_OK or a negative SS_ERR_* code, nothing allocated), but pointers need be aligned to their element only.  Sums
  * are float32 whatever io_dtype is.  rows == 0 is valid.  SS_ERR_UNSUPPORTED: rows ceil(vocab / 8192) of 2^24 and more (of 2^26 up to

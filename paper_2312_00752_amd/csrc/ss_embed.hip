@@ -94,8 +94,8 @@ constexpr int DIGIT_BITS = 9, DIGITS = 1 << DIGIT_BITS;
 constexpr int FILL_STORES = 4;                 // of 16 bytes, of a thread
 constexpr int64_t FILL_WORKGROUPS = 1 << 20;
 
-// The workgroups behind the sorting ones set a share of the gradient to zero, in stretches of four words a thread: 105 MB in 16 us.
-template <typename E>
+// The workgroups behind the sorting ones set a share of the gradient to zero, in stretches of four words a thread: 105 MB in 16 us.  PAST: past the caches.
+template <typename E, bool PAST>
 __device__ __forceinline__ void fill(const EmbedArgs& a, int64_t wg, int64_t wgs)
 {
     E* const to = static_cast<E*>(a.dtable);
@@ -105,7 +105,8 @@ __device__ __forceinline__ void fill(const EmbedArgs& a, int64_t wg, int64_t wgs
         for (int u = 0; u < FILL_STORES; ++u) {
             const int64_t k = k0 + (u * SORT_THREADS + threadIdx.x) * N;
             if (k + N <= a.fill_to) {
-                __builtin_nontemporal_store(u32x4{0u, 0u, 0u, 0u}, reinterpret_cast<typename elem_aligned<u32x4, (int)sizeof(E)>::type*>(to + k));
+                if constexpr (PAST) store_past(to + k, u32x4{0u, 0u, 0u, 0u});
+                else store_any(to + k, 0u, u32x4{0u, 0u, 0u, 0u});
             } else {
                 for (int j = 0; k + j < a.fill_to; ++j) to[k + j] = (E)0;
             }
@@ -119,10 +120,10 @@ __device__ __forceinline__ int sort_key(const EmbedArgs& a, int t)
 }
 
 // How many tokens of each tile have each digit.
-template <typename E, typename I>
+template <typename E, typename I, bool PAST>
 __global__ __launch_bounds__(SORT_THREADS) void embed_count_kernel(EmbedArgs a)
 {
-    if ((int)blockIdx.x >= a.tiles) return fill<E>(a, (int64_t)blockIdx.x - a.tiles, (int64_t)gridDim.x - a.tiles);
+    if ((int)blockIdx.x >= a.tiles) return fill<E, PAST>(a, (int64_t)blockIdx.x - a.tiles, (int64_t)gridDim.x - a.tiles);
     __shared__ int count[DIGITS];
     const int digits = 1 << a.digit;
     if (blockIdx.x == 0 && threadIdx.x == 0) a.shared[0] = 0;
@@ -137,10 +138,10 @@ __global__ __launch_bounds__(SORT_THREADS) void embed_count_kernel(EmbedArgs a)
 
 // Every token to its place: behind all tokens with lower digits, those of earlier tiles, of earlier waves (each has a stretch of the tile) and of
 // earlier lanes with the same.  64 tokens a wave and step; those of a wave with the same digit are found by ballots of its bits.
-template <typename E, typename I>
+template <typename E, typename I, bool PAST>
 __global__ __launch_bounds__(SORT_THREADS) void embed_place_kernel(EmbedArgs a)
 {
-    if ((int)blockIdx.x >= a.tiles) return fill<E>(a, (int64_t)blockIdx.x - a.tiles, (int64_t)gridDim.x - a.tiles);
+    if ((int)blockIdx.x >= a.tiles) return fill<E, PAST>(a, (int64_t)blockIdx.x - a.tiles, (int64_t)gridDim.x - a.tiles);
     __shared__ int place[SORT_WAVES][DIGITS];   // counts, then the next free place of each wave's
     __shared__ int sums[SORT_WAVES];
     const int digits = 1 << a.digit, wave = threadIdx.x / WAVE, lane = threadIdx.x % WAVE;
@@ -417,6 +418,12 @@ void embed_forward(const EmbedArgs& a, hipStream_t st)
     else if (a.tokens < 8192) launch(std::integral_constant<int, 256>{}, std::integral_constant<int, 1>{});
     else launch(std::integral_constant<int, 64>{}, std::integral_constant<int, 4>{});
 }
+template <typename E, typename I, bool PAST>
+void embed_sort(const EmbedArgs& a, bool place, dim3 grid, hipStream_t st)
+{
+    if (place) hipLaunchKernelGGL((embed_place_kernel<E, I, PAST>), grid, dim3(SORT_THREADS), 0, st, a);
+    else hipLaunchKernelGGL((embed_count_kernel<E, I, PAST>), grid, dim3(SORT_THREADS), 0, st, a);
+}
 template <typename E, typename T, typename I>
 void embed_backward(EmbedArgs a, char* ws, hipStream_t st)
 {
@@ -440,8 +447,8 @@ void embed_backward(EmbedArgs a, char* ws, hipStream_t st)
         a.pos_in = pass ? reinterpret_cast<int*>(ws + p.pos[1 - to]) : nullptr;
         a.key_out = reinterpret_cast<int*>(ws + p.key[to]);
         a.pos_out = reinterpret_cast<int*>(ws + p.pos[to]);
-        if (k % 2 == 0) hipLaunchKernelGGL((embed_count_kernel<E, I>), grid, dim3(SORT_THREADS), 0, st, a);
-        else hipLaunchKernelGGL((embed_place_kernel<E, I>), grid, dim3(SORT_THREADS), 0, st, a);
+        if (all * (int64_t)sizeof(E) > STREAM_BYTES) embed_sort<E, I, true>(a, k % 2, grid, st);
+        else embed_sort<E, I, false>(a, k % 2, grid, st);
     }
     if (!a.tokens) return;
     a.key = a.key_out;

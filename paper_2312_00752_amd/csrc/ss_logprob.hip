@@ -25,7 +25,8 @@ struct LogprobArgs {
     float *logp, *entropy, *max, *inv, *top_logp;
     int64_t* top_ids;
     int pieces, piece;        // workgroups of a row, columns of each
-    float* part;              // (rows, pieces): m, S, U and the best
+    int parts;                // what the waves of a row's workgroups leave
+    float* part;              // (rows, parts): m, S, U and the best
     const float *dlogp, *dentropy;
     void* dlogits;
 };
@@ -159,18 +160,21 @@ __device__ __forceinline__ int target_of(const LogprobArgs& a, int row)   // -1:
     const I t = static_cast<const I*>(a.targets)[row];
     return t >= 0 && t < a.vocab ? (int)t : -1;
 }
-template <typename T, typename I, bool TOP>
-__device__ __forceinline__ void results(const LogprobArgs& a, int row, Stat t, const Best& best)
+// The target's logit, requested before the row is done: 0 where there is none.
+template <typename T, typename I>
+__device__ __forceinline__ float target_logit(const LogprobArgs& a, int row, int target)
+{
+    return target < 0 ? 0.0f : io_to_f32<T>(static_cast<const T*>(a.logits)[row * a.row_stride + target]);
+}
+template <bool TOP>
+__device__ __forceinline__ void results(const LogprobArgs& a, int row, Stat t, const Best& best, int target, float logit)
 {
     const int lane = threadIdx.x % WAVE;
     const bool none = t.s == 0.0f;   // the largest logit alone makes S one
     const float ls = logf(t.s);
     auto logp = [&](float x) { return none ? -INFINITY : (x - t.m) - ls; };
     if (lane == 0) {
-        if (a.logp) {
-            const int k = target_of<I>(a, row);
-            a.logp[row] = k < 0 ? 0.0f : logp(io_to_f32<T>(static_cast<const T*>(a.logits)[row * a.row_stride + k]));
-        }
+        if (a.logp) a.logp[row] = target < 0 ? 0.0f : logp(logit);
         a.entropy[row] = none ? 0.0f : ls - t.u / t.s;
         a.max[row] = none ? 0.0f : t.m;
         a.inv[row] = none ? 0.0f : 1.0f / t.s;
@@ -182,7 +186,7 @@ __device__ __forceinline__ void results(const LogprobArgs& a, int row, Stat t, c
         }
     }
 }
-// floats of a workgroup's share of a row: m, S, U, then `top` values and as many columns
+// floats of a part of a row: m, S, U, then `top` values and as many columns
 __host__ __device__ __forceinline__ int part_floats(int top) { return 4 + 2 * top; }
 
 // G lanes a row (a wave: rows side by side) or piece of one; V slices of eight a lane and step, the next step's requested ahead.
@@ -261,11 +265,27 @@ __global__ __launch_bounds__(256) void logprob_fwd_kernel(LogprobArgs a)
         take(f, base);
     }
     t = join_wave(t);
+    const int lane = threadIdx.x % WAVE;
+    auto leave = [&](int part) {
+        float* p = a.part + ((int64_t)row * a.parts + part) * part_floats(a.top);
+        if (lane == 0) {
+            p[0] = t.m;
+            p[1] = t.s;
+            p[2] = t.u;
+        }
+        if constexpr (TOP) {
+            if (lane < a.top) {
+                p[4 + lane] = best.v;
+                p[4 + a.top + lane] = __int_as_float(best.i);
+            }
+        }
+    };
     if constexpr (WAVES > 1) {
+        const int wave = threadIdx.x / WAVE;
+        if (a.pieces > 1) return leave(piece * WAVES + wave);
         __shared__ Stat stats[WAVES];
         __shared__ float values[WAVES][TOP ? WAVE : 1];
         __shared__ int columns[WAVES][TOP ? WAVE : 1];
-        const int wave = threadIdx.x / WAVE, lane = threadIdx.x % WAVE;
         if (lane == 0) stats[wave] = t;
         if constexpr (TOP) {
             values[wave][lane] = best.v;
@@ -280,59 +300,49 @@ __global__ __launch_bounds__(256) void logprob_fwd_kernel(LogprobArgs a)
             for (int w = 1; w < WAVES; ++w) f[w - 1] = values[w][lane];
             best.absorb(f, [&](int j) { return columns[j + 1][lane]; }, a.top);
         }
-        if (a.pieces > 1) {
-            float* p = a.part + (int64_t)group * part_floats(a.top);
-            if (lane == 0) {
-                p[0] = t.m;
-                p[1] = t.s;
-                p[2] = t.u;
-            }
-            if constexpr (TOP) {
-                if (lane < a.top) {
-                    p[4 + lane] = best.v;
-                    p[4 + a.top + lane] = __int_as_float(best.i);
-                }
-            }
-            return;
-        }
     }
-    results<T, I, TOP>(a, row, t, best);
+    const int target = target_of<I>(a, row);
+    results<TOP>(a, row, t, best, target, target_logit<T, I>(a, row, target));
 }
-// The pieces of a row, a wave a row.
+// The parts of a row, a wave a row.
 template <typename T, typename I, bool TOP>
 __global__ __launch_bounds__(64) void logprob_join_kernel(LogprobArgs a)
 {
     const int row = blockIdx.x, lane = threadIdx.x;
-    const float* p = a.part + (int64_t)row * a.pieces * part_floats(a.top);
+    const int target = target_of<I>(a, row);
+    const float* p = a.part + (int64_t)row * a.parts * part_floats(a.top);
     Stat t = {-INFINITY, 0.0f, 0.0f};
-    for (int k = lane; k < a.pieces; k += WAVE) {
+    for (int k = lane; k < a.parts; k += WAVE) {
         const float* q = p + (int64_t)k * part_floats(a.top);
         t = join(t, {q[0], q[1], q[2]});
     }
-    t = join_wave(t);
+    const float logit = target_logit<T, I>(a, row, target);
     Best best;
     if constexpr (TOP) {
         constexpr int N = 8;
-        const int all = a.pieces * a.top;
+        const int all = a.parts * a.top;
         for (int c0 = 0; c0 < all; c0 += N * WAVE) {
             float f[N];
             int k[N];
 #pragma unroll
             for (int j = 0; j < N; ++j) {
-                const int c = c0 + j * WAVE + lane;
-                const float* q = p + (int64_t)(min(c, all - 1) / a.top) * part_floats(a.top) + 4 + min(c, all - 1) % a.top;
+                const int c = min(c0 + j * WAVE + lane, all - 1);
+                const float* q = p + (int64_t)(c / a.top) * part_floats(a.top) + 4 + c % a.top;
                 f[j] = q[0];
-                k[j] = c < all ? __float_as_int(q[a.top]) : -1;
+                k[j] = __float_as_int(q[a.top]);
             }
+#pragma unroll
+            for (int j = 0; j < N; ++j)
+                if (c0 + j * WAVE + lane >= all) k[j] = -1;
             best.absorb(f, [&](int j) { return k[j]; }, a.top);
         }
     }
-    results<T, I, TOP>(a, row, t, best);
+    results<TOP>(a, row, join_wave(t), best, target, logit);
 }
 
 // ---- backward -------------------------------------------------------------------------------------
-// G lanes a row or piece of one, all of its slices requested at once.
-template <typename T, typename I, int G>
+// G lanes a row or piece of one, all of its slices requested at once.  PAST: the gradient goes past the caches.
+template <typename T, typename I, int G, bool PAST>
 __global__ __launch_bounds__(256) void logprob_bwd_kernel(LogprobArgs a)
 {
     constexpr int V = 4, SIDE = 256 / G;
@@ -385,7 +395,8 @@ __global__ __launch_bounds__(256) void logprob_bwd_kernel(LogprobArgs a)
             const int at = from + (v * G + gl) * 8;
             io8<T>::unpack(raw[v], f);
             gradient(f, at);
-            io8<T>::store_elem(out + at, 0u, io8<T>::pack(f), 8);
+            if constexpr (PAST) slice_store_past(out + at, f);
+            else io8<T>::store_elem(out + at, 0u, io8<T>::pack(f), 8);
         }
         return;
     }
@@ -408,19 +419,21 @@ constexpr int LOGPROB_STEP = 4 * 256 * 8;    // columns that a workgroup has in 
 constexpr int LOGPROB_WAVE = 4 * 64 * 8;     // and a wave: up to here a row is one wave's
 
 struct LogprobPlan {
-    int pieces, piece;
+    int pieces, piece, parts;
     size_t bytes;
 };
-// Rows are cut where there are fewer than 2048 workgroups of them, into pieces of 2048 columns at least.
+// Rows are cut where there are fewer than 2048 workgroups of them, into pieces of one step of a workgroup at least: a wave's choice among its 2048 columns takes
+// as long as their sums (64 x 51200 bf16 with eight alternatives in pieces of 2048: 16 us).  The same with and without alternatives, so that the sums are the same to the bit.
 LogprobPlan logprob_plan(int rows, int vocab, int top)
 {
-    LogprobPlan p = {1, vocab, 0};
+    LogprobPlan p = {1, vocab, 1, 0};
     if (vocab <= LOGPROB_WAVE || rows >= 2048) return p;
-    const int units = (vocab + 2047) / 2048, want = std::min({(2048 + rows - 1) / rows, units, 1024});
+    const int step = LOGPROB_STEP, units = (vocab + step - 1) / step, want = std::min({(2048 + rows - 1) / rows, units, 1024});
     const int each = (units + want - 1) / want;
-    p.piece = each * 2048;
+    p.piece = each * step;
     p.pieces = (units + each - 1) / each;
-    if (p.pieces > 1) p.bytes = (size_t)rows * p.pieces * part_floats(top) * sizeof(float);
+    p.parts = p.pieces * 4;
+    if (p.pieces > 1) p.bytes = (size_t)rows * p.parts * part_floats(top) * sizeof(float);
     return p;
 }
 
@@ -432,22 +445,21 @@ void logprob_forward(const LogprobArgs& a, hipStream_t st)
         return;
     }
     const dim3 grid((unsigned)((int64_t)a.rows * a.pieces));
-    if (a.piece <= 2048) hipLaunchKernelGGL((logprob_fwd_kernel<T, I, 256, 1, TOP>), grid, dim3(256), 0, st, a);
-    else hipLaunchKernelGGL((logprob_fwd_kernel<T, I, 256, 2, TOP>), grid, dim3(256), 0, st, a);
+    hipLaunchKernelGGL((logprob_fwd_kernel<T, I, 256, 4, TOP>), grid, dim3(256), 0, st, a);
     if (a.pieces > 1) hipLaunchKernelGGL((logprob_join_kernel<T, I, TOP>), dim3((unsigned)a.rows), dim3(64), 0, st, a);
 }
-template <typename T, typename I>
+template <typename T, typename I, bool PAST>
 void logprob_backward(LogprobArgs a, hipStream_t st)
 {
     if (a.vocab <= LOGPROB_WAVE) {
         a.pieces = 1;
         a.piece = LOGPROB_WAVE;
-        hipLaunchKernelGGL((logprob_bwd_kernel<T, I, 64>), dim3((unsigned)(((int64_t)a.rows + 3) / 4)), dim3(256), 0, st, a);
+        hipLaunchKernelGGL((logprob_bwd_kernel<T, I, 64, PAST>), dim3((unsigned)(((int64_t)a.rows + 3) / 4)), dim3(256), 0, st, a);
         return;
     }
     a.piece = LOGPROB_STEP;
     a.pieces = (a.vocab + LOGPROB_STEP - 1) / LOGPROB_STEP;
-    hipLaunchKernelGGL((logprob_bwd_kernel<T, I, 256>), dim3((unsigned)((int64_t)a.rows * a.pieces)), dim3(256), 0, st, a);
+    hipLaunchKernelGGL((logprob_bwd_kernel<T, I, 256, PAST>), dim3((unsigned)((int64_t)a.rows * a.pieces)), dim3(256), 0, st, a);
 }
 template <typename F>
 void with_types(const ss_logprob_params* p, F go)
@@ -518,7 +530,7 @@ int ss_logprob_fwd(const ss_logprob_params* p, void* stream)
     ss::LogprobArgs a = logprob_args(p);
     a.logp = p->logp;
     a.top_logp = p->top_logp; a.top_ids = p->top_ids;
-    a.pieces = plan.pieces; a.piece = plan.piece;
+    a.pieces = plan.pieces; a.piece = plan.piece; a.parts = plan.parts;
     a.part = static_cast<float*>(p->workspace);
     hipStream_t st = static_cast<hipStream_t>(stream);
     ss::with_types(p, [&](auto t, auto i) {
@@ -541,7 +553,11 @@ int ss_logprob_bwd(const ss_logprob_bwd_params* p, void* stream)
     ss::LogprobArgs a = logprob_args(f);
     a.dlogp = p->dlogp; a.dentropy = p->dentropy;
     a.dlogits = p->dlogits;
-    ss::with_types(f, [&](auto t, auto i) { ss::logprob_backward<decltype(t), decltype(i)>(a, static_cast<hipStream_t>(stream)); });
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    ss::with_types(f, [&](auto t, auto i) {
+        if ((int64_t)f->rows * f->vocab * (int64_t)sizeof(t) > ss::STREAM_BYTES) ss::logprob_backward<decltype(t), decltype(i), true>(a, st);
+        else ss::logprob_backward<decltype(t), decltype(i), false>(a, st);
+    });
     return hipGetLastError() == hipSuccess ? SS_OK : SS_ERR_LAUNCH;
 }
 
