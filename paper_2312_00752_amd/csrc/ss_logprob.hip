@@ -6,8 +6,8 @@
 // S <- c S, U <- c (U + S (m_old - m)) with c = exp(m_old - m); lanes, waves and workgroups are joined by the same rule.  Then
 // lse = m + log S and the entropy log S - U / S.  Few rows are cut into pieces for several workgroups.
 // Alternatives: a wave holds its best, in order, one a lane.  Of 64 groups of logits, one a lane, the top-th largest maximum is a bound below
-// which nothing can be among the top, so of thousands of logits only about `top` are looked at one by one; each is put in its
-// place by a ballot and a shift.
+// which nothing can be among the top, so of thousands of logits only about `top` are left; those are ranked among each other and the ones
+// so far.
 #include <hip/hip_runtime.h>
 #include <algorithm>
 #include <cmath>
@@ -79,75 +79,72 @@ __device__ __forceinline__ Stat join_wave(Stat a)
 }
 
 // ---- the best of a wave ---------------------------------------------------------------------------
-// Lane l holds the l-th best (value, column); a column of -1 is an empty place.  All lanes call; `top` lanes are kept exact.
+// A logit and its column as one number, whose order is theirs: the larger logit first, of equal ones the lower column.  0: none.
+__device__ __forceinline__ uint32_t order_of(float v)
+{
+    const uint32_t b = __float_as_uint(v + 0.0f);   // zeros of both signs are equal
+    return b ^ ((uint32_t)((int)b >> 31) | 0x80000000u);
+}
+__device__ __forceinline__ float logit_of(uint32_t order) { return __uint_as_float(order & 0x80000000u ? order ^ 0x80000000u : ~order); }
+__device__ __forceinline__ uint64_t rank_of(float v, int column) { return (uint64_t)order_of(v) << 32 | (uint32_t)~column; }
+__device__ __forceinline__ uint64_t of_lane(uint64_t v, int lane)
+{
+    return (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(v >> 32), lane) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)v, lane);
+}
+// Lane l holds the l-th best.  All lanes call; `top` lanes are kept exact.  `room`: 64 places of the wave's own in LDS.
 struct Best {
-    float v = -INFINITY;
-    int i = -1;
-    __device__ __forceinline__ bool ahead(float x, int k) const { return i >= 0 && (v > x || (v == x && i < k)); }
-    static __device__ __forceinline__ float value_of(float x, int lane) { return __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(x), lane)); }
-    __device__ __forceinline__ void insert(float x, int k)   // the same in all lanes
+    uint64_t r = 0;
+    __device__ __forceinline__ bool empty() const { return r == 0; }
+    __device__ __forceinline__ float value() const { return logit_of((uint32_t)(r >> 32)); }
+    __device__ __forceinline__ int column() const { return (int)~(uint32_t)r; }
+    // The lanes' proposals, those of `ask`, take their places: every one is compared with all places and all others, none waits for another.
+    __device__ __forceinline__ void merge(uint64_t proposal, uint64_t ask, uint64_t* room)
     {
-        const int place = __popcll(__ballot(ahead(x, k))), lane = threadIdx.x % WAVE;
-        const float pv = from_lane<0x138, 0xf>(v, v);   // of the lane before
-        const int pi = __builtin_amdgcn_update_dpp(i, i, 0x138, 0xf, 0xf, false);
-        v = lane > place ? pv : (lane == place ? x : v);
-        i = lane > place ? pi : (lane == place ? k : i);
+        const int lane = threadIdx.x % WAVE;
+        const bool mine = ask >> lane & 1;
+        int place = lane, rank = 0, behind = 0;
+#pragma unroll 1
+        while (ask) {
+            const int l = __ffsll((long long)ask) - 1;
+            ask &= ask - 1;
+            const uint64_t p = of_lane(proposal, l);
+            place += p > r ? 1 : 0;
+            rank += p > proposal ? 1 : 0;
+            const int before = __popcll(__ballot(r > p));
+            behind = lane == l ? before : behind;
+        }
+        rank += behind;
+        room[lane] = 0;
+        __builtin_amdgcn_wave_barrier();
+        if (r != 0 && place < WAVE) room[place] = r;
+        if (mine && rank < WAVE) room[rank] = proposal;
+        __builtin_amdgcn_wave_barrier();
+        r = room[lane];
+        __builtin_amdgcn_wave_barrier();
     }
-    // N values a lane; column(j) is -1 for those that are left out
-    template <int N, typename F>
-    __device__ __forceinline__ void absorb(const float (&x)[N], F column, int top)
+    // What is no better has no place: the last of the top, or, as long as it is not full, what is below the top-th largest of the lanes' largest
+    // (`most`, in its order, 0 where a lane has none), as that many are no less.  Its upper 16 bits are enough, found from the highest down.
+    __device__ __forceinline__ uint64_t least(uint32_t most, int top) const
     {
-        static_assert(N <= 32, "a bit each");
-        float lv = value_of(v, top - 1);
-        int li = __builtin_amdgcn_readlane(i, top - 1);
-        uint32_t open = 0;   // what the last of the top is not ahead of
-        float most = -INFINITY;
-#pragma unroll
-        for (int j = 0; j < N; ++j) {
-            const int k = column(j);
-            if (k >= 0 && !(li >= 0 && (lv > x[j] || (lv == x[j] && li < k)))) {
-                open |= 1u << j;
-                most = fmaxf(most, x[j]);
-            }
-        }
-        if (!__ballot(open != 0)) return;
-        if (li < 0) {
-            // the top is not full yet: the top-th largest of the lanes' maxima is a bound, as that many values are no less.  Its upper
-            // 16 bits are enough, found from the highest down in numbers whose order is the floats'
-            const uint32_t bits = __float_as_uint(most + 0.0f), order = open ? bits ^ ((uint32_t)((int)bits >> 31) | 0x80000000u) : 0u;
-            uint32_t bound = 0;
-#pragma unroll
-            for (int b = 31; b >= 16; --b) {
-                const uint32_t higher = bound | 1u << b;
-                if (__popcll(__ballot(order >= higher)) >= top) bound = higher;
-            }
-            const float least = __uint_as_float(bound & 0x80000000u ? bound ^ 0x80000000u : ~bound);
-            if (bound > 0x007fffffu) {   // no less than -infinity
-#pragma unroll
-                for (int j = 0; j < N; ++j)
-                    if (!(x[j] >= least)) open &= ~(1u << j);
-            }
-        }
+        const uint64_t last = of_lane(r, top - 1);
+        if (last) return last;
+        uint32_t bound = 0;
+#pragma unroll 1
+        for (uint32_t bit = 0x80000000u; bit >= 0x10000u; bit >>= 1)
+            if (__popcll(__ballot(most >= (bound | bit))) >= top) bound |= bit;
+        return bound ? ((uint64_t)bound << 32) - 1 : 0;
+    }
+    // of(j) of the lanes' open bits j take their places where they are above `than`: the first of every lane, then the second, ...
+    template <typename F>
+    __device__ __forceinline__ void absorb(uint32_t open, F of, uint64_t than, int top, uint64_t* room)
+    {
+#pragma unroll 1
         while (__ballot(open != 0)) {
-            // every lane's first candidate
-            float cv = 0.0f;
-            int ck = -1;
-#pragma unroll
-            for (int j = N - 1; j >= 0; --j)
-                if (open >> j & 1) {
-                    cv = x[j];
-                    ck = column(j);
-                }
+            const uint64_t proposal = open ? of(__ffs((int)open) - 1) : 0, ask = __ballot(proposal > than);
             open &= open - 1;
-            uint64_t ask = __ballot(ck >= 0 && !(li >= 0 && (lv > cv || (lv == cv && li < ck))));
-            while (ask) {
-                const int l = __ffsll((long long)ask) - 1;
-                insert(value_of(cv, l), __builtin_amdgcn_readlane(ck, l));
-                lv = value_of(v, top - 1);
-                li = __builtin_amdgcn_readlane(i, top - 1);
-                ask &= ask - 1;
-                ask &= __ballot(!(li >= 0 && (lv > cv || (lv == cv && li < ck))));
-            }
+            if (!ask) continue;
+            merge(proposal, ask, room);
+            than = max(than, of_lane(r, top - 1));
         }
     }
 };
@@ -181,12 +178,12 @@ __device__ __forceinline__ void results(const LogprobArgs& a, int row, Stat t, c
     }
     if constexpr (TOP) {
         if (lane < a.top) {
-            a.top_logp[(int64_t)row * a.top + lane] = best.i < 0 ? __uint_as_float(0x7fc00000u) : logp(best.v);
-            a.top_ids[(int64_t)row * a.top + lane] = best.i;
+            a.top_logp[(int64_t)row * a.top + lane] = best.empty() ? __uint_as_float(0x7fc00000u) : logp(best.value());
+            a.top_ids[(int64_t)row * a.top + lane] = best.empty() ? -1 : best.column();
         }
     }
 }
-// floats of a part of a row: m, S, U, then `top` values and as many columns
+// floats of a part of a row: m, S, U, then the `top` best, two each
 __host__ __device__ __forceinline__ int part_floats(int top) { return 4 + 2 * top; }
 
 // G lanes a row (a wave: rows side by side) or piece of one; V slices of eight a lane and step, the next step's requested ahead.
@@ -204,6 +201,8 @@ __global__ __launch_bounds__(256) void logprob_fwd_kernel(LogprobArgs a)
     const int W = a.vocab, from = piece * a.piece, to = min(from + a.piece, W);
     Stat t = {-INFINITY, 0.0f, 0.0f};
     Best best;
+    __shared__ uint64_t room[TOP ? 4 : 1][WAVE];
+    __shared__ float logits[TOP ? 4 : 1][V * 8][TOP ? WAVE : 1];   // a lane's, side by side with the others'
     // V slices of eight columns; those behind the piece are -infinity, and no candidates
     auto take = [&](const float (&f)[V][8], int base) {
         float m = t.m;
@@ -223,11 +222,27 @@ __global__ __launch_bounds__(256) void logprob_fwd_kernel(LogprobArgs a)
                 t.u = fmaf(e, fmaxf(d, FAR), t.u);
             }
         if constexpr (TOP) {
-            const float(&all)[V * 8] = reinterpret_cast<const float(&)[V * 8]>(f);
-            best.absorb(all, [&](int j) {
+            const int lane = threadIdx.x % WAVE;
+            float(*const all)[WAVE] = reinterpret_cast<float(*)[WAVE]>(logits[threadIdx.x / WAVE]);
+            float most = -INFINITY;   // of what is no NaN; what is behind the piece is -infinity
+            bool some = false;
+#pragma unroll
+            for (int v = 0; v < V; ++v)
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    all[v * 8 + j][lane] = f[v][j];
+                    some = some || f[v][j] == f[v][j];
+                    most = fmaxf(most, f[v][j]);
+                }
+            const uint64_t than = best.least(some ? order_of(most) : 0u, a.top);
+            const float low = than >> 32 >= 0x007fffffu ? logit_of((uint32_t)(than >> 32)) : -INFINITY;
+            uint32_t open = 0;
+#pragma unroll
+            for (int j = 0; j < V * 8; ++j) open |= f[j / 8][j % 8] >= low ? 1u << j : 0u;
+            best.absorb(open, [&](int j) {
                 const int k = base + (j / 8 * G + gl) * 8 + j % 8;
-                return k < to && all[j] == all[j] ? k : -1;
-            }, a.top);
+                return k < to ? rank_of(all[j][lane], k) : 0;
+            }, than, a.top, room[threadIdx.x / WAVE]);
         }
     };
     // whole steps, whose loads need no bounds and are requested a step ahead
@@ -274,31 +289,24 @@ __global__ __launch_bounds__(256) void logprob_fwd_kernel(LogprobArgs a)
             p[2] = t.u;
         }
         if constexpr (TOP) {
-            if (lane < a.top) {
-                p[4 + lane] = best.v;
-                p[4 + a.top + lane] = __int_as_float(best.i);
-            }
+            if (lane < a.top) reinterpret_cast<uint64_t*>(p + 4)[lane] = best.r;
         }
     };
     if constexpr (WAVES > 1) {
         const int wave = threadIdx.x / WAVE;
         if (a.pieces > 1) return leave(piece * WAVES + wave);
         __shared__ Stat stats[WAVES];
-        __shared__ float values[WAVES][TOP ? WAVE : 1];
-        __shared__ int columns[WAVES][TOP ? WAVE : 1];
+        __shared__ uint64_t ranks[WAVES][TOP ? WAVE : 1];
         if (lane == 0) stats[wave] = t;
-        if constexpr (TOP) {
-            values[wave][lane] = best.v;
-            columns[wave][lane] = lane < a.top ? best.i : -1;
-        }
+        if constexpr (TOP) ranks[wave][lane] = lane < a.top ? best.r : 0;
         __syncthreads();
         if (wave != 0) return;
         for (int w = 1; w < WAVES; ++w) t = join(t, stats[w]);
         if constexpr (TOP) {
-            float f[WAVES - 1];
-#pragma unroll
-            for (int w = 1; w < WAVES; ++w) f[w - 1] = values[w][lane];
-            best.absorb(f, [&](int j) { return columns[j + 1][lane]; }, a.top);
+            for (int w = 1; w < WAVES; ++w) {
+                const uint64_t proposal = ranks[w][lane], ask = __ballot(proposal > of_lane(best.r, a.top - 1));
+                if (ask) best.merge(proposal, ask, room[0]);
+            }
         }
     }
     const int target = target_of<I>(a, row);
@@ -320,21 +328,27 @@ __global__ __launch_bounds__(64) void logprob_join_kernel(LogprobArgs a)
     Best best;
     if constexpr (TOP) {
         constexpr int N = 8;
+        __shared__ uint64_t room[WAVE], held[N][WAVE];
         const int all = a.parts * a.top;
+#pragma unroll 1
         for (int c0 = 0; c0 < all; c0 += N * WAVE) {
-            float f[N];
-            int k[N];
+            uint64_t v[N];
+            uint32_t most = 0, open = 0;
 #pragma unroll
             for (int j = 0; j < N; ++j) {
-                const int c = min(c0 + j * WAVE + lane, all - 1);
-                const float* q = p + (int64_t)(c / a.top) * part_floats(a.top) + 4 + c % a.top;
-                f[j] = q[0];
-                k[j] = __float_as_int(q[a.top]);
+                const int c = c0 + j * WAVE + lane, part = min(c, all - 1) / a.top;
+                const uint64_t r = reinterpret_cast<const uint64_t*>(p + (int64_t)part * part_floats(a.top) + 4)[min(c, all - 1) - part * a.top];
+                v[j] = c < all ? r : 0;
             }
 #pragma unroll
-            for (int j = 0; j < N; ++j)
-                if (c0 + j * WAVE + lane >= all) k[j] = -1;
-            best.absorb(f, [&](int j) { return k[j]; }, a.top);
+            for (int j = 0; j < N; ++j) {
+                held[j][lane] = v[j];
+                most = max(most, (uint32_t)(v[j] >> 32));
+            }
+            const uint64_t than = best.least(most, a.top);
+#pragma unroll
+            for (int j = 0; j < N; ++j) open |= v[j] > than ? 1u << j : 0u;
+            best.absorb(open, [&](int j) { return held[j][lane]; }, than, a.top, room);
         }
     }
     results<TOP>(a, row, join_wave(t), best, target, logit);
