@@ -197,7 +197,6 @@ __global__ __launch_bounds__(256) void logprob_fwd_kernel(LogprobArgs a)
     if (row >= a.rows) return;   // a whole wave
     const T* x = static_cast<const T*>(a.logits) + row * a.row_stride;
     constexpr int STEP = V * G * 8;
-    constexpr bool TINY = G == WAVE;   // rows of less than 8
     const int W = a.vocab, from = piece * a.piece, to = min(from + a.piece, W);
     Stat t = {-INFINITY, 0.0f, 0.0f};
     Best best;
@@ -262,20 +261,25 @@ __global__ __launch_bounds__(256) void logprob_fwd_kernel(LogprobArgs a)
             take(f, base);
         }
     }
-    if (base < to) {
-        const bool whole = W % 8 == 0;
-        const int limit = slice_limit(W, whole);
-        typename io8<T>::raw raw[V];
-        float f[V][8];
+    if (base < to) {   // the rest; the columns behind the last whole eight one by one
+        const int end = W / 8 * 8, slice = (end - base) / 8;
+        const bool mine = slice % G == gl;
+        float f[V][8], rest[8];
 #pragma unroll
-        for (int v = 0; v < V; ++v) raw[v] = slice_request<T, TINY>(x, base + (v * G + gl) * 8, W, limit);
+        for (int j = 0; j < 7; ++j) rest[j] = mine && end + j < W ? io_to_f32<T>(x[end + j]) : -INFINITY;
+        rest[7] = -INFINITY;
+        typename io8<T>::raw raw[V];
 #pragma unroll
         for (int v = 0; v < V; ++v) {
-            const int at = base + (v * G + gl) * 8, n = to - at;
-            slice_settle<T>(raw[v], at, W, limit, whole);
+            const int at = base + (v * G + gl) * 8;
+            if (at + 8 <= to) raw[v] = io8<T>::load_elem(x + at, 0u);
+        }
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            const int at = base + (v * G + gl) * 8;
             io8<T>::unpack(raw[v], f[v]);
 #pragma unroll
-            for (int j = 0; j < 8; ++j) f[v][j] = j < n ? f[v][j] : -INFINITY;
+            for (int j = 0; j < 8; ++j) f[v][j] = at + 8 <= to ? f[v][j] : (at == end ? rest[j] : -INFINITY);
         }
         take(f, base);
     }
@@ -414,15 +418,20 @@ __global__ __launch_bounds__(256) void logprob_bwd_kernel(LogprobArgs a)
         }
         return;
     }
-    const bool whole = W % 8 == 0;
-    const int limit = slice_limit(W, whole);
-#pragma unroll
-    for (int v = 0; v < V; ++v) raw[v] = slice_request<T, G == WAVE>(x, from + (v * G + gl) * 8, W, limit);
 #pragma unroll
     for (int v = 0; v < V; ++v) {
         const int at = from + (v * G + gl) * 8;
-        slice_settle<T>(raw[v], at, W, limit, whole);
-        io8<T>::unpack(raw[v], f);
+        if (at + 8 <= W) raw[v] = io8<T>::load_elem(x + at, 0u);
+    }
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+        const int at = from + (v * G + gl) * 8;
+        if (at >= W) break;
+        if (at + 8 <= W) io8<T>::unpack(raw[v], f);
+        else {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) f[j] = at + j < W ? io_to_f32<T>(x[at + j]) : 0.0f;
+        }
         gradient(f, at);
         slice_store<T>(out, at, W - at, f);
     }
