@@ -8,11 +8,11 @@ projection back (the homogeneous block of arXiv 2312.00752, Section 3.4, with th
 
 ``GatedBlock`` trains: every step is differentiable, and documents packed into rows are kept apart by ``reset``.  ``serving()`` gives the
 same block with both projections in 8-bit integers, for prompts and single tokens.  ``python -m paper_2312_00752_amd.block`` trains one on
-a recall task and serves it.
+a recall task, with the library's embedding before it, its log probabilities behind it and its optimiser, and serves it.
 """
 import torch
 
-from . import autograd, binding as B
+from . import autograd, binding as B, optim
 
 
 def _sum_like(W, terms):
@@ -114,7 +114,7 @@ class ServedBlock:
         if residual is None:
             residual = torch.zeros_like(x)
         q, scale, residual = B.ss_norm_quant(x, self.norm_weight, self.norm_bias, residual=residual, eps=self.eps, rms=self.rms)
-        xs, f, i, z = B.ss_qlinear(q.view(*x.shape[:2], -1), self.W_in, self.in_scale, x_scale=scale, dim=x.shape[2], out_dtype=x.dtype,
+        xs, f, i, z = B.ss_qlinear(q.view(*x.shape[:2], q.shape[1]), self.W_in, self.in_scale, x_scale=scale, dim=x.shape[2], out_dtype=x.dtype,
                                    out_seq_last=True).chunk(4, 1)
         y, state = B.ss_gate_fwd(xs, f, self.rate, i=i, z=z, f_bias=self.f_bias, i_bias=self.i_bias, reset=reset, h0=state,
                                  return_last_state=True)
@@ -131,28 +131,28 @@ class ServedBlock:
         return B.ss_qlinear(y, self.W_out, self.out_scale), residual_t
 
 
-def main(steps=60, batch=16, length=64, width=128, inner=256, symbols=16):
+def main(steps=60, batch=16, length=64, width=128, inner=256, symbols=16, norm="layer", state_bits=32):
     """Recall: the symbol shown at the start of a document is asked for at its end; two documents a row, kept apart by reset."""
     torch.manual_seed(0)
     dev = "cuda"
-    block = GatedBlock(width, inner, device=dev)
+    block = GatedBlock(width, inner, device=dev, norm=norm)
     embed = torch.nn.Parameter(torch.randn(symbols + 1, width, device=dev) * 0.5)
     read = torch.nn.Parameter(torch.randn(symbols, width, device=dev) * width ** -0.5)
     params = list(block.parameters()) + [embed, read]
-    opt = torch.optim.Adam(params, lr=3e-3)
+    opt = optim.AdamW(params, lr=3e-3, weight_decay=0.0, state_bits=state_bits)
     reset = torch.zeros(batch, length, dtype=torch.bool, device=dev)
     reset[:, [0, length // 2]] = True
 
     def task():
         seq = torch.full((batch, length), symbols, device=dev)
         seq[:, 0::length // 2] = torch.randint(0, symbols, (batch, 2), device=dev)
-        return seq, seq[:, 0::length // 2]
+        return seq, seq[:, 0::length // 2].contiguous()
 
     for step in range(steps):
         seq, want = task()
-        out, residual = block(embed[seq], reset=reset)
+        out, residual = block(autograd.embedding(seq, embed), reset=reset)
         logits = (out + residual)[:, length // 2 - 1::length // 2] @ read.t()
-        loss = torch.nn.functional.cross_entropy(logits.reshape(-1, symbols), want.reshape(-1))
+        loss = -autograd.token_logprobs(logits, want)[0].mean()
         opt.zero_grad()
         loss.backward()
         opt.step()
@@ -161,12 +161,13 @@ def main(steps=60, batch=16, length=64, width=128, inner=256, symbols=16):
     with torch.no_grad():   # the first document token by token, in 8 bits
         served = block.serving()
         seq, want = task()
-        x = embed[seq].contiguous()
+        x = B.ss_embed_fwd(seq, embed)
         _, _, state = served.prompt(x[:, :4].contiguous())
         for t in range(4, length // 2):
             out, residual = served.step(x[:, t].contiguous(), state)
-        right = ((out + residual) @ read.t()).argmax(-1) == want[:, 0]
-        print("served in 8 bits: %d of %d recalled" % (int(right.sum()), batch), flush=True)
+        logp, entropy, _, _, best = B.ss_logprob_fwd((out + residual) @ read.t(), want[:, 0].contiguous(), top=1)
+        right = best[:, 0] == want[:, 0]
+        print("served in 8 bits: %d of %d recalled, log probability %.3f, entropy %.3f" % (int(right.sum()), batch, logp.mean().item(), entropy.mean().item()), flush=True)
     return loss.item(), int(right.sum())
 
 
