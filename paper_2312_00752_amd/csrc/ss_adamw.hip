@@ -229,7 +229,7 @@ __device__ __forceinline__ void adamw_chunk_of(const AdamwArgs& a, const AdamwTe
 template <int BITS>
 __global__ __launch_bounds__(ADAMW_THREADS) void adamw_kernel(const AdamwArgs a)
 {
-    const int taken = a.count[0];
+    const int taken = __builtin_amdgcn_readfirstlane(a.count[0]);
     int k = 0, above = a.tensors;   // the tensor that has this chunk: start[k] <= blockIdx.x < start[above]
     while (above - k > 1) {
         const int mid = (k + above) / 2;
@@ -237,7 +237,8 @@ __global__ __launch_bounds__(ADAMW_THREADS) void adamw_kernel(const AdamwArgs a)
         else above = mid;
     }
     if (a.last) {
-        __syncthreads();   // all of the workgroup have read the count; the last workgroup that says so writes it
+        asm volatile("" ::"s"(taken));   // has arrived
+        __syncthreads();                  // all of the workgroup have read the count; the last workgroup that says so writes it
         if (threadIdx.x == 0 && atomicAdd(&a.count[1], 1) == (int)gridDim.x - 1) {
             a.count[1] = 0;
             a.count[0] = taken + 1;

@@ -42,15 +42,6 @@ struct BwdSmem {
     float dbc[NWAVES][2][STATES_PER_LANE][BT];   // this block's dB (0) / dC (1), private to a wave
 };
 
-// LDS traffic between lanes of ONE wave needs no barrier: a wave's LDS instructions
-// execute in order.  This only stops the compiler from moving accesses across the point.
-__device__ __forceinline__ void wave_lds_fence()
-{
-    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-    __builtin_amdgcn_wave_barrier();
-    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
-}
-
 // x summed over lanes l, l^16, l^32, l^48 (result in every lane): two half/row swaps
 __device__ __forceinline__ float sum_over_lane_quarters(float x)
 {

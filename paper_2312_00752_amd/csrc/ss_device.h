@@ -35,6 +35,15 @@ __host__ __device__ __forceinline__ int position_state(int pos, int il) { return
 // slots per lane a kernel is built for when the states are dealt out: 1, 2 or 4
 __host__ __device__ __forceinline__ int slots_for(int N, int il) { return !il ? STATES_PER_LANE : (N <= NWAVES ? 1 : (N <= 2 * NWAVES ? 2 : STATES_PER_LANE)); }
 
+// LDS traffic between lanes of ONE wave needs no barrier: a wave's LDS instructions
+// execute in order.  This only stops the compiler from moving accesses across the point.
+__device__ __forceinline__ void wave_lds_fence()
+{
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
+
 constexpr float LOG2E = 1.4426950408889634f;
 constexpr float LN2 = 0.6931471805599453f;
 

@@ -213,13 +213,13 @@ __global__ __launch_bounds__(SORT_THREADS) void embed_place_kernel(EmbedArgs a)
             }
             const int rank = __popcll(same & ((1ull << lane) - 1));
             const int at = place[wave][d] + rank;
-            __builtin_amdgcn_wave_barrier();   // all lanes have read before the last of each digit writes
+            wave_lds_fence();   // all lanes have read before the last of each digit writes
             if (valid) {
                 if ((same >> lane) == 1ull) place[wave][d] = at + 1;
                 a.key_out[at] = keys[u];
                 a.pos_out[at] = places[u];
             }
-            __builtin_amdgcn_wave_barrier();
+            wave_lds_fence();
         }
     }
 }

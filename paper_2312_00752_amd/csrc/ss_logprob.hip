@@ -115,12 +115,12 @@ struct Best {
         }
         rank += behind;
         room[lane] = 0;
-        __builtin_amdgcn_wave_barrier();
+        wave_lds_fence();
         if (r != 0 && place < WAVE) room[place] = r;
         if (mine && rank < WAVE) room[rank] = proposal;
-        __builtin_amdgcn_wave_barrier();
+        wave_lds_fence();
         r = room[lane];
-        __builtin_amdgcn_wave_barrier();
+        wave_lds_fence();
     }
     // What is no better has no place: the last of the top, or, as long as it is not full, what is below the top-th largest of the lanes' largest
     // (`most`, in its order, 0 where a lane has none), as that many are no less.  Its upper 16 bits are enough, found from the highest down.
@@ -197,7 +197,7 @@ __global__ __launch_bounds__(256) void logprob_fwd_kernel(LogprobArgs a)
     if (row >= a.rows) return;   // a whole wave
     const T* x = static_cast<const T*>(a.logits) + row * a.row_stride;
     constexpr int STEP = V * G * 8;
-    const int W = a.vocab, from = piece * a.piece, to = min(from + a.piece, W);
+    const int W = a.vocab, from = piece * a.piece, to = piece == a.pieces - 1 ? W : from + a.piece;   // the last's own end may lie behind 32 bits
     Stat t = {-INFINITY, 0.0f, 0.0f};
     Best best;
     __shared__ uint64_t room[TOP ? 4 : 1][WAVE];

@@ -324,3 +324,22 @@ def test_refusals():
         B.ss_logprob_fwd(torch.randn(3, 0, device="cuda"), t)
     with pytest.raises(B.SsError):
         B.ss_logprob_fwd(torch.randn(3, 60000, device="cuda"), t, workspace=torch.empty(16, dtype=torch.uint8, device="cuda"))
+
+
+def test_longest_row():
+    """The largest vocabulary that is served, whose last piece ends where 32 bits do: zeros but for two logits, so that every sum is known."""
+    vocab = 2 ** 31 - 1 - 65536
+    x = torch.zeros(1, vocab, dtype=torch.bfloat16, device="cuda")
+    x[0, vocab - 3], x[0, 5] = 20.0, 18.0
+    t = torch.tensor([vocab - 3], device="cuda")
+    logp, entropy, stats, top_logp, top_ids = B.ss_logprob_fwd(x, t, top=3)
+    total = np.exp(20.0) + np.exp(18.0) + (vocab - 2)
+    ref = [20 - np.log(total), 18 - np.log(total), -np.log(total)]
+    assert top_ids.tolist() == [[vocab - 3, 5, 0]]
+    # a lane's 2^13 ones and the pieces' sums are short: the bound of the shorter rows
+    assert np.abs(top_logp.cpu().numpy()[0] - ref).max() <= 64 * 2.0 ** -24 * 44 and logp.item() == top_logp[0, 0].item()
+    p = np.exp(ref)
+    assert abs(entropy.item() + (p[0] * ref[0] + p[1] * ref[1] + (vocab - 2) * p[2] * ref[2])) <= 64 * 2.0 ** -24 * 200
+    grad = B.ss_logprob_bwd(x, stats, t, dlogp=torch.ones(1, device="cuda"))
+    for k, want in ((5, -p[1]), (vocab - 3, 1 - p[0]), (0, -p[2]), (vocab - 1, -p[2]), (vocab // 2, -p[2])):
+        assert abs(grad[0, k].item() - want) <= (2.0 ** -9 + 64 * 44 * 2.0 ** -24) * abs(want)
