@@ -1334,6 +1334,14 @@ def _on_current(*tensors):
             raise ValueError("a tensor lies on %s, the current device is cuda:%d" % (t.device, _device_index()))
 
 
+def _apart(out, **inputs):
+    """``out``, a dense tensor that the caller gave, shares no memory with the inputs that are read while it is written."""
+    for name, t in inputs.items():
+        if t is not None and out.numel() and t.numel() and out.data_ptr() < t.data_ptr() + t.numel() * t.element_size() \
+                and t.data_ptr() < out.data_ptr() + out.numel() * out.element_size():
+            raise ValueError("out must not share memory with %s" % name)
+
+
 def _type_code(dtype):
     """For the compiled module: None, or the code of an io type; what is none of them is refused behind it."""
     return None if dtype is None else (SS_F32 if dtype is torch.float32 else (SS_BF16 if dtype is torch.bfloat16 else -1))
@@ -1370,6 +1378,7 @@ def ss_embed_fwd(ids, table, scale=1.0, out_dtype=None, out=None, stream=None):
     if out is None:
         out = torch.empty(shape, dtype=table.dtype if out_dtype is None else out_dtype, device=table.device)
     p.out = _ptr(out, out_dtype, shape, "out")
+    _apart(out, ids=ids, table=table)
     p.io_dtype = _io_code(out)
     _check(lib().ss_embed_fwd(ctypes.byref(p), _stream(stream)))
     return out
@@ -1398,6 +1407,7 @@ def ss_embed_bwd(dout, ids, vocab, scale=1.0, dtype=None, out=None, workspace=No
     if out is None:
         out = torch.empty((vocab, dim), dtype=dout.dtype if dtype is None else dtype, device=dout.device)
     q.dtable = _ptr(out, dtype, (vocab, dim), "out")
+    _apart(out, ids=ids, dout=dout, workspace=workspace)
     q.fwd.table_dtype = _io_code(out)
     need = int(lib().ss_embed_workspace_bytes(ctypes.byref(q.fwd)))
     if need:

@@ -256,3 +256,15 @@ def test_refusals():
         B.ss_embed_bwd(torch.randn(4, 6, device="cuda"), ids, 0)
     with pytest.raises(B.SsError):
         B.ss_embed_bwd(torch.randn(4, 6, device="cuda"), ids, 5, workspace=torch.empty(256, dtype=torch.uint8, device="cuda"))
+
+
+def test_refuses_shared_memory():
+    room = torch.zeros(64, 8, device="cuda")
+    ids = torch.zeros(32, dtype=torch.int64, device="cuda")
+    with pytest.raises(ValueError, match="table"):
+        B.ss_embed_fwd(ids, room[:40], out=room[32:])
+    with pytest.raises(ValueError, match="dout"):
+        B.ss_embed_bwd(room[:32], ids, 40, out=room[24:])
+    with pytest.raises(ValueError, match="ids"):
+        B.ss_embed_bwd(room[:32], room[40:48].view(torch.int64).view(-1), 20, out=room[44:])
+    B.ss_embed_bwd(room[:32], ids, 32, out=room[32:])
