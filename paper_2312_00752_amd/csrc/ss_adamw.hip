@@ -239,11 +239,17 @@ __global__ __launch_bounds__(ADAMW_THREADS) void adamw_kernel(const AdamwArgs a)
     if (a.last) {
         asm volatile("" ::"s"(taken));   // has arrived
         __syncthreads();                  // all of the workgroup have read the count; the last workgroup that says so writes it
+    }
+    // A workgroup's word costs 13 ns, one behind the other: said first where each has one step to do (the others wait for memory meanwhile), else
+    // last, when they no longer stand in a queue (16 million elements, 8 bits: 45 us against 65 with the word first).
+    auto say = [&]() {
         if (threadIdx.x == 0 && atomicAdd(&a.count[1], 1) == (int)gridDim.x - 1) {
             a.count[1] = 0;
             a.count[0] = taken + 1;
         }
-    }
+    };
+    const bool first = a.chunk == ADAMW_STEP || a.tensors == 0;
+    if (a.last && first) say();
     if (a.tensors == 0) return;
     StepFactors f;
     f.step = (uint32_t)taken + 1u;
@@ -266,6 +272,7 @@ __global__ __launch_bounds__(ADAMW_THREADS) void adamw_kernel(const AdamwArgs a)
         else if (e.master) adamw_chunk_of<BITS, bf16_t, true, float>(a, e, from, n, f);
         else adamw_chunk_of<BITS, bf16_t, false, float>(a, e, from, n, f);
     }
+    if (a.last && !first) say();
 }
 
 template <bool SIGN, typename T>
@@ -329,8 +336,9 @@ int ss_adamw_step(const ss_adamw_params* p, void* stream)
     a.beta2 = (float)p->beta2; a.rest2 = (float)(1.0 - p->beta2);
     a.log1 = std::log(p->beta1); a.log2 = std::log(p->beta2);
     a.lr_device = p->lr_device; a.grad_scale = p->grad_scale;
-    // a step a chunk while that gives few workgroups, up to eight
-    int64_t chunk = std::min(std::max(all / (ss::ADAMW_STEP * (int64_t)4096), (int64_t)1), (int64_t)8) * ss::ADAMW_STEP;
+    // 512 workgroups, more only where each has eight steps.  Float32, 1 million elements in 512 / 1024 workgroups: 9.2 / 11.4 us; 4 million in 512 / 2048: 22 / 27; 67 million with
+    // eight / sixteen steps: 358 / 366.
+    int64_t chunk = std::min(all / (ss::ADAMW_STEP * (int64_t)512) + 1, (int64_t)8) * ss::ADAMW_STEP;
     const hipStream_t st = static_cast<hipStream_t>(stream);
     int k = 0;
     do {
