@@ -54,9 +54,8 @@ __device__ __forceinline__ void row_slice(const T* row, int at, int dim, float (
     io8<T>::unpack(r, v);
 }
 
-// G lanes a token and V slices of eight a lane and step.  A row takes two trips to memory, one behind the other, so there should be many at once: a wave a token
-// where there are tokens enough, else a workgroup.
-template <typename E, typename T, typename I, int G, int V>
+// G lanes a token, a slice of eight a lane and step.
+template <typename E, typename T, typename I, int G>
 __global__ __launch_bounds__(256) void embed_fwd_kernel(EmbedArgs a)
 {
     constexpr int SIDE = 256 / G;
@@ -70,20 +69,12 @@ __global__ __launch_bounds__(256) void embed_fwd_kernel(EmbedArgs a)
         const bool there = id < a.vocab;
         const E* row = static_cast<const E*>(a.table) + (int64_t)(there ? id : 0) * D;
         T* out = static_cast<T*>(a.out) + t * D;
-        for (int at0 = gl * 8; at0 < D; at0 += V * G * 8) {
-            typename io8<E>::raw r[V];
+        for (int at = gl * 8; at < D; at += G * 8) {
+            float f[8];
+            row_slice<E>(row, at, D, f);
 #pragma unroll
-            for (int v = 0; v < V; ++v) r[v] = slice_request<E, true>(row, at0 + v * G * 8, D, limit);
-#pragma unroll
-            for (int v = 0; v < V; ++v) {
-                const int at = at0 + v * G * 8;
-                float f[8];
-                slice_settle<E>(r[v], at, D, limit, whole);
-                io8<E>::unpack(r[v], f);
-#pragma unroll
-                for (int j = 0; j < 8; ++j) f[j] = there ? f[j] * a.scale : 0.0f;
-                slice_store<T>(out, at, D - at, f);
-            }
+            for (int j = 0; j < 8; ++j) f[j] = there ? f[j] * a.scale : 0.0f;
+            slice_store<T>(out, at, D - at, f);
         }
     }
 }
@@ -385,9 +376,12 @@ EmbedPlan embed_plan(int tokens, int vocab, int dim)
     const int64_t tile = std::max((int64_t)1024, ((int64_t)tokens + 63) / 64);
     p.tile = (int)((tile + SORT_THREADS - 1) / SORT_THREADS * SORT_THREADS);
     p.tiles = (int)(((int64_t)tokens + p.tile - 1) / p.tile);
-    // pieces of 8 tokens, of more where there would be over 4096 (an id may have all of them)
+    // pieces of 8 tokens, of more where there would be over 2048 waves for them: few pieces leave the second kernel less to add (16384 tokens of 2048 columns, an eighth
+    // of them with ids that many share: 24.6 and 6 us of the two kernels with 512 pieces, 24.8 and 17 with 2048), too few leave the first short of
+    // loads (65536 of 1024: 31 and 8 us with 512, 25 and 8 with 1024, 27 and 10 with 4096)
+    const int64_t most = std::max((int64_t)512, 2048 / (((int64_t)dim + WAVE * 8 - 1) / (WAVE * 8)));
     p.piece = SPILL;
-    while (((int64_t)tokens + p.piece - 1) / p.piece > 4096) p.piece *= 2;
+    while (((int64_t)tokens + p.piece - 1) / p.piece > most) p.piece *= 2;
     p.pieces = (int)(((int64_t)tokens + p.piece - 1) / p.piece);
     auto take = [&](size_t bytes) {
         const size_t at = p.total;
@@ -407,16 +401,17 @@ EmbedPlan embed_plan(int tokens, int vocab, int dim)
 template <typename E, typename T, typename I>
 void embed_forward(const EmbedArgs& a, hipStream_t st)
 {
-    auto launch = [&](auto g, auto v) {
-        constexpr int G = decltype(g)::value, V = decltype(v)::value, SIDE = 256 / G;
+    auto launch = [&](auto g) {
+        constexpr int G = decltype(g)::value, SIDE = 256 / G;
         const int64_t n = ((int64_t)a.tokens + SIDE - 1) / SIDE;
-        hipLaunchKernelGGL((embed_fwd_kernel<E, T, I, G, V>), dim3((unsigned)std::min(n, (int64_t)65536)), dim3(256), 0, st, a);
+        hipLaunchKernelGGL((embed_fwd_kernel<E, T, I, G>), dim3((unsigned)std::min(n, (int64_t)65536)), dim3(256), 0, st, a);
     };
-    if (a.dim <= 8 * 8) launch(std::integral_constant<int, 8>{}, std::integral_constant<int, 1>{});
-    else if (a.dim <= 64 * 8) launch(std::integral_constant<int, 64>{}, std::integral_constant<int, 1>{});
-    else if (a.dim <= 128 * 8) launch(std::integral_constant<int, 128>{}, std::integral_constant<int, 1>{});
-    else if (a.tokens < 8192) launch(std::integral_constant<int, 256>{}, std::integral_constant<int, 1>{});
-    else launch(std::integral_constant<int, 64>{}, std::integral_constant<int, 4>{});
+    // as many lanes as a row has slices: a row takes two trips to memory, one behind the other, and short waves leave room for others' (a wave a row with four
+    // slices a lane instead: 16384 rows of 2048 bf16 22.1 us against 20.9, of 8192 107 against 99; of 256 rows of 2048 3.5 against 2.5)
+    if (a.dim <= 8 * 8) launch(std::integral_constant<int, 8>{});
+    else if (a.dim <= 64 * 8) launch(std::integral_constant<int, 64>{});
+    else if (a.dim <= 128 * 8) launch(std::integral_constant<int, 128>{});
+    else launch(std::integral_constant<int, 256>{});
 }
 template <typename E, typename I, bool PAST>
 void embed_sort(const EmbedArgs& a, bool place, dim3 grid, hipStream_t st)
