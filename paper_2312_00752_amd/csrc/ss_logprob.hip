@@ -445,13 +445,15 @@ struct LogprobPlan {
     int pieces, piece, parts;
     size_t bytes;
 };
-// Rows are cut where there are fewer than 2048 workgroups of them, into pieces of one step of a workgroup at least: a wave's choice among its 2048 columns takes
-// as long as their sums (64 x 51200 bf16 with eight alternatives in pieces of 2048: 16 us).  The same with and without alternatives, so that the sums are the same to the bit.
+// Fewer than 256 rows are cut, for some 512 workgroups, into pieces of one step of a workgroup at least.  Of 51200 bf16 columns: 64 rows 4.5 us and 3.5 to join them,
+// whole 7.2, with eight alternatives 7.4 and 4.8, whole 16.8; 256 rows whole 8.2, in two pieces 8.3 and 3.4; 512 whole 12.2, in four 12.8 and 4.2.  Smaller
+// pieces: a wave's choice among its 2048 columns takes as long as their sums (64 rows with eight alternatives in pieces of 2048: 12.9 and 7.6).  The same
+// with and without alternatives, so that the sums are the same to the bit.
 LogprobPlan logprob_plan(int rows, int vocab, int top)
 {
     LogprobPlan p = {1, vocab, 1, 0};
-    if (vocab <= LOGPROB_WAVE || rows >= 2048) return p;
-    const int step = LOGPROB_STEP, units = (vocab + step - 1) / step, want = std::min({(2048 + rows - 1) / rows, units, 1024});
+    if (vocab <= LOGPROB_WAVE || rows >= 256) return p;
+    const int step = LOGPROB_STEP, units = (vocab + step - 1) / step, want = std::min({(512 + rows - 1) / rows, units, 1024});
     const int each = (units + want - 1) / want;
     p.piece = each * step;
     p.pieces = (units + each - 1) / each;
