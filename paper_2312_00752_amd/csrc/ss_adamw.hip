@@ -2,15 +2,18 @@
 // include/ss_adamw.h).
 //
 // Every element is read and written once, 28 bytes of a float32 parameter with float32 moments and 16 with 8-bit ones, so a step is
-// bound by HBM, and for small tensors by a launch.  The tensors' pointers travel in the kernel's arguments, as many as these hold, so nothing
-// has to be copied to the device before; a workgroup finds the tensor that its chunk of elements belongs to.  A wave has 256 elements, a block of the
-// 8-bit moments, four consecutive ones a lane.  The number of steps taken is read by all workgroups and counted by the last that ends.
+// bound by HBM (134 million float32 716 us, 5.2 TB/s; 126 million bf16 with float32 copies and 8-bit moments 389 us, 5.2 TB/s), and for small
+// tensors by a launch (0.2 million elements in 16 tensors 5.6 us).  The tensors' pointers travel in the kernel's arguments, as many as these hold, so
+// nothing has to be copied to the device before; a workgroup finds the tensor that its chunk of elements belongs to.  A wave has 256 elements, a
+// block of the 8-bit moments, four consecutive ones a lane.  The number of steps taken is read by all workgroups and counted by the last to say so.
 #include <hip/hip_runtime.h>
 #include <algorithm>
 #include <cmath>
+#include <type_traits>
 
 #include "ss_adamw.h"
 #include "ss_round8.h"
+#include "ss_slices.h"
 
 namespace ss {
 
@@ -275,14 +278,39 @@ __global__ __launch_bounds__(ADAMW_THREADS) void adamw_kernel(const AdamwArgs a)
     if (a.last && !first) say();
 }
 
-template <bool SIGN, typename T>
+// 16 bytes of the result a lane.  PAST: it goes past the caches.  Bound by HBM: 126 million bf16 (378 MB) 62 us, 6.1 TB/s (81 through the caches).
+template <bool SIGN, typename T, bool PAST>
 __global__ __launch_bounds__(256) void adamw_values_kernel(const void* codes, const float* scale, T* out, int64_t n)
 {
-    for (int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4; i < n; i += (int64_t)gridDim.x * 1024) {
-        const int have = (int)min(n - i, (int64_t)4);
-        float v[4];
-        decode<SIGN>(load_codes<false>(static_cast<const uint8_t*>(codes) + i, have), scale[i / SS_ADAMW_BLOCK], v);
-        store4<false>(out + i, have, v);
+    constexpr int N = 16 / sizeof(T);
+    for (int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * N; i < n; i += (int64_t)gridDim.x * 256 * N) {
+        const uint8_t* q = static_cast<const uint8_t*>(codes) + i;
+        const int have = (int)min(n - i, (int64_t)N);
+        const float s = scale[i / SS_ADAMW_BLOCK];
+        float v[N / 4][4];
+        if (have == N) {
+            uint32_t c[N / 4];
+            if constexpr (N == 8) {
+                const u32x2v w = load_any<u32x2v>(q, 0u);
+                c[0] = w.x;
+                c[1] = w.y;
+            } else {
+                c[0] = load_any<uint32_t>(q, 0u);
+            }
+#pragma unroll
+            for (int k = 0; k < N / 4; ++k) decode<SIGN>(c[k], s, v[k]);
+            u32x4 x;
+            if constexpr (N == 8) x = u32x4{pack_bf16x2(v[0][0], v[0][1]), pack_bf16x2(v[0][2], v[0][3]), pack_bf16x2(v[1][0], v[1][1]), pack_bf16x2(v[1][2], v[1][3])};
+            else x = u32x4{__float_as_uint(v[0][0]), __float_as_uint(v[0][1]), __float_as_uint(v[0][2]), __float_as_uint(v[0][3])};
+            if constexpr (PAST) store_past(out + i, x);
+            else store_any(out + i, 0u, x);
+        } else {
+#pragma unroll
+            for (int k = 0; k < N / 4; ++k) {
+                decode<SIGN>(load_codes<false>(q + 4 * k, have - 4 * k), s, v[k]);
+                store4<false>(out + i + 4 * k, have - 4 * k, v[k]);
+            }
+        }
     }
 }
 
@@ -336,8 +364,8 @@ int ss_adamw_step(const ss_adamw_params* p, void* stream)
     a.beta2 = (float)p->beta2; a.rest2 = (float)(1.0 - p->beta2);
     a.log1 = std::log(p->beta1); a.log2 = std::log(p->beta2);
     a.lr_device = p->lr_device; a.grad_scale = p->grad_scale;
-    // 512 workgroups, more only where each has eight steps.  Float32, 1 million elements in 512 / 1024 workgroups: 9.2 / 11.4 us; 4 million in 512 / 2048: 22 / 27; 67 million with
-    // eight / sixteen steps: 358 / 366.
+    // 512 workgroups, more only where each has eight steps.  Float32, 1 million elements in 512 / 1024 workgroups: 9.2 / 17.3 us; 4 million in
+    // 512 / 1366: 22 / 27; 67 million with eight / sixteen steps: 358 / 366.
     int64_t chunk = std::min(all / (ss::ADAMW_STEP * (int64_t)512) + 1, (int64_t)8) * ss::ADAMW_STEP;
     const hipStream_t st = static_cast<hipStream_t>(stream);
     int k = 0;
@@ -382,12 +410,18 @@ int ss_adamw_values(const ss_adamw_values_params* p, void* stream)
     if (p->n == 0) return SS_OK;
     if (!p->codes || !p->scale || !p->out) return SS_ERR_NULL;
     if (!aligned_to(p->scale, 4) || !aligned_to(p->out, bytes_of(p->out_dtype))) return SS_ERR_ALIGN;
-    const dim3 grid((unsigned)std::min((p->n + 1023) / 1024, (int64_t)65536));
     const hipStream_t st = static_cast<hipStream_t>(stream);
-    auto launch = [&](auto t) {
+    auto with = [&](auto t, auto past) {
         typedef decltype(t) T;
-        if (p->with_sign) hipLaunchKernelGGL((ss::adamw_values_kernel<true, T>), grid, dim3(256), 0, st, p->codes, p->scale, static_cast<T*>(p->out), p->n);
-        else hipLaunchKernelGGL((ss::adamw_values_kernel<false, T>), grid, dim3(256), 0, st, p->codes, p->scale, static_cast<T*>(p->out), p->n);
+        constexpr bool PAST = decltype(past)::value;
+        constexpr int64_t EACH = 256 * 16 / sizeof(T);
+        const dim3 grid((unsigned)std::min((p->n + EACH - 1) / EACH, (int64_t)65536));
+        if (p->with_sign) hipLaunchKernelGGL((ss::adamw_values_kernel<true, T, PAST>), grid, dim3(256), 0, st, p->codes, p->scale, static_cast<T*>(p->out), p->n);
+        else hipLaunchKernelGGL((ss::adamw_values_kernel<false, T, PAST>), grid, dim3(256), 0, st, p->codes, p->scale, static_cast<T*>(p->out), p->n);
+    };
+    auto launch = [&](auto t) {
+        if (p->n * (int64_t)sizeof(t) > ss::STREAM_BYTES) with(t, std::true_type());
+        else with(t, std::false_type());
     };
     if (p->out_dtype == SS_F32) launch(float());
     else launch(ss::bf16_t());

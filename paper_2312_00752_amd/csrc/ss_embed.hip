@@ -1,6 +1,6 @@
 // Embedding of token ids and its gradient for gfx950, with the C-ABI entry points (see include/ss_embed.h).
 //
-// Forward: rows of a table are copied, so it is bound by HBM (and for few tokens by a launch).
+// Forward: rows of a table are copied, so it is bound by HBM (16384 rows of 2048 float32 as bf16, 201 MB, 31 us, 6.4 TB/s) and for few tokens by a launch.
 // Backward: every row of the table's gradient is written, most of them with zeros, and every token's row is read once.  To add up a row
 // without atomics, and always in the same order, the tokens are sorted by id first: a radix sort, least digit first and stable, so
 // that the tokens of an id stay in order.  Its launches are short and leave most of the chip idle, so each also fills a share
@@ -85,7 +85,8 @@ constexpr int DIGIT_BITS = 9, DIGITS = 1 << DIGIT_BITS;
 constexpr int FILL_STORES = 4;                 // of 16 bytes, of a thread
 constexpr int64_t FILL_WORKGROUPS = 1 << 20;
 
-// The workgroups behind the sorting ones set a share of the gradient to zero, in stretches of four words a thread: 105 MB in 16 us.  PAST: past the caches.
+// The workgroups behind the sorting ones set a share of the gradient to zero, in stretches of four words a thread.  PAST: past the caches.
+// 105 MB beside the sort of 16384 ids 18 us a launch, 5.7 TB/s; the same zeros in a launch of their own 15.
 template <typename E, bool PAST>
 __device__ __forceinline__ void fill(const EmbedArgs& a, int64_t wg, int64_t wgs)
 {
@@ -228,8 +229,9 @@ __device__ __forceinline__ float* part_of(const EmbedArgs& a, int64_t piece, int
 
 // A wave has a piece and 512 columns.  It adds up every id whose tokens begin in the piece, and goes on behind its end where no more than SPILL tokens of the
 // last one follow; of longer ones it leaves its share.  The share of an id that began before the piece: the same, and nothing where the wave
-// before goes on to its end.  Ids and places come 64 at once, a lane each, eight rows are requested at once.
-constexpr int SPILL = 8;   // a piece has that many at least
+// before goes on to its end.  Ids and places come 64 at once, a lane each, eight rows are requested at once.  Bound by HBM: 65536 rows of 1024 bf16 (135 MB) for
+// 256 ids 25 us, 5.5 TB/s; 16384 of 2048 for 51200 ids, most of which have one row or none (195 MB), 37.
+constexpr int SPILL = 8;   // a piece has that many at least (1024 tokens of 1024 columns: 5.4 us, with 16 7.4)
 template <typename E, typename T>
 __global__ __launch_bounds__(256) void embed_sum_kernel(EmbedArgs a)
 {
@@ -299,7 +301,8 @@ __global__ __launch_bounds__(256) void embed_sum_kernel(EmbedArgs a)
 }
 
 // The rows of ids that go on for more than SPILL tokens behind the piece that they begin in: a workgroup for 512 columns of one, whose waves
-// take a share of its pieces each.
+// take a share of its pieces each (four waves instead of 16: 38 us against 17 where one id has 336 pieces, as in text, 6 against 10 where all
+// have 16).  Bound by the few workgroups' trips to memory: 4 us without any such id, 6 with some, 36 where one id has all of 65536 tokens.
 constexpr int JOIN_WAVES = 16, JOIN_WORKGROUPS = 256;
 template <typename E>
 __global__ __launch_bounds__(JOIN_WAVES * WAVE) void embed_join_kernel(EmbedArgs a)
@@ -376,9 +379,9 @@ EmbedPlan embed_plan(int tokens, int vocab, int dim)
     const int64_t tile = std::max((int64_t)1024, ((int64_t)tokens + 63) / 64);
     p.tile = (int)((tile + SORT_THREADS - 1) / SORT_THREADS * SORT_THREADS);
     p.tiles = (int)(((int64_t)tokens + p.tile - 1) / p.tile);
-    // pieces of 8 tokens, of more where there would be over 2048 waves for them: few pieces leave the second kernel less to add (16384 tokens of 2048 columns, an eighth
-    // of them with ids that many share: 24.6 and 6 us of the two kernels with 512 pieces, 24.8 and 17 with 2048), too few leave the first short of
-    // loads (65536 of 1024: 31 and 8 us with 512, 25 and 8 with 1024, 27 and 10 with 4096)
+    // pieces of 8 tokens, of more where there would be over 2048 waves for them: few pieces leave the second kernel less to add (16384 tokens of
+    // 2048 columns, a sixth of them one id's: 24.6 and 6 us of the two kernels with 512 pieces, 24.8 and 17 with 2048), too few leave the first
+    // short of loads (65536 of 1024: 31 and 8 us with 512, 25 and 8 with 1024, 27 and 10 with 4096)
     const int64_t most = std::max((int64_t)512, 2048 / (((int64_t)dim + WAVE * 8 - 1) / (WAVE * 8)));
     p.piece = SPILL;
     while (((int64_t)tokens + p.piece - 1) / p.piece > most) p.piece *= 2;
