@@ -301,7 +301,7 @@ __global__ __launch_bounds__(256) void adamw_values_kernel(const void* codes, co
             for (int k = 0; k < N / 4; ++k) decode<SIGN>(c[k], s, v[k]);
             u32x4 x;
             if constexpr (N == 8) x = u32x4{pack_bf16x2(v[0][0], v[0][1]), pack_bf16x2(v[0][2], v[0][3]), pack_bf16x2(v[1][0], v[1][1]), pack_bf16x2(v[1][2], v[1][3])};
-            else x = u32x4{__float_as_uint(v[0][0]), __float_as_uint(v[0][1]), __float_as_uint(v[0][2]), __float_as_uint(v[0][3])};
+            else x = words16<float>::pack(v[0]);
             if constexpr (PAST) store_past(out + i, x);
             else store_any(out + i, 0u, x);
         } else {

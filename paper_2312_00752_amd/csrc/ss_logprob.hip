@@ -362,11 +362,11 @@ __global__ __launch_bounds__(64) void logprob_join_kernel(LogprobArgs a)
 
 // ---- backward -------------------------------------------------------------------------------------
 // G lanes a row or piece of one, all of its slices requested at once.  PAST: the gradient goes past the caches.  Bound by HBM: 8192 x 51200 bf16 (1678 MB) 276 us,
-// 6.1 TB/s (a part of the logits is in a cache from the forward pass); 777 x 50021 float32 (311 MB) 59, 5.3 TB/s.
+// 6.1 TB/s (a part of the logits is in a cache from the forward pass); 777 x 50021 float32 (311 MB) 50, 6.2 TB/s.
 template <typename T, typename I, int G, bool PAST>
 __global__ __launch_bounds__(256) void logprob_bwd_kernel(LogprobArgs a)
 {
-    constexpr int V = 4, SIDE = 256 / G;
+    constexpr int N = 16 / sizeof(T), V = 32 / N, SIDE = 256 / G;
     const int gl = threadIdx.x % G;
     const unsigned group = blockIdx.x * SIDE + threadIdx.x / G;
     // the last rows first: the forward pass, which has read them last, may have left them in a cache
@@ -378,11 +378,13 @@ __global__ __launch_bounds__(256) void logprob_bwd_kernel(LogprobArgs a)
     const float dl = a.dlogp && k >= 0 && some ? a.dlogp[row] : 0.0f, dh = a.dentropy && some ? a.dentropy[row] : 0.0f;
     T* out = static_cast<T*>(a.dlogits) + (int64_t)row * W;
     if (dl == 0.0f && dh == 0.0f) {
-        const float z[8] = {};
 #pragma unroll
         for (int v = 0; v < V; ++v) {
-            const int at = from + (v * G + gl) * 8;
-            slice_store<T>(out, at, W - at, z);
+            const int at = from + (v * G + gl) * N;
+            if (at + N <= W) store_any(out + at, 0u, u32x4{0u, 0u, 0u, 0u});
+            else {
+                for (int j = 0; at + j < W; ++j) out[at + j] = (T)0;
+            }
         }
         return;
     }
@@ -390,53 +392,59 @@ __global__ __launch_bounds__(256) void logprob_bwd_kernel(LogprobArgs a)
     const float m = a.max[row], ls = logf(inv);
     // dx = -p (dl + dh (log p + H)) = -p (c0 + dh d), d = x - m
     const float c0 = dh == 0.0f ? dl : fmaf(dh, ls + a.entropy[row], dl), c1 = -c0 * inv;
-    auto gradient = [&](float (&f)[8], int at) {
+    auto gradient = [&](float (&f)[N], int at) {
         if (dh == 0.0f) {
 #pragma unroll
-            for (int j = 0; j < 8; ++j) f[j] = exp_of(f[j] - m) * c1;
+            for (int j = 0; j < N; ++j) f[j] = exp_of(f[j] - m) * c1;
         } else {
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
+            for (int j = 0; j < N; ++j) {
                 const float d = f[j] - m;
                 f[j] = -(exp_of(d) * inv) * fmaf(dh, fmaxf(d, FAR), c0);
             }
         }
-        if ((unsigned)(k - at) < 8u) {
+        if ((unsigned)(k - at) < (unsigned)N) {
 #pragma unroll
-            for (int j = 0; j < 8; ++j) f[j] += at + j == k ? dl : 0.0f;
+            for (int j = 0; j < N; ++j) f[j] += at + j == k ? dl : 0.0f;
         }
     };
-    typename io8<T>::raw raw[V];
-    float f[8];
-    if (from + V * G * 8 <= W) {   // loads and stores need no bounds
+    u32x4 raw[V];
+    float f[N];
+    if (from + V * G * N <= W) {   // loads and stores need no bounds
 #pragma unroll
-        for (int v = 0; v < V; ++v) raw[v] = io8<T>::load_elem(x + from + (v * G + gl) * 8, 0u);
+        for (int v = 0; v < V; ++v) raw[v] = load_any<u32x4>(x + from + (v * G + gl) * N, 0u);
 #pragma unroll
         for (int v = 0; v < V; ++v) {
-            const int at = from + (v * G + gl) * 8;
-            io8<T>::unpack(raw[v], f);
+            const int at = from + (v * G + gl) * N;
+            words16<T>::unpack(raw[v], f);
             gradient(f, at);
-            if constexpr (PAST) slice_store_past(out + at, f);
-            else io8<T>::store_elem(out + at, 0u, io8<T>::pack(f), 8);
+            if constexpr (PAST) store_past(out + at, words16<T>::pack(f));
+            else store_any(out + at, 0u, words16<T>::pack(f));
         }
         return;
     }
 #pragma unroll
     for (int v = 0; v < V; ++v) {
-        const int at = from + (v * G + gl) * 8;
-        if (at + 8 <= W) raw[v] = io8<T>::load_elem(x + at, 0u);
+        const int at = from + (v * G + gl) * N;
+        if (at + N <= W) raw[v] = load_any<u32x4>(x + at, 0u);
     }
 #pragma unroll
     for (int v = 0; v < V; ++v) {
-        const int at = from + (v * G + gl) * 8;
+        const int at = from + (v * G + gl) * N;
         if (at >= W) break;
-        if (at + 8 <= W) io8<T>::unpack(raw[v], f);
+        const bool full = at + N <= W;
+        if (full) words16<T>::unpack(raw[v], f);
         else {
 #pragma unroll
-            for (int j = 0; j < 8; ++j) f[j] = at + j < W ? io_to_f32<T>(x[at + j]) : 0.0f;
+            for (int j = 0; j < N; ++j) f[j] = at + j < W ? io_to_f32<T>(x[at + j]) : 0.0f;
         }
         gradient(f, at);
-        slice_store<T>(out, at, W - at, f);
+        if (full) store_any(out + at, 0u, words16<T>::pack(f));
+        else {
+#pragma unroll
+            for (int j = 0; j < N; ++j)
+                if (at + j < W) out[at + j] = f32_to_io<T>(f[j]);
+        }
     }
 }
 
