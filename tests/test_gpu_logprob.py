@@ -343,3 +343,12 @@ def test_longest_row():
     grad = B.ss_logprob_bwd(x, stats, t, dlogp=torch.ones(1, device="cuda"))
     for k, want in ((5, -p[1]), (vocab - 3, 1 - p[0]), (0, -p[2]), (vocab - 1, -p[2]), (vocab // 2, -p[2])):
         assert abs(grad[0, k].item() - want) <= (2.0 ** -9 + 64 * 44 * 2.0 ** -24) * abs(want)
+
+
+@pytest.mark.parametrize("io", ["f32", "bf16"])
+def test_masked_target(io):
+    """A target that the mask rules out: -infinity, and the gradient of the formula."""
+    for vocab in (300, 9001):
+        rng, x, t, dl, dh = make(4, vocab, io, vocab)
+        x[np.arange(4), t] = -np.inf
+        compare(x, t, 3, io, dl, dh)
