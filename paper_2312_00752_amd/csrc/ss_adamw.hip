@@ -2,8 +2,8 @@
 // include/ss_adamw.h).
 //
 // Every element is read and written once, 28 bytes of a float32 parameter with float32 moments and 16 with 8-bit ones, so a step is
-// bound by HBM (134 million float32 716 us, 5.2 TB/s; 126 million bf16 with float32 copies and 8-bit moments 389 us, 5.2 TB/s), and for small
-// tensors by a launch (0.2 million elements in 16 tensors 5.6 us).  The tensors' pointers travel in the kernel's arguments, as many as these hold, so
+// bound by HBM (67 million float32 350 us, 5.4 TB/s; 126 million bf16 with float32 copies and 8-bit moments 356 us, 5.7 TB/s), and for small
+// tensors by a launch (0.2 million elements in 16 tensors 4.9 us).  The tensors' pointers travel in the kernel's arguments, as many as these hold, so
 // nothing has to be copied to the device before; a workgroup finds the tensor that its chunk of elements belongs to.  A wave has 256 elements, a
 // block of the 8-bit moments, four consecutive ones a lane.  The number of steps taken is read by all workgroups and counted by the last to say so.
 #include <hip/hip_runtime.h>
@@ -18,7 +18,6 @@
 namespace ss {
 
 constexpr int ADAMW_TENSORS = 48;      // of a launch: arguments have 4 KB
-constexpr int ADAMW_THREADS = 256, ADAMW_STEP = ADAMW_THREADS * 4;   // elements of a workgroup and step
 constexpr float ADAMW_LEAST = 7.88860905e-31f;   // 2^-100
 
 struct AdamwTensor {
@@ -169,14 +168,14 @@ struct StepFactors {
     uint32_t step;
 };
 // A workgroup's chunk of a tensor, from element `from` on.  P: the parameter's type; MASTER: its float32 copy is updated; R: the gradient's.
-template <int BITS, typename P, bool MASTER, typename R, bool FULL>
+template <int BITS, int THREADS, typename P, bool MASTER, typename R, bool FULL>
 __device__ __forceinline__ void adamw_chunk(const AdamwArgs& a, const AdamwTensor& e, int64_t from, int n, const StepFactors& f)
 {
 #pragma clang fp contract(off)   // the moments are what the header's products and sums give, each rounded
     P* const param = static_cast<P*>(e.param) + from;
     const R* const grad = static_cast<const R*>(e.grad) + from;
     float* const master = MASTER ? e.master + from : nullptr;
-    for (int i0 = 0; i0 < n; i0 += ADAMW_STEP) {
+    for (int i0 = 0; i0 < n; i0 += THREADS * 4) {
         const int i = i0 + threadIdx.x * 4, have = FULL ? 4 : max(min(n - i, 4), 0);
         float p[4], g[4], m[4], v[4], s[4];
         if constexpr (MASTER) load4<FULL>(master + i, have, p);
@@ -222,15 +221,15 @@ __device__ __forceinline__ void adamw_chunk(const AdamwArgs& a, const AdamwTenso
         }
     }
 }
-template <int BITS, typename P, bool MASTER, typename R>
+template <int BITS, int THREADS, typename P, bool MASTER, typename R>
 __device__ __forceinline__ void adamw_chunk_of(const AdamwArgs& a, const AdamwTensor& e, int64_t from, int n, const StepFactors& f)
 {
-    if (n % ADAMW_STEP == 0) adamw_chunk<BITS, P, MASTER, R, true>(a, e, from, n, f);
-    else adamw_chunk<BITS, P, MASTER, R, false>(a, e, from, n, f);
+    if (n % (THREADS * 4) == 0) adamw_chunk<BITS, THREADS, P, MASTER, R, true>(a, e, from, n, f);
+    else adamw_chunk<BITS, THREADS, P, MASTER, R, false>(a, e, from, n, f);
 }
 
-template <int BITS>
-__global__ __launch_bounds__(ADAMW_THREADS) void adamw_kernel(const AdamwArgs a)
+template <int BITS, int THREADS>
+__global__ __launch_bounds__(THREADS) void adamw_kernel(const AdamwArgs a)
 {
     const int taken = __builtin_amdgcn_readfirstlane(a.count[0]);
     int k = 0, above = a.tensors;   // the tensor that has this chunk: start[k] <= blockIdx.x < start[above]
@@ -244,14 +243,14 @@ __global__ __launch_bounds__(ADAMW_THREADS) void adamw_kernel(const AdamwArgs a)
         __syncthreads();                  // all of the workgroup have read the count; the last workgroup that says so writes it
     }
     // A workgroup's word costs 13 ns, one behind the other: said first where each has one step to do (the others wait for memory meanwhile), else
-    // last, when they no longer stand in a queue (16 million elements, 8 bits: 45 us against 65 with the word first).
+    // last, when they no longer stand in a queue (16 million elements, 8 bits, in 2048 workgroups: 45 us against 65 with the word first).
     auto say = [&]() {
         if (threadIdx.x == 0 && atomicAdd(&a.count[1], 1) == (int)gridDim.x - 1) {
             a.count[1] = 0;
             a.count[0] = taken + 1;
         }
     };
-    const bool first = a.chunk == ADAMW_STEP || a.tensors == 0;
+    const bool first = a.chunk == THREADS * 4 || a.tensors == 0;
     if (a.last && first) say();
     if (a.tensors == 0) return;
     StepFactors f;
@@ -267,18 +266,19 @@ __global__ __launch_bounds__(ADAMW_THREADS) void adamw_kernel(const AdamwArgs a)
     const int64_t from = (int64_t)((int)blockIdx.x - a.start[k]) * a.chunk;
     const int n = (int)min((int64_t)a.chunk, e.n - from);
     if (a.low_grad[k]) {
-        if (!a.low_param[k]) adamw_chunk_of<BITS, float, false, bf16_t>(a, e, from, n, f);
-        else if (e.master) adamw_chunk_of<BITS, bf16_t, true, bf16_t>(a, e, from, n, f);
-        else adamw_chunk_of<BITS, bf16_t, false, bf16_t>(a, e, from, n, f);
+        if (!a.low_param[k]) adamw_chunk_of<BITS, THREADS, float, false, bf16_t>(a, e, from, n, f);
+        else if (e.master) adamw_chunk_of<BITS, THREADS, bf16_t, true, bf16_t>(a, e, from, n, f);
+        else adamw_chunk_of<BITS, THREADS, bf16_t, false, bf16_t>(a, e, from, n, f);
     } else {
-        if (!a.low_param[k]) adamw_chunk_of<BITS, float, false, float>(a, e, from, n, f);
-        else if (e.master) adamw_chunk_of<BITS, bf16_t, true, float>(a, e, from, n, f);
-        else adamw_chunk_of<BITS, bf16_t, false, float>(a, e, from, n, f);
+        if (!a.low_param[k]) adamw_chunk_of<BITS, THREADS, float, false, float>(a, e, from, n, f);
+        else if (e.master) adamw_chunk_of<BITS, THREADS, bf16_t, true, float>(a, e, from, n, f);
+        else adamw_chunk_of<BITS, THREADS, bf16_t, false, float>(a, e, from, n, f);
     }
     if (a.last && !first) say();
 }
 
-// 16 bytes of the result a lane.  PAST: it goes past the caches.  Bound by HBM: 126 million bf16 (378 MB) 62 us, 6.1 TB/s (81 through the caches).
+// 16 bytes of the result a lane.  PAST: it goes past the caches.  Bound by HBM: 126 million bf16 (378 MB) 58 us, 6.5 TB/s (65 through the
+// caches; behind a step 70).
 template <bool SIGN, typename T, bool PAST>
 __global__ __launch_bounds__(256) void adamw_values_kernel(const void* codes, const float* scale, T* out, int64_t n)
 {
@@ -322,7 +322,7 @@ inline bool aligned_to(const void* p, size_t a) { return (reinterpret_cast<uintp
 inline bool known(int32_t dtype) { return dtype == SS_F32 || dtype == SS_BF16; }
 inline size_t bytes_of(int32_t dtype) { return dtype == SS_BF16 ? 2 : 4; }
 constexpr int64_t ADAMW_MOST = (int64_t)1 << 40;           // elements of a tensor
-constexpr int64_t ADAMW_CHUNKS = ((int64_t)1 << 24) - 1;   // of a launch: it has fewer than 2^32 threads
+constexpr int64_t ADAMW_CHUNKS = ((int64_t)1 << 22) - 1;   // of a launch: it has fewer than 2^32 threads
 
 int check_tensor(const ss_adamw_tensor& t, bool eight)
 {
@@ -351,11 +351,12 @@ int ss_adamw_step(const ss_adamw_params* p, void* stream)
     if (!(p->beta1 >= 0.0 && p->beta1 < 1.0) || !(p->beta2 >= 0.0 && p->beta2 < 1.0) || !some(p->eps) || !some(p->weight_decay)) return SS_ERR_UNSUPPORTED;
     if (!p->lr_device && !some(p->lr)) return SS_ERR_UNSUPPORTED;
     const bool eight = p->state_bits == 8;
-    int64_t all = 0;
+    int64_t all = 0, small = 0;   // elements; workgroups of 256 threads for them
     for (int k = 0; k < p->tensors; ++k) {
         const int rc = check_tensor(p->list[k], eight);
         if (rc != SS_OK) return rc;
         all += p->list[k].n;
+        small += (p->list[k].n + 1023) / 1024;
     }
     ss::AdamwArgs a{};
     a.count = p->count;
@@ -364,9 +365,12 @@ int ss_adamw_step(const ss_adamw_params* p, void* stream)
     a.beta2 = (float)p->beta2; a.rest2 = (float)(1.0 - p->beta2);
     a.log1 = std::log(p->beta1); a.log2 = std::log(p->beta2);
     a.lr_device = p->lr_device; a.grad_scale = p->grad_scale;
-    // 512 workgroups, more only where each has eight steps.  Float32, 1 million elements in 512 / 1024 workgroups: 9.2 / 17.3 us; 4 million in
-    // 512 / 1366: 22 / 27; 67 million with eight / sixteen steps: 358 / 366.
-    int64_t chunk = std::min(all / (ss::ADAMW_STEP * (int64_t)512) + 1, (int64_t)8) * ss::ADAMW_STEP;
+    // Few workgroups, for the sake of their words: of 256, 512 or 1024 threads, and 256 of the last, more only where each has two steps.  Float32 in us with
+    // 256 / 512 / 1024 threads: 65536 elements 4.3 / 4.4 / 5.0; 262144 6.2 / 5.0 / 5.2; 2 million 12.3 / 11.2 / 10.2; 67 million 357 / 356 / 350;
+    // 8 bits 5.0 / 5.7 / 6.3; 7.0 / 6.3 / 6.8; 14.2 / 13.6 / 11.6; 214 / 208 / 201.
+    const int threads = small <= 64 ? 256 : (small <= 512 ? 512 : 1024), each = threads * 4;
+    int64_t chunk = std::min(all / (each * (int64_t)256) + 1, (int64_t)(8192 / each)) * each;
+    while (all / chunk > ADAMW_CHUNKS - ss::ADAMW_TENSORS && chunk < (1 << 30)) chunk *= 2;
     const hipStream_t st = static_cast<hipStream_t>(stream);
     int k = 0;
     do {
@@ -396,8 +400,14 @@ int ss_adamw_step(const ss_adamw_params* p, void* stream)
         while (k < p->tensors && p->list[k].n == 0) ++k;
         a.last = k == p->tensors;
         const dim3 grid((unsigned)std::max(chunks, (int64_t)1));
-        if (eight) hipLaunchKernelGGL(ss::adamw_kernel<8>, grid, dim3(ss::ADAMW_THREADS), 0, st, a);
-        else hipLaunchKernelGGL(ss::adamw_kernel<32>, grid, dim3(ss::ADAMW_THREADS), 0, st, a);
+        auto launch = [&](auto n) {
+            constexpr int THREADS = decltype(n)::value;
+            if (eight) hipLaunchKernelGGL((ss::adamw_kernel<8, THREADS>), grid, dim3(THREADS), 0, st, a);
+            else hipLaunchKernelGGL((ss::adamw_kernel<32, THREADS>), grid, dim3(THREADS), 0, st, a);
+        };
+        if (threads == 256) launch(std::integral_constant<int, 256>());
+        else if (threads == 512) launch(std::integral_constant<int, 512>());
+        else launch(std::integral_constant<int, 1024>());
     } while (!a.last);
     return hipGetLastError() == hipSuccess ? SS_OK : SS_ERR_LAUNCH;
 }
