@@ -139,6 +139,17 @@ def test_sizes(kind, bits):
 
 
 @pytest.mark.parametrize("bits", [8, 32])
+@pytest.mark.parametrize("sizes", [[65536], [1, 60000, 3, 5000], [65537], [70001, 2047, 2049, 1, 300000], [530001, 4095, 4097, 255],
+                                   [700001, 1, 8191, 8193, 500000, 4096], [1 << 21, 12287, 12289]])
+def test_workgroups(sizes, bits):
+    """Workgroups of every size, with one step and two, whole and cut short."""
+    c = Case(sizes, bits, low_param=True, master=True, seed=len(sizes))
+    for _ in range(2):
+        c.run()
+        c.check()
+
+
+@pytest.mark.parametrize("bits", [8, 32])
 @pytest.mark.parametrize("n", [0, 1, 47, 48, 49, 96, 97, 200])
 def test_many_tensors(n, bits):
     """As many as a launch's arguments hold, and more; the step is counted once."""
