@@ -81,6 +81,19 @@ def test_neighbouring_ids_share_pieces():
     check(np.random.default_rng(0).permutation(ids), len(runs), 2050, "f32", "bf16")
 
 
+# 2048 pieces at 512 columns, 512 at 2048 and more: of 8 tokens up to there, then of 16 and 32
+@pytest.mark.parametrize("n,dim", [(16384, 16), (16385, 16), (40000, 8), (4096, 2056), (4097, 2056), (9000, 1537)])
+def test_longer_pieces(n, dim):
+    rng = np.random.default_rng(n)
+    lengths = []
+    while sum(lengths) < n:   # runs around the pieces' lengths, and some over many pieces
+        lengths.append(int(rng.choice([1, 7, 8, 9, 15, 16, 17, 31, 32, 33, 40, 41, 64, 200, 3000])))
+    ids = np.repeat(np.arange(len(lengths)), lengths)[:n]
+    check(ids, len(lengths), dim, "f32", "f32", seed=n)
+    check(rng.permutation(ids), len(lengths), dim, "bf16", "bf16", seed=n)
+    check(np.full(n, 1), 3, dim, "f32", "bf16", seed=n)
+
+
 @pytest.mark.parametrize("id_type", [torch.int32, torch.int64])
 def test_padding(id_type):
     rng = np.random.default_rng(1)
