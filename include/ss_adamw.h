@@ -21,11 +21,11 @@
  * whose steps grow with the value, as the error that a moment tolerates does.  Between two codes the upper one is taken when
  *     (y - q^2) / (2 q + 1) > u,    y = |m| (127^2 (1 / a))   (sqrt(v) (255^2 (1 / a))),  q = floor(sqrt(y)),
  *     u = ((i c0 + t c1) mod 2^32) / 2^32 cut to 24 bits
- * for element i of its tensor: over the steps, u goes evenly through [0, 1) (a Weyl sequence: c0 and c1 are the fractional parts of sqrt(2) and sqrt(3),
- * for v of sqrt(5) and sqrt(7), in units of 2^-32), so m and sqrt(v) are right in the mean where they move by less than a code's distance;
- * rounded to the nearest, v would not move at all at beta2 = 0.999.  sqrt(v) > 0 has a code of 1 at least, so a parameter's step stays bounded.  The parameter's step takes the moments as they
- * are before they are rounded.  A block whose largest magnitude is below 2^-100 counts as zero (scale 0); one that holds an
- * infinity or NaN has the scale NaN and comes out as NaN.
+ * for element i of its tensor: over the steps, u goes evenly through [0, 1) (a Weyl sequence: c0 and c1 are the fractional parts of sqrt(2) and
+ * sqrt(3), for v of sqrt(5) and sqrt(7), in units of 2^-32), so m and sqrt(v) are right in the mean where they move by less than a code's distance;
+ * rounded to the nearest, v would not move at all at beta2 = 0.999.  sqrt(v) > 0 has a code of 1 at least, so a parameter's step stays bounded.  The
+ * parameter's step takes the moments as they are before they are rounded.  A block whose largest magnitude is below 2^-100 counts as zero (scale 0);
+ * one that holds an infinity or NaN has the scale NaN and comes out as NaN.
  *
  * Rules as in ss_scan.h (device pointers owned by the caller, host-side validation before any device call, SS_OK or a
  * negative SS_ERR_* code, nothing allocated), but pointers need be aligned to their element only.  The list and the tensors' descriptions are

@@ -9,10 +9,9 @@
  * The sums are float32, their terms in an order that the sizes and ids alone decide, so the same call gives the same bits; they are rounded once.
  * Tokens whose id is outside the table have no gradient, whatever their dout holds.
  *
- * Rules as in ss_scan.h (device pointers owned by the caller, dense row-major layouts, outputs overwritten, host-side
- * validation before any device call, SS_OK or a negative SS_ERR_* code, nothing allocated), but pointers need be
- * aligned to their element only.  No output may overlap an input.  tokens == 0 is valid (dtable is then 0).  SS_ERR_UNSUPPORTED: tokens or vocab of 2^31 - 65536 and more, dim of
- * more than 512 x 65535.
+ * Rules as in ss_scan.h (device pointers owned by the caller, dense row-major layouts, outputs overwritten, host-side validation before any device
+ * call, SS_OK or a negative SS_ERR_* code, nothing allocated), but pointers need be aligned to their element only.  No output may overlap an input.
+ * tokens == 0 is valid (dtable is then 0).  SS_ERR_UNSUPPORTED: tokens or vocab of 2^31 - 65536 and more, dim of more than 512 x 65535.
  *      ids            : (tokens)         int64, or int32 with SS_EMBED_IDS_32
  *      table, dtable  : (vocab, dim)     table_dtype
  *      out, dout      : (tokens, dim)    io_dtype

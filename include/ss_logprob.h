@@ -12,9 +12,10 @@
  *     dlogits_j = dlogp ([j = t] - p_j) - dentropy p_j (log p_j + entropy)
  *
  * Logits of -infinity have probability 0 and the gradient 0 (dlogp, if they are the target); exp(x_j - max) below 2^-126 counts as 0.  A row of
- * nothing else has no distribution: the log probabilities in it are -infinity, its entropy and its gradients are 0.  A row that holds +infinity or NaN has the results NaN (top_ids: the columns that are not NaN in the
- * same order, -1 where there are no more).  Without a target (t outside) dlogp is not read into the row's gradient; a row whose dlogp is 0 or not
- * asked for, and whose dentropy is 0 or not given, has the gradient 0 whatever it holds.
+ * nothing else has no distribution: the log probabilities in it are -infinity, its entropy and its gradients are 0.  A row that holds +infinity or
+ * NaN has the results NaN (top_ids: the columns that are not NaN in the same order, -1 where there are no more).  Without a target (t outside) dlogp
+ * is not read into the row's gradient; a row whose dlogp is 0 or not asked for, and whose dentropy is 0 or not given, has the gradient 0 whatever it
+ * holds.
  *
  * What is asked for beside them does not change the bits of logp, entropy and stats.
  *

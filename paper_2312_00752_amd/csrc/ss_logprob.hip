@@ -456,10 +456,10 @@ struct LogprobPlan {
     int pieces, piece, parts;
     size_t bytes;
 };
-// Fewer than 256 rows are cut, for some 512 workgroups, into pieces of one step of a workgroup at least.  Of 51200 bf16 columns: 64 rows
-// 4.5 us and 3.5 to join them, whole 7.2, with eight alternatives 7.4 and 4.8, whole 16.8; 256 rows whole 8.2, in two pieces 8.3 and 3.4; 512 whole 12.2, in four 12.8 and 4.2.  Smaller
-// pieces: a wave's choice among its 2048 columns takes as long as their sums (64 rows with eight alternatives in pieces of 2048: 12.9 and 7.6).  The same
-// with and without alternatives, so that the sums are the same to the bit.
+// Fewer than 256 rows are cut, for some 512 workgroups, into pieces of one step of a workgroup at least.  Of 51200 bf16 columns: 64 rows 4.5 us and
+// 3.5 to join them, whole 7.2, with eight alternatives 7.4 and 4.8, whole 16.8; 256 rows whole 8.2, in two pieces 8.3 and 3.4; 512 whole 12.2, in
+// four 12.8 and 4.2.  Smaller pieces: a wave's choice among its 2048 columns takes as long as their sums (64 rows with eight alternatives in pieces
+// of 2048: 12.9 and 7.6).  The same with and without alternatives, so that the sums are the same to the bit.
 LogprobPlan logprob_plan(int rows, int vocab, int top)
 {
     LogprobPlan p = {1, vocab, 1, 0};
