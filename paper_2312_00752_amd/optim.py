@@ -113,5 +113,7 @@ class AdamW(torch.optim.Optimizer):
                 if name not in ("params", "count"):
                     if name == "lr" and isinstance(mine["lr"], torch.Tensor):
                         mine["lr"].fill_(float(value))
+                    elif isinstance(value, torch.Tensor):   # read onto whichever device
+                        mine[name] = value.to(mine["count"].device, torch.float32 if name == "lr" else value.dtype, copy=True)
                     else:
-                        mine[name] = value.clone() if isinstance(value, torch.Tensor) else value
+                        mine[name] = value
