@@ -16,17 +16,21 @@ class AdamW(torch.optim.Optimizer):
     A group's ``lr`` may be a float32 tensor of one element on the GPU, which a graph reads as it is at its replay."""
 
     def __init__(self, params, lr=1e-3, betas=(0.9, 0.999), eps=1e-8, weight_decay=1e-2, state_bits=32, master=True):
-        if state_bits not in (8, 32):
-            raise ValueError("state_bits must be 8 or 32, got %r" % (state_bits,))
         self._seen = {}   # parameters with a master: their version and memory when the two last agreed
         super().__init__(params, {"lr": lr, "betas": betas, "eps": eps, "weight_decay": weight_decay, "state_bits": state_bits, "master": master})
 
     def add_param_group(self, group):
         super().add_param_group(group)
         group = self.param_groups[-1]
+        refused = None
+        if group["state_bits"] not in (8, 32):
+            refused = "state_bits must be 8 or 32, got %r" % (group["state_bits"],)
+        elif any(p.dtype not in (torch.float32, torch.bfloat16) or not p.is_cuda or not p.is_contiguous() for p in group["params"]):
+            refused = "parameters must be contiguous float32 or bfloat16 tensors on the GPU"
+        if refused:
+            self.param_groups.pop()
+            raise ValueError(refused)
         for p in group["params"]:
-            if p.dtype not in (torch.float32, torch.bfloat16) or not p.is_cuda or not p.is_contiguous():
-                raise ValueError("parameters must be contiguous float32 or bfloat16 tensors on the GPU")
             s = self.state[p]
             eight = group["state_bits"] == 8
             s["m"] = torch.zeros(p.shape, dtype=torch.int8 if eight else torch.float32, device=p.device)

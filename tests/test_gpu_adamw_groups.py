@@ -1,4 +1,4 @@
-"""AdamW's groups: a rate on the device through a file."""
+"""AdamW's groups: a rate on the device through a file, groups that are refused leave the optimiser as it was."""
 import io
 
 import pytest
@@ -51,3 +51,19 @@ def test_rate_through_a_file(theirs, mine, device):
         a.step()
         b.step()
     assert torch.equal(p, q)
+
+
+def test_a_refused_group_is_not_added():
+    p, opt = made(1e-3)
+    more = torch.nn.Parameter(torch.ones(5, device="cuda"))
+    bad = [torch.nn.Parameter(torch.ones(3)), torch.nn.Parameter(torch.ones(3, device="cuda").half()), torch.nn.Parameter(torch.ones(4, 6, device="cuda")[:, ::2])]
+    for group in [{"params": [more, b]} for b in bad] + [{"params": [more], "state_bits": 16}, {"params": [more], "state_bits": 0}]:
+        with pytest.raises(ValueError):
+            opt.add_param_group(group)
+        assert len(opt.param_groups) == 1 and more not in opt.state
+    opt.step()
+    opt.add_param_group({"params": [more], "state_bits": 8})
+    more.grad = torch.ones_like(more)
+    opt.step()
+    assert opt.state[more]["m"].dtype == torch.int8
+    assert [g["count"].tolist() for g in opt.param_groups] == [[2, 0], [1, 0]]
