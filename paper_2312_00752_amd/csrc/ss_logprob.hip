@@ -214,14 +214,25 @@ __global__ __launch_bounds__(256) void logprob_fwd_kernel(LogprobArgs a)
         const float ref = reference(m);
         shift(t, ref);
         t.m = m;
+        // A slice's values one after another, slices as a tree, and only then onto those of the steps before: all one by one, small terms that
+        // together count are lost beside a large one (rows of 50021 with a few large logits: S off by 2.9e-7 in the mean, now by 0.75e-7).
+        float se[V], su[V];
 #pragma unroll
-        for (int v = 0; v < V; ++v)
+        for (int v = 0; v < V; ++v) {
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
                 const float d = f[v][j] - ref, e = exp_of(d);   // NaN stays NaN in e
-                t.s += e;
-                t.u = fmaf(e, fmaxf(d, FAR), t.u);
+                se[v] = j == 0 ? e : se[v] + e;
+                su[v] = j == 0 ? e * fmaxf(d, FAR) : fmaf(e, fmaxf(d, FAR), su[v]);
             }
+        }
+        if constexpr (V == 4) {
+            t.s += (se[0] + se[1]) + (se[2] + se[3]);
+            t.u += (su[0] + su[1]) + (su[2] + su[3]);
+        } else {
+            t.s += se[0] + se[1];
+            t.u += su[0] + su[1];
+        }
         if constexpr (TOP) {
             const int lane = threadIdx.x % WAVE;
             float(*const all)[WAVE] = reinterpret_cast<float(*)[WAVE]>(logits[threadIdx.x / WAVE]);
