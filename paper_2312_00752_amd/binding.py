@@ -916,6 +916,15 @@ def _lend(given, need, device, name):
     return _ptr(given, torch.uint8, None, name), given.numel()
 
 
+def _on_current(*tensors):
+    """The tensors of a call lie on the device whose stream it takes."""
+    if _raw_stream is None:
+        _find_raw_stream()
+    for t in tensors:
+        if t is not None and t.is_cuda and t.get_device() != _device_index():
+            raise ValueError("a tensor lies on %s, the current device is cuda:%d" % (t.device, _device_index()))
+
+
 def _norm_params(x, weight, bias, residual, eps, rms):
     f32 = torch.float32
     if x.dim() < 1:
@@ -959,9 +968,10 @@ def ss_norm_fwd(x, weight=None, bias=None, residual=None, eps=1e-5, out=None, su
         with _current(stream):
             return ss_norm_fwd(x, weight, bias, residual, eps, out, summed, save_stats, None, rms)
     if out is None and summed is None and x.is_cuda:
-        r = (_native or _marshal()).norm_fwd(x, weight, bias, residual, eps, bool(rms), bool(save_stats), _stream(stream))
+        r = (_native or _marshal()).norm_fwd(x, weight, bias, residual, eps, bool(rms), bool(save_stats), _stream(stream), _device_index())
         if r is not None:
             return _result(r)
+    _on_current(x, weight, bias, residual, out, summed)
     p = _norm_params(x, weight, bias, residual, eps, rms)
     summed = _norm_inputs(p, x, residual, summed)
     if out is None:
@@ -983,9 +993,10 @@ def ss_norm_quant(x, weight=None, bias=None, residual=None, eps=1e-5, rms=False,
         with _current(stream):
             return ss_norm_quant(x, weight, bias, residual, eps, rms, summed)
     if summed is None and x.is_cuda:
-        r = (_native or _marshal()).norm_quant(x, weight, bias, residual, eps, bool(rms), _stream(stream))
+        r = (_native or _marshal()).norm_quant(x, weight, bias, residual, eps, bool(rms), _stream(stream), _device_index())
         if r is not None:
             return _result(r)
+    _on_current(x, weight, bias, residual, summed)
     p = NormQuantParams()
     p.fwd = _norm_params(x, weight, bias, residual, eps, rms)
     summed = _norm_inputs(p.fwd, x, residual, summed)
@@ -1012,9 +1023,10 @@ def ss_norm_bwd(dout, s, stats, weight=None, has_bias=False, residual_dtype=None
             return ss_norm_bwd(dout, s, stats, weight, has_bias, residual_dtype, dsummed, eps, workspace, None, rms)
     if workspace is None and dout.is_cuda and (residual_dtype is None or s.dtype == residual_dtype):
         r = (_native or _marshal()).norm_bwd(dout, s, stats, weight, bool(has_bias), residual_dtype is not None, dsummed, eps, bool(rms),
-                                             _stream(stream))
+                                             _stream(stream), _device_index())
         if r is not None:
             return _result(r)
+    _on_current(dout, s, stats, weight, dsummed, workspace)
     p = NormBwdParams()
     p.fwd = _norm_params(dout, weight, None, None, eps, rms)
     p.fwd.io_dtype = _io_code(dout)
@@ -1325,15 +1337,6 @@ def ss_qlinear(x, weight, scale, bias=None, x_seq_last=False, out_seq_last=False
 
 
 # ---------------------------------------------------------------- embedding
-def _on_current(*tensors):
-    """The tensors of a call lie on the device whose stream it takes."""
-    if _raw_stream is None:
-        _find_raw_stream()
-    for t in tensors:
-        if t is not None and t.is_cuda and t.get_device() != _device_index():
-            raise ValueError("a tensor lies on %s, the current device is cuda:%d" % (t.device, _device_index()))
-
-
 def _apart(out, **inputs):
     """``out``, a dense tensor that the caller gave, shares no memory with the inputs that are read while it is written."""
     for name, t in inputs.items():
@@ -1608,7 +1611,7 @@ def ss_adamw_values(codes, scale, dtype=None, stream=None):
 # ---------------------------------------------------------------- gradient functions of the compiled module
 def layer_norm_node(x, weight, bias, residual, eps, rms=False):
     """(out,) or (out, summed) of autograd.layer_norm or rms_norm from the compiled module, or None where it does not serve the call."""
-    r = (_native or _marshal()).layer_norm(x, weight, bias, residual, eps, rms, _stream(None))
+    r = (_native or _marshal()).layer_norm(x, weight, bias, residual, eps, rms, _stream(None), _device_index())
     return r if r is None else _result(r)
 
 

@@ -553,6 +553,14 @@ bool norm_tensors(Args& a, int at, at::Tensor (&t)[4])
         if (!a.none(at + i)) t[i] = THPVariable_Unpack(a.a[at + i]);
     return true;
 }
+// Whether a tensor lies on the device whose stream the call takes.
+bool on_device(const at::Tensor& t, long device) { return t.is_cuda() && t.device().index() == device; }
+bool all_on_device(const at::Tensor (&t)[4], long device)
+{
+    for (const at::Tensor& v : t)
+        if (v.defined() && !on_device(v, device)) return false;
+    return true;
+}
 bool real_number(PyObject* o, double& v)
 {
     if (!PyFloat_CheckExact(o)) return false;
@@ -571,17 +579,17 @@ at::Tensor given(const Optional& t) { return t.has_value() ? *t : at::Tensor(); 
 Optional optional(const at::Tensor& t) { return t.defined() ? Optional(t) : Optional(); }
 void backward_check(int rc) { TORCH_CHECK(rc == SS_OK, "ss_scan error ", rc, ": ", ss_strerror(rc)); }
 
-// norm_fwd(x, weight, bias, residual, eps, rms, save, stream) -> (out, summed or None, stats or None)
+// norm_fwd(x, weight, bias, residual, eps, rms, save, stream, device) -> (out, summed or None, stats or None)
 PyObject* py_norm_fwd(PyObject*, PyObject* const* argv, Py_ssize_t n)
 {
     HANDLE_TH_ERRORS
-    if (n != 8) Py_RETURN_NONE;
+    if (n != 9) Py_RETURN_NONE;
     Args a{argv};
     at::Tensor t[4];
     double eps;
     if (!norm_tensors(a, 0, t) || !real_number(argv[4], eps)) Py_RETURN_NONE;
     void* stream = a.stream(7);
-    if (!a.ok) Py_RETURN_NONE;
+    if (!all_on_device(t, a.number(8)) || !a.ok) Py_RETURN_NONE;
     Norm c;
     int rc;
     {
@@ -593,18 +601,18 @@ PyObject* py_norm_fwd(PyObject*, PyObject* const* argv, Py_ssize_t n)
     END_HANDLE_TH_ERRORS
 }
 
-// norm_quant(x, weight, bias, residual, eps, rms, stream) -> (q, scale, summed or None)
+// norm_quant(x, weight, bias, residual, eps, rms, stream, device) -> (q, scale, summed or None)
 PyObject* py_norm_quant(PyObject*, PyObject* const* argv, Py_ssize_t n)
 {
     HANDLE_TH_ERRORS
-    if (n != 7) Py_RETURN_NONE;
+    if (n != 8) Py_RETURN_NONE;
     Args a{argv};
     at::Tensor t[4];
     double eps;
     if (!norm_tensors(a, 0, t) || !real_number(argv[4], eps)) Py_RETURN_NONE;
     void* stream = a.stream(6);
     ss_norm_quant_params p{};
-    if (!a.ok || !norm_sizes(t[0], p.fwd) || !p.fwd.width) Py_RETURN_NONE;
+    if (!all_on_device(t, a.number(7)) || !a.ok || !norm_sizes(t[0], p.fwd) || !p.fwd.width) Py_RETURN_NONE;
     p.fwd.eps = (float)eps;
     p.fwd.flags = argv[5] == Py_True ? SS_NORM_RMS : 0u;
     p.fwd.x = t[0].data_ptr();
@@ -629,11 +637,11 @@ PyObject* py_norm_quant(PyObject*, PyObject* const* argv, Py_ssize_t n)
     END_HANDLE_TH_ERRORS
 }
 
-// norm_bwd(dout, s, stats, weight, has_bias, has_residual, dsummed, eps, rms, stream) -> dict of gradients
+// norm_bwd(dout, s, stats, weight, has_bias, has_residual, dsummed, eps, rms, stream, device) -> dict of gradients
 PyObject* py_norm_bwd(PyObject*, PyObject* const* argv, Py_ssize_t n)
 {
     HANDLE_TH_ERRORS
-    if (n != 10) Py_RETURN_NONE;
+    if (n != 11) Py_RETURN_NONE;
     Args a{argv};
     ss_norm_params p{};
     const at::Tensor* dout = a.tensor(0);
@@ -648,9 +656,11 @@ PyObject* py_norm_bwd(PyObject*, PyObject* const* argv, Py_ssize_t n)
     a.ptr(3, at::kFloat, {p.width}, true);
     const at::Tensor* more = a.ok && !a.none(6) ? held(a, 6, *dout) : nullptr;
     void* stream = a.stream(9);
+    const long device = a.number(10);
     if (!a.ok || (more && more->scalar_type() != s->scalar_type())) Py_RETURN_NONE;
     const at::Tensor& stats = THPVariable_Unpack(argv[2]);
     const at::Tensor weight = a.none(3) ? at::Tensor() : THPVariable_Unpack(argv[3]), dsummed = more ? *more : at::Tensor();
+    if (!on_device(*dout, device) || !all_on_device({*s, stats, weight, dsummed}, device)) Py_RETURN_NONE;
     NormGrads g;
     int rc;
     {
@@ -718,18 +728,18 @@ struct NormFunction : torch::autograd::Function<NormFunction> {
         return differentiable_once({g.dx, g.dweight, g.dbias, g.dresidual, at::Tensor(), at::Tensor(), at::Tensor()}, {&saved, &grads});
     }
 };
-// layer_norm(x, weight, bias, residual, eps, rms, stream) -> (out,) or (out, summed), with gradients
+// layer_norm(x, weight, bias, residual, eps, rms, stream, device) -> (out,) or (out, summed), with gradients
 PyObject* py_layer_norm(PyObject*, PyObject* const* argv, Py_ssize_t n)
 {
     HANDLE_TH_ERRORS
-    if (n != 7) Py_RETURN_NONE;
+    if (n != 8) Py_RETURN_NONE;
     Args a{argv};
     at::Tensor t[4];
     double eps;
     if (!norm_tensors(a, 0, t) || !real_number(argv[4], eps)) Py_RETURN_NONE;
     const bool rms = argv[5] == Py_True;
     void* stream = a.stream(6);
-    if (!a.ok) Py_RETURN_NONE;
+    if (!all_on_device(t, a.number(7)) || !a.ok) Py_RETURN_NONE;
     torch::autograd::variable_list r;
     try {
         Unlocked u;
@@ -1047,8 +1057,6 @@ PyObject* py_qlinear(PyObject*, PyObject* const* argv, Py_ssize_t n)
 }
 
 // ---- embedding, log probabilities, AdamW -----------------------------------------------------------
-// Whether a tensor lies on the device whose stream the call takes.
-bool on_device(const at::Tensor& t, long device) { return t.is_cuda() && t.device().index() == device; }
 // whole numbers in 64 or 32 bits
 bool whole_type(const at::Tensor& t, uint32_t flag_of_32, uint32_t& flags)
 {
