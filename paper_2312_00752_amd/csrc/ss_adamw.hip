@@ -116,7 +116,7 @@ __device__ __forceinline__ uint32_t wave_max(uint32_t v)
 #undef SS_MAX_FROM
     return (uint32_t)__builtin_amdgcn_readlane((int)v, WAVE - 1);
 }
-// Correctly rounded for what a moment can be: the hardware's root is off by a unit in the last place at most, and a step of Newton's method from there
+// Correctly rounded from 2^-100 on: the hardware's root is off by a unit in the last place at most, and a step of Newton's method from there
 // has an exact residual.  (The compiler's own takes twice as many instructions; the step of 126 million parameters was bound by them.)
 __device__ __forceinline__ float root_of(float v)
 {
@@ -201,6 +201,15 @@ __device__ __forceinline__ void adamw_chunk(const AdamwArgs& a, const AdamwTenso
             m[j] = m[j] * a.beta1 + g[j] * a.rest1;
             v[j] = v[j] * a.beta2 + g[j] * g[j] * a.rest2;
             s[j] = root_of(v[j]);
+        }
+        // below 2^-100 the residual of the root is no normal number, and below 2^-126 neither is v, whose
+        // root the hardware takes as 0 (a step of m / eps: 10^10 for a gradient of 1e-18 and eps of 1e-30)
+        if (fminf(fminf(v[0], v[1]), fminf(v[2], v[3])) < 0x1p-100f) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) s[j] = v[j] < 0x1p-100f ? root_of(v[j] * 0x1p64f) * 0x1p-32f : s[j];
+        }
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
             p[j] = fmaf(-f.rate, m[j] * __builtin_amdgcn_rcpf(fmaf(s[j], f.root, a.eps)), fmaf(-f.decay, p[j], p[j]));
         }
         if constexpr (MASTER) store4<FULL>(master + i, have, p);
