@@ -59,7 +59,7 @@ typedef struct {
     const ss_adamw_tensor *list;
     int32_t *count;                  /* (2), device: steps taken; 0, the call's own while it runs */
     double lr, beta1, beta2;         /* 0 <= beta < 1                                       */
-    double eps, weight_decay;        /* >= 0, finite                                        */
+    double eps, weight_decay;        /* >= 0, finite in float32; eps 0, or 2^-126 and more  */
     const float *lr_device;          /* or NULL; else lr is read there (lr is not)          */
     const float *grad_scale;         /* or NULL: 1                                          */
 } ss_adamw_params;

@@ -358,6 +358,7 @@ int ss_adamw_step(const ss_adamw_params* p, void* stream)
     if (!p->count || (p->tensors > 0 && !p->list)) return SS_ERR_NULL;
     if (!aligned_to(p->count, 4) || !aligned_to(p->lr_device, 4) || !aligned_to(p->grad_scale, 4)) return SS_ERR_ALIGN;
     if (!(p->beta1 >= 0.0 && p->beta1 < 1.0) || !(p->beta2 >= 0.0 && p->beta2 < 1.0) || !some(p->eps) || !some(p->weight_decay)) return SS_ERR_UNSUPPORTED;
+    if (p->eps != 0.0 && p->eps < 0x1p-126) return SS_ERR_UNSUPPORTED;   // the reciprocal of no normal number is infinite: 0 / eps would be NaN
     if (!p->lr_device && !some(p->lr)) return SS_ERR_UNSUPPORTED;
     const bool eight = p->state_bits == 8;
     int64_t all = 0, small = 0;   // elements; workgroups of 256 threads for them
