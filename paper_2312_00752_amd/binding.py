@@ -1288,9 +1288,9 @@ def ss_qlinear(x, weight, scale, bias=None, x_seq_last=False, out_seq_last=False
     if stream is not None:
         with _current(stream):
             return ss_qlinear(x, weight, scale, bias, x_seq_last, out_seq_last, x_scale, dim, out_dtype, out, scratch)
-    if x_scale is None and out is None and scratch is None and out_dtype is None and x.is_cuda:
+    if out is None and scratch is None and (out_dtype is None if x_scale is None else dim is not None) and x.is_cuda:
         r = (_native or _marshal()).qlinear(x, weight, scale, bias, (SS_Q_X_SEQ_LAST if x_seq_last else 0) | (SS_Q_OUT_SEQ_LAST if out_seq_last else 0),
-                                            _stream(stream))
+                                            x_scale, dim, _type_code(out_dtype), _stream(stream))
         if r is not None:
             return _result(r)
     if weight.dim() != 2 or x.dim() < 1:

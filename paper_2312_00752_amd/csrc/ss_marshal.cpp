@@ -1013,32 +1013,50 @@ PyObject* py_gate_step(PyObject*, PyObject* const* argv, Py_ssize_t n)
     END_HANDLE_TH_ERRORS
 }
 
-// qlinear(x, weight, scale, bias, flags, stream) -> out: tokens that are not quantised yet, scratch of the call's own
+// The type of a code of io types; `ok` falls if it is none.
+at::ScalarType type_of_code(long code, bool& ok)
+{
+    if (code == SS_F32) return at::kFloat;
+    if (code != SS_BF16) ok = false;
+    return at::kBFloat16;
+}
+// qlinear(x, weight, scale, bias, flags, x_scale or None, dim, type of the result, stream) -> out, scratch of the call's own; dim and the type are looked at where
+// there is x_scale: the tokens are quantised (else x's)
 PyObject* py_qlinear(PyObject*, PyObject* const* argv, Py_ssize_t n)
 {
     HANDLE_TH_ERRORS
-    if (n != 6) Py_RETURN_NONE;
+    if (n != 9) Py_RETURN_NONE;
     Args a{argv};
     ss_qlinear_params p{};
     const at::Tensor *x = a.tensor(0), *w = a.ok ? a.tensor(1) : nullptr;
     p.flags = (uint32_t)a.number(4);
-    void* stream = a.stream(5);
-    if (!a.ok || w->dim() != 2 || x->dim() < 1 || !io_type(*x, p.io_dtype)) Py_RETURN_NONE;
+    void* stream = a.stream(8);
+    const bool quantised = !a.none(5);
+    if (!a.ok || w->dim() != 2 || x->dim() < 1) Py_RETURN_NONE;
+    const at::ScalarType io = quantised ? (a.none(7) ? at::kBFloat16 : type_of_code(a.number(7), a.ok)) : x->scalar_type();
+    if (!a.ok || (!quantised && !io_type(*x, p.io_dtype))) Py_RETURN_NONE;
     const bool x_last = p.flags & SS_Q_X_SEQ_LAST, out_last = p.flags & SS_Q_OUT_SEQ_LAST;
     if ((x_last || out_last) && x->dim() != 3) Py_RETURN_NONE;
-    const int64_t dim = x_last ? x->size(1) : x->size(-1), features = w->size(0);
-    if (dim < 1 || !fits(dim) || !fits(features)) Py_RETURN_NONE;
-    const int64_t batch = x_last || out_last ? x->size(0) : 1, seqlen = x_last ? x->size(2) : (out_last ? x->size(1) : x->numel() / dim);
+    if (quantised && (x_last || x->scalar_type() != at::kChar)) Py_RETURN_NONE;
+    const int64_t dim = quantised ? a.number(6) : (x_last ? x->size(1) : x->size(-1)), features = w->size(0);
+    if (!a.ok || dim < 1 || !fits(dim) || !fits(features)) Py_RETURN_NONE;
+    const int64_t batch = x_last || out_last ? x->size(0) : 1, seqlen = x_last ? x->size(2) : (out_last ? x->size(1) : x->numel() / std::max<int64_t>(x->size(-1), 1));
     if (!fits(batch) || !fits(seqlen)) Py_RETURN_NONE;
     p.batch = (int32_t)batch; p.seqlen = (int32_t)seqlen; p.dim = (int32_t)dim; p.features = (int32_t)features;
     p.x = x->data_ptr();
     p.weight = a.ptr(1, at::kChar, {features, (int64_t)ss_quant_pitch((int32_t)dim)});
     p.scale = static_cast<const float*>(a.ptr(2, at::kFloat, {features}));
     p.bias = static_cast<const float*>(a.ptr(3, at::kFloat, {features}, true));
+    if (quantised) {
+        p.flags |= SS_Q_X_QUANTISED;
+        p.io_dtype = io == at::kFloat ? SS_F32 : SS_BF16;
+        p.x_scale = static_cast<const float*>(a.ptr(5, at::kFloat, {batch * seqlen}));
+        if (x->size(-1) != (int64_t)ss_quant_pitch((int32_t)dim)) Py_RETURN_NONE;
+    }
     if (!a.ok) Py_RETURN_NONE;
     if (p.bias) p.flags |= SS_Q_HAS_BIAS;
     at::Tensor out;
-    const at::TensorOptions options = x->options().requires_grad(false);
+    const at::TensorOptions options = x->options().dtype(io).requires_grad(false);
     if (out_last) out = at::empty({batch, features, seqlen}, options);
     else if (x_last) out = at::empty({batch, seqlen, features}, options);
     else {
@@ -1063,13 +1081,6 @@ bool whole_type(const at::Tensor& t, uint32_t flag_of_32, uint32_t& flags)
     if (t.scalar_type() == at::kInt) flags |= flag_of_32;
     else if (t.scalar_type() != at::kLong) return false;
     return true;
-}
-// The type of a code of io types; `ok` falls if it is none.
-at::ScalarType type_of_code(long code, bool& ok)
-{
-    if (code == SS_F32) return at::kFloat;
-    if (code != SS_BF16) ok = false;
-    return at::kBFloat16;
 }
 struct Embed {
     at::Tensor out;
