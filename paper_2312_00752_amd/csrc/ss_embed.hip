@@ -1,6 +1,7 @@
 // Embedding of token ids and its gradient for gfx950, with the C-ABI entry points (see include/ss_embed.h).
 //
-// Forward: rows of a table are copied, so it is bound by HBM (16384 rows of 2048 float32 as bf16, 201 MB, 31 us, 6.4 TB/s) and for few tokens by a launch.
+// Forward: rows of a table are copied, so it is bound by HBM (16384 rows of 2048 float32 as bf16, 201 MB, 31 us, 6.4 TB/s, of ids that
+// are drawn evenly; as in text, where every other row has been read before, 24) and for few tokens by a launch.
 // Backward: every row of the table's gradient is written, most of them with zeros, and every token's row is read once.  To add up a row
 // without atomics, and always in the same order, the tokens are sorted by id first: a radix sort, least digit first and stable, so
 // that the tokens of an id stay in order.  Its launches are short and leave most of the chip idle, so each also fills a share
@@ -237,7 +238,7 @@ __device__ __forceinline__ float* part_of(const EmbedArgs& a, int64_t piece, int
 // A wave has a piece and 512 columns.  It adds up every id whose tokens begin in the piece, and goes on behind its end where no more than SPILL tokens of the
 // last one follow; of longer ones it leaves its share.  The share of an id that began before the piece: the same, and nothing where the wave
 // before goes on to its end.  Ids and places come 64 at once, a lane each, eight rows are requested at once.  Bound by HBM: 65536 rows of 1024 bf16 (135 MB) for
-// 256 ids 25 us, 5.5 TB/s; 16384 of 2048 for 51200 ids, most of which have one row or none (195 MB), 37.
+// 256 ids 25 to 30 us, 4.5 TB/s and more; 16384 of 2048 for 51200 ids, most of which have one row or none (195 MB), 41, as in text 32.
 constexpr int SPILL = 8;   // a piece has that many at least (1024 tokens of 1024 columns: 5.4 us, with 16 7.4)
 template <typename E, typename T>
 __global__ __launch_bounds__(256) void embed_sum_kernel(EmbedArgs a)

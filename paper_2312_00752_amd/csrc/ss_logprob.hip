@@ -187,7 +187,7 @@ __device__ __forceinline__ void results(const LogprobArgs& a, int row, Stat t, c
 __host__ __device__ __forceinline__ int part_floats(int top) { return 4 + 2 * top; }
 
 // G lanes a row (a wave: rows side by side) or piece of one; V slices of eight a lane and step, the next step's requested ahead.  Bound by HBM: 8192 x
-// 51200 bf16 (839 MB) 151 us, 5.6 TB/s (163 where a gradient has been written before); few rows by a launch and, with alternatives, by the
+// 51200 bf16 (839 MB) 151 us, 5.6 TB/s (156 to 182 where a gradient has been written before); few rows by a launch and, with alternatives, by the
 // lanes' choice: 64 x 51200 4.5 us, with eight 7.2.
 template <typename T, typename I, int G, int V, bool TOP>
 __global__ __launch_bounds__(256) void logprob_fwd_kernel(LogprobArgs a)
