@@ -66,6 +66,8 @@ class GatedBlock(torch.nn.Module):
     """x (B,L,width) of ``dtype``; the residual stream is float32 or of that type.  ``norm`` is "layer" or "rms" (which has no bias).
     Calls give (out, residual)."""
 
+    rms = False   # of blocks that were pickled before there was a choice
+
     def __init__(self, width, inner, dtype=torch.float32, device="cuda", eps=1e-5, norm="layer"):
         super().__init__()
         if norm not in ("layer", "rms"):
@@ -101,6 +103,8 @@ class GatedBlock(torch.nn.Module):
 class ServedBlock:
     """A block as it stands, with its projections in 8-bit integers: ``prompt`` gives (out, residual, state), ``step`` continues from
     the state, which it updates in place."""
+
+    rms = False   # as GatedBlock's
 
     @torch.no_grad()
     def __init__(self, block):
